@@ -42,12 +42,14 @@ extern "C" {
 
 typedef enum {
   DMA_OK = 0,
-  DMA_EINVAL = -1,       /* null pointer, misaligned pointer, T<=0, k<=0, n_docs<=0, H_q % H_kv != 0 */
+  DMA_EINVAL = -1,       /* null pointer, misaligned pointer, T<=0, k<=0, n_docs<=0, H_q % H_kv != 0;
+                            of the paged cache: n_rows<0, a stride below the row or not a multiple of 8 */
   DMA_EUNSUPPORTED = -2, /* d not in {64,128,256} (cross-head scores: {64,128}),
                             unknown dtype, more than 256 q-heads per kv-head,
                             more than 32 heads for the cross-head scores,
-                            bf16 dma_fwd / dma_bwd with T >= 2^24 or Q (or K, V) larger than 4 GiB         */
-  DMA_EWORKSPACE = -3,   /* ws_bytes smaller than dma_workspace_bytes() */
+                            bf16 dma_fwd / dma_bwd with T >= 2^24 or Q (or K, V) larger than 4 GiB;
+                            of the paged cache: page sizes and numbers other than stated there             */
+  DMA_EWORKSPACE = -3,   /* ws_bytes smaller than dma_workspace_bytes() / dma_cache_decode_bytes() */
   DMA_EHIP = -4          /* a launch failed (hipGetLastError) */
 } dma_status;
 
@@ -289,6 +291,123 @@ int dma_decode_static(const dma_shape* shape, const void* q, const void* K, cons
 int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const void* V, const float* z,
                     const int32_t* cu_seqlens, const int32_t* seq_lens, int refresh, void* o, float* lse,
                     int32_t* kept, size_t kept_bytes, void* stream);
+
+/*
+ * A paged key/value cache in 4 bits, and decode over it: the cache of a server that holds many requests of different
+ * and growing lengths.  Four calls make a step: dma_cache_assign gives the step's new tokens their places, dma_cache_append
+ * writes their K, V and content scores there, dma_cache_decode attends from them, and, where a request ends or drafts of it
+ * are rejected, the next dma_cache_assign takes their places back.  None of them looks at a length on the host, allocates
+ * or synchronises, so a step can be captured in a graph.
+ *
+ *   pages        dma_cache_bytes(shape) bytes: the pool of n_pages pages of page_size tokens (dma_cache_describe)
+ *   block_table  [n_reqs, max_pages] int32: the pages of each request, in order; -1 behind its last one
+ *   seq_lens     [n_reqs] int32: cached tokens of each request
+ *   free_list    dma_cache_free_bytes(shape) bytes, int32: [0] number of free pages, [4 ...] a stack of them
+ *   slots        [n_rows] int32: place of a token, page * page_size + place in the page; below 0: none
+ *   row_req      [n_rows] int32: request of a row; below 0: none
+ *   row_len      [n_rows] int32: keys that a row sees, the first row_len of its request; 0: none
+ * n_rows is the capacity of a step's row arrays, not its number of rows, and may be 0 (nothing is done, or enqueued, but by
+ * dma_cache_assign).  dtype is the type of K, V, q and o; what the cache holds does not depend on it.
+ *
+ * A token's K (and V) of one kv-head is held as d codes of 4 bits and d / 32 scale bytes (OCP microscaling, e2m1 with e8m0): channel c
+ * stands for  code[c] * 2^(byte[c / 32] - 127),  code in {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign.  The power of two is the one
+ * at which the largest of the 32 rounds to at most 6 (byte 2 to 252), values go to the nearest code, ties to the even one: an
+ * error of at most a fifth of the largest value of the 32.  A block with an infinity or NaN has byte 255 and reads as NaN.
+ *
+ * Numbers of pages, slots and requests in device memory are checked where they are used: one out of range is a key (or row)
+ * that is not there, never an address.  Calls that write the same arrays must be ordered by the caller (one stream).
+ */
+typedef struct {
+  int32_t n_reqs;      /* places for requests, 1 to 4096                                        */
+  int32_t n_pages;     /* pages of the pool; n_pages * page_size < 2^31                         */
+  int32_t max_pages;   /* pages of one request at most; max_pages * page_size < 2^31            */
+  int32_t page_size;   /* tokens of a page: 16, 32, 64, 128 or 256                              */
+  int32_t H_q;         /* query heads                                                           */
+  int32_t H_kv;        /* key/value heads, divides H_q                                          */
+  int32_t d;           /* head dimension: 64, 128 or 256                                        */
+  int32_t dtype;       /* dma_dtype of K, V, q, o                                               */
+} dma_cache_shape;
+
+/* Bytes of the pool, of the free list, and of the scratch of one dma_cache_decode; 0 if an argument is invalid. */
+size_t dma_cache_bytes(const dma_cache_shape* shape);
+size_t dma_cache_free_bytes(const dma_cache_shape* shape);
+size_t dma_cache_decode_bytes(const dma_cache_shape* shape, int32_t n_rows, int32_t k);
+
+/* Where things lie in a page, bytes from its start: for kv-head g and place t of the page
+ *   K codes  off_codes + ((g * page_size + t) * 2    ) * d / 2,  V codes  ... * 2 + 1 ...   d / 2 bytes each, low nibble first
+ *   K scales off_scales + ((g * page_size + t) * 2   ) * d / 32, V scales ... * 2 + 1 ...   d / 32 bytes each
+ *   score of q-head h: float at off_scores + (h * page_size + t) * 4
+ * Pages are page_bytes apart (a multiple of 256) and hold nothing of each other: one can be copied or moved as a whole. */
+typedef struct {
+  uint64_t page_bytes, off_codes, off_scales, off_scores;
+} dma_cache_layout;
+int dma_cache_describe(const dma_cache_shape* shape, dma_cache_layout* out);
+
+/* An empty cache: seq_lens 0, block_table -1, all pages free (the lowest are taken first).  The pool needs no clearing. */
+int dma_cache_reset(const dma_cache_shape* shape, int32_t* seq_lens, int32_t* block_table, int32_t* free_list, void* stream);
+
+/*
+ * Places for a step.  Request b grows by change[b] tokens, or, below 0, gives back its last -change[b] (at most all it has:
+ * INT32_MIN ends it).  The pages given back go on the free list first, then those that grow take theirs.
+ *   change     in      [n_reqs]
+ *   seq_lens, block_table, free_list   in and out
+ *   cu_rows    out     [n_reqs + 1]: the new tokens of request b are the rows cu_rows[b] .. cu_rows[b + 1]
+ *   row_req, row_len, slots   out   [n_rows], fully written: -1, 0, -1 for rows behind the last and of requests not served.
+ *                      A row sees the keys up to and with its own token: row_len = its position + 1
+ *   status     out     [n_reqs]: 0 served, or why not.  A request that is not served keeps its length and pages; its rows keep
+ *                      their places among the rows.  Pages are promised in order of the requests: once one does not find enough,
+ *                      those behind it that need any are not served either.
+ */
+typedef enum {
+  DMA_CACHE_SERVED = 0,
+  DMA_CACHE_NO_PAGES = 1,  /* the free list is too short                     */
+  DMA_CACHE_TOO_LONG = 2,  /* more than max_pages pages                      */
+  DMA_CACHE_NO_ROWS = 3    /* its rows end behind n_rows                     */
+} dma_cache_status;
+int dma_cache_assign(const dma_cache_shape* shape, int32_t n_rows, const int32_t* change, int32_t* seq_lens,
+                     int32_t* block_table, int32_t* free_list, int32_t* cu_rows, int32_t* row_req, int32_t* row_len,
+                     int32_t* slots, int32_t* status, void* stream);
+
+/*
+ * Rows into the cache.
+ *   K, V   in  n_rows rows of [H_kv, d], k_stride and v_stride elements apart (multiples of 8 of at least H_kv * d: K and V may be parts of
+ *              one projection's output)
+ *   W, A   in  the score parameters as for dma_mask_gen: the cache gets z = exp(A softplus(w . v)), of V as given, the
+ *              scores that dma_mask_gen forms, bit for bit
+ *   z      in  if W == NULL: the scores, [H_q, n_rows] (A is then ignored); else ignored.  A score of -infinity takes its key
+ *              out of the attention; NaN and +infinity make the rows that keep the key NaN.
+ *   slots  in  where each row goes; rows without a slot are left out.  No two rows may have the same slot.
+ */
+int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K, int64_t k_stride, const void* V,
+                     int64_t v_stride, const float* W, const float* A, const float* z, const int32_t* slots, void* pages,
+                     void* stream);
+
+/*
+ * Rows out of the cache, for the entry points over plain K, V and z (dma_mask_gen with W == NULL, dma_fwd, dma_decode).
+ *   K, V   out [n_rows, H_kv, d]: the values that the codes stand for, exact in either dtype
+ *   z      out [H_q, n_rows].  Rows without a slot: K = V = 0, z = -infinity.
+ */
+int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* slots, const void* pages, void* K, void* V,
+                   float* z, void* stream);
+
+/*
+ * Decode over the cache: row r keeps the min(k, n) best of the first n = row_len[r] keys of its request by (z descending,
+ * position ascending) and attends to them (Eq. 4-6), with the arithmetic of the values that dma_cache_read returns.  Several
+ * rows of a request, each with its own length, are independent (drafts, the end of a prompt).
+ *   q        in  n_rows rows of [H_q, d], q_stride elements apart (a multiple of 8 of at least H_q * d)
+ *   row_req  in  nullable: row r is then request r (n_rows <= n_reqs), and seq_lens may serve as row_len
+ *   softmax_scale  0 => d^-1/2
+ *   o        out [n_rows, H_q, d];  lse out [H_q, n_rows], natural log.  A row that sees nothing, or nothing but scores of
+ *                -infinity: o = 0, lse = -infinity
+ *   kept     out [n_rows, H_q, min(k, max_pages * page_size)] int32: the slots of the kept keys in order of position, -1 behind
+ *                them (and for keys whose page is out of range)
+ *   ws       dma_cache_decode_bytes(shape, n_rows, k) bytes of scratch; calls that overlap need one each
+ * DMA_EUNSUPPORTED where (n_rows + 8) * H_q * ceil(min(k, max_pages * page_size) / 256) reaches 2^22: a whole prompt goes through
+ * dma_mask_gen and dma_fwd.
+ */
+int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
+                     int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,
+                     const int32_t* row_len, void* o, float* lse, int32_t* kept, void* ws, size_t ws_bytes, void* stream);
 
 /*
  * Per-stage timing aid.  dma_mask_gen, dma_fwd and dma_bwd each launch several kernels, so a

@@ -36,6 +36,19 @@ class DmaMaskLayout(ctypes.Structure):
     ]
 
 
+class DmaCacheShape(ctypes.Structure):
+    _fields_ = [
+        ("n_reqs", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
+class DmaCacheLayout(ctypes.Structure):
+    _fields_ = [("page_bytes", ctypes.c_uint64), ("off_codes", ctypes.c_uint64), ("off_scales", ctypes.c_uint64),
+                ("off_scores", ctypes.c_uint64)]
+
+
 class DmaError(RuntimeError):
     def __init__(self, status, what):
         super().__init__(f"{what}: {strerror(status)} (status {status})")
@@ -89,6 +102,25 @@ def lib():
         L.dma_decode_static.restype = i32
         L.dma_decode_step.argtypes = [shp] + [vp] * 6 + [i32] + [vp] * 3 + [sz, vp]
         L.dma_decode_step.restype = i32
+        cshp, i64 = ctypes.POINTER(DmaCacheShape), ctypes.c_int64
+        L.dma_cache_bytes.argtypes = [cshp]
+        L.dma_cache_bytes.restype = sz
+        L.dma_cache_free_bytes.argtypes = [cshp]
+        L.dma_cache_free_bytes.restype = sz
+        L.dma_cache_decode_bytes.argtypes = [cshp, i32, i32]
+        L.dma_cache_decode_bytes.restype = sz
+        L.dma_cache_describe.argtypes = [cshp, ctypes.POINTER(DmaCacheLayout)]
+        L.dma_cache_describe.restype = i32
+        L.dma_cache_reset.argtypes = [cshp] + [vp] * 4
+        L.dma_cache_reset.restype = i32
+        L.dma_cache_assign.argtypes = [cshp, i32] + [vp] * 10
+        L.dma_cache_assign.restype = i32
+        L.dma_cache_append.argtypes = [cshp, i32, vp, i64, vp, i64] + [vp] * 6
+        L.dma_cache_append.restype = i32
+        L.dma_cache_read.argtypes = [cshp, i32] + [vp] * 6
+        L.dma_cache_read.restype = i32
+        L.dma_cache_decode.argtypes = [cshp, i32, i32, ctypes.c_float, vp, i64] + [vp] * 8 + [sz, vp]
+        L.dma_cache_decode.restype = i32
         L.dma_profile_events.argtypes = [vp]
         L.dma_profile_events.restype = None
         L.dma_strerror.argtypes = [i32]
@@ -240,3 +272,59 @@ def dma_bwd_scores(shape, Q, K, V, O, dO, LSE, z, expiry, mask, cu_seqlens, W, A
     _check(lib().dma_bwd_scores(ctypes.byref(shape), _ptr(Q), _ptr(K), _ptr(V), _ptr(O), _ptr(dO), _ptr(LSE), _ptr(z),
                                 _ptr(expiry), _ptr(mask), _ptr(cu_seqlens), _ptr(W), _ptr(A), _ptr(dQ), _ptr(dK), _ptr(dV),
                                 _ptr(dz), _ptr(dW), _ptr(dA), _ptr(ws), int(ws_bytes), _stream(stream)), "dma_bwd_scores")
+
+
+CACHE_SERVED, CACHE_NO_PAGES, CACHE_TOO_LONG, CACHE_NO_ROWS = 0, 1, 2, 3
+
+
+def make_cache_shape(n_reqs, n_pages, max_pages, page_size, H_q, H_kv, d, dtype=DMA_BF16):
+    return DmaCacheShape(int(n_reqs), int(n_pages), int(max_pages), int(page_size), int(H_q), int(H_kv), int(d), int(dtype))
+
+
+def dma_cache_bytes(shape):
+    return int(lib().dma_cache_bytes(ctypes.byref(shape)))
+
+
+def dma_cache_free_bytes(shape):
+    return int(lib().dma_cache_free_bytes(ctypes.byref(shape)))
+
+
+def dma_cache_decode_bytes(shape, n_rows, k):
+    return int(lib().dma_cache_decode_bytes(ctypes.byref(shape), int(n_rows), int(k)))
+
+
+def dma_cache_describe(shape):
+    """Where things lie in a page (a DmaCacheLayout)."""
+    out = DmaCacheLayout()
+    _check(lib().dma_cache_describe(ctypes.byref(shape), ctypes.byref(out)), "dma_cache_describe")
+    return out
+
+
+def dma_cache_reset(shape, seq_lens, block_table, free_list, stream=None):
+    _check(lib().dma_cache_reset(ctypes.byref(shape), _ptr(seq_lens), _ptr(block_table), _ptr(free_list),
+                                 _stream(stream)), "dma_cache_reset")
+
+
+def dma_cache_assign(shape, n_rows, change, seq_lens, block_table, free_list, cu_rows, row_req, row_len, slots, status,
+                     stream=None):
+    _check(lib().dma_cache_assign(ctypes.byref(shape), int(n_rows), _ptr(change), _ptr(seq_lens), _ptr(block_table),
+                                  _ptr(free_list), _ptr(cu_rows), _ptr(row_req), _ptr(row_len), _ptr(slots),
+                                  _ptr(status), _stream(stream)), "dma_cache_assign")
+
+
+def dma_cache_append(shape, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, stream=None):
+    _check(lib().dma_cache_append(ctypes.byref(shape), int(n_rows), _ptr(K), int(k_stride), _ptr(V), int(v_stride),
+                                  _ptr(W), _ptr(A), _ptr(z), _ptr(slots), _ptr(pages), _stream(stream)),
+           "dma_cache_append")
+
+
+def dma_cache_read(shape, n_rows, slots, pages, K, V, z, stream=None):
+    _check(lib().dma_cache_read(ctypes.byref(shape), int(n_rows), _ptr(slots), _ptr(pages), _ptr(K), _ptr(V), _ptr(z),
+                                _stream(stream)), "dma_cache_read")
+
+
+def dma_cache_decode(shape, n_rows, k, softmax_scale, q, q_stride, pages, block_table, row_req, row_len, o, lse, kept, ws,
+                     ws_bytes, stream=None):
+    _check(lib().dma_cache_decode(ctypes.byref(shape), int(n_rows), int(k), float(softmax_scale), _ptr(q), int(q_stride),
+                                  _ptr(pages), _ptr(block_table), _ptr(row_req), _ptr(row_len), _ptr(o), _ptr(lse),
+                                  _ptr(kept), _ptr(ws), int(ws_bytes), _stream(stream)), "dma_cache_decode")

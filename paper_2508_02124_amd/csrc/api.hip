@@ -1,6 +1,7 @@
 // Host side of the C ABI: argument validation, layout computation, dispatch.  No allocation, no
 // synchronisation.  State kept between calls: the caller's array of stage events while
 // dma_profile_events has one set (per host thread), nothing else in this file.
+#include "cache.h"
 #include "common.h"
 
 using namespace dma;
@@ -48,6 +49,22 @@ size_t ws_bytes_for(const dma_shape& s) {
   if (s.dtype == DMA_F32) return align_up((size_t)s.H_q * s.T * 8, 256);  // D_i in fp64
   return ws_layout(s).total;
 }
+
+int check_cache(const dma_cache_shape* s) {
+  if (!s) return DMA_EINVAL;
+  if (s->n_reqs <= 0 || s->n_pages <= 0 || s->max_pages <= 0 || s->H_q <= 0 || s->H_kv <= 0) return DMA_EINVAL;
+  if (s->H_q % s->H_kv != 0) return DMA_EINVAL;
+  if (s->d != 64 && s->d != 128 && s->d != 256) return DMA_EUNSUPPORTED;
+  if (s->dtype != DMA_BF16 && s->dtype != DMA_F32) return DMA_EUNSUPPORTED;
+  if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return DMA_EUNSUPPORTED;
+  if (s->n_reqs > CACHE_REQS_MAX) return DMA_EUNSUPPORTED;
+  if ((long)s->n_pages * s->page_size > INT32_MAX || (long)s->max_pages * s->page_size > INT32_MAX) return DMA_EUNSUPPORTED;
+  if (s->H_q > 4096 || s->H_q / s->H_kv > 256) return DMA_EUNSUPPORTED;  // (a page stays below 2^31 bytes, a group's scores below 64 KiB)
+  return DMA_OK;
+}
+
+// n_rows rows of `heads` heads, `stride` elements apart
+bool bad_rows(const dma_cache_shape& s, int64_t stride, int heads) { return stride < (int64_t)heads * s.d || stride % 8 != 0; }
 
 Ptrs make_ptrs(const dma_shape* s, const void* mask) {
   Ptrs p;
@@ -274,19 +291,110 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
                        reinterpret_cast<char*>(kept) + decode_list_bytes(*shape), (hipStream_t)stream);
 }
 
+size_t dma_cache_bytes(const dma_cache_shape* shape) {
+  if (check_cache(shape) != DMA_OK) return 0;
+  return (size_t)shape->n_pages * cache_layout(*shape).page_bytes;
+}
+
+size_t dma_cache_free_bytes(const dma_cache_shape* shape) {
+  if (check_cache(shape) != DMA_OK) return 0;
+  return ((size_t)shape->n_pages + FREE_HEADER) * 4;
+}
+
+// The grids of a decode: rows x heads x parts of the list, in workgroups of up to 1024 threads, 2^32 threads at most.
+static int check_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (n_rows < 0 || k <= 0) return DMA_EINVAL;
+  const long cap = (long)shape->max_pages * shape->page_size, parts = ((k < cap ? k : cap) + 255) / 256;
+  if (((long)n_rows + 8) * shape->H_q * parts >= 1 << 22) return DMA_EUNSUPPORTED;
+  return DMA_OK;
+}
+
+size_t dma_cache_decode_bytes(const dma_cache_shape* shape, int32_t n_rows, int32_t k) {
+  if (check_cache_decode(shape, n_rows, k) != DMA_OK) return 0;
+  return cache_decode_bytes(*shape, n_rows, k);
+}
+
+int dma_cache_describe(const dma_cache_shape* shape, dma_cache_layout* out) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (!out) return DMA_EINVAL;
+  const CacheLayout l = cache_layout(*shape);
+  out->page_bytes = l.page_bytes; out->off_codes = 0; out->off_scales = l.off_scales; out->off_scores = l.off_z;
+  return DMA_OK;
+}
+
+int dma_cache_reset(const dma_cache_shape* shape, int32_t* seq_lens, int32_t* block_table, int32_t* free_list, void* stream) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (!seq_lens || !block_table || !free_list) return DMA_EINVAL;
+  return launch_cache_reset(*shape, seq_lens, block_table, free_list, (hipStream_t)stream);
+}
+
+int dma_cache_assign(const dma_cache_shape* shape, int32_t n_rows, const int32_t* change, int32_t* seq_lens,
+                     int32_t* block_table, int32_t* free_list, int32_t* cu_rows, int32_t* row_req, int32_t* row_len,
+                     int32_t* slots, int32_t* status, void* stream) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (n_rows < 0 || !change || !seq_lens || !block_table || !free_list || !cu_rows || !status) return DMA_EINVAL;
+  if (n_rows > 0 && (!row_req || !row_len || !slots)) return DMA_EINVAL;
+  return launch_cache_assign(*shape, n_rows, change, seq_lens, block_table, free_list, cu_rows, row_req, row_len, slots,
+                             status, (hipStream_t)stream);
+}
+
+int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K, int64_t k_stride, const void* V,
+                     int64_t v_stride, const float* W, const float* A, const float* z, const int32_t* slots, void* pages,
+                     void* stream) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (n_rows < 0 || bad_rows(*shape, k_stride, shape->H_kv) || bad_rows(*shape, v_stride, shape->H_kv)) return DMA_EINVAL;
+  if (n_rows == 0) return DMA_OK;
+  if (!K || !V || !slots || !pages || (W ? !A : !z)) return DMA_EINVAL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(W) || !aligned16(pages)) return DMA_EINVAL;
+  return launch_cache_append(*shape, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, (hipStream_t)stream);
+}
+
+int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* slots, const void* pages, void* K, void* V,
+                   float* z, void* stream) {
+  int rc = check_cache(shape);
+  if (rc != DMA_OK) return rc;
+  if (n_rows < 0) return DMA_EINVAL;
+  if (n_rows == 0) return DMA_OK;
+  if (!slots || !pages || !K || !V || !z) return DMA_EINVAL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(pages)) return DMA_EINVAL;
+  return launch_cache_read(*shape, n_rows, slots, pages, K, V, z, (hipStream_t)stream);
+}
+
+int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
+                     int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,
+                     const int32_t* row_len, void* o, float* lse, int32_t* kept, void* ws, size_t ws_bytes, void* stream) {
+  int rc = check_cache_decode(shape, n_rows, k);
+  if (rc != DMA_OK) return rc;
+  if (softmax_scale < 0.f || softmax_scale != softmax_scale || bad_rows(*shape, q_stride, shape->H_q)) return DMA_EINVAL;
+  if (!row_req && n_rows > shape->n_reqs) return DMA_EINVAL;
+  if (n_rows == 0) return DMA_OK;
+  if (!q || !pages || !block_table || !row_len || !o || !lse || !kept) return DMA_EINVAL;
+  if (!aligned16(q) || !aligned16(pages) || !aligned16(o) || !aligned16(kept) || !aligned16(ws)) return DMA_EINVAL;
+  if (!ws || ws_bytes < cache_decode_bytes(*shape, n_rows, k)) return DMA_EWORKSPACE;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->d);
+  return launch_cache_decode(*shape, n_rows, k, scale, q, q_stride, pages, block_table, row_req, row_len, o, lse, kept, ws,
+                             (hipStream_t)stream);
+}
+
 void dma_profile_events(void** events) { dma::g_stage_events = events; }
 
 const char* dma_strerror(int status) {
   switch (status) {
     case DMA_OK: return "ok";
     case DMA_EINVAL: return "invalid argument (null or misaligned pointer, non-positive size, H_q % H_kv != 0)";
-    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens)";
-    case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
+    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, fewer than 2^31 slots)";
+    case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes, dma_cache_decode_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
     case DMA_EHIP: return "HIP launch failed";
     default: return "unknown status";
   }
 }
 
-int dma_version(void) { return 141; }
+int dma_version(void) { return 142; }
 
 }  // extern "C"

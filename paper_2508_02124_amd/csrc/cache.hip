@@ -1,0 +1,410 @@
+// The paged cache: pages and slots for a step's new tokens (assign), rows into it (append) and out of it (read).
+//
+// K and V are held in 4 bits: an OCP e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and a sign) per channel and one power of two per
+// 32 channels of a token's head, 17 / 32 bytes a channel against bf16's 2.  The content scores (Eq. 3) are formed from V as it comes, not
+// as it is stored, and held in fp32: they decide which keys a row keeps.
+#include "cache.h"
+
+namespace dma {
+
+// ------------------------------------------------------------------ pages and slots
+// A request with n tokens owns ceil(n / ps) pages.  Requests that shrink push the pages they no longer need on the stack of
+// free pages, in order of request and page; those that grow pop theirs, in the same order.  The places on the stack are
+// exclusive prefix sums over the requests, so no step depends on another request's outcome but through the sum: a request
+// that asks for pages is served if all pages asked for up to and with it are there.
+struct AssignArgs {
+  const int32_t* change;
+  int32_t *lens, *table, *free_list, *cu_rows, *row_req, *row_len, *slots, *status;
+  int n_reqs, n_pages, max_pages, shift, n_rows;
+};
+
+// Inclusive sum over the workgroup's 1024 threads (s_part: 16 words); the total in `total`.
+__device__ __forceinline__ long long scan_1024(long long x, long long* s_part, long long& total) {
+  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const long long t = __shfl_up(x, off);
+    if (l >= off) x += t;
+  }
+  __syncthreads();  // (s_part may still be read from the sum before)
+  if (l == 63) s_part[w] = x;
+  __syncthreads();
+  total = 0;
+#pragma unroll
+  for (int i = 0; i < 16; i++) {
+    x += i < w ? s_part[i] : 0;
+    total += s_part[i];
+  }
+  return x;
+}
+
+// The last b with first[b] <= i, of n > 0 ascending entries.
+__device__ __forceinline__ int find_request(const int32_t* first, int n, int i) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (first[mid] <= i) lo = mid; else hi = mid;
+  }
+  return lo;
+}
+
+// Row r of the step: the request that has it, how many keys it sees (its position + 1), its slot.
+__device__ __forceinline__ void assign_row(const AssignArgs& p, const int32_t* first, int r) {
+  int req = -1, len = 0, slot = -1;
+  if (r < first[p.n_reqs]) {
+    const int b = find_request(first, p.n_reqs, r);
+    if (p.status[b] == 0) {
+      const int pos = p.lens[b] - (first[b + 1] - first[b]) + (r - first[b]);  // (lens: with the new tokens)
+      const int page = p.table[(size_t)b * p.max_pages + (pos >> p.shift)];
+      req = b;
+      len = pos + 1;
+      slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+    }
+  }
+  p.row_req[r] = req;
+  p.row_len[r] = len;
+  p.slots[r] = slot;
+}
+
+// Rows that the one workgroup writes itself.
+constexpr int ASSIGN_ROWS = 4096;
+
+__global__ __launch_bounds__(1024) void cache_assign_kernel(AssignArgs p) {
+  __shared__ int32_t first[CACHE_REQS_MAX + 1];  // first row of every request
+  __shared__ int32_t upto[CACHE_REQS_MAX + 1];   // pages given back, then pages taken, by the requests before this one
+  __shared__ long long s_part[16];
+  const int tid = threadIdx.x, ps = 1 << p.shift;
+  const long long cap = (long long)p.max_pages << p.shift;
+  int32_t* stack = p.free_list + FREE_HEADER;
+  const int have0 = max(0, min(p.free_list[0], p.n_pages));
+  auto length = [&](int b) { return (int)max(0ll, min((long long)p.lens[b], cap)); };
+  auto pages = [&](long long n) { return (int)((n + ps - 1) >> p.shift); };
+  // pages given back
+  long long base = 0, total;
+  for (int b0 = 0; b0 < p.n_reqs; b0 += 1024) {
+    const int b = b0 + tid;
+    int freed = 0;
+    if (b < p.n_reqs) {
+      const int old = length(b), c = p.change[b];
+      if (c < 0) freed = pages(old) - pages(max(0ll, (long long)old + c));
+    }
+    const long long inc = scan_1024(freed, s_part, total);
+    if (b < p.n_reqs) upto[b] = (int)min(base + inc - freed, (long long)p.n_pages);
+    base += total;
+  }
+  const int freed_all = (int)min(base, (long long)(p.n_pages - have0));  // (never more, unless the caller's tables are damaged)
+  if (tid == 0) upto[p.n_reqs] = freed_all;
+  __syncthreads();
+  for (int i = tid; i < freed_all; i += 1024) {
+    const int b = find_request(upto, p.n_reqs, i), old = length(b);
+    const int place = pages(max(0ll, (long long)old + p.change[b])) + i - upto[b];
+    if (place >= pages(old)) continue;  // (as above)
+    int32_t* entry = p.table + (size_t)b * p.max_pages + place;
+    stack[have0 + i] = *entry;
+    *entry = -1;
+  }
+  const int have = have0 + freed_all;
+  __syncthreads();
+  // pages taken
+  long long rows = 0, used = 0;
+  base = 0;
+  for (int b0 = 0; b0 < p.n_reqs; b0 += 1024) {
+    const int b = b0 + tid;
+    int old = 0, need = 0, state = 0;
+    long long grow = 0, after = 0;
+    if (b < p.n_reqs) {
+      old = length(b);
+      const int c = p.change[b];
+      grow = max(c, 0);
+      after = max(0ll, (long long)old + c);
+    }
+    const long long end = rows + scan_1024(grow, s_part, total);
+    rows += total;
+    if (grow) {
+      if (after > cap) state = DMA_CACHE_TOO_LONG;
+      else if (end > p.n_rows) state = DMA_CACHE_NO_ROWS;
+      else need = pages(after) - pages(old);
+    }
+    const long long inc = base + scan_1024(need, s_part, total);
+    base += total;
+    if (need && inc > have) state = DMA_CACHE_NO_PAGES;
+    if (need && state) need = 0;
+    (void)scan_1024(need, s_part, total);
+    if (b < p.n_reqs) {
+      first[b] = (int)min(end - grow, (long long)p.n_rows);
+      upto[b] = (int)min(inc - need, (long long)have);  // (served requests are those of a prefix of the sum)
+      p.cu_rows[b] = first[b];
+      p.status[b] = state;
+      p.lens[b] = state ? old : (int)after;
+    }
+    used += total;
+  }
+  if (tid == 0) {
+    first[p.n_reqs] = (int)min(rows, (long long)p.n_rows);
+    p.cu_rows[p.n_reqs] = first[p.n_reqs];
+    p.free_list[0] = have - (int)used;
+  }
+  __syncthreads();
+  for (int i = tid; i < (int)used; i += 1024) {
+    const int b = find_request(upto, p.n_reqs, i), n = p.lens[b];
+    const int place = pages(n - (first[b + 1] - first[b])) + i - upto[b];
+    p.table[(size_t)b * p.max_pages + place] = stack[have - 1 - i];
+  }
+  __syncthreads();
+  if (p.n_rows <= ASSIGN_ROWS)
+    for (int r = tid; r < p.n_rows; r += 1024) assign_row(p, first, r);
+}
+
+__global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
+  __shared__ int32_t first[CACHE_REQS_MAX + 1];
+  for (int b = threadIdx.x; b <= p.n_reqs; b += 256) first[b] = p.cu_rows[b];
+  __syncthreads();
+  for (int r = blockIdx.x * 1024 + threadIdx.x, i = 0; i < 4 && r < p.n_rows; r += 256, i++) assign_row(p, first, r);
+}
+
+__global__ __launch_bounds__(256) void cache_reset_kernel(int32_t* lens, int32_t* table, int32_t* free_list, int n_reqs,
+                                                          int n_pages, size_t entries) {
+  const size_t i = blockIdx.x * (size_t)256 + threadIdx.x;
+  if (i < entries) table[i] = -1;
+  if (i < (size_t)n_reqs) lens[i] = 0;
+  if (i < (size_t)n_pages) free_list[FREE_HEADER + i] = n_pages - 1 - (int)i;  // (the lowest pages are taken first)
+  if (i < FREE_HEADER) free_list[i] = i == 0 ? n_pages : 0;
+}
+
+int launch_cache_reset(const dma_cache_shape& s, int32_t* lens, int32_t* table, int32_t* free_list, hipStream_t st) {
+  const size_t entries = (size_t)s.n_reqs * s.max_pages;
+  const size_t n = entries > (size_t)s.n_pages + FREE_HEADER ? entries : (size_t)s.n_pages + FREE_HEADER;
+  cache_reset_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(lens, table, free_list, s.n_reqs, s.n_pages, entries);
+  return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
+}
+
+int launch_cache_assign(const dma_cache_shape& s, int n_rows, const int32_t* change, int32_t* lens, int32_t* table,
+                        int32_t* free_list, int32_t* cu_rows, int32_t* row_req, int32_t* row_len, int32_t* slots,
+                        int32_t* status, hipStream_t st) {
+  const AssignArgs p = {change, lens, table, free_list, cu_rows, row_req, row_len, slots, status,
+                        s.n_reqs, s.n_pages, s.max_pages, cache_layout(s).shift, n_rows};
+  cache_assign_kernel<<<1, 1024, 0, st>>>(p);
+  if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  if (n_rows > ASSIGN_ROWS) cache_rows_kernel<<<(unsigned)((n_rows + 1023) / 1024), 256, 0, st>>>(p);
+  return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
+}
+
+// ------------------------------------------------------------------ rows into the cache
+// Eight channels of a lane.
+template <typename T> __device__ __forceinline__ void load8(const T* src, float* x) {
+  if constexpr (sizeof(T) == 2) {
+    const uint4 raw = *reinterpret_cast<const uint4*>(src);
+    const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      x[2 * e] = __uint_as_float(u[e] << 16);
+      x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
+    }
+  } else {
+    const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
+    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
+    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  }
+}
+
+template <int CTRL> __device__ __forceinline__ uint32_t dpp_quad(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
+}
+
+// The codes of a lane's eight channels, and the scale byte that four neighbouring lanes (32 channels) share: the power of two at
+// which the largest value rounds to at most 6, 2^(exponent - 2) or, from a mantissa of 1.75 on, twice that.  A block that holds
+// an infinity or NaN has the byte 255.  Bytes 2 to 252: what the cache holds is finite and normal in fp32 and bf16 alike.
+__device__ __forceinline__ uint32_t quantise8(const float* x, uint32_t& byte) {
+  uint32_t top = 0;  // (as integers: the bits of NaN are above those of every number)
+#pragma unroll
+  for (int e = 0; e < 8; e++) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  top = max(top, dpp_quad<0xb1>(top));
+  top = max(top, dpp_quad<0x4e>(top));
+  byte = top >= 0x7f800000u ? 255u : (uint32_t)max(2, min(252, (int)((top + 0x200000u) >> 23) - 2));
+  const float scale = mx_scale(byte);
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], scale, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], scale, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], scale, 3);
+}
+
+// One workgroup per (64 rows, kv-head).  A row is held by D / 8 lanes; K and V of all rows of the tile are requested before the
+// first is used.  The scores are those of z_kernel, bit for bit: the same sums in the same order.
+template <typename T, int D, int GMAX>
+__global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* __restrict__ K, long k_stride,
+                                                           const T* __restrict__ V, long v_stride,
+                                                           const float* __restrict__ W, const float* __restrict__ A,
+                                                           const float* __restrict__ z, const int32_t* __restrict__ slots,
+                                                           int n_rows) {
+  extern __shared__ float zs[];  // [G][64]
+  __shared__ uint32_t s_slot[64];
+  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
+  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
+  const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
+  if (tid < 64) s_slot[tid] = t0 + tid < n_rows ? (uint32_t)slots[t0 + tid] : 0xffffffffu;
+  float k[NP][8], v[NP][8];
+#pragma unroll
+  for (int pass = 0; pass < NP; pass++) {
+    const long t = min(t0 + pass * RPP + rl, n_rows - 1);
+    load8(K + t * k_stride + (long)g * D + 8 * sub, k[pass]);
+    load8(V + t * v_stride + (long)g * D + 8 * sub, v[pass]);
+  }
+  __syncthreads();
+#pragma unroll
+  for (int pass = 0; pass < NP; pass++) {
+    const uint32_t slot = s_slot[pass * RPP + rl];
+    uint32_t kb, vb;
+    const uint32_t kc = quantise8(k[pass], kb), vc = quantise8(v[pass], vb);
+    if (slot < c.n_slots) {
+      char* page = cache_page(c, slot);
+      const uint32_t at = ((uint32_t)g << c.shift) + cache_place(c, slot);
+      uint32_t* codes = reinterpret_cast<uint32_t*>(page + (size_t)at * D);
+      codes[sub] = kc;
+      codes[LPR + sub] = vc;
+      uint8_t* scales = reinterpret_cast<uint8_t*>(page) + c.off_scales + (size_t)at * (D / 16);
+      if (sub % 4 == 0) {
+        scales[sub / 4] = (uint8_t)kb;
+        scales[D / 32 + sub / 4] = (uint8_t)vb;
+      }
+    }
+  }
+  if (W) {
+    for (int h0 = 0; h0 < G; h0 += GMAX) {
+      float wreg[GMAX][8];
+#pragma unroll
+      for (int hh = 0; hh < GMAX; hh++) load8(W + (size_t)(g * G + min(h0 + hh, G - 1)) * D + 8 * sub, wreg[hh]);
+#pragma unroll
+      for (int pass = 0; pass < NP; pass++) {
+#pragma unroll
+        for (int hh = 0; hh < GMAX; hh++) {
+          float acc = 0.f;
+#pragma unroll
+          for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], v[pass][e], acc);
+          acc = group_sum<LPR>(acc);
+          if (sub == hh % LPR && h0 + hh < G) zs[(h0 + hh) * 64 + pass * RPP + rl] = acc;
+        }
+      }
+    }
+    __syncthreads();
+  }
+  for (int i = tid; i < G * 64; i += 256) {
+    const int h = g * G + (i >> 6), r = i & 63;
+    const uint32_t slot = s_slot[r];
+    if (slot >= c.n_slots) continue;
+    float zv;
+    if (W) {
+      const float x = zs[i], sp = fmaxf(x, 0.f) + log1pf(expf(-fabsf(x)));
+      zv = expf(A[h] * sp);
+    } else {
+      zv = z[(size_t)h * n_rows + t0 + r];
+    }
+    float* zp = reinterpret_cast<float*>(cache_page(c, slot) + c.off_z);
+    zp[((size_t)h << c.shift) + cache_place(c, slot)] = zv;
+  }
+}
+
+// ------------------------------------------------------------------ rows out of it
+// The same tiles; rows without a slot come back as zeros with a score of -infinity.
+template <typename T, int D>
+__global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32_t* __restrict__ slots, T* __restrict__ K,
+                                                         T* __restrict__ V, float* __restrict__ z, int n_rows) {
+  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
+  __shared__ uint32_t s_slot[64];
+  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
+  const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
+  if (tid < 64) s_slot[tid] = t0 + tid < n_rows ? (uint32_t)slots[t0 + tid] : 0xffffffffu;
+  __syncthreads();
+  uint32_t kc[NP], vc[NP], kb[NP], vb[NP];
+#pragma unroll
+  for (int pass = 0; pass < NP; pass++) {
+    const uint32_t slot = s_slot[pass * RPP + rl];
+    kc[pass] = vc[pass] = kb[pass] = vb[pass] = 0;
+    if (slot < c.n_slots) {
+      const char* page = cache_page(c, slot);
+      const uint32_t at = ((uint32_t)g << c.shift) + cache_place(c, slot);
+      const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + (size_t)at * D);
+      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page) + c.off_scales + (size_t)at * (D / 16);
+      kc[pass] = codes[sub];
+      vc[pass] = codes[LPR + sub];
+      kb[pass] = scales[sub / 4];
+      vb[pass] = scales[D / 32 + sub / 4];
+    }
+  }
+  auto put = [&](T* dst, uint32_t code, uint32_t byte) {
+    const float sc = mx_scale(byte);
+    if constexpr (sizeof(T) == 2) {
+      const uint4 out = make_uint4(
+          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, sc, 0)),
+          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, sc, 1)),
+          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, sc, 2)),
+          __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code, sc, 3)));
+      *reinterpret_cast<uint4*>(dst) = out;
+    } else {
+      const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, sc, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, sc, 1);
+      const auto e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, sc, 2), f = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code, sc, 3);
+      reinterpret_cast<float4*>(dst)[0] = make_float4(a[0], a[1], b[0], b[1]);
+      reinterpret_cast<float4*>(dst)[1] = make_float4(e[0], e[1], f[0], f[1]);
+    }
+  };
+#pragma unroll
+  for (int pass = 0; pass < NP; pass++) {
+    const int t = t0 + pass * RPP + rl;
+    if (t < n_rows) {
+      put(K + ((size_t)t * c.H_kv + g) * D + 8 * sub, kc[pass], kb[pass]);
+      put(V + ((size_t)t * c.H_kv + g) * D + 8 * sub, vc[pass], vb[pass]);
+    }
+  }
+  for (int i = tid; i < G * 64; i += 256) {
+    const int h = g * G + (i >> 6), r = i & 63;
+    if (t0 + r >= n_rows) continue;
+    const uint32_t slot = s_slot[r];
+    float zv = -INFINITY;
+    if (slot < c.n_slots)
+      zv = reinterpret_cast<const float*>(cache_page(c, slot) + c.off_z)[((size_t)h << c.shift) + cache_place(c, slot)];
+    z[(size_t)h * n_rows + t0 + r] = zv;
+  }
+}
+
+template <typename T, int D>
+static void append_t(const dma_cache_shape& s, int n_rows, const void* K, long k_stride, const void* V, long v_stride,
+                     const float* W, const float* A, const float* z, const int32_t* slots, void* pages, hipStream_t st) {
+  const CacheRef c = cache_ref(s, pages);
+  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)s.H_kv);
+  const int G = s.H_q / s.H_kv;
+  const size_t sh = W ? (size_t)G * 64 * 4 : 0;
+#define DMA_APPEND(GM) \
+  cache_append_kernel<T, D, GM><<<grid, 256, sh, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
+  if (G == 1) DMA_APPEND(1);
+  else if (G == 2) DMA_APPEND(2);
+  else DMA_APPEND(4);
+#undef DMA_APPEND
+}
+
+int launch_cache_append(const dma_cache_shape& s, int n_rows, const void* K, long k_stride, const void* V, long v_stride,
+                        const float* W, const float* A, const float* z, const int32_t* slots, void* pages, hipStream_t st) {
+  auto go = [&](auto t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (s.d == 256) append_t<T, 256>(s, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, st);
+    else if (s.d == 128) append_t<T, 128>(s, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, st);
+    else append_t<T, 64>(s, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, st);
+  };
+  if (s.dtype == DMA_BF16) go((__bf16*)nullptr); else go((float*)nullptr);
+  return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
+}
+
+int launch_cache_read(const dma_cache_shape& s, int n_rows, const int32_t* slots, const void* pages, void* K, void* V,
+                      float* z, hipStream_t st) {
+  const CacheRef c = cache_ref(s, pages);
+  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)s.H_kv);
+  auto go = [&](auto t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (s.d == 256) cache_read_kernel<T, 256><<<grid, 256, 0, st>>>(c, slots, (T*)K, (T*)V, z, n_rows);
+    else if (s.d == 128) cache_read_kernel<T, 128><<<grid, 256, 0, st>>>(c, slots, (T*)K, (T*)V, z, n_rows);
+    else cache_read_kernel<T, 64><<<grid, 256, 0, st>>>(c, slots, (T*)K, (T*)V, z, n_rows);
+  };
+  if (s.dtype == DMA_BF16) go((__bf16*)nullptr); else go((float*)nullptr);
+  return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
+}
+
+}  // namespace dma

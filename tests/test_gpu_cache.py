@@ -1,0 +1,431 @@
+"""The paged 4-bit cache on the GPU against the oracle's plain loops."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+import oracle as orc
+from cache_harness import GpuCache, f64, normal
+from oracle import cache_oracle as co
+from paper_2508_02124_amd import binding as B
+
+pytestmark = pytest.mark.gpu
+
+
+# ---------------------------------------------------------------- pages and slots
+def check_assign(cache, change, n_rows):
+    got = [x.cpu().tolist() for x in cache.assign(change, n_rows)]
+    want = cache.model.assign(change, n_rows)
+    for name, x, y in zip(("cu_rows", "row_req", "row_len", "slots", "status"), got, want):
+        assert x == list(y), name
+    assert cache.lens.cpu().tolist() == cache.model.lens
+    assert (cache.table.cpu().numpy() == cache.model.table()).all()
+    free = cache.free.cpu().tolist()
+    assert free[0] == len(cache.model.free) and free[4:4 + free[0]] == cache.model.free
+    return want[4]
+
+
+@pytest.mark.parametrize("n_reqs,n_pages,max_pages,ps,n_rows", [(1, 3, 2, 16, 40), (5, 40, 9, 16, 200), (70, 300, 31, 32, 900),
+                                                               (1025, 3000, 7, 16, 5000), (4096, 9000, 4, 16, 4096), (9, 700, 90, 256, 9001)])
+def test_steps_of_a_server(gpu, n_reqs, n_pages, max_pages, ps, n_rows):
+    print(f"[case] assign {n_reqs} requests {n_pages} pages of {ps}", flush=True)
+    r = np.random.default_rng(n_reqs)
+    cache, seen = GpuCache(gpu, n_reqs, n_pages, max_pages, ps, 2, 1, 64), set()
+    for step in range(8):
+        change = []
+        for b in range(n_reqs):
+            what = r.random()
+            if step and what < 0.1:
+                change.append(-2**31)                                   # the request ends
+            elif step and what < 0.2:
+                change.append(-int(r.integers(1, 2 * ps)))
+            elif what < 0.4:
+                change.append(int(r.integers(1, max_pages * ps // 2 + 2)))
+            elif what < 0.43:
+                change.append(int(r.integers(max_pages * ps, 2**31)))   # never fits
+            else:
+                change.append(int(r.integers(0, 3)))
+        seen |= set(check_assign(cache, change, n_rows))
+    check_assign(cache, [-2**31] * n_reqs, 0)
+    assert cache.free.cpu()[0] == n_pages
+    assert co.SERVED in seen and (n_reqs < 50 or co.TOO_LONG in seen)   # (3 of 100 ask for too much)
+
+
+def test_refusals_in_order(gpu):
+    cache = GpuCache(gpu, 5, 4, 3, 16, 2, 1, 64)
+    assert check_assign(cache, [16, 16, 5, 0, 0], 64) == [0, 0, 0, 0, 0]
+    # request 2 has room in its page; request 0 takes the last page, 1 and 3 find none, 4 wants none
+    assert check_assign(cache, [1, 1, 11, 1, 0], 64) == [0, 1, 0, 1, 0]
+    assert check_assign(cache, [0, -1, 0, 17, 0], 64) == [0, 0, 0, 1, 0]      # request 1 keeps its page: 15 tokens need it
+    assert check_assign(cache, [0, -15, 0, 16, 0], 64) == [0, 0, 0, 0, 0]     # now its page goes over in the same step
+    assert check_assign(cache, [40, 0, 0, 3, 0], 42) == [2, 0, 0, 3, 0]       # 40 too many for it, then rows 40 to 43 of 42
+    assert check_assign(cache, [-2**31] * 5, 0) == [0] * 5
+    assert check_assign(cache, [0] * 5, 0) == [0] * 5
+
+
+# ---------------------------------------------------------------- rows in and out
+def rows_with_edges(gpu, dtype, n, H, d, seed):
+    x = normal(gpu, seed, n, H, d)
+    x[0] = 0.0
+    if n > 3:
+        x[1] *= 1e30
+        x[2] *= 1e-37
+        x[3, :, :32] = 3.0e38                                    # saturates: the largest value is 6 * 2^125
+        x[3, :, 32:64] = torch.tensor([6.0, 5.0, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25], device=gpu).repeat(4) * 2.0 ** -20
+    return x.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H_q,H_kv,d,ps,n", [(2, 2, 64, 16, 1), (8, 2, 128, 32, 65), (6, 1, 256, 64, 70), (4, 4, 128, 256, 130),
+                                             (10, 1, 64, 16, 33)])
+def test_values_and_scores(gpu, dtype, H_q, H_kv, d, ps, n):
+    """Values are exactly those of the definition, the scores those of dma_mask_gen; whatever is not a row's slot stays as it was."""
+    print(f"[case] append {dtype} {H_q}/{H_kv} d={d} ps={ps} n={n}", flush=True)
+    n_pages = n // ps + 3
+    cache = GpuCache(gpu, 1, n_pages, n_pages, ps, H_q, H_kv, d, dtype)
+    K, V = rows_with_edges(gpu, dtype, n, H_kv, d, 1), rows_with_edges(gpu, dtype, n, H_kv, d, 2)
+    V[n // 2] = normal(gpu, 7, H_kv, d).to(V.dtype)
+    if n > 3:
+        V[1:4] /= 2e38                                           # (the scores' sums stay finite)
+    W, A = normal(gpu, 3, H_q, d, scale=d ** -0.5), normal(gpu, 4, H_q)
+    order = torch.randperm(n_pages * ps, generator=torch.Generator().manual_seed(5))[:n]
+    slots = order.to(torch.int32).to(gpu)
+    left_out = {} if n < 9 else {5: -1, 6: n_pages * ps, 7: 2**31 - 1, 8: -2**31}
+    given = slots.clone()
+    for i, s in left_out.items():
+        given[i] = s
+    before = cache.pages.clone()
+    fused = torch.full((n, H_q + 2 * H_kv, d), float("nan"), dtype=cache.type, device=gpu)   # as a projection leaves them
+    fused[:, H_q:H_q + H_kv], fused[:, H_q + H_kv:] = K, V
+    cache.append(fused[:, H_q:H_q + H_kv], fused[:, H_q + H_kv:], given, W, A)
+    gK, gV, gz = cache.read(given)
+    z = torch.empty((H_q, n), device=gpu)
+    s = B.make_shape(n, 1, H_q, H_kv, d, 1, dtype=cache.shape.dtype)
+    mask = torch.empty(B.dma_mask_bytes(s), dtype=torch.uint8, device=gpu)
+    expiry = torch.empty((H_q, n), dtype=torch.int32, device=gpu)
+    B.dma_mask_gen(s, V.contiguous(), W, A, torch.tensor([0, n], dtype=torch.int32, device=gpu), z, expiry, None, mask)
+    there = np.array([i not in left_out for i in range(n)])
+    wantK, wantV, wz = co.quantise(f64(K)), co.quantise(f64(V)), f64(z)
+    assert (f64(gK)[there] == wantK[there]).all() and (f64(gV)[there] == wantV[there]).all()
+    assert (f64(gz)[:, there] == wz[:, there]).all()
+    assert (f64(gK)[~there] == 0).all() and (f64(gV)[~there] == 0).all() and np.isneginf(f64(gz)[:, ~there]).all()
+    assert (np.abs(wz - orc.z_scores(f64(V), f64(W), f64(A), H_q)) <= 1e-5 * np.abs(wz)).all()
+    # only the rows' own bytes changed
+    lay = B.dma_cache_describe(cache.shape)
+    own = torch.zeros((n_pages, lay.page_bytes), dtype=torch.bool)
+    for slot in order[there].tolist():
+        page, t = divmod(slot, ps)
+        own[page, :lay.off_scales].view(H_kv, ps, d)[:, t] = True
+        own[page, lay.off_scales:lay.off_scores].view(H_kv, ps, d // 16)[:, t] = True
+        own[page, lay.off_scores:lay.off_scores + 4 * H_q * ps].view(H_q, ps, 4)[:, t] = True
+    changed = (cache.pages != before).cpu().view(n_pages, -1)
+    assert not (changed & ~own).any()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_blocks_that_are_not_finite(gpu, dtype):
+    cache = GpuCache(gpu, 1, 2, 2, 16, 2, 2, 64, dtype)
+    K, V = normal(gpu, 1, 5, 2, 64).to(cache.type), normal(gpu, 2, 5, 2, 64).to(cache.type)
+    K[0, 0, 3], K[1, 1, 40], V[2, 0, 63], V[3, 1, 0] = float("inf"), float("nan"), -float("inf"), float("nan")
+    z = torch.tensor([[0.5, -float("inf"), 3.0, -0.0, 1e30], [-7.0, 0.0, -3.4028235e38, 2.0, 1e-40]], device=gpu)
+    slots = torch.tensor([3, 31, 0, 16, 9], dtype=torch.int32, device=gpu)
+    cache.append(K, V, slots, z=z)
+    gK, gV, gz = cache.read(slots)
+    assert np.array_equal(f64(gK), co.quantise(f64(K)), equal_nan=True) and np.array_equal(f64(gV), co.quantise(f64(V)), equal_nan=True)
+    assert torch.equal(gz, z)
+
+
+# ---------------------------------------------------------------- decode
+def fill(cache, lens, seed, z="ordinary"):
+    """Requests of these lengths, their pages in no order: several steps whose requests take turns."""
+    left, steps = list(lens), 3
+    parts = []
+    for i in range(steps):
+        change = [min(n, -(-m // steps)) if i < steps - 1 else n for n, m in zip(left, lens)]
+        left = [n - c for n, c in zip(left, change)]
+        rows = sum(change)
+        out = cache.assign(change, rows)
+        assert cache.model.assign(change, rows)[4] == [0] * len(lens) and int(out[4].abs().sum()) == 0
+        if rows:
+            K = normal(cache.dev, seed + 10 * i, rows, cache.H_kv, cache.d).to(cache.type)
+            V = normal(cache.dev, seed + 10 * i + 1, rows, cache.H_kv, cache.d).to(cache.type)
+            cache.append(K, V, out[3], z=scores(z, cache.H_q, rows, seed + i).to(cache.dev))
+            parts.append(out[3])
+
+
+def scores(kind, H, n, seed):
+    r = np.random.default_rng(seed)
+    if kind == "ordinary":
+        z = np.exp(-np.log1p(np.exp(r.standard_normal((H, n)))))
+    elif kind == "equal":
+        z = np.full((H, n), 0.5)
+    elif kind == "levels":
+        z = np.round(r.random((H, n)) * 24) / 24
+    elif kind == "outlier":                     # nearly all scores share a few leading bits
+        z = 0.5 + 1e-3 * r.random((H, n))
+        z[:, n // 3] = 1e-30
+    elif kind == "wide":
+        z = np.exp(12 * r.standard_normal((H, n)))
+        z = np.minimum(z, 60.0)
+    elif kind == "signed":
+        z = r.standard_normal((H, n))
+        z[:, ::7], z[:, 3::7] = 0.0, -0.0
+    elif kind == "masked":                      # a third of the keys out, a third of the others at the type's lowest value
+        z = r.standard_normal((H, n))
+        z[:, ::3] = -np.inf
+        z[:, 1::9] = -3.4028235e38
+    else:
+        raise ValueError(kind)
+    return torch.from_numpy(np.ascontiguousarray(z).astype(np.float32))
+
+
+def request_slots(cache, b):
+    n, ps = cache.model.lens[b], cache.model.ps
+    return np.array([cache.model.tables[b][j // ps] * ps + j % ps for j in range(n)], np.int64)
+
+
+def check_rows(cache, q, k, rows, got, scale=None):
+    """got of the rows [(request, length)] against the oracle on the values that the cache holds.
+
+    With sums in fp32 (u = 2^-24) a score is off by at most E = (d + 4) u (sum |q||k| scale + |z|), a weight by a factor of
+    1 + 2 E + 2^-20 (the exponential, its argument), a sum of n weighted values by n + 16 further roundings; the output by half a step."""
+    o, lse, kept = f64(got[0]), f64(got[1]), got[2].cpu().numpy()
+    scale = cache.d ** -0.5 if scale is None else scale
+    kcap = min(k, cache.cap)
+    half, u = torch.finfo(cache.type).eps / 2, 2.0 ** -24
+    held = {}
+    for r, (b, n) in enumerate(rows):
+        if b not in held:
+            slots = request_slots(cache, b) if b >= 0 else np.zeros(0, np.int64)
+            t = torch.from_numpy(slots.astype(np.int32)).to(cache.dev)
+            held[b] = (slots, *(f64(x) for x in cache.read(t))) if len(slots) else (slots, *[np.zeros((0, cache.H_kv, cache.d))] * 2, np.zeros((cache.H_q, 0)))
+        slots, K, V, z = held[b]
+        ro, rl, rk = co.decode_row(f64(q)[r], K[:n], V[:n], z[:, :n], k, scale)
+        for h in range(cache.H_q):
+            want = np.full(kcap, -1)
+            want[: len(rk[h])] = slots[rk[h]]
+            assert (kept[r, h] == want).all(), (r, h)
+            if np.isneginf(rl[h]):
+                assert np.isneginf(lse[h, r]) and (o[r, h] == 0).all(), (r, h)
+                continue
+            g, use = h // (cache.H_q // cache.H_kv), rk[h][~np.isneginf(z[h, rk[h]])]
+            zu = z[h, use]
+            s = K[use, g] @ f64(q)[r, h] * scale + zu
+            p = np.exp(s - rl[h])
+            live = zu > -1e30
+            E = (cache.d + 4) * u * (np.abs(K[use, g]) @ np.abs(f64(q)[r, h]) * scale + np.where(live, np.abs(zu), 0.0)).max()
+            w = 2 * E + 2.0 ** -20 + (len(use) + 16) * u
+            bound = w * (p @ np.abs(V[use, g])) + half * np.abs(ro[h]) * (1 + w)
+            assert (np.abs(o[r, h] - ro[h]) <= bound + 1e-37).all(), (r, h, np.abs(o[r, h] - ro[h]).max(), bound.min())
+            assert abs(lse[h, r] - rl[h]) <= w + 2.0 ** -22 * abs(rl[h]), (r, h, lse[h, r], rl[h])
+
+
+CASES = [((1, 15, 16, 17, 0), 8), ((255, 256, 257, 40), 64), ((1023, 3, 700), 5000), ((2049, 1025), 1024), ((4100, 0, 515), 1)]
+
+
+@pytest.mark.parametrize("kind", ["ordinary", "equal", "levels", "outlier", "wide", "signed", "masked"])
+@pytest.mark.parametrize("lens,k", CASES)
+def test_kept_sets_and_outputs(gpu, kind, lens, k):
+    print(f"[case] decode {kind} {lens} k={k}", flush=True)
+    ps = 16 if max(lens) < 2000 else 64
+    per = -(-max(lens) // ps)
+    cache = GpuCache(gpu, len(lens), sum(-(-n // ps) for n in lens) + 2, per, ps, 4, 2, 64)
+    fill(cache, lens, 31, kind)
+    q = normal(gpu, 5, len(lens), 4, 64).to(cache.type)
+    got = cache.decode(q, k, None, cache.lens)
+    check_rows(cache, q, k, list(enumerate(lens)), got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H_q,H_kv,d,ps", [(3, 1, 64, 16), (8, 2, 128, 32), (6, 6, 256, 64), (16, 1, 128, 128), (5, 5, 64, 256)])
+def test_heads_types_and_drafts(gpu, dtype, H_q, H_kv, d, ps):
+    """Rows of several lengths of a request, rows that see nothing, queries inside a projection's output, a scale of their own."""
+    print(f"[case] decode {dtype} {H_q}/{H_kv} d={d} ps={ps}", flush=True)
+    lens = (700, 1, 290, 0)
+    cache = GpuCache(gpu, 4, sum(-(-n // ps) for n in lens) + 3, -(-700 // ps) + 1, ps, H_q, H_kv, d, dtype)
+    fill(cache, lens, 77)
+    rows = [(0, 700), (0, 699), (0, 513), (1, 1), (-1, 9), (2, 290), (2, 0), (3, 0), (2, 1), (0, 256)]
+    fused = normal(gpu, 6, len(rows), H_q + 2 * H_kv, d).to(cache.type)
+    q = fused[:, :H_q]
+    req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
+    length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
+    seen = [(b, n if b >= 0 else 0) for b, n in rows]
+    for k, scale in ((300, 0.0), (1000, 0.25)):
+        got = cache.decode(q, k, req, length, scale)
+        check_rows(cache, q, k, seen, got, scale or None)
+
+
+def test_many_rows_of_long_lists(gpu):
+    """Enough rows and heads that a workgroup takes longer parts of the lists, and more parts than one round of the merge."""
+    lens = (5000, 4000, 300, 2500)
+    cache = GpuCache(gpu, 4, 800, 320, 16, 32, 8, 64)
+    fill(cache, lens, 13)
+    rows = [(b, n - i) for b, n in enumerate(lens) for i in range(3)]
+    q = normal(gpu, 9, len(rows), 32, 64).to(cache.type)
+    req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
+    length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
+    check_rows(cache, q, 4600, rows, cache.decode(q, 4600, req, length))
+
+
+def test_masked_keys_take_no_part(gpu):
+    """A key with a score of -infinity counts for nothing, whatever its K and V hold; a row that keeps only such keys is empty."""
+    cache = GpuCache(gpu, 2, 8, 4, 16, 2, 1, 128)
+    cache.assign([40, 20], 60)
+    slots = cache.model.assign([40, 20], 60)[3]
+    K, V = normal(gpu, 1, 60, 1, 128).to(cache.type), normal(gpu, 2, 60, 1, 128).to(cache.type)
+    z = scores("ordinary", 2, 60, 3)
+    K[5], V[5], V[6], K[7] = float("nan"), float("inf"), float("nan"), float("inf")
+    z[:, 5:8] = -float("inf")
+    z[1, 40:] = -float("inf")
+    cache.append(K, V, torch.tensor(slots, dtype=torch.int32, device=gpu), z=z.to(gpu))
+    q = normal(gpu, 4, 2, 2, 128).to(cache.type)
+    for k in (64, 39, 7):
+        got = cache.decode(q, k, None, cache.lens)
+        assert torch.isfinite(got[0].float()).all()
+        assert np.isneginf(f64(got[1])[1, 1]) and np.isfinite(f64(got[1])[0]).all()
+        check_rows(cache, q, k, [(0, 40), (1, 20)], got)
+    bad = torch.tensor([0.0, float("nan")], device=gpu)[:, None].expand(2, 60).contiguous()       # head 1: scores that are not numbers
+    cache.append(normal(gpu, 1, 60, 1, 128).to(cache.type), normal(gpu, 2, 60, 1, 128).to(cache.type),
+                 torch.tensor(slots, dtype=torch.int32, device=gpu), z=bad)
+    o, lse, _ = cache.decode(q, 16, None, cache.lens)
+    assert torch.isfinite(o[:, 0].float()).all() and torch.isnan(o[:, 1]).all() and torch.isnan(lse[1]).all()
+
+
+def test_pages_that_are_not_there(gpu):
+    """Page numbers and requests out of range are keys and rows that are missing; lengths beyond the table end with it."""
+    cache = GpuCache(gpu, 3, 9, 3, 16, 2, 1, 64)
+    fill(cache, (48, 33, 16), 3)
+    q = normal(gpu, 4, 5, 2, 64).to(cache.type)
+    table = cache.table.clone()
+    table[0, 1], table[1, 0], table[1, 2] = 9, -5, 2**31 - 1
+    req = torch.tensor([0, 1, 2, 3, -4], dtype=torch.int32, device=gpu)
+    length = torch.tensor([48, 2**31 - 1, -3, 7, 7], dtype=torch.int32, device=gpu)
+    o, lse, kept = cache.decode(q, 40, req, length, table=table)
+    assert (f64(o)[2:] == 0).all() and np.isneginf(f64(lse)[:, 2:]).all() and (kept[2:] == -1).all()
+    for b, there in ((0, [0, 2]), (1, [1])):
+        slots = np.concatenate([np.arange(16) + 16 * int(table[b, p]) for p in there])
+        n = 48
+        K, V, z = (f64(x) for x in cache.read(torch.tensor(slots, dtype=torch.int32, device=gpu)))
+        ro, rl, rk = co.decode_row(f64(q)[b], K, V, z, 40, 64 ** -0.5)
+        for h in range(2):
+            got = kept[b, h].cpu().numpy()
+            assert sorted(got[got >= 0]) == sorted(slots[rk[h]]) and len(got) == 40
+            assert np.abs(f64(o)[b, h] - ro[h]).max() <= 2.0 ** -8 * np.abs(ro[h]).max() + 1e-4 and abs(f64(lse)[h, b] - rl[h]) < 1e-4
+            if b == 0:       # 32 keys that are there, then eight of the missing ones in their places
+                assert (got >= 0).sum() == 32 and (got[:16] == slots[:16]).all()
+
+
+def test_offsets_beyond_four_gigabytes(gpu):
+    n_pages = 8000
+    cache = GpuCache(gpu, 1, 1, 1, 256, 8, 8, 256)
+    cache.shape = B.make_cache_shape(1, n_pages, 4, 256, 8, 8, 256)
+    assert B.dma_cache_bytes(cache.shape) > 1 << 32
+    cache.pages, cache.cap = torch.empty(B.dma_cache_bytes(cache.shape), dtype=torch.uint8, device=gpu), 4 * 256
+    cache.table = torch.tensor([[7999, 0, 7990, -1]], dtype=torch.int32, device=gpu)
+    cache.model = co.Pages(1, 1, 4, 256)
+    cache.model.tables, cache.model.lens = [[7999, 0, 7990]], [700]
+    slots = torch.from_numpy(request_slots(cache, 0).astype(np.int32)).to(gpu)
+    K, V = normal(gpu, 1, 700, 8, 256).to(cache.type), normal(gpu, 2, 700, 8, 256).to(cache.type)
+    cache.append(K, V, slots, z=scores("ordinary", 8, 700, 3).to(gpu))
+    assert (f64(cache.read(slots)[0])[::50] == co.quantise(f64(K[::50]))).all()
+    q = normal(gpu, 4, 1, 8, 256).to(cache.type)
+    got = cache.decode(q, 300, None, torch.tensor([700], dtype=torch.int32, device=gpu))
+    check_rows(cache, q, 300, [(0, 700)], got)
+
+
+# ---------------------------------------------------------------- together
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_serving_loop(gpu, dtype):
+    """Prompts, single tokens, drafts taken back, requests that end and new ones in their places: after every step each
+    row equals dma_decode over the rows read back."""
+    print(f"[case] serving loop {dtype}", flush=True)
+    H_q, H_kv, d, k = 8, 2, 128, 100
+    cache = GpuCache(gpu, 4, 60, 20, 16, H_q, H_kv, d, dtype)
+    W, A = normal(gpu, 3, H_q, d, scale=d ** -0.5), -torch.ones(H_q, device=gpu)
+    script = [[150, 40, 0, 1], [1, 1, 1, 1], [3, 3, 3, 3], [-2, -1, 0, -3], [1, -2**31, 200, 1], [1, 90, 1, 1]]
+    for step, change in enumerate(script):
+        rows = sum(max(0, c) for c in change) + 2                 # (two rows more than there are)
+        cu, req, length, slots, status = cache.assign(change, rows)
+        assert list(cache.model.assign(change, rows)[4]) == [0] * 4 == status.cpu().tolist()
+        qkv = normal(gpu, 100 + step, rows, H_q + 2 * H_kv, d).to(cache.type)
+        q, K, V = qkv.split((H_q, H_kv, H_kv), 1)
+        cache.append(K, V, slots, W, A)
+        got = cache.decode(q, k, req, length)
+        pairs = list(zip(req.cpu().tolist(), length.cpu().tolist()))
+        some = [i for i, (b, n) in enumerate(pairs) if b < 0 or n > cache.model.lens[b] - 4]     # the last rows of each prompt
+        check_rows(cache, q[some], k, [pairs[i] for i in some], (got[0][some], got[1][:, some], got[2][some]))
+        for b in range(4):
+            n = cache.model.lens[b]
+            mine = [i for i, (x, m) in enumerate(pairs) if x == b and m == n]
+            if not mine:
+                continue
+            at = request_slots(cache, b)
+            Kb, Vb, zb = cache.read(torch.from_numpy(at.astype(np.int32)).to(gpu))
+            s = B.make_shape(n, 1, H_q, H_kv, d, k, dtype=cache.shape.dtype)
+            size = B.dma_decode_kept_bytes(s)
+            kept = torch.empty(size // 4, dtype=torch.int32, device=gpu)
+            o, lse = torch.empty((1, H_q, d), dtype=cache.type, device=gpu), torch.empty((H_q, 1), device=gpu)
+            B.dma_decode(s, q[mine[0]].contiguous(), Kb, Vb, zb, torch.tensor([0, n], dtype=torch.int32, device=gpu), o, lse, kept, size)
+            m = min(k, n)
+            lists = kept[: H_q * m].view(H_q, m).cpu().numpy()
+            assert (at[lists] == got[2][mine[0], :, :m].cpu().numpy()).all()
+            half = torch.finfo(cache.type).eps / 2
+            a, c = f64(o)[0], f64(got[0])[mine[0]]
+            assert (np.abs(a - c) <= 2 * half * np.maximum(np.abs(a), np.abs(c)) + 2e-5).all()
+
+
+def test_captured_step_replays(gpu):
+    """assign, append and decode in one graph, with eager work of another cache and synchronizations between the replays."""
+    H_q, H_kv, d, k = 4, 2, 64, 50
+
+    def run(captured):
+        cache, other = GpuCache(gpu, 3, 30, 10, 16, H_q, H_kv, d), GpuCache(gpu, 3, 30, 10, 16, H_q, H_kv, d)
+        fill(cache, (60, 3, 100), 5)
+        fill(other, (20, 90, 7), 6)
+        qkv = normal(gpu, 8, 6, H_q + 2 * H_kv, d).to(cache.type)
+        q, K, V = qkv.split((H_q, H_kv, H_kv), 1)
+        W, A = normal(gpu, 3, H_q, d, scale=d ** -0.5), -torch.ones(H_q, device=gpu)
+        change = torch.tensor([1, 2, 1], dtype=torch.int32, device=gpu)
+        rows = [cache.ints(4), cache.ints(6), cache.ints(6), cache.ints(6), cache.ints(3)]
+        o, lse = torch.zeros((6, H_q, d), dtype=cache.type, device=gpu), torch.zeros((H_q, 6), device=gpu)
+        kept, size = cache.ints(6, H_q, k), B.dma_cache_decode_bytes(cache.shape, 6, k)
+        ws = torch.empty(max(size, 16), dtype=torch.uint8, device=gpu)
+
+        def step():
+            B.dma_cache_assign(cache.shape, 6, change, cache.lens, cache.table, cache.free, *rows)
+            B.dma_cache_append(cache.shape, 6, K, K.stride(0), V, V.stride(0), W, A, None, rows[3], cache.pages)
+            B.dma_cache_decode(cache.shape, 6, k, 0.0, q, q.stride(0), cache.pages, cache.table, rows[1], rows[2], o, lse, kept, ws, size)
+
+        torch.cuda.synchronize()
+        if captured:
+            graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+            with torch.cuda.graph(graph, stream=side):
+                step()
+        out = []
+        for _ in range(5):
+            graph.replay() if captured else step()
+            other.decode(q[:3].contiguous(), k, None, other.lens)
+            torch.cuda.synchronize()
+            out.append([x.cpu().clone() for x in (*rows, cache.lens, o, lse, kept)])
+        return out
+
+    for a, b in zip(run(False), run(True)):
+        for x, y in zip(a, b):
+            assert torch.equal(x, y)
+
+
+def test_another_stream(gpu):
+    cache = GpuCache(gpu, 2, 12, 6, 16, 4, 2, 64)
+    fill(cache, (70, 33), 5)
+    q = normal(gpu, 5, 2, 4, 64).to(cache.type)
+    want = cache.decode(q, 30, None, cache.lens)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    got = cache.decode(q, 30, None, cache.lens, stream=side)      # (its buffers were filled on the current stream)
+    torch.cuda.synchronize()
+    with torch.cuda.stream(side):
+        again = cache.decode(q, 30, None, cache.lens)
+    torch.cuda.synchronize()
+    for x, y, z in zip(want, got, again):
+        assert torch.equal(x, z)

@@ -314,8 +314,8 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
  * at which the largest of the 32 rounds to at most 6 (byte 2 to 252), values go to the nearest code, ties to the even one: an
  * error of at most a fifth of the largest value of the 32.  A block with an infinity or NaN has byte 255 and reads as NaN.
  *
- * Numbers of pages, slots and requests in device memory are checked where they are used: one out of range is a key (or row)
- * that is not there, never an address.  Calls that write the same arrays must be ordered by the caller (one stream).
+ * Numbers of pages, slots and requests in device memory are checked where they are used: one out of range is a row that is not
+ * there, never an address.  Calls that write the same arrays must be ordered by the caller (one stream).
  */
 typedef struct {
   int32_t n_reqs;      /* places for requests, 1 to 4096                                        */
@@ -397,10 +397,10 @@ int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* 
  *   q        in  n_rows rows of [H_q, d], q_stride elements apart (a multiple of 8 of at least H_q * d)
  *   row_req  in  nullable: row r is then request r (n_rows <= n_reqs), and seq_lens may serve as row_len
  *   softmax_scale  0 => d^-1/2
- *   o        out [n_rows, H_q, d];  lse out [H_q, n_rows], natural log.  A row that sees nothing, or nothing but scores of
- *                -infinity: o = 0, lse = -infinity
+ *   o        out [n_rows, H_q, d];  lse out [H_q, n_rows], natural log.  A row that sees nothing (no request, no keys, or a page out
+ *                of range among its own), or nothing but scores of -infinity: o = 0, lse = -infinity
  *   kept     out [n_rows, H_q, min(k, max_pages * page_size)] int32: the slots of the kept keys in order of position, -1 behind
- *                them (and for keys whose page is out of range)
+ *                them
  *   ws       dma_cache_decode_bytes(shape, n_rows, k) bytes of scratch; calls that overlap need one each
  * DMA_EUNSUPPORTED where (n_rows + 8) * H_q * ceil(min(k, max_pages * page_size) / 256) reaches 2^22: a whole prompt goes through
  * dma_mask_gen and dma_fwd.

@@ -16,13 +16,13 @@ struct CacheRow {
   int n;
 };
 __device__ __forceinline__ CacheRow cache_row(const CacheRef& c, const CacheRows& p, int r) {
-  const int b = p.row_req ? p.row_req[r] : r;
-  if (b < 0 || b >= c.n_reqs) return {p.table, 0};
+  const int len = p.row_len[r], b = p.row_req ? p.row_req[r] : r;  // (requested together)
+  const bool there = b >= 0 && b < c.n_reqs;
   const long long cap = (long long)c.max_pages << c.shift;
-  return {p.table + (size_t)b * c.max_pages, (int)max(0ll, min((long long)p.row_len[r], cap))};
+  return {p.table + (size_t)(there ? b : 0) * c.max_pages, there ? (int)max(0ll, min((long long)len, cap)) : 0};
 }
 
-// Slot and score of position j (a page number out of range: no slot, and a score behind all others).
+// Slot of position j, and a slot's score (a page number out of range: no slot, and a score behind all others).
 __device__ __forceinline__ uint32_t cache_slot(const CacheRef& c, const CacheRow& row, int j) {
   const uint32_t page = (uint32_t)row.pages[j >> c.shift];
   return page < (uint32_t)c.n_pages ? page << c.shift | ((uint32_t)j & ((1u << c.shift) - 1u)) : 0xffffffffu;
@@ -32,71 +32,350 @@ __device__ __forceinline__ float cache_score(const CacheRef& c, uint32_t slot, i
   return reinterpret_cast<const float*>(cache_page(c, slot) + c.off_z)[((size_t)h << c.shift) + cache_place(c, slot)];
 }
 
-// ------------------------------------------------------------------ the kept set
-// One workgroup per (row, head): the threshold digit by digit, then the list in order of position.
-__global__ __launch_bounds__(1024) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept) {
-  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q;
+// ------------------------------------------------------------------ scores of chunks of positions
+// A wave reads 64 consecutive positions at a time (a chunk), every NW-th chunk.  The page numbers of its 64 next chunks are one
+// load (S = 1: pages of 64 tokens or more, one page a chunk) or four (S = 4: lane l has the pages of the quarters of the l-th); a
+// chunk's page then comes out of a lane into a scalar register, and so does the address.
+template <int S> struct PageRun {
+  uint32_t pg[S];
+  // The pages of the chunks first, first + step, ... of a row (the last entries of the table for those behind its end).
+  __device__ __forceinline__ void load(const CacheRef& c, const CacheRow& row, int first, int step, int l) {
+#pragma unroll
+    for (int q = 0; q < S; q++) pg[q] = (uint32_t)row.pages[min((64 * (first + step * l) + 16 * q) >> c.shift, c.max_pages - 1)];
+  }
+  // Whether one of them, of the row's n positions, is out of range (it is page 0 from here on).
+  __device__ __forceinline__ bool check(const CacheRef& c, int n, int first, int step, int l) {
+    bool bad = false;
+#pragma unroll
+    for (int q = 0; q < S; q++) {
+      const bool out = pg[q] >= (uint32_t)c.n_pages;
+      bad |= out && 64 * (first + step * l) + 16 * q < n;
+      pg[q] = out ? 0u : pg[q];
+    }
+    return __ballot(bad) != 0;
+  }
+  // page of this lane's position in the u-th chunk
+  __device__ __forceinline__ uint32_t page(int u, int l) const {
+    uint32_t x = (uint32_t)__builtin_amdgcn_readlane((int)pg[0], u);
+#pragma unroll
+    for (int q = 1; q < S; q++) {
+      const uint32_t y = (uint32_t)__builtin_amdgcn_readlane((int)pg[q], u);
+      x = l >= 16 * q ? y : x;
+    }
+    return x;
+  }
+  // The score of this lane's position in it (read also where the row has ended: a place of some page); j: the chunk's first
+  // position, scores: those of page 0.
+  __device__ __forceinline__ float score(const CacheRef& c, const char* scores, int j, int u, int l) const {
+    const uint32_t mask = (1u << c.shift) - 1u;
+    const float* z = reinterpret_cast<const float*>(scores + (size_t)page(u, l) * c.page_bytes);
+    return S == 1 ? (z + ((uint32_t)j & mask))[l] : z[(uint32_t)l & mask];
+  }
+  __device__ __forceinline__ int32_t slot(const CacheRef& c, int j, int u, int l) const {
+    const uint32_t mask = (1u << c.shift) - 1u, first = page(u, l) << c.shift;
+    return (int32_t)(S == 1 ? (first | ((uint32_t)j & mask)) | (uint32_t)l : first | ((uint32_t)l & mask));
+  }
+};
+
+// Keys ascend from the best score to the worst, -0 and +0 the same; NO_KEY is behind every score's.
+constexpr uint32_t NO_KEY = 0xffffffffu;
+__device__ __forceinline__ uint32_t score_key(float z) { return min(desc_key(z), NO_KEY - 1); }
+__device__ __forceinline__ uint32_t lanes_before(unsigned long long m) {
+  return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
+}
+
+// ------------------------------------------------------------------ the kept set by one workgroup
+// The chunks of a row go round the waves, R to each; a lane holds its keys in registers (longer rows: in rounds of as many, read
+// again in every pass).  A histogram of 1024 equal bins between the row's smallest and largest key finds the bin of the kk-th best.
+// Keys before the bin are counted chunk by chunk; those of the bin move to LDS, each wave's to places of its own, where each
+// counts those before it, by key and position, and adds itself to its chunk's count if it is kept.  A scan of the counts says where the
+// chunks' slots go.  (A bin of many keys, ties above all, is narrowed down digit by digit, and the chunks are counted afterwards.)
+// What bounds it is the chain: the row, its pages, the scores, and six barriers with a few LDS accesses between.  So the
+// chunks do not depend on the length (the page numbers are on their way before it is known), and nothing goes through an atomic
+// that returns.
+template <int NT> struct SelectShared {
+  static constexpr int REP = 4, BITS = 10, NDIG = 1 << BITS, NW = NT / 64, NEAR = NT / NW;  // keys of a bin that a wave can list
+  __align__(16) uint32_t hist[NDIG * REP];
+  __align__(16) uint32_t near[NT];  // entry e of wave w at e * NW + w
+  uint32_t near_pos[NT];
+  __align__(16) uint32_t kept[256], equal[256];  // per chunk of a round
+  uint32_t wsum[NW][2];
+  uint32_t st[4];
+};
+
+// The digit at which the running count of the histogram reaches `remaining` (st[0..2]); leaves it cleared.
+template <int NT> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m, uint32_t remaining) {
+  constexpr int DPT = SelectShared<NT>::NDIG / NT;
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
-  const CacheRow row = cache_row(c, p, r);
-  const int n = row.n, kk = min(p.k, n);
-  int32_t* list = kept + (size_t)rh * p.kcap;
-  for (int i = kk + tid; i < p.kcap; i += 1024) list[i] = -1;
-  if (kk == n) {
-    for (int j = tid; j < n; j += 1024) list[j] = (int32_t)cache_slot(c, row, j);
-    return;
+  uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
+  __syncthreads();
+  uint32_t cn[DPT], sum = 0;  // this thread's digits
+#pragma unroll
+  for (int i = 0; i < DPT; i++) {
+    const uint4 x = hist4[DPT * tid + i];
+    hist4[DPT * tid + i] = make_uint4(0, 0, 0, 0);
+    cn[i] = x.x + x.y + x.z + x.w;
+    sum += cn[i];
   }
-  __shared__ uint32_t hist[256], s_prefix, s_left, wsum[16][2];
-  uint32_t prefix = 0, left = (uint32_t)kk;
-  for (int pass = 3; pass >= 0; pass--) {
-    if (tid < 256) hist[tid] = 0;
-    __syncthreads();
-    for (int j = tid; j < n; j += 1024) {
-      const uint32_t key = desc_key(cache_score(c, cache_slot(c, row, j), h));
-      if (pass == 3 || key >> (8 * pass + 8) == prefix) atomicAdd(&hist[(key >> (8 * pass)) & 255u], 1u);
+  const uint32_t inc = wave_scan(sum, 0u, [](uint32_t x, uint32_t y) { return x + y; });
+  if (l == 63) m.wsum[w][0] = inc;
+  __syncthreads();
+  uint32_t run = inc - sum;
+#pragma unroll
+  for (int i = 0; i < NT / 64; i++) run += i < w ? m.wsum[i][0] : 0u;
+#pragma unroll
+  for (int i = 0; i < DPT; i++) {
+    if (run < remaining && remaining <= run + cn[i]) {  // exactly one digit of one thread
+      m.st[0] = (uint32_t)(DPT * tid + i);
+      m.st[1] = remaining - run;
+      m.st[2] = cn[i];
     }
-    __syncthreads();
-    if (tid == 0) {
-      uint32_t digit = 0, run = 0;
-      while (run + hist[digit] < left) run += hist[digit++];
-      s_prefix = prefix << 8 | digit;
-      s_left = left - run;
-    }
-    __syncthreads();
-    prefix = s_prefix;
-    left = s_left;
-  }
-  // keys before the threshold, and the first `left` of those equal to it
-  const int per = (n + 16 * 64 - 1) / (16 * 64) * 64, j0 = w * per, j1 = min(n, j0 + per);
-  uint32_t better = 0, equal = 0;
-  for (int jb = j0; jb < j1; jb += 64) {
-    const int j = jb + l;
-    const uint32_t key = j < j1 ? desc_key(cache_score(c, cache_slot(c, row, j), h)) : 0xffffffffu;
-    better += (uint32_t)__popcll(__ballot(j < j1 && key < prefix));
-    equal += (uint32_t)__popcll(__ballot(j < j1 && key == prefix));
-  }
-  if (l == 0) {
-    wsum[w][0] = better;
-    wsum[w][1] = equal;
+    run += cn[i];
   }
   __syncthreads();
-  better = equal = 0;
-  for (int i = 0; i < w; i++) {
-    better += wsum[i][0];
-    equal += wsum[i][1];
+}
+
+// Exclusive sums of a table of 256 counts at the entries u * 8 + w of this wave: entry u comes out of lane 2 u + w / 4.
+__device__ __forceinline__ uint32_t chunk_offsets(const uint32_t* counts, int w, int l, uint32_t& total) {
+  const uint4 x = reinterpret_cast<const uint4*>(counts)[l];
+  const uint32_t sum = x.x + x.y + x.z + x.w, inc = wave_scan(sum, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+  total = last_lane(inc);
+  const int i = w & 3;
+  return inc - sum + (i > 0 ? x.x : 0u) + (i > 1 ? x.y : 0u) + (i > 2 ? x.z : 0u);
+}
+
+template <int NT, int R, int S, bool LONG>
+__device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& row, int h, int kk, int32_t* list, SelectShared<NT>& m) {
+  using M = SelectShared<NT>;
+  constexpr int NW = M::NW, REP = M::REP, BITS = M::BITS, NDIG = M::NDIG, NEAR = M::NEAR, STEP = 4;
+  static_assert(NW == 8 && R <= 32 && R % STEP == 0, "");
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
+  const char* scores = c.pages + c.off_z + ((size_t)h << c.shift) * 4;
+  const int rounds = LONG ? (n + NW * R * 64 - 1) / (NW * R * 64) : 1;
+  PageRun<S> run;
+  uint32_t key[R];
+  bool bad = false;
+  auto chunk = [&](int round, int u) { return ((round * R + u) * NW + w) * 64; };  // its first position
+  auto fetch = [&](int round) {
+    if (LONG) run.load(c, row, round * R * NW + w, NW, l);
+    bad |= run.check(c, n, round * R * NW + w, NW, l);
+#pragma unroll
+    for (int u = 0; u < R; u++) key[u] = NO_KEY;
+#pragma unroll
+    for (int u0 = 0; u0 < R; u0 += STEP)
+      if ((round * R + u0) * NW * 64 < n) {
+#pragma unroll
+        for (int u = u0; u < u0 + STEP; u++) key[u] = __float_as_uint(run.score(c, scores, chunk(round, u), u, l));
+        __builtin_amdgcn_sched_barrier(0);  // (addresses of all chunks at once would spill)
+      }
+  };
+  auto to_keys = [&](int round) {
+#pragma unroll
+    for (int u = 0; u < R; u++)
+      if ((round * R + u / STEP * STEP) * NW * 64 < n) key[u] = l < n - chunk(round, u) ? score_key(__uint_as_float(key[u])) : NO_KEY;
+  };
+  // f(key, u) for the keys of a round; positions behind the row's end have NO_KEY
+  auto each = [&](int round, auto f) {
+    int left = n - round * R * NW * 64;
+    asm volatile("" : "+s"(left));  // (comparisons kept from one pass to the next would spill)
+#pragma unroll
+    for (int u0 = 0; u0 < R; u0 += STEP)
+      if (u0 * NW * 64 < left) {
+#pragma unroll
+        for (int u = u0; u < u0 + STEP; u++) f(key[u], u);
+      }
+  };
+  auto every = [&](auto f) {
+    if constexpr (!LONG) {
+      each(0, f);
+    } else {
+      for (int round = 0; round < rounds; round++) {
+        fetch(round);
+        to_keys(round);
+        each(round, f);
+      }
+    }
+  };
+  uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
+  uint32_t kmin = NO_KEY, kmax = 0;
+  if (!LONG) run.load(c, row, w, NW, l);
+  for (int i = tid; i < NDIG; i += NT) hist4[i] = make_uint4(0, 0, 0, 0);
+  m.near[tid] = NO_KEY;
+  if (tid == 0) m.st[3] = NO_KEY;
+  if (!LONG) {
+    fetch(0);
+    to_keys(0);
   }
-  const unsigned long long before = (1ull << l) - 1ull;
-  for (int jb = j0; jb < j1; jb += 64) {
-    const int j = jb + l;
-    const uint32_t slot = j < j1 ? cache_slot(c, row, j) : 0xffffffffu;
-    const uint32_t key = j < j1 ? desc_key(cache_score(c, slot, h)) : 0xffffffffu;
-    const bool b = j < j1 && key < prefix, e = j < j1 && key == prefix;
-    const unsigned long long bm = __ballot(b), em = __ballot(e);
-    const uint32_t eq = equal + (uint32_t)__popcll(em & before);
-    const uint32_t at = better + (uint32_t)__popcll(bm & before) + min(eq, left);
-    if (b || (e && eq < left)) list[at] = (int32_t)slot;
-    better += (uint32_t)__popcll(bm);
-    equal += (uint32_t)__popcll(em);
+  every([&](uint32_t k32, int) {
+    kmin = min(kmin, k32);
+    kmax = max(kmax, k32 == NO_KEY ? 0u : k32);
+  });
+  kmin = last_lane(wave_scan(kmin, NO_KEY, [](uint32_t x, uint32_t y) { return min(x, y); }));
+  kmax = last_lane(wave_scan(kmax, 0u, [](uint32_t x, uint32_t y) { return max(x, y); }));
+  if (l == 0) {
+    m.wsum[w][0] = kmin;
+    m.wsum[w][1] = bad ? NO_KEY : kmax;
   }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; i++) {
+    kmin = min(kmin, m.wsum[i][0]);
+    kmax = max(kmax, m.wsum[i][1]);
+  }
+  if (kmax == NO_KEY) {  // a page is out of range: the row sees nothing
+    for (int i = tid; i < kk; i += NT) list[i] = -1;
+    return;
+  }
+  kmin = (uint32_t)__builtin_amdgcn_readfirstlane((int)kmin);
+  const uint32_t range = (uint32_t)__builtin_amdgcn_readfirstlane((int)(kmax - kmin));
+  const int sh0 = max(0, 32 - (range ? __clz((int)range) : 32) - BITS);  // (key - kmin) >> sh0 < NDIG
+  // (positions without a key count in the last bin, behind every key of it)
+  every([&](uint32_t k32, int) {
+    atomicAdd(&m.hist[min((k32 - kmin) >> sh0, (uint32_t)NDIG - 1) * REP + (l & (REP - 1))], 1u);
+  });
+  pick_digit<NT>(m, (uint32_t)kk);
+  const uint32_t base = kmin + (m.st[0] << sh0);  // first key of the bin
+  uint32_t need_eq = m.st[1], n_eq = m.st[2], sub = 0;
+  auto put = [&](int round, uint32_t at, auto keeps) {  // keeps(key, position - chunk's first)
+#pragma unroll
+    for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));  // (the pages out of their lanes again, not kept since the scores)
+    each(round, [&](uint32_t k32, int u) {
+      const unsigned long long k = __ballot(keeps(k32, u));
+      if (k) {
+        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2));
+        const int32_t x = run.slot(c, chunk(round, u), u, l);
+        if (keeps(k32, u)) list[first + lanes_before(k)] = x;
+      }
+    });
+  };
+  if constexpr (!LONG) {
+    uint32_t kept = 0, count = 0;  // lane u: keys of this wave's chunk u that are before the bin; the wave's keys of the bin
+    each(0, [&](uint32_t k32, int u) {
+      const uint32_t b = (uint32_t)__popcll(__ballot(k32 < base));
+      kept = l == u ? b : kept;
+      const bool in = ((k32 - base) >> sh0) == 0 && k32 != NO_KEY;
+      const unsigned long long in_bin = __ballot(in);
+      if (in_bin) {
+        const uint32_t e = count + lanes_before(in_bin);
+        if (in && e < NEAR) {
+          m.near[e * NW + w] = k32 - base;
+          m.near_pos[e * NW + w] = (uint32_t)(chunk(0, u) + l);
+        }
+        count += (uint32_t)__popcll(in_bin);
+      }
+    });
+    if (l < 32) m.kept[l * NW + w] = kept;
+    if (l == 0) m.wsum[w][1] = count;
+    __syncthreads();
+    uint32_t most = 0;
+#pragma unroll
+    for (int i = 0; i < NW; i++) most = max(most, m.wsum[i][1]);
+    if (most <= NEAR) {
+      const uint32_t x = m.near[tid];
+      if (x != NO_KEY) {
+        uint32_t less = 0, equal = 0;
+        for (uint32_t i = 0; i < most * NW; i += 8) {
+          const uint4 q = *reinterpret_cast<const uint4*>(&m.near[i]), r = *reinterpret_cast<const uint4*>(&m.near[i + 4]);
+          const uint32_t cs[8] = {q.x, q.y, q.z, q.w, r.x, r.y, r.z, r.w};
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            less += cs[e] < x;
+            equal += cs[e] == x;
+          }
+        }
+        const uint32_t pos = m.near_pos[tid];
+        if (equal > 1)
+          for (uint32_t i = 0; i < most * NW; i++) less += m.near[i] == x && m.near_pos[i] < pos;
+        if (less < need_eq) atomicAdd(&m.kept[pos >> 6], 1u);
+        if (less + 1 == need_eq) {  // the last one that is kept, and the first that is not
+          m.st[0] = x;
+          m.st[1] = pos;
+        }
+        if (less == need_eq) m.st[3] = x;
+      }
+      __syncthreads();
+      const uint32_t thr = (uint32_t)__builtin_amdgcn_readfirstlane((int)(base + m.st[0]));
+      const int last = __builtin_amdgcn_readfirstlane((int)m.st[1]);
+      uint32_t total;
+      const uint32_t at = chunk_offsets(m.kept, w, l, total);
+      if (m.st[3] != m.st[0]) put(0, at, [&](uint32_t k32, int) { return k32 <= thr; });
+      else put(0, at, [&](uint32_t k32, int u) { return k32 < thr || (k32 == thr && l <= last - chunk(0, u)); });
+      return;
+    }
+  }
+  for (int sh = sh0; sh > 0;) {  // (at most 22 bits are left: three rounds)
+    const int bits = min(BITS, sh), s2 = sh - bits;
+    uint32_t from = base;
+    asm volatile("" : "+v"(from));  // (the differences of all keys, kept from round to round, would spill)
+    every([&](uint32_t k32, int) {
+      const uint32_t x = k32 - from;  // (of keys before the bin it wraps round to the far end: never equal to `sub`)
+      if (k32 != NO_KEY && (x >> sh) == sub) atomicAdd(&m.hist[((x >> s2) & ((1u << bits) - 1u)) * REP + (l & (REP - 1))], 1u);
+    });
+    pick_digit<NT>(m, need_eq);
+    sub = (sub << bits) | m.st[0];
+    need_eq = m.st[1];
+    n_eq = m.st[2];
+    sh = s2;
+  }
+  const uint32_t thr = (uint32_t)__builtin_amdgcn_readfirstlane((int)(base + sub));
+  const bool ties = n_eq != need_eq;  // some keys equal to the threshold are left out: those of the highest positions
+  uint32_t done = 0, done_eq = 0;
+  for (int round = 0; round < rounds; round++) {
+    if (LONG) {
+      fetch(round);
+      to_keys(round);
+    }
+    uint32_t kept = 0, equal = 0;  // lane u: of this wave's chunk u
+    each(round, [&](uint32_t k32, int u) {
+      const uint32_t b = (uint32_t)__popcll(__ballot(ties ? k32 < thr : k32 <= thr)), e = (uint32_t)__popcll(__ballot(k32 == thr));
+      kept = l == u ? b : kept;
+      equal = l == u ? e : equal;
+    });
+    if (l < 32) {
+      m.kept[l * NW + w] = kept;
+      m.equal[l * NW + w] = equal;
+    }
+    __syncthreads();
+    uint32_t total, total_eq = 0;
+    const uint32_t at = done + chunk_offsets(m.kept, w, l, total);
+    if (!ties) {
+      put(round, at, [&](uint32_t k32, int) { return k32 <= thr; });
+    } else {
+      const uint32_t at_eq = done_eq + chunk_offsets(m.equal, w, l, total_eq);
+      each(round, [&](uint32_t k32, int u) {
+        const unsigned long long bm = __ballot(k32 < thr), em = __ballot(k32 == thr);
+        if (bm | em) {
+          const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2));
+          const uint32_t eq = (uint32_t)__builtin_amdgcn_readlane((int)at_eq, 2 * u + (w >> 2)) + lanes_before(em);  // equal ones before
+          const int32_t x = run.slot(c, chunk(round, u), u, l);
+          if (k32 < thr || (k32 == thr && eq < need_eq)) list[first + lanes_before(bm) + min(eq, need_eq)] = x;
+        }
+      });
+    }
+    done += total;
+    done_eq += total_eq;
+    if (round + 1 < rounds) __syncthreads();
+  }
+}
+
+// One workgroup per (row, head), for rows of up to SELECT_SHORT keys, or, LONG, of more.
+constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
+template <int S, bool LONG>
+__global__ __launch_bounds__(512, 8) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept) {
+  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, tid = threadIdx.x;
+  const CacheRow row = cache_row(c, p, r);
+  const int n = row.n, kk = min(p.k, n);
+  if (LONG != (n > SELECT_SHORT)) return;
+  int32_t* list = kept + (size_t)rh * p.kcap;
+  if (kk == n) {
+    bool bad = false;
+    for (int j = tid << c.shift; j < n; j += 512 << c.shift) bad |= (uint32_t)row.pages[j >> c.shift] >= (uint32_t)c.n_pages;
+    const int there = __syncthreads_or(bad) ? 0 : n;
+    for (int j = tid; j < p.kcap; j += 512) list[j] = j < there ? (int32_t)cache_slot(c, row, j) : -1;
+    return;
+  }
+  __shared__ SelectShared<512> m;
+  select_row<512, SELECT_REGS, S, LONG>(c, row, h, kk, list, m);
 }
 
 // ------------------------------------------------------------------ attention over a part of the list
@@ -157,13 +436,14 @@ template <> struct Query<float> {
   }
 };
 
-// One workgroup per (CH kept keys, row, head).  A key's K (and V) row is held by D / 32 lanes, 32 channels with one scale each; a
+// One workgroup per (ch kept keys, row, head).  A key's K (and V) row is held by D / 32 lanes, 32 channels with one scale each; a
 // wave takes 64 keys at a time, all of them requested before the first is used, and has one running maximum.  The G heads
 // of a kv-head have the same part of their lists on one XCD at the same time (decode_attend_kernel).
-template <typename TQ, int D, int CH>
+template <typename TQ, int D>
 __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows p, const TQ* __restrict__ q, long q_stride,
                                                            const int32_t* __restrict__ kept, float* __restrict__ part,
-                                                           TQ* __restrict__ o, float* __restrict__ lse, int nsplit, float scale) {
+                                                           TQ* __restrict__ o, float* __restrict__ lse, int ch, int nsplit,
+                                                           float scale) {
   constexpr int LPG = D / 32, NG = 64 / LPG, U = 64 / NG;
   const unsigned wg = blockIdx.x;
   const int G = c.H_q / c.H_kv, idx = (int)(wg >> 3), unit = (idx / G) * 8 + (int)(wg & 7);
@@ -171,56 +451,56 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   if (sp >= nsplit) return;
   const int r = rg / c.H_kv, g = rg - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
-  const int kk = min(p.k, cache_row(c, p, r).n), i0 = sp * CH, cnt = min(CH, kk - i0);
-  if (cnt <= 0) {
+  const int32_t* list = kept + (size_t)rh * p.kcap;
+  int i0 = sp * ch + w * 64;
+  uint32_t id[U];  // (requested before the number of kept keys is known)
+#pragma unroll
+  for (int u = 0; u < U; u++) id[u] = (uint32_t)list[min(i0 + u * NG + grp, p.kcap - 1)];
+  Query<TQ> qv;
+  qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
+  const int kk = min(p.k, cache_row(c, p, r).n), end = min(kk, (sp + 1) * ch);
+  if (sp * ch >= kk) {
     if (nsplit == 1) {
       if (tid < D) o[(size_t)rh * D + tid] = TQ(0.f);
       if (tid == 0) lse[(size_t)h * p.n_rows + r] = -INFINITY;
     }
     return;
   }
-  __shared__ uint32_t ids[CH];
-  __shared__ float zs[CH];  // scores; -inf: the key takes no part
-  const int32_t* list = kept + (size_t)rh * p.kcap + i0;
-#pragma unroll
-  for (int i = tid; i < CH; i += 256) {
-    const uint32_t slot = i < cnt ? (uint32_t)list[i] : 0xffffffffu;
-    ids[i] = slot < c.n_slots ? slot : 0u;
-    zs[i] = cache_score(c, slot, h);
-  }
-  Query<TQ> qv;
-  qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
+  const char* zh = c.pages + c.off_z + ((size_t)h << c.shift) * 4;
   float m = -INFINITY, lsum = 0.f, acc[32];
 #pragma unroll
   for (int e = 0; e < 32; e++) acc[e] = 0.f;
-  __syncthreads();
 #pragma unroll 1
-  for (int base = w * 64; base < cnt; base += 256) {
+  for (; i0 < end; i0 += 256) {
     uint4 kr[U], vr[U];
     uint32_t kb[U], vb[U];
     float s2[U];
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const uint32_t slot = ids[base + u * NG + grp];
-      const char* page = cache_page(c, slot);
-      const uint32_t at = ((uint32_t)g << c.shift) + cache_place(c, slot);
-      const uint4* codes = reinterpret_cast<const uint4*>(page + (size_t)at * D);
-      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page) + c.off_scales + (size_t)at * (D / 16);
+      const bool there = i0 + u * NG + grp < end && id[u] < c.n_slots;
+      const uint32_t slot = there ? id[u] : 0u, place = cache_place(c, slot);
+      const size_t page = (size_t)(slot >> c.shift) * c.page_bytes;
+      const uint32_t at = ((uint32_t)g << c.shift) + place;
+      const uint4* codes = reinterpret_cast<const uint4*>(c.pages + page + (size_t)at * D);
+      const uint8_t* scales = reinterpret_cast<const uint8_t*>(c.pages) + page + c.off_scales + (size_t)at * (D / 16);
       kr[u] = codes[sub];
       vr[u] = codes[LPG + sub];
       kb[u] = scales[sub];
       vb[u] = scales[LPG + sub];
+      s2[u] = reinterpret_cast<const float*>(zh + page)[place];
+      id[u] = there ? 1u : 0u;
     }
     float top = m;
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const float sc = mx_scale(kb[u]), zb = zs[base + u * NG + grp];
+      const float sc = mx_scale(kb[u]), zb = id[u] ? s2[u] : -INFINITY;
       float s = qv.template dot8<0>(kr[u].x, sc, 0.f);
       s = qv.template dot8<1>(kr[u].y, sc, s);
       s = qv.template dot8<2>(kr[u].z, sc, s);
       s = lanes_sum<LPG>(qv.template dot8<3>(kr[u].w, sc, s));
       s2[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
       top = fmaxf(top, s2[u]);
+      id[u] = (uint32_t)list[min(i0 + 256 + u * NG + grp, p.kcap - 1)];
     }
     top = over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); });
     const float ref = top == -INFINITY ? 0.f : top, alpha = weight(m, ref);
@@ -286,30 +566,30 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
 // The parts of one (row, head) together: o = sum_s o_s e^(M_s - M) / sum_s l_s e^(M_s - M), eight parts requested at a time.
 template <typename TQ, int D>
 __global__ __launch_bounds__(D) void cache_merge_kernel(CacheRef c, CacheRows p, const float* __restrict__ part,
-                                                        TQ* __restrict__ o, float* __restrict__ lse, int nsplit, int ch) {
+                                                        TQ* __restrict__ o, float* __restrict__ lse, int ch, int nsplit) {
   const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, t = threadIdx.x;
-  const int kk = min(p.k, cache_row(c, p, r).n), ns = (kk + ch - 1) / ch;
   const float* ps = part + (size_t)rh * nsplit * (D + 2);
+  const int kk = min(p.k, cache_row(c, p, r).n), ns = (kk + ch - 1) / ch;
   float M = -INFINITY, num = 0.f, den = 0.f;
-  for (int s0 = 0; s0 < ns; s0 += 8) {
+  for (int s0 = 0; s0 == 0 || s0 < ns; s0 += 8) {  // (the first parts are requested before their number is known)
     float Ms[8], ls[8], os[8];
 #pragma unroll
     for (int u = 0; u < 8; u++) {
-      const float* x = ps + (size_t)min(s0 + u, ns - 1) * (D + 2);
+      const float* x = ps + (size_t)min(s0 + u, nsplit - 1) * (D + 2);
       Ms[u] = x[D];
       ls[u] = x[D + 1];
       os[u] = x[t];
     }
     float top = M;
 #pragma unroll
-    for (int u = 0; u < 8; u++) top = fmaxf(top, Ms[u]);
+    for (int u = 0; u < 8; u++) top = fmaxf(top, s0 + u < ns ? Ms[u] : -INFINITY);
     const float ref = top == -INFINITY ? 0.f : top, alpha = weight(M, ref);
     M = top;
     num *= alpha;
     den *= alpha;
 #pragma unroll
     for (int u = 0; u < 8; u++) {
-      if (s0 + u >= ns) continue;  // (past the end the last part was read again)
+      if (s0 + u >= ns) continue;  // (not written)
       const float w8 = weight(Ms[u], ref);
       num = fmaf(os[u], w8, num);
       den = fmaf(ls[u], w8, den);
@@ -319,33 +599,35 @@ __global__ __launch_bounds__(D) void cache_merge_kernel(CacheRef c, CacheRows p,
   if (t == 0) lse[(size_t)h * p.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
 }
 
-// Kept keys per workgroup of the attention.
-static int attend_chunk(const dma_cache_shape& s, int n_rows, int kcap) {
-  return (long)n_rows * s.H_q * ((kcap + 511) / 512) >= 4 * CUS ? 512 : 256;
-}
-
 static int list_length(const dma_cache_shape& s, int k) {
   const long cap = (long)s.max_pages * s.page_size;
   return (int)(k < cap ? k : cap);
 }
 
+// Kept keys per workgroup of the attention, a multiple of 256 (64 for each wave): shorter parts where there are few lists.
+constexpr int ATTEND_WGS = 2 * CUS;
+static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
+  const long lists = (long)n_rows * s.H_q, most = (kcap + 255) / 256;
+  long parts = (ATTEND_WGS + lists - 1) / lists;
+  if (parts > most) parts = most;
+  return (int)(((kcap + parts - 1) / parts + 255) / 256 * 256);
+}
+
 size_t cache_decode_bytes(const dma_cache_shape& s, int n_rows, int k) {
-  const int kcap = list_length(s, k), ch = attend_chunk(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
+  if (n_rows == 0) return 0;
+  const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
   return align_up((size_t)n_rows * s.H_q * nsplit * (s.d + 2) * 4, 256);
 }
 
 template <typename TQ, int D>
 static void decode_t(const dma_cache_shape& s, const CacheRef& c, const CacheRows& p, float scale, const void* q, long q_stride,
                      void* o, float* lse, const int32_t* kept, float* part, hipStream_t st) {
-  const int ch = attend_chunk(s, p.n_rows, p.kcap), nsplit = (p.kcap + ch - 1) / ch;
+  const int ch = attend_part(s, p.n_rows, p.kcap), nsplit = (p.kcap + ch - 1) / ch;
   const long units = ((long)p.n_rows * s.H_kv * nsplit + 7) / 8 * 8;
   const unsigned grid = (unsigned)(units * (s.H_q / s.H_kv));
-  if (ch == 512)
-    cache_attend_kernel<TQ, D, 512><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, nsplit, scale);
-  else
-    cache_attend_kernel<TQ, D, 256><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, nsplit, scale);
+  cache_attend_kernel<TQ, D><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, ch, nsplit, scale);
   if (nsplit > 1)
-    cache_merge_kernel<TQ, D><<<(unsigned)(p.n_rows * s.H_q), D, 0, st>>>(c, p, part, (TQ*)o, lse, nsplit, ch);
+    cache_merge_kernel<TQ, D><<<(unsigned)(p.n_rows * s.H_q), D, 0, st>>>(c, p, part, (TQ*)o, lse, ch, nsplit);
 }
 
 int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale, const void* q, long q_stride,
@@ -353,8 +635,16 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
                         float* lse, int32_t* kept, void* ws, hipStream_t st) {
   const CacheRef c = cache_ref(s, pages);
   const CacheRows p = {table, row_req, row_len, n_rows, k, list_length(s, k)};
-  cache_select_kernel<<<(unsigned)(n_rows * s.H_q), 1024, 0, st>>>(c, p, kept);
+  const unsigned pairs = (unsigned)(n_rows * s.H_q);
+  const bool wide = s.page_size >= 64;
+  if (wide) cache_select_kernel<1, false><<<pairs, 512, 0, st>>>(c, p, kept);
+  else cache_select_kernel<4, false><<<pairs, 512, 0, st>>>(c, p, kept);
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  if ((long)s.max_pages * s.page_size > SELECT_SHORT) {
+    if (wide) cache_select_kernel<1, true><<<pairs, 512, 0, st>>>(c, p, kept);
+    else cache_select_kernel<4, true><<<pairs, 512, 0, st>>>(c, p, kept);
+    if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  }
   auto go = [&](auto t) {
     using T = std::remove_pointer_t<decltype(t)>;
     if (s.d == 256) decode_t<T, 256>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, st);

@@ -293,27 +293,22 @@ def test_masked_keys_take_no_part(gpu):
 
 
 def test_pages_that_are_not_there(gpu):
-    """Page numbers and requests out of range are keys and rows that are missing; lengths beyond the table end with it."""
-    cache = GpuCache(gpu, 3, 9, 3, 16, 2, 1, 64)
-    fill(cache, (48, 33, 16), 3)
-    q = normal(gpu, 4, 5, 2, 64).to(cache.type)
+    """A row one of whose pages is out of range, or whose request is, sees nothing; lengths beyond the table end with it."""
+    cache = GpuCache(gpu, 5, 16, 3, 16, 2, 1, 64)
+    fill(cache, (48, 33, 16, 48, 20), 3)
+    req = torch.tensor([0, 1, 2, 3, 4, 5, -4, 2, 4], dtype=torch.int32, device=gpu)
+    length = torch.tensor([48, 2**31 - 1, -3, 33, 16, 7, 7, 17, 17], dtype=torch.int32, device=gpu)
+    q = normal(gpu, 4, 9, 2, 64).to(cache.type)
     table = cache.table.clone()
-    table[0, 1], table[1, 0], table[1, 2] = 9, -5, 2**31 - 1
-    req = torch.tensor([0, 1, 2, 3, -4], dtype=torch.int32, device=gpu)
-    length = torch.tensor([48, 2**31 - 1, -3, 7, 7], dtype=torch.int32, device=gpu)
-    o, lse, kept = cache.decode(q, 40, req, length, table=table)
-    assert (f64(o)[2:] == 0).all() and np.isneginf(f64(lse)[:, 2:]).all() and (kept[2:] == -1).all()
-    for b, there in ((0, [0, 2]), (1, [1])):
-        slots = np.concatenate([np.arange(16) + 16 * int(table[b, p]) for p in there])
-        n = 48
-        K, V, z = (f64(x) for x in cache.read(torch.tensor(slots, dtype=torch.int32, device=gpu)))
-        ro, rl, rk = co.decode_row(f64(q)[b], K, V, z, 40, 64 ** -0.5)
-        for h in range(2):
-            got = kept[b, h].cpu().numpy()
-            assert sorted(got[got >= 0]) == sorted(slots[rk[h]]) and len(got) == 40
-            assert np.abs(f64(o)[b, h] - ro[h]).max() <= 2.0 ** -8 * np.abs(ro[h]).max() + 1e-4 and abs(f64(lse)[h, b] - rl[h]) < 1e-4
-            if b == 0:       # 32 keys that are there, then eight of the missing ones in their places
-                assert (got >= 0).sum() == 32 and (got[:16] == slots[:16]).all()
+    table[0, 1], table[1, 2], table[3, 2], table[4, 1] = 16, 2**31 - 1, -5, -1
+    for k in (10, 40, 100):                       # (selected, and all kept)
+        o, lse, kept = cache.decode(q, k, req, length, table=table)
+        for r in (0, 1, 2, 3, 5, 6, 7, 8):
+            assert (o[r] == 0).all() and torch.isneginf(lse[:, r]).all() and (kept[r] == -1).all(), r
+        check_rows(cache, q[4:5], k, [(4, 16)], (o[4:5], lse[:, 4:5], kept[4:5]))
+        whole = cache.decode(q, k, req, torch.where(length < 0, 0, length).clamp(max=33).int())
+        check_rows(cache, q, k, [(0, 33), (1, 33), (2, 0), (3, 33), (4, 16), (-1, 0), (-1, 0), (2, 16), (4, 17)][:7], tuple(
+            x[:7] if x.shape[0] == 9 else x[:, :7] for x in whole))
 
 
 def test_offsets_beyond_four_gigabytes(gpu):

@@ -402,8 +402,8 @@ int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* 
  *   kept     out [n_rows, H_q, min(k, max_pages * page_size)] int32: the slots of the kept keys in order of position, -1 behind
  *                them
  *   ws       dma_cache_decode_bytes(shape, n_rows, k) bytes of scratch; calls that overlap need one each
- * DMA_EUNSUPPORTED where (n_rows + 8) * H_q * ceil(min(k, max_pages * page_size) / 256) reaches 2^22: a whole prompt goes through
- * dma_mask_gen and dma_fwd.
+ * DMA_EUNSUPPORTED where (n_rows + 8) * H_q, times the larger of ceil(min(k, n) / 256) and min(n / 8192 + 1, 64) for
+ * n = max_pages * page_size, reaches 2^22: a whole prompt goes through dma_mask_gen and dma_fwd.
  */
 int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
                      int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,

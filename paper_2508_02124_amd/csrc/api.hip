@@ -301,13 +301,15 @@ size_t dma_cache_free_bytes(const dma_cache_shape* shape) {
   return ((size_t)shape->n_pages + FREE_HEADER) * 4;
 }
 
-// The grids of a decode: rows x heads x parts of the list, in workgroups of up to 1024 threads, 2^32 threads at most.
+// The grids of a decode: rows x heads x parts of the list, or slices of a long row, in workgroups of up to 512 threads, fewer than
+// 2^32 threads in all.
 static int check_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k) {
   int rc = check_cache(shape);
   if (rc != DMA_OK) return rc;
   if (n_rows < 0 || k <= 0) return DMA_EINVAL;
   const long cap = (long)shape->max_pages * shape->page_size, parts = ((k < cap ? k : cap) + 255) / 256;
-  if (((long)n_rows + 8) * shape->H_q * parts >= 1 << 22) return DMA_EUNSUPPORTED;
+  const long slices = cap / 8192 + 1 < 64 ? cap / 8192 + 1 : 64;
+  if (((long)n_rows + 8) * shape->H_q * (parts > slices ? parts : slices) >= 1 << 22) return DMA_EUNSUPPORTED;
   return DMA_OK;
 }
 

@@ -77,9 +77,9 @@ template <int S> struct PageRun {
   }
 };
 
-// Keys ascend from the best score to the worst, -0 and +0 the same; NO_KEY is behind every score's.
-constexpr uint32_t NO_KEY = 0xffffffffu;
-__device__ __forceinline__ uint32_t score_key(float z) { return min(desc_key(z), NO_KEY - 1); }
+// Keys ascend from the best score to the worst, -0 and +0 the same, NaN beside one of the infinities; NO_KEY is behind every score's.
+constexpr uint32_t BEST_KEY = 0x007fffffu, NO_KEY = 0xffffffffu;
+__device__ __forceinline__ uint32_t score_key(float z) { return max(BEST_KEY, min(desc_key(z), NO_KEY - 1)); }
 __device__ __forceinline__ uint32_t lanes_before(unsigned long long m) {
   return __builtin_amdgcn_mbcnt_hi((uint32_t)(m >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)m, 0u));
 }
@@ -103,8 +103,8 @@ template <int NT> struct SelectShared {
   uint32_t st[4];
 };
 
-// The digit at which the running count of the histogram reaches `remaining` (st[0..2]); leaves it cleared.
-template <int NT> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m, uint32_t remaining) {
+// The digit at which the running count of the histogram reaches `remaining` (st[0..2]); CLEAR: leaves it cleared.
+template <int NT, bool CLEAR = true> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m, uint32_t remaining) {
   constexpr int DPT = SelectShared<NT>::NDIG / NT;
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
@@ -113,7 +113,7 @@ template <int NT> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m
 #pragma unroll
   for (int i = 0; i < DPT; i++) {
     const uint4 x = hist4[DPT * tid + i];
-    hist4[DPT * tid + i] = make_uint4(0, 0, 0, 0);
+    if (CLEAR) hist4[DPT * tid + i] = make_uint4(0, 0, 0, 0);
     cn[i] = x.x + x.y + x.z + x.w;
     sum += cn[i];
   }
@@ -358,14 +358,14 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   }
 }
 
-// One workgroup per (row, head), for rows of up to SELECT_SHORT keys, or, LONG, of more.
+// One workgroup per (row, head), for rows of up to SELECT_SHORT keys (or of any length, where the window keeps them all).
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
-template <int S, bool LONG>
-__global__ __launch_bounds__(512, 8) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept) {
+template <int S>
+__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept, int longest) {
   const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);
   const int n = row.n, kk = min(p.k, n);
-  if (LONG != (n > SELECT_SHORT)) return;
+  if (n > longest) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
   if (kk == n) {
     bool bad = false;
@@ -375,7 +375,263 @@ __global__ __launch_bounds__(512, 8) void cache_select_kernel(CacheRef c, CacheR
     return;
   }
   __shared__ SelectShared<512> m;
-  select_row<512, SELECT_REGS, S, LONG>(c, row, h, kk, list, m);
+  select_row<512, SELECT_REGS, S, false>(c, row, h, kk, list, m);
+}
+
+// ------------------------------------------------------------------ the kept set of a long row, by slices
+// Rows of more than SELECT_SHORT keys are cut into slices of SLICE keys, a workgroup each, in two launches.  The first looks at
+// the same sample of the whole row in every slice and takes from it two keys that the kk-th best very likely lies between (3.5
+// standard deviations of its rank in the sample to either side); it counts the slice's keys that are better and lists those between, with
+// their positions.  The second ranks the listed keys of all slices, a few per cent of the row, for the exact threshold (by
+// key and position: no ties are left), and writes the slice's kept slots behind those of the slices before it.  Where the threshold lies
+// outside after all, or a list is too short for its keys (ties, above all), or the row has more than SLICES_MAX slices, the first
+// slice's workgroup selects alone.
+constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS;
+constexpr int SAMPLE = 2048, LISTED = 1024, LISTED_ALL = 8192, SLICES_MAX = 64;
+
+struct SliceWork {
+  uint2* counts;  // [pairs][slices]: better keys, listed keys (more than LISTED: not all are)
+  uint2* listed;  // [pairs][slices][LISTED]: key, position
+  uint2* bounds;  // [pairs]: first and last key of the lists
+  int slices;
+};
+
+// How a slice's chunks go round the waves, and its keys (NO_KEY behind the row's end).  False: a page is out of range.
+template <int S>
+__device__ __forceinline__ bool slice_keys(const CacheRef& c, const CacheRow& row, int h, int slice, PageRun<S>& run, uint32_t* key) {
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = row.n;
+  const char* scores = c.pages + c.off_z + ((size_t)h << c.shift) * 4;
+  const bool bad = run.check(c, n, slice * (SLICE / 64) + w, 8, l);
+#pragma unroll
+  for (int u0 = 0; u0 < SLICE_CHUNKS; u0 += 4) {
+#pragma unroll
+    for (int u = u0; u < u0 + 4; u++) key[u] = __float_as_uint(run.score(c, scores, slice * SLICE + (u * 8 + w) * 64, u, l));
+    __builtin_amdgcn_sched_barrier(0);
+  }
+#pragma unroll
+  for (int u = 0; u < SLICE_CHUNKS; u++) key[u] = l < n - (slice * SLICE + (u * 8 + w) * 64) ? score_key(__uint_as_float(key[u])) : NO_KEY;
+  return !bad;
+}
+
+template <int S>
+__global__ __launch_bounds__(512, 6) void cache_bracket_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+  const int pairs = p.n_rows * c.H_q, slice = blockIdx.x / pairs, rh = blockIdx.x - slice * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  const CacheRow row = cache_row(c, p, r);
+  PageRun<S> run;
+  run.load(c, row, slice * (SLICE / 64) + w, 8, l);
+  const int n = row.n, kk = min(p.k, n), first = slice * SLICE;
+  if (n <= SELECT_SHORT || first >= n) return;
+  if (kk == n) {  // every key is kept (a page out of range anywhere: none)
+    int32_t* list = kept + (size_t)rh * p.kcap;
+    bool bad = false;
+    for (int j = tid; j <= (n - 1) >> c.shift; j += 512) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;
+    const int there = __syncthreads_or(bad) ? 0 : n;  // (the last workgroup goes on to the list's end)
+    const int end = first + SLICE >= n || slice == sw.slices - 1 ? p.kcap : first + SLICE;
+    for (int j = first + tid; j < end; j += 512) list[j] = j < there ? (int32_t)cache_slot(c, row, j) : -1;
+    return;
+  }
+  if (n > SLICES_MAX * SLICE) return;
+  __shared__ SelectShared<512> m;
+  uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
+  for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+  // the sample: one key of each of 2048 equal parts of the row, at a place in it that follows no period
+  uint32_t sample[SAMPLE / 512], key[SLICE_CHUNKS];
+#pragma unroll
+  for (int e = 0; e < SAMPLE / 512; e++) {
+    const uint32_t i = (uint32_t)(e * 512 + tid), part = (uint32_t)n / SAMPLE;
+    const int j = (int)((unsigned long long)i * (uint32_t)n / SAMPLE) + (int)((i * 2654435761u >> 16) * part >> 16);
+    sample[e] = score_key(cache_score(c, cache_slot(c, row, j), h));
+  }
+  const bool good = slice_keys<S>(c, row, h, slice, run, key);
+  uint32_t kmin = NO_KEY, kmax = 0;
+#pragma unroll
+  for (int e = 0; e < SAMPLE / 512; e++) {
+    kmin = min(kmin, sample[e]);
+    kmax = max(kmax, sample[e]);
+  }
+  kmin = last_lane(wave_scan(kmin, NO_KEY, [](uint32_t x, uint32_t y) { return min(x, y); }));
+  kmax = last_lane(wave_scan(kmax, 0u, [](uint32_t x, uint32_t y) { return max(x, y); }));
+  if (l == 0) {
+    m.wsum[w][0] = kmin;
+    m.wsum[w][1] = good ? kmax : NO_KEY;
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    kmin = min(kmin, m.wsum[i][0]);
+    kmax = max(kmax, m.wsum[i][1]);
+  }
+  uint2* counts = sw.counts + (size_t)rh * sw.slices + slice;
+  if (kmax == NO_KEY) {  // (a page is out of range: the second launch sees an impossible count)
+    if (tid == 0) *counts = make_uint2(0, NO_KEY);
+    return;
+  }
+  const uint32_t range = kmax - kmin;
+  const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
+#pragma unroll
+  for (int e = 0; e < SAMPLE / 512; e++) atomicAdd(&m.hist[((sample[e] - kmin) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
+  const float share = (float)kk / (float)n, middle = share * SAMPLE, off = 3.5f * sqrtf(middle * (1.f - share)) + 3.f;
+  uint32_t lo = 0, hi = NO_KEY - 1;
+  if (middle - off >= 1.f) {
+    pick_digit<512, false>(m, (uint32_t)(middle - off));
+    lo = kmin + (m.st[0] << sh);
+  }
+  if (middle + off < (float)SAMPLE) {
+    pick_digit<512, false>(m, (uint32_t)(middle + off) + 1u);
+    const uint32_t top = (m.st[0] << sh) + ((1u << sh) - 1u);
+    hi = top < hi - kmin ? kmin + top : hi;
+  }
+  lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
+  hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
+  uint32_t better = 0, mine = 0;  // keys of this wave
+#pragma unroll
+  for (int u = 0; u < SLICE_CHUNKS; u++) {
+    better += (uint32_t)__popcll(__ballot(key[u] < lo));
+    mine += (uint32_t)__popcll(__ballot(key[u] - lo <= hi - lo));
+  }
+  __syncthreads();
+  if (l == 0) {
+    m.wsum[w][0] = better;
+    m.wsum[w][1] = mine;
+  }
+  __syncthreads();
+  uint32_t all_better = 0, all = 0, at = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    at += i < w ? m.wsum[i][1] : 0u;
+    all_better += m.wsum[i][0];
+    all += m.wsum[i][1];
+  }
+  uint2* listed = sw.listed + ((size_t)rh * sw.slices + slice) * LISTED;
+#pragma unroll
+  for (int u = 0; u < SLICE_CHUNKS; u++) {
+    const bool in = key[u] - lo <= hi - lo;
+    const unsigned long long b = __ballot(in);
+    const uint32_t i = at + lanes_before(b);
+    if (in && i < LISTED) listed[i] = make_uint2(key[u], (uint32_t)(first + (u * 8 + w) * 64 + l));
+    at += (uint32_t)__popcll(b);
+  }
+  if (tid == 0) {
+    *counts = make_uint2(all_better, all);
+    if (slice == 0) sw.bounds[rh] = make_uint2(lo, hi);
+  }
+}
+
+template <int S>
+__global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+  const int pairs = p.n_rows * c.H_q, slice = blockIdx.x / pairs, rh = blockIdx.x - slice * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  const CacheRow row = cache_row(c, p, r);
+  PageRun<S> run;
+  run.load(c, row, slice * (SLICE / 64) + w, 8, l);
+  uint2 cnt = sw.counts[(size_t)rh * sw.slices + min(l, sw.slices - 1)];  // lane s: of slice s
+  const uint2 bounds = sw.bounds[rh];
+  const int n = row.n, kk = min(p.k, n), first = slice * SLICE;
+  if (n <= SELECT_SHORT || first >= n || kk == n) return;
+  int32_t* list = kept + (size_t)rh * p.kcap;
+  __shared__ SelectShared<512> m;
+  __shared__ __align__(16) uint32_t cand[LISTED_ALL];
+  const int slices = (n - 1) / SLICE + 1;
+  const auto add = [](uint32_t x, uint32_t y) { return x + y; };
+  if (l >= slices) cnt = make_uint2(0, 0);
+  const unsigned long long over = __ballot(cnt.y > LISTED);
+  const uint32_t upto_better = wave_scan(cnt.x, 0u, add), upto = wave_scan(min(cnt.y, (uint32_t)LISTED), 0u, add);
+  const uint32_t better = last_lane(upto_better), all = last_lane(upto);
+  if (slices > SLICES_MAX || over || all > LISTED_ALL || better >= (uint32_t)kk || (uint32_t)kk - better > all) {
+    if (slice == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
+    return;
+  }
+  const uint32_t want = (uint32_t)kk - better;  // of the listed keys
+  uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
+  for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+  uint32_t* near_all = &m.st[3];
+  if (tid == 0) *near_all = 0;
+  // The listed keys of all slices; a wave takes every eighth slice's.
+  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.x), range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.y) - lo;
+  const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
+  const uint2* lists = sw.listed + (size_t)rh * sw.slices * LISTED;
+  for (int s = w; s < slices; s += 8) {
+    const uint32_t have = (uint32_t)__builtin_amdgcn_readlane((int)cnt.y, s), to = (uint32_t)__builtin_amdgcn_readlane((int)upto, s) - have;
+    for (uint32_t i0 = 0; i0 < have; i0 += 256) {
+      uint32_t k[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) k[e] = lists[(size_t)s * LISTED + min(i0 + e * 64 + l, have - 1)].x;
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        if (i0 + e * 64 + l < have) cand[to + i0 + e * 64 + l] = k[e];
+    }
+  }
+  uint32_t key[SLICE_CHUNKS];
+  (void)slice_keys<S>(c, row, h, slice, run, key);
+  __syncthreads();
+  for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[((cand[i] - lo) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
+  pick_digit<512>(m, want);
+  const uint32_t base = lo + (m.st[0] << sh), rank = m.st[1], n_near = m.st[2];
+  if (n_near > 512) {  // (ties)
+    __syncthreads();
+    if (slice == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
+    return;
+  }
+  // Keys of that bin, with their positions (again from the lists), and the keys before it in the slices before this one.
+  uint32_t ahead = 0;
+  for (int s = w; s < slices; s += 8) {
+    const uint32_t have = (uint32_t)__builtin_amdgcn_readlane((int)cnt.y, s), to = (uint32_t)__builtin_amdgcn_readlane((int)upto, s) - have;
+    for (uint32_t i0 = 0; i0 < have; i0 += 64) {
+      const bool there = i0 + l < have;
+      const uint32_t k = there ? cand[to + i0 + l] : NO_KEY;
+      if (s < slice) ahead += (uint32_t)__popcll(__ballot(k < base));
+      if (there && ((k - base) >> sh) == 0) {
+        const uint32_t e = atomicAdd(near_all, 1u);
+        m.near[e] = k;
+        m.near_pos[e] = lists[(size_t)s * LISTED + i0 + l].y;
+      }
+    }
+  }
+  if (l == 0) m.wsum[w][0] = ahead;
+  __syncthreads();
+  if (tid < (int)n_near) {
+    const uint32_t k = m.near[tid], pos = m.near_pos[tid];
+    uint32_t less = 0;
+    for (uint32_t i = 0; i < n_near; i++) less += m.near[i] < k || (m.near[i] == k && m.near_pos[i] < pos);
+    if (less + 1 == rank) {  // the last one that is kept
+      m.st[0] = k;
+      m.st[1] = pos;
+    }
+  }
+  __syncthreads();
+  const uint32_t thr = (uint32_t)__builtin_amdgcn_readfirstlane((int)m.st[0]);
+  const int last = __builtin_amdgcn_readfirstlane((int)m.st[1]);
+  // kept keys of the slices before: better ones, listed ones before the bin, those of the bin up to the threshold
+  uint32_t done = slice ? (uint32_t)__builtin_amdgcn_readlane((int)upto_better, slice - 1) : 0u;
+#pragma unroll
+  for (int i = 0; i < 8; i++) done += m.wsum[i][0];
+  for (uint32_t i0 = 0; i0 < n_near; i0 += 64) {
+    const bool there = i0 + l < n_near;
+    const uint32_t k = there ? m.near[i0 + l] : NO_KEY;
+    const int pos = there ? (int)m.near_pos[i0 + l] : 0;
+    done += (uint32_t)__popcll(__ballot(pos < first && (k < thr || (k == thr && pos <= last))));
+  }
+  uint32_t count = 0;
+#pragma unroll
+  for (int u = 0; u < SLICE_CHUNKS; u++) {
+    const uint32_t b = (uint32_t)__popcll(__ballot(key[u] < thr || (key[u] == thr && l <= last - (first + (u * 8 + w) * 64))));
+    count = l == u ? b : count;
+  }
+  if (l < 32) m.kept[l * 8 + w] = l < SLICE_CHUNKS ? count : 0u;
+  __syncthreads();
+  uint32_t total;
+  const uint32_t at = done + chunk_offsets(m.kept, w, l, total);
+#pragma unroll
+  for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));
+#pragma unroll
+  for (int u = 0; u < SLICE_CHUNKS; u++) {
+    const int j = first + (u * 8 + w) * 64;
+    const bool in = key[u] < thr || (key[u] == thr && l <= last - j);
+    const unsigned long long b = __ballot(in);
+    const int32_t slot = run.slot(c, j, u, l);
+    if (in) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
+  }
 }
 
 // ------------------------------------------------------------------ attention over a part of the list
@@ -613,10 +869,29 @@ static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
   return (int)(((kcap + parts - 1) / parts + 255) / 256 * 256);
 }
 
-size_t cache_decode_bytes(const dma_cache_shape& s, int n_rows, int k) {
-  if (n_rows == 0) return 0;
+// The workspace: partial outputs, then, where rows can be long, what the slices of a row tell each other.
+struct DecodeWork {
+  size_t off_counts, off_listed, off_bounds, total;
+  int slices;
+};
+static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
-  return align_up((size_t)n_rows * s.H_q * nsplit * (s.d + 2) * 4, 256);
+  const size_t pairs = (size_t)n_rows * s.H_q;
+  DecodeWork wk;
+  size_t o = nsplit > 1 ? align_up(pairs * nsplit * (s.d + 2) * 4, 256) : 0;
+  auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
+  const long cap = (long)s.max_pages * s.page_size;
+  const long slices = cap <= SELECT_SHORT || kcap == cap ? 0 : (cap + SLICE - 1) / SLICE;
+  wk.slices = (int)(slices < SLICES_MAX ? slices : SLICES_MAX);
+  wk.off_counts = take(pairs * wk.slices * 8);
+  wk.off_listed = take(pairs * wk.slices * LISTED * 8);
+  wk.off_bounds = take(wk.slices ? pairs * 8 : 0);
+  wk.total = o;
+  return wk;
+}
+
+size_t cache_decode_bytes(const dma_cache_shape& s, int n_rows, int k) {
+  return n_rows == 0 ? 0 : decode_work(s, n_rows, k).total;
 }
 
 template <typename TQ, int D>
@@ -637,12 +912,19 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   const CacheRows p = {table, row_req, row_len, n_rows, k, list_length(s, k)};
   const unsigned pairs = (unsigned)(n_rows * s.H_q);
   const bool wide = s.page_size >= 64;
-  if (wide) cache_select_kernel<1, false><<<pairs, 512, 0, st>>>(c, p, kept);
-  else cache_select_kernel<4, false><<<pairs, 512, 0, st>>>(c, p, kept);
+  const DecodeWork wk = decode_work(s, n_rows, k);
+  const int longest = wk.slices ? SELECT_SHORT : INT32_MAX;
+  if (wide) cache_select_kernel<1><<<pairs, 512, 0, st>>>(c, p, kept, longest);
+  else cache_select_kernel<4><<<pairs, 512, 0, st>>>(c, p, kept, longest);
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
-  if ((long)s.max_pages * s.page_size > SELECT_SHORT) {
-    if (wide) cache_select_kernel<1, true><<<pairs, 512, 0, st>>>(c, p, kept);
-    else cache_select_kernel<4, true><<<pairs, 512, 0, st>>>(c, p, kept);
+  if (wk.slices) {
+    char* base = (char*)ws;
+    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.slices};
+    if (wide) cache_bracket_kernel<1><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
+    else cache_bracket_kernel<4><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
+    if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+    if (wide) cache_slice_kernel<1><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
+    else cache_slice_kernel<4><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
     if (hipGetLastError() != hipSuccess) return DMA_EHIP;
   }
   auto go = [&](auto t) {

@@ -237,6 +237,94 @@ def test_kept_sets_and_outputs(gpu, kind, lens, k):
     check_rows(cache, q, k, list(enumerate(lens)), got)
 
 
+def check_kept(cache, k, rows, kept):
+    """The kept sets alone: by score descending and position ascending, from the scores that the cache holds."""
+    for r, (b, n) in enumerate(rows):
+        slots = request_slots(cache, b)[:n]
+        z = cache.read(torch.from_numpy(slots.astype(np.int32)).to(cache.dev))[2].cpu().numpy() + np.float32(0.0)
+        for h in range(cache.H_q):
+            best = np.sort(np.argsort(-z[h], kind="stable")[: min(k, n)])
+            got = kept[r, h].cpu().numpy()
+            assert (got[: len(best)] == slots[best]).all() and (got[len(best):] == -1).all(), (r, h)
+
+
+# Around the sizes at which a row's path changes: registers of one workgroup (12288 keys), slices of 8192, lists that are too short
+# (ties, scores that rise along the row, so that the listed keys are all in one slice), windows that keep nearly all.
+@pytest.mark.parametrize("kind", ["ordinary", "equal", "levels", "outlier", "wide", "signed", "masked", "rising", "period"])
+@pytest.mark.parametrize("lens,k", [((12288, 12289, 700), 2048), ((16384, 16385, 8193), 16300), ((40007, 5), 300), ((24576, 12300), 1),
+                                    ((33000, 20), 32999), ((70001,), 9000)])
+@pytest.mark.parametrize("ps", [16, 64, 256])
+def test_kept_sets_of_long_rows(gpu, kind, lens, k, ps):
+    print(f"[case] long {kind} {lens} k={k} ps={ps}", flush=True)
+    cache = GpuCache(gpu, len(lens), sum(-(-n // ps) for n in lens), -(-max(lens) // ps), ps, 2, 1, 64)
+    if kind in ("rising", "period"):
+        fill(cache, lens, 31)
+        for b, n in enumerate(lens):
+            slots = torch.from_numpy(request_slots(cache, b).astype(np.int32)).to(gpu)
+            K, V, z = cache.read(slots)
+            z = torch.linspace(0.1, 0.9, n, device=gpu).expand(2, n) if kind == "rising" else torch.where(
+                torch.arange(n, device=gpu) % 32 == 0, z + 1.0, z)
+            cache.append(K, V, slots, z=z.contiguous())
+    else:
+        fill(cache, lens, 31, kind)
+    q = normal(gpu, 5, len(lens), 2, 64).to(cache.type)
+    got = cache.decode(q, k, None, cache.lens)
+    check_kept(cache, k, list(enumerate(lens)), got[2])
+
+
+def test_a_row_of_more_slices_than_are_listed(gpu):
+    n, ps = 600000, 256
+    cache = GpuCache(gpu, 2, n // ps + 3, n // ps + 2, ps, 1, 1, 64)
+    fill(cache, (n, 300), 3)
+    q = normal(gpu, 5, 2, 1, 64).to(cache.type)
+    for k in (500, 599999, 700000):
+        got = cache.decode(q, k, None, cache.lens)
+        check_kept(cache, k, [(0, n), (1, 300)], got[2])
+        assert torch.isfinite(got[0].float()).all()
+
+
+def test_long_rows_with_outputs(gpu):
+    lens = (30000, 13000, 100)
+    cache = GpuCache(gpu, 3, 700, 470, 64, 4, 2, 128)
+    fill(cache, lens, 8)
+    rows = [(0, 30000), (0, 29999), (1, 13000), (0, 12288), (2, 100), (0, 20001)]
+    q = normal(gpu, 5, len(rows), 4, 128).to(cache.type)
+    req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
+    length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
+    for k in (1500, 30080, 20000):
+        check_rows(cache, q, k, rows, cache.decode(q, k, req, length))
+
+
+@pytest.mark.parametrize("lens", [(900, 5000), (20000, 40)])
+def test_scores_that_are_not_numbers(gpu, lens):
+    """NaN of any sign and payload among the scores: the lists hold min(k, n) different slots of the row in order of position and
+    nothing is written beside them."""
+    k = 333
+    cache = GpuCache(gpu, 2, 700, 320, 64, 2, 1, 64)
+    fill(cache, lens, 3)
+    odd = torch.tensor([0x7fffffff, -1, 0x7fc00000, -0x400000, 0x7f800001, 0x7f800000, -0x800000], dtype=torch.int32).view(torch.float32)
+    for b, n in enumerate(lens):
+        slots = torch.from_numpy(request_slots(cache, b).astype(np.int32)).to(gpu)
+        K, V, z = cache.read(slots)
+        z = z.cpu()
+        z[0, 3::17] = odd[torch.arange(len(range(3, n, 17))) % 7]
+        z[1] = odd[torch.arange(n) % 7]
+        cache.append(K, V, slots, z=z.to(gpu))
+    q = normal(gpu, 5, 2, 2, 64).to(cache.type)
+    size = B.dma_cache_decode_bytes(cache.shape, 2, k)
+    ws, kept = torch.empty(size, dtype=torch.uint8, device=gpu), cache.ints(6, 2, k)
+    o, lse = torch.zeros((2, 2, 64), dtype=cache.type, device=gpu), torch.zeros((2, 2), device=gpu)
+    B.dma_cache_decode(cache.shape, 2, k, 0.0, q, q.stride(0), cache.pages, cache.table, None, cache.lens, o, lse, kept[2:], ws, size)
+    kept = kept.cpu().numpy()
+    assert (kept[:2] == -77).all() and (kept[4:] == -77).all()
+    for b, n in enumerate(lens):
+        place = {int(x): i for i, x in enumerate(request_slots(cache, b))}
+        for h in range(2):
+            at = [place.get(int(x), -1) for x in kept[2 + b, h]]
+            m = min(k, n)
+            assert at[0] >= 0 and all(x < y for x, y in zip(at[:m], at[1:m])) and at[m:] == [-1] * (k - m), (b, h)
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("H_q,H_kv,d,ps", [(3, 1, 64, 16), (8, 2, 128, 32), (6, 6, 256, 64), (16, 1, 128, 128), (5, 5, 64, 256)])
 def test_heads_types_and_drafts(gpu, dtype, H_q, H_kv, d, ps):

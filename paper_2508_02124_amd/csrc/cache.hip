@@ -4,6 +4,7 @@
 // 32 channels of a token's head, 17 / 32 bytes a channel against bf16's 2.  The content scores (Eq. 3) are formed from V as it comes, not
 // as it is stored, and held in fp32: they decide which keys a row keeps.
 #include "cache.h"
+#include "select.h"
 
 namespace dma {
 
@@ -18,24 +19,29 @@ struct AssignArgs {
   int n_reqs, n_pages, max_pages, shift, n_rows;
 };
 
-// Inclusive sum over the workgroup's 1024 threads (s_part: 16 words); the total in `total`.
-__device__ __forceinline__ long long scan_1024(long long x, long long* s_part, long long& total) {
-  const int l = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const long long t = __shfl_up(x, off);
-    if (l >= off) x += t;
+// Sums that stay at 2^32 - 1 once they reach it, above every number of rows or pages.
+__device__ __forceinline__ uint32_t add_sat(uint32_t x, uint32_t y) { return __builtin_elementwise_add_sat(x, y); }
+
+// Exclusive sums over the workgroup's threads of two numbers each, and the totals; s_part: 2 x 16 words, for this call alone.
+__device__ __forceinline__ void scan_block(uint32_t& x, uint32_t& y, uint32_t* s_part, uint32_t& all_x, uint32_t& all_y) {
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), nw = blockDim.x >> 6;
+  x = wave_scan(x, 0u, add_sat);
+  y = wave_scan(y, 0u, add_sat);
+  if (l == 63) {
+    s_part[w] = x;
+    s_part[16 + w] = y;
   }
-  __syncthreads();  // (s_part may still be read from the sum before)
-  if (l == 63) s_part[w] = x;
+  x = dpp<0x138, 0xf>(0u, x);  // wave_shr:1
+  y = dpp<0x138, 0xf>(0u, y);
   __syncthreads();
-  total = 0;
-#pragma unroll
-  for (int i = 0; i < 16; i++) {
-    x += i < w ? s_part[i] : 0;
-    total += s_part[i];
+  const uint32_t ix = wave_scan(l < nw ? s_part[l & 15] : 0u, 0u, add_sat);  // (lane i: up to wave i)
+  const uint32_t iy = wave_scan(l < nw ? s_part[16 + (l & 15)] : 0u, 0u, add_sat);
+  all_x = last_lane(ix);
+  all_y = last_lane(iy);
+  if (w) {
+    x = add_sat(x, (uint32_t)__builtin_amdgcn_readlane((int)ix, w - 1));
+    y = add_sat(y, (uint32_t)__builtin_amdgcn_readlane((int)iy, w - 1));
   }
-  return x;
 }
 
 // The last b with first[b] <= i, of n > 0 ascending entries.
@@ -48,13 +54,161 @@ __device__ __forceinline__ int find_request(const int32_t* first, int n, int i) 
   return lo;
 }
 
-// Row r of the step: the request that has it, how many keys it sees (its position + 1), its slot.
-__device__ __forceinline__ void assign_row(const AssignArgs& p, const int32_t* first, int r) {
+// Rows that the one workgroup writes itself: a launch of their own costs more than these (see cache_rows_kernel).
+constexpr int ASSIGN_ROWS = 4096;
+
+// One workgroup, four requests to a thread.  All that it waits for is one after another -- the lengths, two scans, the pages -- so the
+// sums are formed in registers (data-parallel moves, saturating 32 bits), and the rows take the pages of their tokens from the
+// same place of the stack as the table does, not from the table.
+template <int NT>
+__global__ __launch_bounds__(NT) void cache_assign_kernel(AssignArgs p) {
+  constexpr int PER = 4, REQS = NT * PER;
+  __shared__ int32_t first[REQS + 1];               // first row of every request
+  __shared__ int32_t back[REQS + 1], taken[REQS];   // pages given back, and taken, by the requests before it
+  __shared__ int32_t length[REQS];                  // its tokens so far; -1 if it is not served
+  __shared__ uint32_t s_part[2][32];
+  __shared__ uint32_t s_used;
+  const int tid = threadIdx.x;
+  const long long cap = (long long)p.max_pages << p.shift;
+  int32_t* stack = p.free_list + FREE_HEADER;
+  auto pages = [&](long long n) { return (int)((n + (1 << p.shift) - 1) >> p.shift); };
+  int old[PER], change[PER];
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int b = tid * PER + e;
+    old[e] = b < p.n_reqs ? p.lens[b] : 0;
+    change[e] = b < p.n_reqs ? p.change[b] : 0;
+  }
+  const int have0 = max(0, min(p.free_list[0], p.n_pages));
+  if (tid == 0) s_used = 0;
+  uint32_t freed[PER], ends[PER], sum_f = 0, sum_g = 0;
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    old[e] = (int)max(0ll, min((long long)old[e], cap));
+    freed[e] = change[e] < 0 ? (uint32_t)(pages(old[e]) - pages(max(0ll, (long long)old[e] + change[e]))) : 0u;
+    sum_f = add_sat(sum_f, freed[e]);
+    sum_g = add_sat(sum_g, (uint32_t)max(change[e], 0));
+  }
+  uint32_t run_f = sum_f, run_g = sum_g, all_f, all_g;
+  scan_block(run_f, run_g, s_part[0], all_f, all_g);
+  const uint32_t freed_all = min(all_f, (uint32_t)(p.n_pages - have0));  // (never more, unless the caller's tables are damaged)
+  const uint32_t have = (uint32_t)have0 + freed_all;
+  uint32_t need[PER], sum_n = 0;
+  int state[PER];
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int b = tid * PER + e;
+    const uint32_t grow = (uint32_t)max(change[e], 0);
+    if (b < p.n_reqs) {
+      back[b] = (int)min(run_f, (uint32_t)p.n_pages);
+      first[b] = (int)min(run_g, (uint32_t)p.n_rows);
+      p.cu_rows[b] = first[b];
+    }
+    run_f = add_sat(run_f, freed[e]);
+    run_g = add_sat(run_g, grow);
+    ends[e] = run_g;
+    const long long after = (long long)old[e] + change[e];
+    state[e] = !grow ? DMA_CACHE_SERVED : after > cap ? DMA_CACHE_TOO_LONG : ends[e] > (uint32_t)p.n_rows ? DMA_CACHE_NO_ROWS : DMA_CACHE_SERVED;
+    need[e] = grow && !state[e] ? (uint32_t)(pages(after) - pages(old[e])) : 0u;
+    sum_n = add_sat(sum_n, need[e]);
+  }
+  uint32_t run_n = sum_n, none = 0, all_n, all_0, used = 0;
+  scan_block(run_n, none, s_part[1], all_n, all_0);
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int b = tid * PER + e;
+    const uint32_t before = run_n;
+    run_n = add_sat(run_n, need[e]);
+    if (need[e] && run_n > have) state[e] = DMA_CACHE_NO_PAGES;
+    if (need[e] && !state[e]) used = run_n;  // (those that are served are the first ones of all that need any)
+    if (b < p.n_reqs) {
+      taken[b] = (int)min(before, have);
+      length[b] = state[e] ? -1 : old[e];
+      p.status[b] = state[e];
+      p.lens[b] = state[e] ? old[e] : (int)max(0ll, (long long)old[e] + change[e]);
+    }
+  }
+  used = last_lane(wave_scan(used, 0u, [](uint32_t x, uint32_t y) { return max(x, y); }));
+  if ((tid & 63) == 0 && used) atomicMax(&s_used, used);
+  if (tid == 0) {
+    first[p.n_reqs] = (int)min(all_g, (uint32_t)p.n_rows);
+    p.cu_rows[p.n_reqs] = first[p.n_reqs];
+    back[p.n_reqs] = (int)freed_all;
+  }
+  __syncthreads();
+  if (freed_all) {
+    for (int i0 = tid; i0 < (int)freed_all; i0 += 4 * NT) {
+      int32_t* entry[4];
+      int32_t page[4];
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const int i = i0 + e * NT;
+        entry[e] = nullptr;
+        if (i < (int)freed_all) {
+          const int b = find_request(back, p.n_reqs, i);  // (it shrank: its pages are the last ones of its old length)
+          const int place = pages(length[b]) - (back[b + 1] - back[b]) + i - back[b];
+          entry[e] = p.table + (size_t)b * p.max_pages + min(max(place, 0), p.max_pages - 1);
+          page[e] = *entry[e];
+        }
+      }
+#pragma unroll
+      for (int e = 0; e < 4; e++)
+        if (entry[e]) {
+          stack[have0 + i0 + e * NT] = page[e];
+          *entry[e] = -1;
+        }
+    }
+    __syncthreads();  // (the stack's new top is read below)
+  }
+  const int n_used = (int)s_used;
+  if (tid == 0) p.free_list[0] = (int)have - n_used;
+  for (int i0 = tid; i0 < n_used; i0 += 4 * NT) {
+    int at[4], to[4];
+    int32_t page[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) {
+      const int i = i0 + e * NT;
+      if (i < n_used) {
+        at[e] = find_request(taken, p.n_reqs, i);
+        to[e] = pages(length[at[e]]) + i - taken[at[e]];
+        page[e] = stack[(int)have - 1 - i];
+      }
+    }
+#pragma unroll
+    for (int e = 0; e < 4; e++)
+      if (i0 + e * NT < n_used) p.table[(size_t)at[e] * p.max_pages + to[e]] = page[e];
+  }
+  if (p.n_rows > ASSIGN_ROWS) return;
+  for (int r = tid; r < p.n_rows; r += NT) {
+    int req = -1, len = 0, slot = -1;
+    if (r < first[p.n_reqs]) {
+      const int b = find_request(first, p.n_reqs, r), n = length[b];
+      if (n >= 0) {
+        const int pos = n + (r - first[b]), place = pos >> p.shift, more = place - pages(n);
+        const int page = more >= 0 ? stack[(int)have - 1 - (taken[b] + more)] : p.table[(size_t)b * p.max_pages + place];
+        req = b;
+        len = pos + 1;
+        slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+      }
+    }
+    p.row_req[r] = req;
+    p.row_len[r] = len;
+    p.slots[r] = slot;
+  }
+}
+
+// The rows of a step with many of them, from what cache_assign_kernel wrote.
+__global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
+  __shared__ int32_t first[CACHE_REQS_MAX + 1];
+  for (int b = threadIdx.x; b <= p.n_reqs; b += 256) first[b] = p.cu_rows[b];
+  __syncthreads();
+  const int r = blockIdx.x * 256 + threadIdx.x;
+  if (r >= p.n_rows) return;
   int req = -1, len = 0, slot = -1;
   if (r < first[p.n_reqs]) {
     const int b = find_request(first, p.n_reqs, r);
-    if (p.status[b] == 0) {
-      const int pos = p.lens[b] - (first[b + 1] - first[b]) + (r - first[b]);  // (lens: with the new tokens)
+    const int state = p.status[b], pos = p.lens[b] - (first[b + 1] - first[b]) + (r - first[b]);  // (the length has the new tokens)
+    if (state == DMA_CACHE_SERVED) {
       const int page = p.table[(size_t)b * p.max_pages + (pos >> p.shift)];
       req = b;
       len = pos + 1;
@@ -64,102 +218,6 @@ __device__ __forceinline__ void assign_row(const AssignArgs& p, const int32_t* f
   p.row_req[r] = req;
   p.row_len[r] = len;
   p.slots[r] = slot;
-}
-
-// Rows that the one workgroup writes itself.
-constexpr int ASSIGN_ROWS = 4096;
-
-__global__ __launch_bounds__(1024) void cache_assign_kernel(AssignArgs p) {
-  __shared__ int32_t first[CACHE_REQS_MAX + 1];  // first row of every request
-  __shared__ int32_t upto[CACHE_REQS_MAX + 1];   // pages given back, then pages taken, by the requests before this one
-  __shared__ long long s_part[16];
-  const int tid = threadIdx.x, ps = 1 << p.shift;
-  const long long cap = (long long)p.max_pages << p.shift;
-  int32_t* stack = p.free_list + FREE_HEADER;
-  const int have0 = max(0, min(p.free_list[0], p.n_pages));
-  auto length = [&](int b) { return (int)max(0ll, min((long long)p.lens[b], cap)); };
-  auto pages = [&](long long n) { return (int)((n + ps - 1) >> p.shift); };
-  // pages given back
-  long long base = 0, total;
-  for (int b0 = 0; b0 < p.n_reqs; b0 += 1024) {
-    const int b = b0 + tid;
-    int freed = 0;
-    if (b < p.n_reqs) {
-      const int old = length(b), c = p.change[b];
-      if (c < 0) freed = pages(old) - pages(max(0ll, (long long)old + c));
-    }
-    const long long inc = scan_1024(freed, s_part, total);
-    if (b < p.n_reqs) upto[b] = (int)min(base + inc - freed, (long long)p.n_pages);
-    base += total;
-  }
-  const int freed_all = (int)min(base, (long long)(p.n_pages - have0));  // (never more, unless the caller's tables are damaged)
-  if (tid == 0) upto[p.n_reqs] = freed_all;
-  __syncthreads();
-  for (int i = tid; i < freed_all; i += 1024) {
-    const int b = find_request(upto, p.n_reqs, i), old = length(b);
-    const int place = pages(max(0ll, (long long)old + p.change[b])) + i - upto[b];
-    if (place >= pages(old)) continue;  // (as above)
-    int32_t* entry = p.table + (size_t)b * p.max_pages + place;
-    stack[have0 + i] = *entry;
-    *entry = -1;
-  }
-  const int have = have0 + freed_all;
-  __syncthreads();
-  // pages taken
-  long long rows = 0, used = 0;
-  base = 0;
-  for (int b0 = 0; b0 < p.n_reqs; b0 += 1024) {
-    const int b = b0 + tid;
-    int old = 0, need = 0, state = 0;
-    long long grow = 0, after = 0;
-    if (b < p.n_reqs) {
-      old = length(b);
-      const int c = p.change[b];
-      grow = max(c, 0);
-      after = max(0ll, (long long)old + c);
-    }
-    const long long end = rows + scan_1024(grow, s_part, total);
-    rows += total;
-    if (grow) {
-      if (after > cap) state = DMA_CACHE_TOO_LONG;
-      else if (end > p.n_rows) state = DMA_CACHE_NO_ROWS;
-      else need = pages(after) - pages(old);
-    }
-    const long long inc = base + scan_1024(need, s_part, total);
-    base += total;
-    if (need && inc > have) state = DMA_CACHE_NO_PAGES;
-    if (need && state) need = 0;
-    (void)scan_1024(need, s_part, total);
-    if (b < p.n_reqs) {
-      first[b] = (int)min(end - grow, (long long)p.n_rows);
-      upto[b] = (int)min(inc - need, (long long)have);  // (served requests are those of a prefix of the sum)
-      p.cu_rows[b] = first[b];
-      p.status[b] = state;
-      p.lens[b] = state ? old : (int)after;
-    }
-    used += total;
-  }
-  if (tid == 0) {
-    first[p.n_reqs] = (int)min(rows, (long long)p.n_rows);
-    p.cu_rows[p.n_reqs] = first[p.n_reqs];
-    p.free_list[0] = have - (int)used;
-  }
-  __syncthreads();
-  for (int i = tid; i < (int)used; i += 1024) {
-    const int b = find_request(upto, p.n_reqs, i), n = p.lens[b];
-    const int place = pages(n - (first[b + 1] - first[b])) + i - upto[b];
-    p.table[(size_t)b * p.max_pages + place] = stack[have - 1 - i];
-  }
-  __syncthreads();
-  if (p.n_rows <= ASSIGN_ROWS)
-    for (int r = tid; r < p.n_rows; r += 1024) assign_row(p, first, r);
-}
-
-__global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
-  __shared__ int32_t first[CACHE_REQS_MAX + 1];
-  for (int b = threadIdx.x; b <= p.n_reqs; b += 256) first[b] = p.cu_rows[b];
-  __syncthreads();
-  for (int r = blockIdx.x * 1024 + threadIdx.x, i = 0; i < 4 && r < p.n_rows; r += 256, i++) assign_row(p, first, r);
 }
 
 __global__ __launch_bounds__(256) void cache_reset_kernel(int32_t* lens, int32_t* table, int32_t* free_list, int n_reqs,
@@ -183,9 +241,10 @@ int launch_cache_assign(const dma_cache_shape& s, int n_rows, const int32_t* cha
                         int32_t* status, hipStream_t st) {
   const AssignArgs p = {change, lens, table, free_list, cu_rows, row_req, row_len, slots, status,
                         s.n_reqs, s.n_pages, s.max_pages, cache_layout(s).shift, n_rows};
-  cache_assign_kernel<<<1, 1024, 0, st>>>(p);
+  if (s.n_reqs <= 1024 && n_rows <= 1024) cache_assign_kernel<256><<<1, 256, 0, st>>>(p);
+  else cache_assign_kernel<1024><<<1, 1024, 0, st>>>(p);
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
-  if (n_rows > ASSIGN_ROWS) cache_rows_kernel<<<(unsigned)((n_rows + 1023) / 1024), 256, 0, st>>>(p);
+  if (n_rows > ASSIGN_ROWS) cache_rows_kernel<<<(unsigned)((n_rows + 255) / 256), 256, 0, st>>>(p);
   return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
 }
 

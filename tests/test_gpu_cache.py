@@ -52,6 +52,19 @@ def test_steps_of_a_server(gpu, n_reqs, n_pages, max_pages, ps, n_rows):
     assert co.SERVED in seen and (n_reqs < 50 or co.TOO_LONG in seen)   # (3 of 100 ask for too much)
 
 
+@pytest.mark.parametrize("n_reqs,n_rows", [(7, 30), (300, 1000), (1500, 900), (4000, 70000)])
+def test_sums_that_pass_32_bits(gpu, n_reqs, n_rows):
+    """Changes of up to 2^31 - 1 in any place: their sums pass 32 bits, the rows of the others stay where they belong."""
+    cache = GpuCache(gpu, n_reqs, 2 * n_reqs + 50, 1 << 12, 16, 2, 1, 64)
+    r = np.random.default_rng(5)
+    for share in (0.02, 0.5, 1.0):
+        change = [int(r.integers(2**30, 2**31)) if r.random() < share else int(r.integers(-3, 6)) for _ in range(n_reqs)]
+        if share == 1.0:
+            change = [2**31 - 1] * n_reqs
+        check_assign(cache, change, n_rows)
+        check_assign(cache, [int(r.integers(-20, 20)) for _ in range(n_reqs)], n_rows)
+
+
 def test_refusals_in_order(gpu):
     cache = GpuCache(gpu, 5, 4, 3, 16, 2, 1, 64)
     assert check_assign(cache, [16, 16, 5, 0, 0], 64) == [0, 0, 0, 0, 0]

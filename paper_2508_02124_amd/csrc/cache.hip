@@ -249,37 +249,64 @@ int launch_cache_assign(const dma_cache_shape& s, int n_rows, const int32_t* cha
 }
 
 // ------------------------------------------------------------------ rows into the cache
-// Eight channels of a lane.
-template <typename T> __device__ __forceinline__ void load8(const T* src, float* x) {
-  if constexpr (sizeof(T) == 2) {
-    const uint4 raw = *reinterpret_cast<const uint4*>(src);
-    const uint32_t u[4] = {raw.x, raw.y, raw.z, raw.w};
+// Eight channels of a lane, as they come, and as fp32.
+template <typename T> struct Raw8;
+template <> struct Raw8<__bf16> { uint4 x; };
+template <> struct Raw8<float> { float4 a, b; };
+__device__ __forceinline__ void load_raw(const __bf16* src, Raw8<__bf16>& r) { r.x = *reinterpret_cast<const uint4*>(src); }
+__device__ __forceinline__ void load_raw(const float* src, Raw8<float>& r) {
+  r.a = reinterpret_cast<const float4*>(src)[0];
+  r.b = reinterpret_cast<const float4*>(src)[1];
+}
+__device__ __forceinline__ void to_f32(const Raw8<__bf16>& r, float* x) {
+  const uint32_t u[4] = {r.x.x, r.x.y, r.x.z, r.x.w};
 #pragma unroll
-    for (int e = 0; e < 4; e++) {
-      x[2 * e] = __uint_as_float(u[e] << 16);
-      x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-    }
-  } else {
-    const float4 a = *reinterpret_cast<const float4*>(src), b = *reinterpret_cast<const float4*>(src + 4);
-    x[0] = a.x; x[1] = a.y; x[2] = a.z; x[3] = a.w;
-    x[4] = b.x; x[5] = b.y; x[6] = b.z; x[7] = b.w;
+  for (int e = 0; e < 4; e++) {
+    x[2 * e] = __uint_as_float(u[e] << 16);
+    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
   }
+}
+__device__ __forceinline__ void to_f32(const Raw8<float>& r, float* x) {
+  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
+  x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
 }
 
 template <int CTRL> __device__ __forceinline__ uint32_t dpp_quad(uint32_t x) {
   return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
 }
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
-// The codes of a lane's eight channels, and the scale byte that four neighbouring lanes (32 channels) share: the power of two at
-// which the largest value rounds to at most 6, 2^(exponent - 2) or, from a mantissa of 1.75 on, twice that.  A block that holds
-// an infinity or NaN has the byte 255.  Bytes 2 to 252: what the cache holds is finite and normal in fp32 and bf16 alike.
-__device__ __forceinline__ uint32_t quantise8(const float* x, uint32_t& byte) {
-  uint32_t top = 0;  // (as integers: the bits of NaN are above those of every number)
-#pragma unroll
-  for (int e = 0; e < 8; e++) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+// The scale byte that four neighbouring lanes (32 channels) share, from the bits of the largest magnitude of a lane's (as integers: the
+// bits of NaN are above those of every number): the power of two at which it rounds to at most 6, 2^(exponent - 2) or, from a
+// mantissa of 1.75 on, twice that.  A block that holds an infinity or NaN has the byte 255.  Bytes 2 to 252: what the cache holds is
+// finite and normal in fp32 and bf16 alike.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   top = max(top, dpp_quad<0xb1>(top));
   top = max(top, dpp_quad<0x4e>(top));
-  byte = top >= 0x7f800000u ? 255u : (uint32_t)max(2, min(252, (int)((top + 0x200000u) >> 23) - 2));
+  return top >= 0x7f800000u ? 255u : (uint32_t)max(2, min(252, (int)((top + 0x200000u) >> 23) - 2));
+}
+// The codes of a lane's eight channels, and that byte.
+__device__ __forceinline__ uint32_t quantise8(const Raw8<__bf16>& r, uint32_t& byte) {
+  const uint32_t u[4] = {r.x.x, r.x.y, r.x.z, r.x.w};
+  u16x2 top = __builtin_bit_cast(u16x2, u[0] & 0x7fff7fffu);
+#pragma unroll
+  for (int e = 1; e < 4; e++) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, u[e] & 0x7fff7fffu));
+  byte = scale_byte((uint32_t)max(top[0], top[1]) << 16);
+  const float scale = mx_scale(byte);
+  uint32_t code = 0;
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[0]), scale, 0);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[1]), scale, 1);
+  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[2]), scale, 2);
+  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[3]), scale, 3);
+}
+__device__ __forceinline__ uint32_t quantise8(const Raw8<float>& r, uint32_t& byte) {
+  float x[8];
+  to_f32(r, x);
+  uint32_t top = 0;
+#pragma unroll
+  for (int e = 0; e < 8; e++) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
+  byte = scale_byte(top);
   const float scale = mx_scale(byte);
   uint32_t code = 0;
   code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], scale, 0);
@@ -288,8 +315,27 @@ __device__ __forceinline__ uint32_t quantise8(const float* x, uint32_t& byte) {
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], scale, 3);
 }
 
+// Where the rows of a tile of 64 go: the page (none: null) and the place in it, worked out once for all of a row's lanes (a 64-bit
+// product each).
+struct TileRows {
+  char* page[64];
+  uint32_t place[64];
+};
+__device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __restrict__ slots, int t0, int n_rows, TileRows& rows) {
+  if (threadIdx.x < 64) {
+    const int t = t0 + threadIdx.x;
+    const uint32_t slot = t < n_rows ? (uint32_t)slots[t] : 0xffffffffu;
+    rows.page[threadIdx.x] = slot < c.n_slots ? cache_page(c, slot) : nullptr;
+    rows.place[threadIdx.x] = cache_place(c, slot);
+  }
+}
+
 // One workgroup per (64 rows, kv-head).  A row is held by D / 8 lanes; K and V of all rows of the tile are requested before the
 // first is used.  The scores are those of z_kernel, bit for bit: the same sums in the same order.
+// Bound by HBM: 65536 rows of 8 heads of 128 channels, 32 scores each, out of a projection of 48 heads, 81 us for 350 MB (4.3 TB/s;
+// a copy reaches 4.75), 50 us without a slot to write to.  (A row's pages worked out by each of its lanes, and fp32 values where
+// bf16 ones do, 960 vector instructions instead of 730, took as long; so do heads before rows in the order of the workgroups.  Passes
+// without a row left out: + 3 us, a call of one row as before.)
 template <typename T, int D, int GMAX>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* __restrict__ K, long k_stride,
                                                            const T* __restrict__ V, long v_stride,
@@ -297,60 +343,71 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
                                                            const float* __restrict__ z, const int32_t* __restrict__ slots,
                                                            int n_rows) {
   extern __shared__ float zs[];  // [G][64]
-  __shared__ uint32_t s_slot[64];
+  __shared__ TileRows rows;
   constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
+  __shared__ __align__(16) uint8_t bytes[64][D / 16];  // the rows' scales, K's and V's, which leave together
   const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
   const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
-  if (tid < 64) s_slot[tid] = t0 + tid < n_rows ? (uint32_t)slots[t0 + tid] : 0xffffffffu;
-  float k[NP][8], v[NP][8];
+  tile_rows(c, slots, t0, n_rows, rows);
+  Raw8<T> k[NP], v[NP];
 #pragma unroll
   for (int pass = 0; pass < NP; pass++) {
     const long t = min(t0 + pass * RPP + rl, n_rows - 1);
-    load8(K + t * k_stride + (long)g * D + 8 * sub, k[pass]);
-    load8(V + t * v_stride + (long)g * D + 8 * sub, v[pass]);
+    load_raw(K + t * k_stride + (long)g * D + 8 * sub, k[pass]);
+    load_raw(V + t * v_stride + (long)g * D + 8 * sub, v[pass]);
   }
   __syncthreads();
 #pragma unroll
   for (int pass = 0; pass < NP; pass++) {
-    const uint32_t slot = s_slot[pass * RPP + rl];
+    const int r = pass * RPP + rl;
+    char* page = rows.page[r];
+    const uint32_t at = ((uint32_t)g << c.shift) + rows.place[r];
     uint32_t kb, vb;
     const uint32_t kc = quantise8(k[pass], kb), vc = quantise8(v[pass], vb);
-    if (slot < c.n_slots) {
-      char* page = cache_page(c, slot);
-      const uint32_t at = ((uint32_t)g << c.shift) + cache_place(c, slot);
-      uint32_t* codes = reinterpret_cast<uint32_t*>(page + (size_t)at * D);
-      codes[sub] = kc;
-      codes[LPR + sub] = vc;
-      uint8_t* scales = reinterpret_cast<uint8_t*>(page) + c.off_scales + (size_t)at * (D / 16);
-      if (sub % 4 == 0) {
-        scales[sub / 4] = (uint8_t)kb;
-        scales[D / 32 + sub / 4] = (uint8_t)vb;
-      }
+    if (page) {
+      uint32_t* codes = reinterpret_cast<uint32_t*>(page + (at * D + 4 * sub));
+      codes[0] = kc;
+      codes[LPR] = vc;
+    }
+    if (sub % 4 == 0) {
+      bytes[r][sub / 4] = (uint8_t)kb;
+      bytes[r][D / 32 + sub / 4] = (uint8_t)vb;
     }
   }
   if (W) {
     for (int h0 = 0; h0 < G; h0 += GMAX) {
       float wreg[GMAX][8];
 #pragma unroll
-      for (int hh = 0; hh < GMAX; hh++) load8(W + (size_t)(g * G + min(h0 + hh, G - 1)) * D + 8 * sub, wreg[hh]);
+      for (int hh = 0; hh < GMAX; hh++) {
+        Raw8<float> raw;
+        load_raw(W + (size_t)(g * G + min(h0 + hh, G - 1)) * D + 8 * sub, raw);
+        to_f32(raw, wreg[hh]);
+      }
 #pragma unroll
       for (int pass = 0; pass < NP; pass++) {
+        float x[8];
+        to_f32(v[pass], x);
 #pragma unroll
         for (int hh = 0; hh < GMAX; hh++) {
           float acc = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], v[pass][e], acc);
+          for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], x[e], acc);
           acc = group_sum<LPR>(acc);
           if (sub == hh % LPR && h0 + hh < G) zs[(h0 + hh) * 64 + pass * RPP + rl] = acc;
         }
       }
     }
-    __syncthreads();
+  }
+  __syncthreads();
+  if (tid < 64 && rows.page[tid]) {
+    using Bytes = std::conditional_t<D == 64, uint32_t, std::conditional_t<D == 128, uint2, uint4>>;
+    char* to = rows.page[tid] + (c.off_scales + (((uint32_t)g << c.shift) + rows.place[tid]) * (D / 16));
+    *reinterpret_cast<Bytes*>(to) = *reinterpret_cast<const Bytes*>(bytes[tid]);
   }
   for (int i = tid; i < G * 64; i += 256) {
     const int h = g * G + (i >> 6), r = i & 63;
-    const uint32_t slot = s_slot[r];
-    if (slot >= c.n_slots) continue;
+    char* page = rows.page[r];
+    if (!page) continue;
     float zv;
     if (W) {
       const float x = zs[i], sp = fmaxf(x, 0.f) + log1pf(expf(-fabsf(x)));
@@ -358,8 +415,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
     } else {
       zv = z[(size_t)h * n_rows + t0 + r];
     }
-    float* zp = reinterpret_cast<float*>(cache_page(c, slot) + c.off_z);
-    zp[((size_t)h << c.shift) + cache_place(c, slot)] = zv;
+    reinterpret_cast<float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] = zv;
   }
 }
 
@@ -369,25 +425,25 @@ template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32_t* __restrict__ slots, T* __restrict__ K,
                                                          T* __restrict__ V, float* __restrict__ z, int n_rows) {
   constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
-  __shared__ uint32_t s_slot[64];
+  __shared__ TileRows rows;
   const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
   const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
-  if (tid < 64) s_slot[tid] = t0 + tid < n_rows ? (uint32_t)slots[t0 + tid] : 0xffffffffu;
+  tile_rows(c, slots, t0, n_rows, rows);
   __syncthreads();
   uint32_t kc[NP], vc[NP], kb[NP], vb[NP];
 #pragma unroll
   for (int pass = 0; pass < NP; pass++) {
-    const uint32_t slot = s_slot[pass * RPP + rl];
+    const int r = pass * RPP + rl;
+    const char* page = rows.page[r];
+    const uint32_t at = ((uint32_t)g << c.shift) + rows.place[r];
     kc[pass] = vc[pass] = kb[pass] = vb[pass] = 0;
-    if (slot < c.n_slots) {
-      const char* page = cache_page(c, slot);
-      const uint32_t at = ((uint32_t)g << c.shift) + cache_place(c, slot);
-      const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + (size_t)at * D);
-      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page) + c.off_scales + (size_t)at * (D / 16);
-      kc[pass] = codes[sub];
-      vc[pass] = codes[LPR + sub];
-      kb[pass] = scales[sub / 4];
-      vb[pass] = scales[D / 32 + sub / 4];
+    if (page) {
+      const uint32_t* codes = reinterpret_cast<const uint32_t*>(page + (at * D + 4 * sub));
+      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (c.off_scales + at * (D / 16) + sub / 4));
+      kc[pass] = codes[0];
+      vc[pass] = codes[LPR];
+      kb[pass] = scales[0];
+      vb[pass] = scales[D / 32];
     }
   }
   auto put = [&](T* dst, uint32_t code, uint32_t byte) {
@@ -417,11 +473,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32
   for (int i = tid; i < G * 64; i += 256) {
     const int h = g * G + (i >> 6), r = i & 63;
     if (t0 + r >= n_rows) continue;
-    const uint32_t slot = s_slot[r];
-    float zv = -INFINITY;
-    if (slot < c.n_slots)
-      zv = reinterpret_cast<const float*>(cache_page(c, slot) + c.off_z)[((size_t)h << c.shift) + cache_place(c, slot)];
-    z[(size_t)h * n_rows + t0 + r] = zv;
+    const char* page = rows.page[r];
+    z[(size_t)h * n_rows + t0 + r] = page ? reinterpret_cast<const float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] : -INFINITY;
   }
 }
 

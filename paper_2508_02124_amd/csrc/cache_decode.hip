@@ -358,14 +358,14 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   }
 }
 
-// One workgroup per (row, head), for rows of up to SELECT_SHORT keys (or of any length, where the window keeps them all).
+// One workgroup per (row, head), for rows of up to SELECT_SHORT keys.
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
 template <int S>
-__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept, int longest) {
+__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept) {
   const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);
   const int n = row.n, kk = min(p.k, n);
-  if (n > longest) return;
+  if (n > SELECT_SHORT) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
   if (kk == n) {
     bool bad = false;
@@ -693,11 +693,13 @@ template <> struct Query<float> {
 };
 
 // One workgroup per (ch kept keys, row, head).  A key's K (and V) row is held by D / 32 lanes, 32 channels with one scale each; a
-// wave takes 64 keys at a time, all of them requested before the first is used, and has one running maximum.  The G heads
-// of a kv-head have the same part of their lists on one XCD at the same time (decode_attend_kernel).
-template <typename TQ, int D>
+// wave takes 64 keys at a time, all of them requested before the first is used.  Weights are formed with the reference so far; only
+// a score more than 5 above it leads to the wave's maximum and a rescaling (sums in 32 bits hold weights up to e^5 as well as
+// up to 1).  The G heads of a kv-head have the same part of their lists on one XCD at the same time (decode_attend_kernel).
+// ALL: the window keeps every key that a request can have, so nothing was selected, and the lists are written here.
+template <typename TQ, int D, bool ALL>
 __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows p, const TQ* __restrict__ q, long q_stride,
-                                                           const int32_t* __restrict__ kept, float* __restrict__ part,
+                                                           int32_t* __restrict__ kept, float* __restrict__ part,
                                                            TQ* __restrict__ o, float* __restrict__ lse, int ch, int nsplit,
                                                            float scale) {
   constexpr int LPG = D / 32, NG = 64 / LPG, U = 64 / NG;
@@ -707,23 +709,47 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   if (sp >= nsplit) return;
   const int r = rg / c.H_kv, g = rg - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
-  const int32_t* list = kept + (size_t)rh * p.kcap;
+  int32_t* list = kept + (size_t)rh * p.kcap;
   int i0 = sp * ch + w * 64;
-  uint32_t id[U];  // (requested before the number of kept keys is known)
+  uint32_t id[U];
+  if (!ALL) {  // (requested before the number of kept keys is known)
 #pragma unroll
-  for (int u = 0; u < U; u++) id[u] = (uint32_t)list[min(i0 + u * NG + grp, p.kcap - 1)];
+    for (int u = 0; u < U; u++) id[u] = (uint32_t)list[min(i0 + u * NG + grp, p.kcap - 1)];
+  }
   Query<TQ> qv;
   qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
-  const int kk = min(p.k, cache_row(c, p, r).n), end = min(kk, (sp + 1) * ch);
-  if (sp * ch >= kk) {
+  const CacheRow row = cache_row(c, p, r);
+  const int kk = min(p.k, row.n), end = min(kk, (sp + 1) * ch);
+  auto finish = [&](float num, float den, float M) {  // (all threads)
+    if (tid >= D) return;
     if (nsplit == 1) {
-      if (tid < D) o[(size_t)rh * D + tid] = TQ(0.f);
-      if (tid == 0) lse[(size_t)h * p.n_rows + r] = -INFINITY;
+      o[(size_t)rh * D + tid] = TQ(den == 0.f ? 0.f : num / den);
+      if (tid == 0) lse[(size_t)h * p.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
+    } else {
+      float* out = part + ((size_t)rh * nsplit + sp) * (D + 2);
+      out[tid] = num;
+      if (tid == 0) {
+        out[D] = M;
+        out[D + 1] = den;
+      }
     }
+  };
+  bool bad = false;
+  if constexpr (ALL) {
+#pragma unroll
+    for (int u = 0; u < U; u++) id[u] = cache_slot(c, row, min(i0 + u * NG + grp, p.kcap - 1));
+    for (int j = tid; j << c.shift < row.n; j += 256) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;
+  }
+  if (sp * ch >= kk) {
+    if (ALL)
+      for (int i = sp * ch + tid; i < min(p.kcap, (sp + 1) * ch); i += 256) list[i] = -1;
+    if (nsplit == 1) finish(0.f, 0.f, -INFINITY);
     return;
   }
-  const char* zh = c.pages + c.off_z + ((size_t)h << c.shift) * 4;
-  float m = -INFINITY, lsum = 0.f, acc[32];
+  // byte offsets in a page of this lane's part of the head's first token
+  const uint32_t k_off = ((uint32_t)g << c.shift) * D + 16 * sub, z_off = c.off_z + ((uint32_t)h << c.shift) * 4;
+  const uint32_t b_off = c.off_scales + ((uint32_t)g << c.shift) * (D / 16) + sub, page_bytes = (uint32_t)c.page_bytes;
+  float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f, acc[32];
 #pragma unroll
   for (int e = 0; e < 32; e++) acc[e] = 0.f;
 #pragma unroll 1
@@ -735,18 +761,17 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
     for (int u = 0; u < U; u++) {
       const bool there = i0 + u * NG + grp < end && id[u] < c.n_slots;
       const uint32_t slot = there ? id[u] : 0u, place = cache_place(c, slot);
-      const size_t page = (size_t)(slot >> c.shift) * c.page_bytes;
-      const uint32_t at = ((uint32_t)g << c.shift) + place;
-      const uint4* codes = reinterpret_cast<const uint4*>(c.pages + page + (size_t)at * D);
-      const uint8_t* scales = reinterpret_cast<const uint8_t*>(c.pages) + page + c.off_scales + (size_t)at * (D / 16);
-      kr[u] = codes[sub];
-      vr[u] = codes[LPG + sub];
-      kb[u] = scales[sub];
-      vb[u] = scales[LPG + sub];
-      s2[u] = reinterpret_cast<const float*>(zh + page)[place];
+      const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
+      const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
+      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (b_off + place * (D / 16)));
+      kr[u] = codes[0];
+      vr[u] = codes[LPG];
+      kb[u] = scales[0];
+      vb[u] = scales[LPG];
+      s2[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
       id[u] = there ? 1u : 0u;
     }
-    float top = m;
+    float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const float sc = mx_scale(kb[u]), zb = id[u] ? s2[u] : -INFINITY;
@@ -756,14 +781,18 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
       s = lanes_sum<LPG>(qv.template dot8<3>(kr[u].w, sc, s));
       s2[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
       top = fmaxf(top, s2[u]);
-      id[u] = (uint32_t)list[min(i0 + 256 + u * NG + grp, p.kcap - 1)];
+      const int next = min(i0 + 256 + u * NG + grp, p.kcap - 1);
+      id[u] = ALL ? cache_slot(c, row, next) : (uint32_t)list[next];
     }
-    top = over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); });
-    const float ref = top == -INFINITY ? 0.f : top, alpha = weight(m, ref);
-    m = top;
-    lsum *= alpha;
+    if (__ballot(top > limit)) {
+      top = fmaxf(m, over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); }));
+      const float alpha = weight(m, top);
+      m = ref = top;
+      limit = top + 5.f;
+      lsum *= alpha;
 #pragma unroll
-    for (int e = 0; e < 32; e++) acc[e] *= alpha;
+      for (int e = 0; e < 32; e++) acc[e] *= alpha;
+    }
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const float pv = weight(s2[u], ref), sc = s2[u] == -INFINITY ? 0.f : mx_scale(vb[u]);
@@ -795,28 +824,22 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
     ml[w][0] = m;
     ml[w][1] = lsum;
   }
-  __syncthreads();
-  if (tid < D) {
-    const float M = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), ref = M == -INFINITY ? 0.f : M;
-    float num = 0.f, den = 0.f;
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      const float w8 = weight(ml[i][0], ref);
-      num = fmaf(mo[i][tid], w8, num);
-      den = fmaf(ml[i][1], w8, den);
-    }
-    if (nsplit == 1) {
-      o[(size_t)rh * D + tid] = TQ(den == 0.f ? 0.f : num / den);
-      if (tid == 0) lse[(size_t)h * p.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
-    } else {
-      float* out = part + ((size_t)rh * nsplit + sp) * (D + 2);
-      out[tid] = num;
-      if (tid == 0) {
-        out[D] = M;
-        out[D + 1] = den;
-      }
-    }
+  if (ALL ? __syncthreads_or(bad) : (__syncthreads(), 0)) {  // a page is out of range: the row sees nothing
+    for (int i = sp * ch + tid; i < min(p.kcap, (sp + 1) * ch); i += 256) list[i] = -1;
+    finish(0.f, 0.f, -INFINITY);
+    return;
   }
+  if (ALL)
+    for (int i = sp * ch + tid; i < min(p.kcap, (sp + 1) * ch); i += 256) list[i] = i < kk ? (int32_t)cache_slot(c, row, i) : -1;
+  const float M = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), mr = M == -INFINITY ? 0.f : M;
+  float num = 0.f, den = 0.f;
+#pragma unroll
+  for (int i = 0; i < 4; i++) {
+    const float w8 = weight(ml[i][0], mr);
+    num = fmaf(mo[i][tid % D], w8, num);
+    den = fmaf(ml[i][1], w8, den);
+  }
+  finish(num, den, M);
 }
 
 // The parts of one (row, head) together: o = sum_s o_s e^(M_s - M) / sum_s l_s e^(M_s - M), eight parts requested at a time.
@@ -896,11 +919,14 @@ size_t cache_decode_bytes(const dma_cache_shape& s, int n_rows, int k) {
 
 template <typename TQ, int D>
 static void decode_t(const dma_cache_shape& s, const CacheRef& c, const CacheRows& p, float scale, const void* q, long q_stride,
-                     void* o, float* lse, const int32_t* kept, float* part, hipStream_t st) {
+                     void* o, float* lse, int32_t* kept, float* part, bool all, hipStream_t st) {
   const int ch = attend_part(s, p.n_rows, p.kcap), nsplit = (p.kcap + ch - 1) / ch;
   const long units = ((long)p.n_rows * s.H_kv * nsplit + 7) / 8 * 8;
   const unsigned grid = (unsigned)(units * (s.H_q / s.H_kv));
-  cache_attend_kernel<TQ, D><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, ch, nsplit, scale);
+  if (all)
+    cache_attend_kernel<TQ, D, true><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, ch, nsplit, scale);
+  else
+    cache_attend_kernel<TQ, D, false><<<grid, 256, 0, st>>>(c, p, (const TQ*)q, q_stride, kept, part, (TQ*)o, lse, ch, nsplit, scale);
   if (nsplit > 1)
     cache_merge_kernel<TQ, D><<<(unsigned)(p.n_rows * s.H_q), D, 0, st>>>(c, p, part, (TQ*)o, lse, ch, nsplit);
 }
@@ -913,10 +939,12 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   const unsigned pairs = (unsigned)(n_rows * s.H_q);
   const bool wide = s.page_size >= 64;
   const DecodeWork wk = decode_work(s, n_rows, k);
-  const int longest = wk.slices ? SELECT_SHORT : INT32_MAX;
-  if (wide) cache_select_kernel<1><<<pairs, 512, 0, st>>>(c, p, kept, longest);
-  else cache_select_kernel<4><<<pairs, 512, 0, st>>>(c, p, kept, longest);
-  if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  const bool all = k >= (long)s.max_pages * s.page_size;
+  if (!all) {
+    if (wide) cache_select_kernel<1><<<pairs, 512, 0, st>>>(c, p, kept);
+    else cache_select_kernel<4><<<pairs, 512, 0, st>>>(c, p, kept);
+    if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  }
   if (wk.slices) {
     char* base = (char*)ws;
     const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.slices};
@@ -929,9 +957,9 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   }
   auto go = [&](auto t) {
     using T = std::remove_pointer_t<decltype(t)>;
-    if (s.d == 256) decode_t<T, 256>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, st);
-    else if (s.d == 128) decode_t<T, 128>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, st);
-    else decode_t<T, 64>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, st);
+    if (s.d == 256) decode_t<T, 256>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, all, st);
+    else if (s.d == 128) decode_t<T, 128>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, all, st);
+    else decode_t<T, 64>(s, c, p, scale, q, q_stride, o, lse, kept, (float*)ws, all, st);
   };
   if (s.dtype == DMA_BF16) go((__bf16*)nullptr); else go((float*)nullptr);
   return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;

@@ -304,7 +304,7 @@ def test_long_rows_with_outputs(gpu):
     q = normal(gpu, 5, len(rows), 4, 128).to(cache.type)
     req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
     length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
-    for k in (1500, 30080, 20000):
+    for k in (1500, 30080, 20000, 30079):
         check_rows(cache, q, k, rows, cache.decode(q, k, req, length))
 
 

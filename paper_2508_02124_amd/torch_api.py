@@ -160,3 +160,20 @@ class DynamicMaskAttention(torch.nn.Module):
             raise ValueError("packed inputs need cu_seqlens")
         return dynamic_mask_attention(q, k, v, self.W, self.A, cu_seqlens, self.keep_window, max_seqlen,
                                       self.softmax_scale)
+
+    def step(self, q, k, v, cache, rows):
+        """A decoding step over a paged cache (paged_cache.PagedCache): k, v [n, H_kv, d] of the step's new rows go to their places
+        with this module's scores, then q [n, H_q, d] attends from them.  rows: what cache.assign returned.  Without
+        gradients; o [n, H_q, d]."""
+        with torch.no_grad():
+            W, A = self.W.detach(), self.A.detach()
+            if W.shape[1] == self.head_dim:
+                cache.append(rows.slots, k, v, W=W, A=A)
+            else:                                    # the cross-head scores have an entry point of their own
+                n = v.shape[0]
+                z = torch.empty((self.num_heads, n), dtype=torch.float32, device=v.device)
+                if n:
+                    shape = B.make_shape(n, 1, self.num_heads, self.num_kv_heads, self.head_dim, 1, dtype=_dtype_code(v))
+                    cache._call_with(shape, B.dma_scores_xhead, v.contiguous(), W, A, z)
+                cache.append(rows.slots, k, v, z=z)
+            return cache.decode(q, self.keep_window, rows, self.softmax_scale)[0]

@@ -702,7 +702,7 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
                                                            int32_t* __restrict__ kept, float* __restrict__ part,
                                                            TQ* __restrict__ o, float* __restrict__ lse, int ch, int nsplit,
                                                            float scale) {
-  constexpr int LPG = D / 32, NG = 64 / LPG, U = 64 / NG;
+  constexpr int LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
   const unsigned wg = blockIdx.x;
   const int G = c.H_q / c.H_kv, idx = (int)(wg >> 3), unit = (idx / G) * 8 + (int)(wg & 7);
   const int rows_g = p.n_rows * c.H_kv, sp = unit / rows_g, rg = unit - sp * rows_g;
@@ -710,7 +710,7 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   const int r = rg / c.H_kv, g = rg - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
   int32_t* list = kept + (size_t)rh * p.kcap;
-  int i0 = sp * ch + w * 64;
+  int i0 = sp * ch + w * KEYS;
   uint32_t id[U];
   if (!ALL) {  // (requested before the number of kept keys is known)
 #pragma unroll
@@ -752,11 +752,15 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f, acc[32];
 #pragma unroll
   for (int e = 0; e < 32; e++) acc[e] = 0.f;
-#pragma unroll 1
-  for (; i0 < end; i0 += 256) {
+  struct Keys {  // of a step, on their way
     uint4 kr[U], vr[U];
     uint32_t kb[U], vb[U];
-    float s2[U];
+    float s[U];
+    uint32_t there;
+  };
+  // the keys at i0 (in id), and the ids of those behind them
+  auto fetch = [&](Keys& x) {
+    x.there = 0;
 #pragma unroll
     for (int u = 0; u < U; u++) {
       const bool there = i0 + u * NG + grp < end && id[u] < c.n_slots;
@@ -764,25 +768,31 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
       const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
       const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
       const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (b_off + place * (D / 16)));
-      kr[u] = codes[0];
-      vr[u] = codes[LPG];
-      kb[u] = scales[0];
-      vb[u] = scales[LPG];
-      s2[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
-      id[u] = there ? 1u : 0u;
+      x.kr[u] = codes[0];
+      x.vr[u] = codes[LPG];
+      x.kb[u] = scales[0];
+      x.vb[u] = scales[LPG];
+      x.s[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
+      x.there |= there ? 1u << u : 0u;
     }
+    i0 += 4 * KEYS;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int next = min(i0 + u * NG + grp, p.kcap - 1);
+      id[u] = ALL ? cache_slot(c, row, next) : (uint32_t)list[next];
+    }
+  };
+  auto take = [&](Keys& x) {
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const float sc = mx_scale(kb[u]), zb = id[u] ? s2[u] : -INFINITY;
-      float s = qv.template dot8<0>(kr[u].x, sc, 0.f);
-      s = qv.template dot8<1>(kr[u].y, sc, s);
-      s = qv.template dot8<2>(kr[u].z, sc, s);
-      s = lanes_sum<LPG>(qv.template dot8<3>(kr[u].w, sc, s));
-      s2[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
-      top = fmaxf(top, s2[u]);
-      const int next = min(i0 + 256 + u * NG + grp, p.kcap - 1);
-      id[u] = ALL ? cache_slot(c, row, next) : (uint32_t)list[next];
+      const float sc = mx_scale(x.kb[u]), zb = x.there >> u & 1 ? x.s[u] : -INFINITY;
+      float s = qv.template dot8<0>(x.kr[u].x, sc, 0.f);
+      s = qv.template dot8<1>(x.kr[u].y, sc, s);
+      s = qv.template dot8<2>(x.kr[u].z, sc, s);
+      s = lanes_sum<LPG>(qv.template dot8<3>(x.kr[u].w, sc, s));
+      x.s[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
+      top = fmaxf(top, x.s[u]);
     }
     if (__ballot(top > limit)) {
       top = fmaxf(m, over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); }));
@@ -795,9 +805,9 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
     }
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const float pv = weight(s2[u], ref), sc = s2[u] == -INFINITY ? 0.f : mx_scale(vb[u]);
+      const float pv = weight(x.s[u], ref), sc = x.s[u] == -INFINITY ? 0.f : mx_scale(x.vb[u]);
       lsum += pv;
-      const uint32_t code[4] = {vr[u].x, vr[u].y, vr[u].z, vr[u].w};
+      const uint32_t code[4] = {x.vr[u].x, x.vr[u].y, x.vr[u].z, x.vr[u].w};
 #pragma unroll
       for (int i = 0; i < 4; i++) {
         static_for<4>([&](auto b) {
@@ -808,6 +818,18 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
         });
       }
     }
+  };
+  if (i0 < end) {
+    Keys now;
+    fetch(now);
+#pragma unroll 1
+    while (i0 < end) {
+      Keys next;
+      fetch(next);
+      take(now);
+      now = next;
+    }
+    take(now);
   }
   const auto add = [](float a, float b) { return a + b; };
   lsum = over_groups<LPG>(lsum, add);
@@ -884,7 +906,7 @@ static int list_length(const dma_cache_shape& s, int k) {
 }
 
 // Kept keys per workgroup of the attention, a multiple of 256 (64 for each wave): shorter parts where there are few lists.
-constexpr int ATTEND_WGS = 2 * CUS;
+constexpr int ATTEND_WGS = CUS;
 static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
   const long lists = (long)n_rows * s.H_q, most = (kcap + 255) / 256;
   long parts = (ATTEND_WGS + lists - 1) / lists;

@@ -326,6 +326,8 @@ typedef struct {
   int32_t H_kv;        /* key/value heads, divides H_q                                          */
   int32_t d;           /* head dimension: 64, 128 or 256                                        */
   int32_t dtype;       /* dma_dtype of K, V, q, o                                               */
+  int32_t max_len;     /* upper bound on the keys that a row of dma_cache_decode sees (0 => max_pages * page_size).  It chooses
+                          between equal ways of working; a bound that is too small costs time but changes no result          */
 } dma_cache_shape;
 
 /* Bytes of the pool, of the free list, and of the scratch of one dma_cache_decode; 0 if an argument is invalid. */
@@ -402,8 +404,8 @@ int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* 
  *   kept     out [n_rows, H_q, min(k, max_pages * page_size)] int32: the slots of the kept keys in order of position, -1 behind
  *                them
  *   ws       dma_cache_decode_bytes(shape, n_rows, k) bytes of scratch; calls that overlap need one each
- * DMA_EUNSUPPORTED where (n_rows + 8) * H_q, times the larger of ceil(min(k, n) / 256) and min(n / 8192 + 1, 64) for
- * n = max_pages * page_size, reaches 2^22: a whole prompt goes through dma_mask_gen and dma_fwd.
+ * DMA_EUNSUPPORTED where (n_rows + 8) * H_q * ceil(min(k, max_pages * page_size) / 256) reaches 2^22: a whole prompt goes through
+ * dma_mask_gen and dma_fwd.
  */
 int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
                      int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,

@@ -40,7 +40,7 @@ class DmaCacheShape(ctypes.Structure):
     _fields_ = [
         ("n_reqs", ctypes.c_int32), ("n_pages", ctypes.c_int32), ("max_pages", ctypes.c_int32),
         ("page_size", ctypes.c_int32), ("H_q", ctypes.c_int32), ("H_kv", ctypes.c_int32), ("d", ctypes.c_int32),
-        ("dtype", ctypes.c_int32),
+        ("dtype", ctypes.c_int32), ("max_len", ctypes.c_int32),
     ]
 
 
@@ -277,8 +277,9 @@ def dma_bwd_scores(shape, Q, K, V, O, dO, LSE, z, expiry, mask, cu_seqlens, W, A
 CACHE_SERVED, CACHE_NO_PAGES, CACHE_TOO_LONG, CACHE_NO_ROWS = 0, 1, 2, 3
 
 
-def make_cache_shape(n_reqs, n_pages, max_pages, page_size, H_q, H_kv, d, dtype=DMA_BF16):
-    return DmaCacheShape(int(n_reqs), int(n_pages), int(max_pages), int(page_size), int(H_q), int(H_kv), int(d), int(dtype))
+def make_cache_shape(n_reqs, n_pages, max_pages, page_size, H_q, H_kv, d, dtype=DMA_BF16, max_len=0):
+    return DmaCacheShape(int(n_reqs), int(n_pages), int(max_pages), int(page_size), int(H_q), int(H_kv), int(d), int(dtype),
+                         int(max_len))
 
 
 def dma_cache_bytes(shape):

@@ -53,7 +53,7 @@ size_t ws_bytes_for(const dma_shape& s) {
 int check_cache(const dma_cache_shape* s) {
   if (!s) return DMA_EINVAL;
   if (s->n_reqs <= 0 || s->n_pages <= 0 || s->max_pages <= 0 || s->H_q <= 0 || s->H_kv <= 0) return DMA_EINVAL;
-  if (s->H_q % s->H_kv != 0) return DMA_EINVAL;
+  if (s->H_q % s->H_kv != 0 || s->max_len < 0) return DMA_EINVAL;
   if (s->d != 64 && s->d != 128 && s->d != 256) return DMA_EUNSUPPORTED;
   if (s->dtype != DMA_BF16 && s->dtype != DMA_F32) return DMA_EUNSUPPORTED;
   if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return DMA_EUNSUPPORTED;
@@ -301,15 +301,13 @@ size_t dma_cache_free_bytes(const dma_cache_shape* shape) {
   return ((size_t)shape->n_pages + FREE_HEADER) * 4;
 }
 
-// The grids of a decode: rows x heads x parts of the list, or slices of a long row, in workgroups of up to 512 threads, fewer than
-// 2^32 threads in all.
+// The grids of a decode: rows x heads x parts of the list, in workgroups of up to 512 threads, fewer than 2^32 threads in all.
 static int check_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k) {
   int rc = check_cache(shape);
   if (rc != DMA_OK) return rc;
   if (n_rows < 0 || k <= 0) return DMA_EINVAL;
   const long cap = (long)shape->max_pages * shape->page_size, parts = ((k < cap ? k : cap) + 255) / 256;
-  const long slices = cap / 8192 + 1 < 64 ? cap / 8192 + 1 : 64;
-  if (((long)n_rows + 8) * shape->H_q * (parts > slices ? parts : slices) >= 1 << 22) return DMA_EUNSUPPORTED;
+  if (((long)n_rows + 8) * shape->H_q * parts >= 1 << 22) return DMA_EUNSUPPORTED;
   return DMA_OK;
 }
 

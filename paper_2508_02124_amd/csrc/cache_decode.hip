@@ -358,45 +358,32 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   }
 }
 
-// One workgroup per (row, head), for rows of up to SELECT_SHORT keys.
-constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
-template <int S>
-__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, int32_t* kept) {
-  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, tid = threadIdx.x;
-  const CacheRow row = cache_row(c, p, r);
-  const int n = row.n, kk = min(p.k, n);
-  if (n > SELECT_SHORT) return;
-  int32_t* list = kept + (size_t)rh * p.kcap;
-  if (kk == n) {
-    bool bad = false;
-    for (int j = tid << c.shift; j < n; j += 512 << c.shift) bad |= (uint32_t)row.pages[j >> c.shift] >= (uint32_t)c.n_pages;
-    const int there = __syncthreads_or(bad) ? 0 : n;
-    for (int j = tid; j < p.kcap; j += 512) list[j] = j < there ? (int32_t)cache_slot(c, row, j) : -1;
-    return;
-  }
-  __shared__ SelectShared<512> m;
-  select_row<512, SELECT_REGS, S, false>(c, row, h, kk, list, m);
-}
-
 // ------------------------------------------------------------------ the kept set of a long row, by slices
-// Rows of more than SELECT_SHORT keys are cut into slices of SLICE keys, a workgroup each, in two launches.  The first looks at
-// the same sample of the whole row in every slice and takes from it two keys that the kk-th best very likely lies between (3.5
-// standard deviations of its rank in the sample to either side); it counts the slice's keys that are better and lists those between, with
-// their positions.  The second ranks the listed keys of all slices, a few per cent of the row, for the exact threshold (by
-// key and position: no ties are left), and writes the slice's kept slots behind those of the slices before it.  Where the threshold lies
-// outside after all, or a list is too short for its keys (ties, above all), or the row has more than SLICES_MAX slices, the first
-// slice's workgroup selects alone.
-constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS;
-constexpr int SAMPLE = 2048, LISTED = 1024, LISTED_ALL = 8192, SLICES_MAX = 64;
+// Rows of more than SELECT_SHORT keys are cut into slices of SLICE keys.  The first launch takes from a sample of the whole row two
+// keys that the kk-th best very likely lies between (3.5 standard deviations of its rank in the sample to either side); it counts a
+// slice's keys that are better and lists those between, with their positions.  The second ranks the listed keys of all slices, a few
+// per cent of the row, for the exact threshold (by key and position: no ties are left), and writes a slice's kept slots behind those
+// of the slices before it.  Where the threshold lies outside after all, or a list is too short for its keys (ties, above all), or
+// the row has more than SLICES_MAX slices, one workgroup selects alone.
+// A row's slices go round its `parts` workgroups.  How many rows are long the host does not know, so there are only as many parts
+// as keep the chip busy: workgroups that find nothing to do cost 1 ns each.
+constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
+constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS, SLICES_MAX = 64;
+constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together, an equal share for each slice
 
 struct SliceWork {
-  uint2* counts;  // [pairs][slices]: better keys, listed keys (more than LISTED: not all are)
-  uint2* listed;  // [pairs][slices][LISTED]: key, position
+  uint2* counts;  // [pairs][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
+  uint2* listed;  // [pairs][LISTED]: key, position
   uint2* bounds;  // [pairs]: first and last key of the lists
-  int slices;
+  int parts;
 };
 
-// How a slice's chunks go round the waves, and its keys (NO_KEY behind the row's end).  False: a page is out of range.
+// The keys of a slice, its chunks in turn to the waves (NO_KEY behind the row's end), once slice_pages has asked for its pages.
+// False: a page is out of range.
+template <int S>
+__device__ __forceinline__ void slice_pages(const CacheRef& c, const CacheRow& row, int slice, PageRun<S>& run) {
+  run.load(c, row, slice * (SLICE / 64) + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), 8, threadIdx.x & 63);
+}
 template <int S>
 __device__ __forceinline__ bool slice_keys(const CacheRef& c, const CacheRow& row, int h, int slice, PageRun<S>& run, uint32_t* key) {
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = threadIdx.x & 63, n = row.n;
@@ -413,37 +400,26 @@ __device__ __forceinline__ bool slice_keys(const CacheRef& c, const CacheRow& ro
   return !bad;
 }
 
+// Counts and lists of one workgroup's slices of a long row.
 template <int S>
-__global__ __launch_bounds__(512, 6) void cache_bracket_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int pairs = p.n_rows * c.H_q, slice = blockIdx.x / pairs, rh = blockIdx.x - slice * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
-  const CacheRow row = cache_row(c, p, r);
+__device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& row, int h, int kk, int rh, int part, const SliceWork& sw,
+                                            SelectShared<512>& m) {
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
+  const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
+  if (slices > SLICES_MAX || part >= slices) return;
   PageRun<S> run;
-  run.load(c, row, slice * (SLICE / 64) + w, 8, l);
-  const int n = row.n, kk = min(p.k, n), first = slice * SLICE;
-  if (n <= SELECT_SHORT || first >= n) return;
-  if (kk == n) {  // every key is kept (a page out of range anywhere: none)
-    int32_t* list = kept + (size_t)rh * p.kcap;
-    bool bad = false;
-    for (int j = tid; j <= (n - 1) >> c.shift; j += 512) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;
-    const int there = __syncthreads_or(bad) ? 0 : n;  // (the last workgroup goes on to the list's end)
-    const int end = first + SLICE >= n || slice == sw.slices - 1 ? p.kcap : first + SLICE;
-    for (int j = first + tid; j < end; j += 512) list[j] = j < there ? (int32_t)cache_slot(c, row, j) : -1;
-    return;
-  }
-  if (n > SLICES_MAX * SLICE) return;
-  __shared__ SelectShared<512> m;
+  slice_pages<S>(c, row, part, run);
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
   for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
   // the sample: one key of each of 2048 equal parts of the row, at a place in it that follows no period
   uint32_t sample[SAMPLE / 512], key[SLICE_CHUNKS];
 #pragma unroll
   for (int e = 0; e < SAMPLE / 512; e++) {
-    const uint32_t i = (uint32_t)(e * 512 + tid), part = (uint32_t)n / SAMPLE;
-    const int j = (int)((unsigned long long)i * (uint32_t)n / SAMPLE) + (int)((i * 2654435761u >> 16) * part >> 16);
+    const uint32_t i = (uint32_t)(e * 512 + tid), width = (uint32_t)n / SAMPLE;
+    const int j = (int)((unsigned long long)i * (uint32_t)n / SAMPLE) + (int)((i * 2654435761u >> 16) * width >> 16);
     sample[e] = score_key(cache_score(c, cache_slot(c, row, j), h));
   }
-  const bool good = slice_keys<S>(c, row, h, slice, run, key);
+  bool good = slice_keys<S>(c, row, h, part, run, key);
   uint32_t kmin = NO_KEY, kmax = 0;
 #pragma unroll
   for (int e = 0; e < SAMPLE / 512; e++) {
@@ -454,7 +430,7 @@ __global__ __launch_bounds__(512, 6) void cache_bracket_kernel(CacheRef c, Cache
   kmax = last_lane(wave_scan(kmax, 0u, [](uint32_t x, uint32_t y) { return max(x, y); }));
   if (l == 0) {
     m.wsum[w][0] = kmin;
-    m.wsum[w][1] = good ? kmax : NO_KEY;
+    m.wsum[w][1] = kmax;
   }
   __syncthreads();
 #pragma unroll
@@ -462,16 +438,11 @@ __global__ __launch_bounds__(512, 6) void cache_bracket_kernel(CacheRef c, Cache
     kmin = min(kmin, m.wsum[i][0]);
     kmax = max(kmax, m.wsum[i][1]);
   }
-  uint2* counts = sw.counts + (size_t)rh * sw.slices + slice;
-  if (kmax == NO_KEY) {  // (a page is out of range: the second launch sees an impossible count)
-    if (tid == 0) *counts = make_uint2(0, NO_KEY);
-    return;
-  }
   const uint32_t range = kmax - kmin;
   const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
 #pragma unroll
   for (int e = 0; e < SAMPLE / 512; e++) atomicAdd(&m.hist[((sample[e] - kmin) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
-  const float share = (float)kk / (float)n, middle = share * SAMPLE, off = 3.5f * sqrtf(middle * (1.f - share)) + 3.f;
+  const float kept_share = (float)kk / (float)n, middle = kept_share * SAMPLE, off = 3.5f * sqrtf(middle * (1.f - kept_share)) + 3.f;
   uint32_t lo = 0, hi = NO_KEY - 1;
   if (middle - off >= 1.f) {
     pick_digit<512, false>(m, (uint32_t)(middle - off));
@@ -484,116 +455,149 @@ __global__ __launch_bounds__(512, 6) void cache_bracket_kernel(CacheRef c, Cache
   }
   lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
   hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
-  uint32_t better = 0, mine = 0;  // keys of this wave
+  if (tid == 0 && part == 0) sw.bounds[rh] = make_uint2(lo, hi);
+  for (int slice = part; slice < slices; slice += sw.parts) {
+    if (slice != part) {
+      slice_pages<S>(c, row, slice, run);
+      good = slice_keys<S>(c, row, h, slice, run, key);
+    }
+    uint32_t better = 0, mine = 0;  // keys of this wave
 #pragma unroll
-  for (int u = 0; u < SLICE_CHUNKS; u++) {
-    better += (uint32_t)__popcll(__ballot(key[u] < lo));
-    mine += (uint32_t)__popcll(__ballot(key[u] - lo <= hi - lo));
-  }
-  __syncthreads();
-  if (l == 0) {
-    m.wsum[w][0] = better;
-    m.wsum[w][1] = mine;
-  }
-  __syncthreads();
-  uint32_t all_better = 0, all = 0, at = 0;
+    for (int u = 0; u < SLICE_CHUNKS; u++) {
+      better += (uint32_t)__popcll(__ballot(key[u] < lo));
+      mine += (uint32_t)__popcll(__ballot(key[u] - lo <= hi - lo));
+    }
+    __syncthreads();  // (wsum: the last digit's, or the slice's before)
+    if (l == 0) {
+      m.wsum[w][0] = better;
+      m.wsum[w][1] = good ? mine : NO_KEY >> 4;  // (a page is out of range: the second launch sees an impossible count)
+    }
+    __syncthreads();
+    uint32_t all_better = 0, all = 0, at = 0;
 #pragma unroll
-  for (int i = 0; i < 8; i++) {
-    at += i < w ? m.wsum[i][1] : 0u;
-    all_better += m.wsum[i][0];
-    all += m.wsum[i][1];
-  }
-  uint2* listed = sw.listed + ((size_t)rh * sw.slices + slice) * LISTED;
+    for (int i = 0; i < 8; i++) {
+      at += i < w ? m.wsum[i][1] : 0u;
+      all_better += m.wsum[i][0];
+      all += m.wsum[i][1];
+    }
+    uint2* listed = sw.listed + (size_t)rh * LISTED + slice * share;
 #pragma unroll
-  for (int u = 0; u < SLICE_CHUNKS; u++) {
-    const bool in = key[u] - lo <= hi - lo;
-    const unsigned long long b = __ballot(in);
-    const uint32_t i = at + lanes_before(b);
-    if (in && i < LISTED) listed[i] = make_uint2(key[u], (uint32_t)(first + (u * 8 + w) * 64 + l));
-    at += (uint32_t)__popcll(b);
+    for (int u = 0; u < SLICE_CHUNKS; u++) {
+      const bool in = key[u] - lo <= hi - lo;
+      const unsigned long long b = __ballot(in);
+      const uint32_t i = at + lanes_before(b);
+      if (in && i < (uint32_t)share) listed[i] = make_uint2(key[u], (uint32_t)(slice * SLICE + (u * 8 + w) * 64 + l));
+      at += (uint32_t)__popcll(b);
+    }
+    if (tid == 0) sw.counts[(size_t)rh * SLICES_MAX + slice] = make_uint2(all_better, all);
   }
-  if (tid == 0) {
-    *counts = make_uint2(all_better, all);
-    if (slice == 0) sw.bounds[rh] = make_uint2(lo, hi);
+}
+
+// Workgroups per (row, head): one that selects for a short row, or, SLICED, parts of a long one (a second launch follows).  Not SLICED:
+// the caller's bound says that no row is long; one that is all the same is selected by one workgroup.
+template <int S, bool SLICED>
+__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+  const int pairs = p.n_rows * c.H_q, part = SLICED ? blockIdx.x / pairs : 0, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int tid = threadIdx.x;
+  const CacheRow row = cache_row(c, p, r);
+  const int n = row.n, kk = min(p.k, n), parts = SLICED && n > SELECT_SHORT ? sw.parts : 1;
+  if (part && n <= SELECT_SHORT) return;
+  int32_t* list = kept + (size_t)rh * p.kcap;
+  if (kk == n) {  // (a page out of range anywhere: none is kept)
+    bool bad = false;
+    for (long long j = tid; j << c.shift < n; j += 512) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;
+    const int there = __syncthreads_or(bad) ? 0 : n;
+    for (long long j = part * 512 + tid; j < p.kcap; j += parts * 512) list[j] = j < there ? (int32_t)cache_slot(c, row, (int)j) : -1;
+    return;
   }
+  __shared__ SelectShared<512> m;
+  if (n <= SELECT_SHORT) select_row<512, SELECT_REGS, S, false>(c, row, h, kk, list, m);
+  else if constexpr (SLICED) list_slices<S>(c, row, h, kk, rh, part, sw, m);
+  else select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
 }
 
 template <int S>
 __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int pairs = p.n_rows * c.H_q, slice = blockIdx.x / pairs, rh = blockIdx.x - slice * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int pairs = p.n_rows * c.H_q, part = blockIdx.x / pairs, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  uint2 cnt = sw.counts[(size_t)rh * SLICES_MAX + l];  // lane s: of slice s
+  const uint2 bounds = sw.bounds[rh];
   const CacheRow row = cache_row(c, p, r);
   PageRun<S> run;
-  run.load(c, row, slice * (SLICE / 64) + w, 8, l);
-  uint2 cnt = sw.counts[(size_t)rh * sw.slices + min(l, sw.slices - 1)];  // lane s: of slice s
-  const uint2 bounds = sw.bounds[rh];
-  const int n = row.n, kk = min(p.k, n), first = slice * SLICE;
-  if (n <= SELECT_SHORT || first >= n || kk == n) return;
+  slice_pages<S>(c, row, part, run);
+  const int n = row.n, kk = min(p.k, n);
+  if (n <= SELECT_SHORT || part * SLICE >= n || kk == n) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
   __shared__ SelectShared<512> m;
-  __shared__ __align__(16) uint32_t cand[LISTED_ALL];
-  const int slices = (n - 1) / SLICE + 1;
+  __shared__ __align__(16) uint32_t cand[LISTED];
+  const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
   const auto add = [](uint32_t x, uint32_t y) { return x + y; };
   if (l >= slices) cnt = make_uint2(0, 0);
-  const unsigned long long over = __ballot(cnt.y > LISTED);
-  const uint32_t upto_better = wave_scan(cnt.x, 0u, add), upto = wave_scan(min(cnt.y, (uint32_t)LISTED), 0u, add);
-  const uint32_t better = last_lane(upto_better), all = last_lane(upto);
-  if (slices > SLICES_MAX || over || all > LISTED_ALL || better >= (uint32_t)kk || (uint32_t)kk - better > all) {
-    if (slice == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
-    return;
-  }
-  const uint32_t want = (uint32_t)kk - better;  // of the listed keys
-  uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
-  for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
-  uint32_t* near_all = &m.st[3];
-  if (tid == 0) *near_all = 0;
-  // The listed keys of all slices; a wave takes every eighth slice's.
-  const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.x), range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.y) - lo;
-  const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
-  const uint2* lists = sw.listed + (size_t)rh * sw.slices * LISTED;
-  for (int s = w; s < slices; s += 8) {
-    const uint32_t have = (uint32_t)__builtin_amdgcn_readlane((int)cnt.y, s), to = (uint32_t)__builtin_amdgcn_readlane((int)upto, s) - have;
-    for (uint32_t i0 = 0; i0 < have; i0 += 256) {
-      uint32_t k[4];
-#pragma unroll
-      for (int e = 0; e < 4; e++) k[e] = lists[(size_t)s * LISTED + min(i0 + e * 64 + l, have - 1)].x;
-#pragma unroll
-      for (int e = 0; e < 4; e++)
-        if (i0 + e * 64 + l < have) cand[to + i0 + e * 64 + l] = k[e];
+  const unsigned long long over = __ballot(cnt.y > (uint32_t)share);
+  const uint32_t upto = wave_scan(min(cnt.y, (uint32_t)share), 0u, add);
+  const uint32_t better = last_lane(wave_scan(cnt.x, 0u, add)), all = last_lane(upto);
+  const bool found = slices <= SLICES_MAX && !over && better < (uint32_t)kk && (uint32_t)kk - better <= all;
+  // f(first listed key of slice s in LDS, their number, s) for the slices of this wave, every eighth
+  auto lists = [&](auto f) {
+    for (int s = w; s < slices; s += 8) {
+      const uint32_t have = (uint32_t)__builtin_amdgcn_readlane((int)cnt.y, s), end = (uint32_t)__builtin_amdgcn_readlane((int)upto, s);
+      f(end - have, have, s);
     }
-  }
-  uint32_t key[SLICE_CHUNKS];
-  (void)slice_keys<S>(c, row, h, slice, run, key);
-  __syncthreads();
-  for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[((cand[i] - lo) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
-  pick_digit<512>(m, want);
-  const uint32_t base = lo + (m.st[0] << sh), rank = m.st[1], n_near = m.st[2];
-  if (n_near > 512) {  // (ties)
+  };
+  const uint2* listed = sw.listed + (size_t)rh * LISTED;
+  uint32_t* near_all = &m.st[3];
+  uint32_t key[SLICE_CHUNKS], base = 0, rank = 0, n_near = NO_KEY;
+  int sh = 0;
+  if (found) {
+    uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
+    for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+    if (tid == 0) *near_all = 0;
+    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.x), range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.y) - lo;
+    sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
+    lists([&](uint32_t to, uint32_t have, int s) {
+      for (uint32_t i0 = 0; i0 < have; i0 += 256) {
+        uint32_t k[4];
+#pragma unroll
+        for (int e = 0; e < 4; e++) k[e] = listed[s * share + min(i0 + e * 64 + l, have - 1)].x;
+#pragma unroll
+        for (int e = 0; e < 4; e++)
+          if (i0 + e * 64 + l < have) cand[to + i0 + e * 64 + l] = k[e];
+      }
+    });
+    (void)slice_keys<S>(c, row, h, part, run, key);  // (on its way under the search for the threshold)
     __syncthreads();
-    if (slice == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
+    for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[((cand[i] - lo) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
+    pick_digit<512>(m, (uint32_t)kk - better);
+    base = lo + (m.st[0] << sh);
+    rank = m.st[1];
+    n_near = m.st[2];
+  }
+  if (n_near > 512) {  // (ties, or nothing found at all)
+    __syncthreads();
+    if (part == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
     return;
   }
-  // Keys of that bin, with their positions (again from the lists), and the keys before it in the slices before this one.
-  uint32_t ahead = 0;
-  for (int s = w; s < slices; s += 8) {
-    const uint32_t have = (uint32_t)__builtin_amdgcn_readlane((int)cnt.y, s), to = (uint32_t)__builtin_amdgcn_readlane((int)upto, s) - have;
+  // The bin's keys with their positions (again from the lists); kept keys of every slice that are before the bin (m.equal).
+  lists([&](uint32_t to, uint32_t have, int s) {
+    uint32_t ahead = (uint32_t)__builtin_amdgcn_readlane((int)cnt.x, s);
     for (uint32_t i0 = 0; i0 < have; i0 += 64) {
       const bool there = i0 + l < have;
       const uint32_t k = there ? cand[to + i0 + l] : NO_KEY;
-      if (s < slice) ahead += (uint32_t)__popcll(__ballot(k < base));
+      ahead += (uint32_t)__popcll(__ballot(k < base));
       if (there && ((k - base) >> sh) == 0) {
         const uint32_t e = atomicAdd(near_all, 1u);
         m.near[e] = k;
-        m.near_pos[e] = lists[(size_t)s * LISTED + i0 + l].y;
+        m.near_pos[e] = listed[s * share + i0 + l].y;
       }
     }
-  }
-  if (l == 0) m.wsum[w][0] = ahead;
+    if (l == 0) m.equal[s] = ahead;
+  });
   __syncthreads();
   if (tid < (int)n_near) {
     const uint32_t k = m.near[tid], pos = m.near_pos[tid];
     uint32_t less = 0;
     for (uint32_t i = 0; i < n_near; i++) less += m.near[i] < k || (m.near[i] == k && m.near_pos[i] < pos);
+    if (less < rank) atomicAdd(&m.equal[pos / SLICE], 1u);
     if (less + 1 == rank) {  // the last one that is kept
       m.st[0] = k;
       m.st[1] = pos;
@@ -602,35 +606,32 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   __syncthreads();
   const uint32_t thr = (uint32_t)__builtin_amdgcn_readfirstlane((int)m.st[0]);
   const int last = __builtin_amdgcn_readfirstlane((int)m.st[1]);
-  // kept keys of the slices before: better ones, listed ones before the bin, those of the bin up to the threshold
-  uint32_t done = slice ? (uint32_t)__builtin_amdgcn_readlane((int)upto_better, slice - 1) : 0u;
+  const uint32_t of_slice = l < slices ? m.equal[l] : 0u, before = wave_scan(of_slice, 0u, add) - of_slice;  // lane s: kept before slice s
+  for (int slice = part; slice < slices; slice += sw.parts) {
+    if (slice != part) {
+      slice_pages<S>(c, row, slice, run);
+      (void)slice_keys<S>(c, row, h, slice, run, key);
+    }
+    auto keeps = [&](int u) { return key[u] < thr || (key[u] == thr && l <= last - (slice * SLICE + (u * 8 + w) * 64)); };
+    uint32_t count = 0;  // lane u: of this wave's chunk u
 #pragma unroll
-  for (int i = 0; i < 8; i++) done += m.wsum[i][0];
-  for (uint32_t i0 = 0; i0 < n_near; i0 += 64) {
-    const bool there = i0 + l < n_near;
-    const uint32_t k = there ? m.near[i0 + l] : NO_KEY;
-    const int pos = there ? (int)m.near_pos[i0 + l] : 0;
-    done += (uint32_t)__popcll(__ballot(pos < first && (k < thr || (k == thr && pos <= last))));
-  }
-  uint32_t count = 0;
+    for (int u = 0; u < SLICE_CHUNKS; u++) {
+      const uint32_t b = (uint32_t)__popcll(__ballot(keeps(u)));
+      count = l == u ? b : count;
+    }
+    if (slice != part) __syncthreads();
+    if (l < 32) m.kept[l * 8 + w] = l < SLICE_CHUNKS ? count : 0u;
+    __syncthreads();
+    uint32_t total;
+    const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)before, slice) + chunk_offsets(m.kept, w, l, total);
 #pragma unroll
-  for (int u = 0; u < SLICE_CHUNKS; u++) {
-    const uint32_t b = (uint32_t)__popcll(__ballot(key[u] < thr || (key[u] == thr && l <= last - (first + (u * 8 + w) * 64))));
-    count = l == u ? b : count;
-  }
-  if (l < 32) m.kept[l * 8 + w] = l < SLICE_CHUNKS ? count : 0u;
-  __syncthreads();
-  uint32_t total;
-  const uint32_t at = done + chunk_offsets(m.kept, w, l, total);
+    for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));
 #pragma unroll
-  for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));
-#pragma unroll
-  for (int u = 0; u < SLICE_CHUNKS; u++) {
-    const int j = first + (u * 8 + w) * 64;
-    const bool in = key[u] < thr || (key[u] == thr && l <= last - j);
-    const unsigned long long b = __ballot(in);
-    const int32_t slot = run.slot(c, j, u, l);
-    if (in) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
+    for (int u = 0; u < SLICE_CHUNKS; u++) {
+      const unsigned long long b = __ballot(keeps(u));
+      const int32_t slot = run.slot(c, slice * SLICE + (u * 8 + w) * 64, u, l);
+      if (keeps(u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
+    }
   }
 }
 
@@ -914,23 +915,24 @@ static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
   return (int)(((kcap + parts - 1) / parts + 255) / 256 * 256);
 }
 
-// The workspace: partial outputs, then, where rows can be long, what the slices of a row tell each other.
+// The workspace: partial outputs, then, where rows can be long, what the parts of a row tell each other.
 struct DecodeWork {
   size_t off_counts, off_listed, off_bounds, total;
-  int slices;
+  int parts;  // of a long row; 0: no row is long
 };
+constexpr int SELECT_WGS = 8 * CUS;  // workgroups that the parts are chosen for
 static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
   const size_t pairs = (size_t)n_rows * s.H_q;
   DecodeWork wk;
   size_t o = nsplit > 1 ? align_up(pairs * nsplit * (s.d + 2) * 4, 256) : 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
-  const long cap = (long)s.max_pages * s.page_size;
-  const long slices = cap <= SELECT_SHORT || kcap == cap ? 0 : (cap + SLICE - 1) / SLICE;
-  wk.slices = (int)(slices < SLICES_MAX ? slices : SLICES_MAX);
-  wk.off_counts = take(pairs * wk.slices * 8);
-  wk.off_listed = take(pairs * wk.slices * LISTED * 8);
-  wk.off_bounds = take(wk.slices ? pairs * 8 : 0);
+  const long cap = (long)s.max_pages * s.page_size, longest = s.max_len > 0 && s.max_len < cap ? s.max_len : cap;
+  const long slices = longest <= SELECT_SHORT || kcap == cap ? 0 : (longest + SLICE - 1) / SLICE, most = SELECT_WGS / (long)pairs;
+  wk.parts = (int)(slices < most ? slices : most < 1 && slices ? 1 : most);
+  wk.off_counts = take(wk.parts ? pairs * SLICES_MAX * 8 : 0);
+  wk.off_listed = take(wk.parts ? pairs * LISTED * 8 : 0);
+  wk.off_bounds = take(wk.parts ? pairs * 8 : 0);
   wk.total = o;
   return wk;
 }
@@ -959,22 +961,21 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   const CacheRef c = cache_ref(s, pages);
   const CacheRows p = {table, row_req, row_len, n_rows, k, list_length(s, k)};
   const unsigned pairs = (unsigned)(n_rows * s.H_q);
-  const bool wide = s.page_size >= 64;
-  const DecodeWork wk = decode_work(s, n_rows, k);
-  const bool all = k >= (long)s.max_pages * s.page_size;
+  const bool wide = s.page_size >= 64, all = k >= (long)s.max_pages * s.page_size;
   if (!all) {
-    if (wide) cache_select_kernel<1><<<pairs, 512, 0, st>>>(c, p, kept);
-    else cache_select_kernel<4><<<pairs, 512, 0, st>>>(c, p, kept);
-    if (hipGetLastError() != hipSuccess) return DMA_EHIP;
-  }
-  if (wk.slices) {
+    const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
-    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.slices};
-    if (wide) cache_bracket_kernel<1><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
-    else cache_bracket_kernel<4><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
-    if (hipGetLastError() != hipSuccess) return DMA_EHIP;
-    if (wide) cache_slice_kernel<1><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
-    else cache_slice_kernel<4><<<pairs * wk.slices, 512, 0, st>>>(c, p, sw, kept);
+    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.parts};
+    if (!wk.parts) {
+      if (wide) cache_select_kernel<1, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+      else cache_select_kernel<4, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+    } else {
+      if (wide) cache_select_kernel<1, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      else cache_select_kernel<4, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+      if (wide) cache_slice_kernel<1><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      else cache_slice_kernel<4><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+    }
     if (hipGetLastError() != hipSuccess) return DMA_EHIP;
   }
   auto go = [&](auto t) {

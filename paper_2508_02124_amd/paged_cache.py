@@ -99,11 +99,13 @@ class PagedCache:
         self._call(B.dma_cache_read, n, slots, self.pages, k, v, z)
         return k, v, z
 
-    def decode(self, q, keep_window, rows=None, softmax_scale=0.0):
+    def decode(self, q, keep_window, rows=None, softmax_scale=0.0, max_len=0):
         """Attention of q [n, num_heads, head_dim] over the cache: o, lse [num_heads, n] and the kept slots
         [n, num_heads, min(keep_window, longest request)].  rows: the step's (CacheRows), or (row_req, row_len); None: row r
-        is request r with all its tokens."""
+        is request r with all its tokens.  max_len: the most keys that a row sees, where the host knows it (a matter of speed)."""
         s, n = self.shape, q.shape[0]
+        if max_len:
+            s = B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype, max_len)
         self._check("q", q, (n, s.H_q, s.d), self.dtype, whole=False)
         row_req, row_len = (None, self.seq_lens) if rows is None else (rows.row_req, rows.row_len) if isinstance(rows, CacheRows) else rows
         if rows is not None:
@@ -115,7 +117,7 @@ class PagedCache:
         kept = self._ints(n, s.H_q, min(int(keep_window), s.max_pages * s.page_size))
         size = B.dma_cache_decode_bytes(s, n, keep_window)
         ws = torch.empty(size + 16, dtype=torch.uint8, device=self.device)   # (never empty: its address is passed)
-        self._call(B.dma_cache_decode, n, keep_window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
+        self._call_with(s, B.dma_cache_decode, n, keep_window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
                    row_len, o, lse, kept, ws, size)
         return o, lse, kept
 

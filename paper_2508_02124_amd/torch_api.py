@@ -161,10 +161,10 @@ class DynamicMaskAttention(torch.nn.Module):
         return dynamic_mask_attention(q, k, v, self.W, self.A, cu_seqlens, self.keep_window, max_seqlen,
                                       self.softmax_scale)
 
-    def step(self, q, k, v, cache, rows):
+    def step(self, q, k, v, cache, rows, max_len=0):
         """A decoding step over a paged cache (paged_cache.PagedCache): k, v [n, H_kv, d] of the step's new rows go to their places
-        with this module's scores, then q [n, H_q, d] attends from them.  rows: what cache.assign returned.  Without
-        gradients; o [n, H_q, d]."""
+        with this module's scores, then q [n, H_q, d] attends from them.  rows: what cache.assign returned; max_len: as for
+        cache.decode.  Without gradients; o [n, H_q, d]."""
         with torch.no_grad():
             W, A = self.W.detach(), self.A.detach()
             if W.shape[1] == self.head_dim:
@@ -176,4 +176,4 @@ class DynamicMaskAttention(torch.nn.Module):
                     shape = B.make_shape(n, 1, self.num_heads, self.num_kv_heads, self.head_dim, 1, dtype=_dtype_code(v))
                     cache._call_with(shape, B.dma_scores_xhead, v.contiguous(), W, A, z)
                 cache.append(rows.slots, k, v, z=z)
-            return cache.decode(q, self.keep_window, rows, self.softmax_scale)[0]
+            return cache.decode(q, self.keep_window, rows, self.softmax_scale, max_len)[0]

@@ -60,7 +60,7 @@ def test_layout(H_q, H_kv, d, ps):
     assert B.dma_cache_decode_bytes(s, 3, 100) >= 0 and B.dma_cache_decode_bytes(s, 0, 100) == 0
 
 
-EINVAL = [dict(n_reqs=0), dict(n_pages=0), dict(max_pages=0), dict(H_q=0), dict(H_kv=0), dict(H_q=9), dict(n_reqs=-1)]
+EINVAL = [dict(n_reqs=0), dict(n_pages=0), dict(max_pages=0), dict(H_q=0), dict(H_kv=0), dict(H_q=9), dict(n_reqs=-1), dict(max_len=-1)]
 UNSUPPORTED = [dict(d=96), dict(d=32), dict(dtype=2), dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(page_size=0),
                dict(n_reqs=4097), dict(n_pages=1 << 27), dict(max_pages=1 << 27), dict(H_q=514, H_kv=2), dict(H_q=8192, H_kv=4096)]
 

@@ -56,4 +56,4 @@ def test_every_failed_launch_is_reported(tmp_path):
     subprocess.run(["g++", "-O1", "-shared", "-fPIC", str(source), "-o", str(stand_in)], check=True)
     r = subprocess.run([sys.executable, str(calls), str(stand_in), ROOT], capture_output=True, text=True, timeout=100)
     assert r.returncode == 0, r.stdout + r.stderr
-    assert "LOST" not in r.stdout and "('decode', 5)" in r.stdout and "('assign', 2)" in r.stdout, r.stdout
+    assert "LOST" not in r.stdout and "('decode', 4)" in r.stdout and "('assign', 2)" in r.stdout, r.stdout

@@ -296,6 +296,24 @@ def test_a_row_of_more_slices_than_are_listed(gpu):
         assert torch.isfinite(got[0].float()).all()
 
 
+@pytest.mark.parametrize("H_q,n_rows,max_pages,max_len", [(32, 70, 470, 0), (32, 30, 2000, 0), (8, 9, 470, 12288), (8, 9, 470, 100), (8, 9, 470, 30000),
+                                                          (4, 5, 20000, 0)])
+def test_bounds_and_numbers_of_rows_change_nothing(gpu, H_q, n_rows, max_pages, max_len):
+    """A row's slices over many, few and one workgroup, under bounds that hold and ones that do not, in tables far longer than the
+    requests: the same lists and outputs."""
+    lens, k = (29000, 12289, 12288, 300), 1500
+    cache = GpuCache(gpu, 4, 900, max_pages, 64, H_q, 2, 64)
+    cache.shape.max_len = max_len
+    fill(cache, lens, 8)
+    rows = [(i % 4, lens[i % 4] - i // 4) for i in range(n_rows)]
+    q = normal(gpu, 5, n_rows, H_q, 64).to(cache.type)
+    req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
+    length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
+    got = cache.decode(q, k, req, length)
+    check_kept(cache, k, rows[-5:], got[2][-5:])
+    check_rows(cache, q[:4], k, rows[:4], tuple(x[:4] if i != 1 else x[:, :4] for i, x in enumerate(got)))
+
+
 def test_long_rows_with_outputs(gpu):
     lens = (30000, 13000, 100)
     cache = GpuCache(gpu, 3, 700, 470, 64, 4, 2, 128)

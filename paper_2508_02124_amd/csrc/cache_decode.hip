@@ -592,16 +592,20 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
     }
     if (l == 0) m.equal[s] = ahead;
   });
+  if (tid < 256 - 16 * 8) m.kept[16 * 8 + tid] = 0;  // (chunks that a slice does not have)
+  uint32_t* first_out = &m.wsum[0][0];
+  if (tid == 0) *first_out = NO_KEY;
   __syncthreads();
   if (tid < (int)n_near) {
     const uint32_t k = m.near[tid], pos = m.near_pos[tid];
     uint32_t less = 0;
     for (uint32_t i = 0; i < n_near; i++) less += m.near[i] < k || (m.near[i] == k && m.near_pos[i] < pos);
     if (less < rank) atomicAdd(&m.equal[pos / SLICE], 1u);
-    if (less + 1 == rank) {  // the last one that is kept
+    if (less + 1 == rank) {  // the last one that is kept, and the first that is not
       m.st[0] = k;
       m.st[1] = pos;
     }
+    if (less == rank) *first_out = k;
   }
   __syncthreads();
   const uint32_t thr = (uint32_t)__builtin_amdgcn_readfirstlane((int)m.st[0]);
@@ -612,26 +616,31 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       slice_pages<S>(c, row, slice, run);
       (void)slice_keys<S>(c, row, h, slice, run, key);
     }
-    auto keeps = [&](int u) { return key[u] < thr || (key[u] == thr && l <= last - (slice * SLICE + (u * 8 + w) * 64)); };
-    uint32_t count = 0;  // lane u: of this wave's chunk u
+    // keeps(u): whether this lane's key of chunk u is kept
+    auto put = [&](auto keeps) {
+      if (slice != part) __syncthreads();
+      uint32_t count[SLICE_CHUNKS];
 #pragma unroll
-    for (int u = 0; u < SLICE_CHUNKS; u++) {
-      const uint32_t b = (uint32_t)__popcll(__ballot(keeps(u)));
-      count = l == u ? b : count;
-    }
-    if (slice != part) __syncthreads();
-    if (l < 32) m.kept[l * 8 + w] = l < SLICE_CHUNKS ? count : 0u;
-    __syncthreads();
-    uint32_t total;
-    const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)before, slice) + chunk_offsets(m.kept, w, l, total);
+      for (int u = 0; u < SLICE_CHUNKS; u++) count[u] = (uint32_t)__popcll(__ballot(keeps(u)));
+      if (l == 0) {
 #pragma unroll
-    for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));
+        for (int u = 0; u < SLICE_CHUNKS; u++) m.kept[u * 8 + w] = count[u];
+      }
+      __syncthreads();
+      uint32_t total;
+      const uint32_t at = (uint32_t)__builtin_amdgcn_readlane((int)before, slice) + chunk_offsets(m.kept, w, l, total);
 #pragma unroll
-    for (int u = 0; u < SLICE_CHUNKS; u++) {
-      const unsigned long long b = __ballot(keeps(u));
-      const int32_t slot = run.slot(c, slice * SLICE + (u * 8 + w) * 64, u, l);
-      if (keeps(u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
-    }
+      for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));
+#pragma unroll
+      for (int u = 0; u < SLICE_CHUNKS; u++) {
+        const unsigned long long b = __ballot(keeps(u));
+        const int32_t slot = run.slot(c, slice * SLICE + (u * 8 + w) * 64, u, l);
+        if (keeps(u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
+        if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (addresses of all chunks at once would spill)
+      }
+    };
+    if (*first_out != thr) put([&](int u) { return key[u] <= thr; });
+    else put([&](int u) { return key[u] < thr || (key[u] == thr && l <= last - (slice * SLICE + (u * 8 + w) * 64)); });
   }
 }
 

@@ -201,6 +201,7 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   if (!LONG) run.load(c, row, w, NW, l);
   for (int i = tid; i < NDIG; i += NT) hist4[i] = make_uint4(0, 0, 0, 0);
   m.near[tid] = NO_KEY;
+  if (tid < 256) m.kept[tid] = 0;
   if (tid == 0) m.st[3] = NO_KEY;
   if (!LONG) {
     fetch(0);
@@ -235,36 +236,55 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   });
   pick_digit<NT>(m, (uint32_t)kk);
   const uint32_t base = kmin + (m.st[0] << sh0);  // first key of the bin
+  const uint32_t width = min(1u << sh0, NO_KEY - base);
   uint32_t need_eq = m.st[1], n_eq = m.st[2], sub = 0;
-  auto put = [&](int round, uint32_t at, auto keeps) {  // keeps(key, position - chunk's first)
+  auto put = [&](int round, uint32_t at, auto keeps) {  // keeps(key, chunk)
 #pragma unroll
     for (int q = 0; q < S; q++) asm volatile("" : "+v"(run.pg[q]));  // (the pages out of their lanes again, not kept since the scores)
-    each(round, [&](uint32_t k32, int u) {
-      const unsigned long long k = __ballot(keeps(k32, u));
-      if (k) {
-        const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2));
-        const int32_t x = run.slot(c, chunk(round, u), u, l);
-        if (keeps(k32, u)) list[first + lanes_before(k)] = x;
+    int left = n - round * R * NW * 64;
+    asm volatile("" : "+s"(left));
+#pragma unroll
+    for (int u0 = 0; u0 < R; u0 += STEP)
+      if (u0 * NW * 64 < left) {
+#pragma unroll
+        for (int u = u0; u < u0 + STEP; u++) {
+          const unsigned long long k = __ballot(keeps(key[u], u));
+          const int32_t x = run.slot(c, chunk(round, u), u, l);
+          if (keeps(key[u], u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(k)] = x;
+        }
+        __builtin_amdgcn_sched_barrier(0);
       }
-    });
   };
   if constexpr (!LONG) {
-    uint32_t kept = 0, count = 0;  // lane u: keys of this wave's chunk u that are before the bin; the wave's keys of the bin
-    each(0, [&](uint32_t k32, int u) {
-      const uint32_t b = (uint32_t)__popcll(__ballot(k32 < base));
-      kept = l == u ? b : kept;
-      const bool in = ((k32 - base) >> sh0) == 0 && k32 != NO_KEY;
-      const unsigned long long in_bin = __ballot(in);
-      if (in_bin) {
-        const uint32_t e = count + lanes_before(in_bin);
-        if (in && e < NEAR) {
-          m.near[e * NW + w] = k32 - base;
-          m.near_pos[e * NW + w] = (uint32_t)(chunk(0, u) + l);
+    uint32_t count = 0;  // the wave's keys of the bin
+    int left = n;
+    asm volatile("" : "+s"(left));
+#pragma unroll
+    for (int u0 = 0; u0 < R; u0 += STEP)
+      if (u0 * NW * 64 < left) {  // (four chunks are compared before the first result is used)
+        unsigned long long in[STEP];
+        uint32_t before[STEP];
+#pragma unroll
+        for (int e = 0; e < STEP; e++) {
+          before[e] = (uint32_t)__popcll(__ballot(key[u0 + e] < base));
+          in[e] = __ballot(key[u0 + e] - base < width);
         }
-        count += (uint32_t)__popcll(in_bin);
+        if (l == 0) {
+#pragma unroll
+          for (int e = 0; e < STEP; e++) m.kept[(u0 + e) * NW + w] = before[e];
+        }
+        if (in[0] | in[1] | in[2] | in[3]) {
+#pragma unroll
+          for (int e = 0; e < STEP; e++) {
+            const uint32_t i = count + lanes_before(in[e]);
+            if (key[u0 + e] - base < width && i < NEAR) {
+              m.near[i * NW + w] = key[u0 + e] - base;
+              m.near_pos[i * NW + w] = (uint32_t)(chunk(0, u0 + e) + l);
+            }
+            count += (uint32_t)__popcll(in[e]);
+          }
+        }
       }
-    });
-    if (l < 32) m.kept[l * NW + w] = kept;
     if (l == 0) m.wsum[w][1] = count;
     __syncthreads();
     uint32_t most = 0;

@@ -306,8 +306,8 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
  *   slots        [n_rows] int32: place of a token, page * page_size + place in the page; below 0: none
  *   row_req      [n_rows] int32: request of a row; below 0: none
  *   row_len      [n_rows] int32: keys that a row sees, the first row_len of its request; 0: none
- * n_rows is the capacity of a step's row arrays, not its number of rows, and may be 0 (nothing is done, or enqueued, but by
- * dma_cache_assign).  dtype is the type of K, V, q and o; what the cache holds does not depend on it.
+ * n_rows is the capacity of a step's row arrays, not its number of rows, at most 2^30, and may be 0 (nothing is done, or
+ * enqueued, but by dma_cache_assign).  dtype is the type of K, V, q and o; what the cache holds does not depend on it.
  *
  * A token's K (and V) of one kv-head is held as d codes of 4 bits and d / 32 scale bytes (OCP microscaling, e2m1 with e8m0): channel c
  * stands for  code[c] * 2^(byte[c / 32] - 127),  code in {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign.  The power of two is the one
@@ -319,8 +319,8 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
  */
 typedef struct {
   int32_t n_reqs;      /* places for requests, 1 to 4096                                        */
-  int32_t n_pages;     /* pages of the pool; n_pages * page_size < 2^31                         */
-  int32_t max_pages;   /* pages of one request at most; max_pages * page_size < 2^31            */
+  int32_t n_pages;     /* pages of the pool; n_pages * page_size <= 2^30                        */
+  int32_t max_pages;   /* pages of one request at most; max_pages * page_size <= 2^30           */
   int32_t page_size;   /* tokens of a page: 16, 32, 64, 128 or 256                              */
   int32_t H_q;         /* query heads                                                           */
   int32_t H_kv;        /* key/value heads, divides H_q                                          */

@@ -58,9 +58,17 @@ int check_cache(const dma_cache_shape* s) {
   if (s->dtype != DMA_BF16 && s->dtype != DMA_F32) return DMA_EUNSUPPORTED;
   if (s->page_size < 16 || s->page_size > 256 || (s->page_size & (s->page_size - 1))) return DMA_EUNSUPPORTED;
   if (s->n_reqs > CACHE_REQS_MAX) return DMA_EUNSUPPORTED;
-  if ((long)s->n_pages * s->page_size > INT32_MAX || (long)s->max_pages * s->page_size > INT32_MAX) return DMA_EUNSUPPORTED;
-  if (s->H_q > 4096 || s->H_q / s->H_kv > 256) return DMA_EUNSUPPORTED;  // (a page stays below 2^31 bytes, a group's scores below 64 KiB)
+  if ((long)s->n_pages * s->page_size > CACHE_TOKENS_MAX || (long)s->max_pages * s->page_size > CACHE_TOKENS_MAX) return DMA_EUNSUPPORTED;
+  if (s->H_q > 4096 || s->H_q / s->H_kv > 256) return DMA_EUNSUPPORTED;  // (a page stays below 2^31 bytes)
   return DMA_OK;
+}
+
+// the shape, and the number of rows
+int check_rows(const dma_cache_shape* s, int32_t n_rows) {
+  int rc = check_cache(s);
+  if (rc != DMA_OK) return rc;
+  if (n_rows < 0) return DMA_EINVAL;
+  return n_rows > CACHE_TOKENS_MAX ? DMA_EUNSUPPORTED : DMA_OK;
 }
 
 // n_rows rows of `heads` heads, `stride` elements apart
@@ -303,9 +311,9 @@ size_t dma_cache_free_bytes(const dma_cache_shape* shape) {
 
 // The grids of a decode: rows x heads x parts of the list, in workgroups of up to 512 threads, fewer than 2^32 threads in all.
 static int check_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k) {
-  int rc = check_cache(shape);
+  int rc = check_rows(shape, n_rows);
   if (rc != DMA_OK) return rc;
-  if (n_rows < 0 || k <= 0) return DMA_EINVAL;
+  if (k <= 0) return DMA_EINVAL;
   const long cap = (long)shape->max_pages * shape->page_size, parts = ((k < cap ? k : cap) + 255) / 256;
   if (((long)n_rows + 8) * shape->H_q * parts >= 1 << 22) return DMA_EUNSUPPORTED;
   return DMA_OK;
@@ -335,9 +343,9 @@ int dma_cache_reset(const dma_cache_shape* shape, int32_t* seq_lens, int32_t* bl
 int dma_cache_assign(const dma_cache_shape* shape, int32_t n_rows, const int32_t* change, int32_t* seq_lens,
                      int32_t* block_table, int32_t* free_list, int32_t* cu_rows, int32_t* row_req, int32_t* row_len,
                      int32_t* slots, int32_t* status, void* stream) {
-  int rc = check_cache(shape);
+  int rc = check_rows(shape, n_rows);
   if (rc != DMA_OK) return rc;
-  if (n_rows < 0 || !change || !seq_lens || !block_table || !free_list || !cu_rows || !status) return DMA_EINVAL;
+  if (!change || !seq_lens || !block_table || !free_list || !cu_rows || !status) return DMA_EINVAL;
   if (n_rows > 0 && (!row_req || !row_len || !slots)) return DMA_EINVAL;
   return launch_cache_assign(*shape, n_rows, change, seq_lens, block_table, free_list, cu_rows, row_req, row_len, slots,
                              status, (hipStream_t)stream);
@@ -346,9 +354,9 @@ int dma_cache_assign(const dma_cache_shape* shape, int32_t n_rows, const int32_t
 int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K, int64_t k_stride, const void* V,
                      int64_t v_stride, const float* W, const float* A, const float* z, const int32_t* slots, void* pages,
                      void* stream) {
-  int rc = check_cache(shape);
+  int rc = check_rows(shape, n_rows);
   if (rc != DMA_OK) return rc;
-  if (n_rows < 0 || bad_rows(*shape, k_stride, shape->H_kv) || bad_rows(*shape, v_stride, shape->H_kv)) return DMA_EINVAL;
+  if (bad_rows(*shape, k_stride, shape->H_kv) || bad_rows(*shape, v_stride, shape->H_kv)) return DMA_EINVAL;
   if (n_rows == 0) return DMA_OK;
   if (!K || !V || !slots || !pages || (W ? !A : !z)) return DMA_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(W) || !aligned16(pages)) return DMA_EINVAL;
@@ -357,9 +365,8 @@ int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K
 
 int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* slots, const void* pages, void* K, void* V,
                    float* z, void* stream) {
-  int rc = check_cache(shape);
+  int rc = check_rows(shape, n_rows);
   if (rc != DMA_OK) return rc;
-  if (n_rows < 0) return DMA_EINVAL;
   if (n_rows == 0) return DMA_OK;
   if (!slots || !pages || !K || !V || !z) return DMA_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(pages)) return DMA_EINVAL;
@@ -388,7 +395,7 @@ const char* dma_strerror(int status) {
   switch (status) {
     case DMA_OK: return "ok";
     case DMA_EINVAL: return "invalid argument (null or misaligned pointer, non-positive size, H_q % H_kv != 0)";
-    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, fewer than 2^31 slots)";
+    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, 2^30 tokens)";
     case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes, dma_cache_decode_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
     case DMA_EHIP: return "HIP launch failed";
     default: return "unknown status";

@@ -342,7 +342,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
                                                            const float* __restrict__ W, const float* __restrict__ A,
                                                            const float* __restrict__ z, const int32_t* __restrict__ slots,
                                                            int n_rows) {
-  extern __shared__ float zs[];  // [G][64]
+  __shared__ float zs[GMAX * 64];
   __shared__ TileRows rows;
   constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
   __shared__ __align__(16) uint8_t bytes[64][D / 16];  // the rows' scales, K's and V's, which leave together
@@ -374,48 +374,55 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
       bytes[r][D / 32 + sub / 4] = (uint8_t)vb;
     }
   }
-  if (W) {
-    for (int h0 = 0; h0 < G; h0 += GMAX) {
-      float wreg[GMAX][8];
+  auto put_score = [&](int h, int r, float zv) {
+    if (char* page = rows.page[r])
+      reinterpret_cast<float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] = zv;
+  };
+  auto put_bytes = [&]() {  // (behind a barrier)
+    if (tid < 64 && rows.page[tid]) {
+      using Bytes = std::conditional_t<D == 64, uint32_t, std::conditional_t<D == 128, uint2, uint4>>;
+      char* to = rows.page[tid] + (c.off_scales + (((uint32_t)g << c.shift) + rows.place[tid]) * (D / 16));
+      *reinterpret_cast<Bytes*>(to) = *reinterpret_cast<const Bytes*>(bytes[tid]);
+    }
+  };
+  if (!W) {
+    __syncthreads();
+    put_bytes();
+    for (int i = tid; i < G * 64; i += 256) {
+      const int h = g * G + (i >> 6), t = t0 + (i & 63);
+      if (t < n_rows) put_score(h, i & 63, z[(size_t)h * n_rows + t]);
+    }
+    return;
+  }
+  for (int h0 = 0; h0 < G; h0 += GMAX) {
+    float wreg[GMAX][8];
+#pragma unroll
+    for (int hh = 0; hh < GMAX; hh++) {
+      Raw8<float> raw;
+      load_raw(W + (size_t)(g * G + min(h0 + hh, G - 1)) * D + 8 * sub, raw);
+      to_f32(raw, wreg[hh]);
+    }
+    if (h0) __syncthreads();  // (the scores of the heads before are on their way)
+#pragma unroll
+    for (int pass = 0; pass < NP; pass++) {
+      float x[8];
+      to_f32(v[pass], x);
 #pragma unroll
       for (int hh = 0; hh < GMAX; hh++) {
-        Raw8<float> raw;
-        load_raw(W + (size_t)(g * G + min(h0 + hh, G - 1)) * D + 8 * sub, raw);
-        to_f32(raw, wreg[hh]);
-      }
+        float acc = 0.f;
 #pragma unroll
-      for (int pass = 0; pass < NP; pass++) {
-        float x[8];
-        to_f32(v[pass], x);
-#pragma unroll
-        for (int hh = 0; hh < GMAX; hh++) {
-          float acc = 0.f;
-#pragma unroll
-          for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], x[e], acc);
-          acc = group_sum<LPR>(acc);
-          if (sub == hh % LPR && h0 + hh < G) zs[(h0 + hh) * 64 + pass * RPP + rl] = acc;
-        }
+        for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], x[e], acc);
+        acc = group_sum<LPR>(acc);
+        if (sub == hh % LPR) zs[hh * 64 + pass * RPP + rl] = acc;
       }
     }
-  }
-  __syncthreads();
-  if (tid < 64 && rows.page[tid]) {
-    using Bytes = std::conditional_t<D == 64, uint32_t, std::conditional_t<D == 128, uint2, uint4>>;
-    char* to = rows.page[tid] + (c.off_scales + (((uint32_t)g << c.shift) + rows.place[tid]) * (D / 16));
-    *reinterpret_cast<Bytes*>(to) = *reinterpret_cast<const Bytes*>(bytes[tid]);
-  }
-  for (int i = tid; i < G * 64; i += 256) {
-    const int h = g * G + (i >> 6), r = i & 63;
-    char* page = rows.page[r];
-    if (!page) continue;
-    float zv;
-    if (W) {
+    __syncthreads();
+    if (!h0) put_bytes();
+    for (int i = tid; i < min(GMAX, G - h0) * 64; i += 256) {
+      const int h = g * G + h0 + (i >> 6);
       const float x = zs[i], sp = fmaxf(x, 0.f) + log1pf(expf(-fabsf(x)));
-      zv = expf(A[h] * sp);
-    } else {
-      zv = z[(size_t)h * n_rows + t0 + r];
+      put_score(h, i & 63, expf(A[h] * sp));
     }
-    reinterpret_cast<float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] = zv;
   }
 }
 
@@ -484,9 +491,8 @@ static void append_t(const dma_cache_shape& s, int n_rows, const void* K, long k
   const CacheRef c = cache_ref(s, pages);
   const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)s.H_kv);
   const int G = s.H_q / s.H_kv;
-  const size_t sh = W ? (size_t)G * 64 * 4 : 0;
 #define DMA_APPEND(GM) \
-  cache_append_kernel<T, D, GM><<<grid, 256, sh, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
+  cache_append_kernel<T, D, GM><<<grid, 256, 0, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
   if (G == 1) DMA_APPEND(1);
   else if (G == 2) DMA_APPEND(2);
   else DMA_APPEND(4);

@@ -62,7 +62,7 @@ def test_layout(H_q, H_kv, d, ps):
 
 EINVAL = [dict(n_reqs=0), dict(n_pages=0), dict(max_pages=0), dict(H_q=0), dict(H_kv=0), dict(H_q=9), dict(n_reqs=-1), dict(max_len=-1)]
 UNSUPPORTED = [dict(d=96), dict(d=32), dict(dtype=2), dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(page_size=0),
-               dict(n_reqs=4097), dict(n_pages=1 << 27), dict(max_pages=1 << 27), dict(H_q=514, H_kv=2), dict(H_q=8192, H_kv=4096)]
+               dict(n_reqs=4097), dict(n_pages=(1 << 26) + 1), dict(max_pages=(1 << 26) + 1), dict(H_q=514, H_kv=2), dict(H_q=8192, H_kv=4096)]
 
 
 def refused(status, call, *args):
@@ -112,6 +112,15 @@ def test_arguments_refused():
     refused(inval, B.dma_cache_decode, s, 5, 9, 0.0, P, row, P, P, None, *[P] * 5, 1 << 30)   # row r is request r: only four
     refused(B.DMA_EUNSUPPORTED, B.dma_cache_decode, big, 1 << 17, 1000, 0.0, P, row, *[P] * 8, 1 << 40)
     assert B.dma_cache_decode_bytes(big, 1 << 17, 1000) == 0 and B.dma_cache_decode_bytes(big, 4, 0) == 0
+
+
+def test_numbers_of_rows_refused():
+    s, many = shape(), (1 << 30) + 1
+    refused(B.DMA_EUNSUPPORTED, B.dma_cache_assign, s, many, *[P] * 9)
+    refused(B.DMA_EUNSUPPORTED, B.dma_cache_append, s, many, P, 256, P, 256, P, P, None, P, P)
+    refused(B.DMA_EUNSUPPORTED, B.dma_cache_read, s, many, P, P, P, P, P)
+    refused(B.DMA_EUNSUPPORTED, B.dma_cache_decode, s, many, 9, 0.0, P, 1024, *[P] * 8, 1 << 60)
+    assert B.dma_cache_bytes(shape(n_pages=1 << 26)) > 0 and B.dma_cache_free_bytes(shape(max_pages=1 << 26)) > 0
 
 
 def test_no_rows_is_no_work():

@@ -91,7 +91,7 @@ def rows_with_edges(gpu, dtype, n, H, d, seed):
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("H_q,H_kv,d,ps,n", [(2, 2, 64, 16, 1), (8, 2, 128, 32, 65), (6, 1, 256, 64, 70), (4, 4, 128, 256, 130),
-                                             (10, 1, 64, 16, 33)])
+                                             (10, 1, 64, 16, 33), (256, 1, 64, 16, 67), (78, 6, 128, 16, 40)])
 def test_values_and_scores(gpu, dtype, H_q, H_kv, d, ps, n):
     """Values are exactly those of the definition, the scores those of dma_mask_gen; whatever is not a row's slot stays as it was."""
     print(f"[case] append {dtype} {H_q}/{H_kv} d={d} ps={ps} n={n}", flush=True)
@@ -357,7 +357,8 @@ def test_scores_that_are_not_numbers(gpu, lens):
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("H_q,H_kv,d,ps", [(3, 1, 64, 16), (8, 2, 128, 32), (6, 6, 256, 64), (16, 1, 128, 128), (5, 5, 64, 256)])
+@pytest.mark.parametrize("H_q,H_kv,d,ps", [(3, 1, 64, 16), (8, 2, 128, 32), (6, 6, 256, 64), (16, 1, 128, 128), (5, 5, 64, 256),
+                                            (256, 1, 64, 16)])
 def test_heads_types_and_drafts(gpu, dtype, H_q, H_kv, d, ps):
     """Rows of several lengths of a request, rows that see nothing, queries inside a projection's output, a scale of their own."""
     print(f"[case] decode {dtype} {H_q}/{H_kv} d={d} ps={ps}", flush=True)

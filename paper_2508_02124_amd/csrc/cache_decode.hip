@@ -34,14 +34,14 @@ __device__ __forceinline__ float cache_score(const CacheRef& c, uint32_t slot, i
 
 // ------------------------------------------------------------------ scores of chunks of positions
 // A wave reads 64 consecutive positions at a time (a chunk), every NW-th chunk.  The page numbers of its 64 next chunks are one
-// load (S = 1: pages of 64 tokens or more, one page a chunk) or four (S = 4: lane l has the pages of the quarters of the l-th); a
-// chunk's page then comes out of a lane into a scalar register, and so does the address.
+// load (S = 1: pages of 64 tokens or more, one page a chunk), two (S = 2) or four (S = 4: lane l has the pages of the quarters of the
+// l-th); a chunk's page then comes out of a lane into a scalar register, and so does the address.
 template <int S> struct PageRun {
   uint32_t pg[S];
   // The pages of the chunks first, first + step, ... of a row (the last entries of the table for those behind its end).
   __device__ __forceinline__ void load(const CacheRef& c, const CacheRow& row, int first, int step, int l) {
 #pragma unroll
-    for (int q = 0; q < S; q++) pg[q] = (uint32_t)row.pages[min((64 * (first + step * l) + 16 * q) >> c.shift, c.max_pages - 1)];
+    for (int q = 0; q < S; q++) pg[q] = (uint32_t)row.pages[min((64 * (first + step * l) + 64 / S * q) >> c.shift, c.max_pages - 1)];
   }
   // Whether one of them, of the row's n positions, is out of range (it is page 0 from here on).
   __device__ __forceinline__ bool check(const CacheRef& c, int n, int first, int step, int l) {
@@ -49,7 +49,7 @@ template <int S> struct PageRun {
 #pragma unroll
     for (int q = 0; q < S; q++) {
       const bool out = pg[q] >= (uint32_t)c.n_pages;
-      bad |= out && 64 * (first + step * l) + 16 * q < n;
+      bad |= out && 64 * (first + step * l) + 64 / S * q < n;
       pg[q] = out ? 0u : pg[q];
     }
     return __ballot(bad) != 0;
@@ -60,7 +60,7 @@ template <int S> struct PageRun {
 #pragma unroll
     for (int q = 1; q < S; q++) {
       const uint32_t y = (uint32_t)__builtin_amdgcn_readlane((int)pg[q], u);
-      x = l >= 16 * q ? y : x;
+      x = l >= 64 / S * q ? y : x;
     }
     return x;
   }
@@ -990,21 +990,23 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   const CacheRef c = cache_ref(s, pages);
   const CacheRows p = {table, row_req, row_len, n_rows, k, list_length(s, k)};
   const unsigned pairs = (unsigned)(n_rows * s.H_q);
-  const bool wide = s.page_size >= 64, all = k >= (long)s.max_pages * s.page_size;
+  const bool all = k >= (long)s.max_pages * s.page_size;
   if (!all) {
     const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
     const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.parts};
-    if (!wk.parts) {
-      if (wide) cache_select_kernel<1, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
-      else cache_select_kernel<4, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
-    } else {
-      if (wide) cache_select_kernel<1, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-      else cache_select_kernel<4, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-      if (hipGetLastError() != hipSuccess) return DMA_EHIP;
-      if (wide) cache_slice_kernel<1><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-      else cache_slice_kernel<4><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-    }
+    auto select = [&](auto width) {
+      constexpr int S = decltype(width)::value;
+      if (!wk.parts) {
+        cache_select_kernel<S, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+        return;
+      }
+      cache_select_kernel<S, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      cache_slice_kernel<S><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+    };
+    if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
+    else if (s.page_size == 32) select(std::integral_constant<int, 2>{});
+    else select(std::integral_constant<int, 4>{});
     if (hipGetLastError() != hipSuccess) return DMA_EHIP;
   }
   auto go = [&](auto t) {

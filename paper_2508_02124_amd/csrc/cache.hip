@@ -315,14 +315,20 @@ __device__ __forceinline__ uint32_t quantise8(const Raw8<float>& r, uint32_t& by
   return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], scale, 3);
 }
 
-// Where the rows of a tile of 64 go: the page (none: null) and the place in it, worked out once for all of a row's lanes (a 64-bit
+// Rows of a tile, for rows of that many bytes: more workgroups of fewer registers where a row is long.  In and out, 64 / 32 rows, us:
+// 5003 x 4 heads of 256 fp32 channels 27.0 / 24.4, 9001 x 4 of 256 in bf16 24.9 / 22.8, 9001 x 4 of 128 in fp32 22.0 / 20.8, 65536 x 8 of
+// 128 in bf16 163.2 / 162.0, 20001 x 16 of 64 in bf16 50.7 / 51.8.
+constexpr int tile_size(int bytes) { return bytes >= 256 ? 32 : 64; }
+
+// Where the rows of a tile go: the page (none: null) and the place in it, worked out once for all of a row's lanes (a 64-bit
 // product each).
 struct TileRows {
   char* page[64];
   uint32_t place[64];
 };
-__device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __restrict__ slots, int t0, int n_rows, TileRows& rows) {
-  if (threadIdx.x < 64) {
+__device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __restrict__ slots, int tile, int t0, int n_rows,
+                                          TileRows& rows) {
+  if ((int)threadIdx.x < tile) {
     const int t = t0 + threadIdx.x;
     const uint32_t slot = t < n_rows ? (uint32_t)slots[t] : 0xffffffffu;
     rows.page[threadIdx.x] = slot < c.n_slots ? cache_page(c, slot) : nullptr;
@@ -330,7 +336,7 @@ __device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __re
   }
 }
 
-// One workgroup per (64 rows, kv-head).  A row is held by D / 8 lanes; K and V of all rows of the tile are requested before the
+// One workgroup per (tile of rows, kv-head).  A row is held by D / 8 lanes; K and V of all rows of the tile are requested before the
 // first is used.  The scores are those of z_kernel, bit for bit: the same sums in the same order.
 // Bound by HBM: 65536 rows of 8 heads of 128 channels, 32 scores each, out of a projection of 48 heads, 81 us for 350 MB (4.3 TB/s;
 // a copy reaches 4.75), 50 us without a slot to write to.  (A row's pages worked out by each of its lanes, and fp32 values where
@@ -342,13 +348,14 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
                                                            const float* __restrict__ W, const float* __restrict__ A,
                                                            const float* __restrict__ z, const int32_t* __restrict__ slots,
                                                            int n_rows) {
-  __shared__ float zs[GMAX * 64];
+  constexpr int TILE = tile_size(D * sizeof(T));
+  __shared__ float zs[GMAX * TILE];
   __shared__ TileRows rows;
-  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
-  __shared__ __align__(16) uint8_t bytes[64][D / 16];  // the rows' scales, K's and V's, which leave together
-  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
+  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = TILE / RPP;
+  __shared__ __align__(16) uint8_t bytes[TILE][D / 16];  // the rows' scales, K's and V's, which leave together
+  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * TILE;
   const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
-  tile_rows(c, slots, t0, n_rows, rows);
+  tile_rows(c, slots, TILE, t0, n_rows, rows);
   Raw8<T> k[NP], v[NP];
 #pragma unroll
   for (int pass = 0; pass < NP; pass++) {
@@ -379,7 +386,7 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
       reinterpret_cast<float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] = zv;
   };
   auto put_bytes = [&]() {  // (behind a barrier)
-    if (tid < 64 && rows.page[tid]) {
+    if (tid < TILE && rows.page[tid]) {
       using Bytes = std::conditional_t<D == 64, uint32_t, std::conditional_t<D == 128, uint2, uint4>>;
       char* to = rows.page[tid] + (c.off_scales + (((uint32_t)g << c.shift) + rows.place[tid]) * (D / 16));
       *reinterpret_cast<Bytes*>(to) = *reinterpret_cast<const Bytes*>(bytes[tid]);
@@ -388,9 +395,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
   if (!W) {
     __syncthreads();
     put_bytes();
-    for (int i = tid; i < G * 64; i += 256) {
-      const int h = g * G + (i >> 6), t = t0 + (i & 63);
-      if (t < n_rows) put_score(h, i & 63, z[(size_t)h * n_rows + t]);
+    for (int i = tid; i < G * TILE; i += 256) {
+      const int h = g * G + i / TILE, r = i % TILE;
+      if (t0 + r < n_rows) put_score(h, r, z[(size_t)h * n_rows + t0 + r]);
     }
     return;
   }
@@ -413,15 +420,15 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
 #pragma unroll
         for (int e = 0; e < 8; e++) acc = fmaf(wreg[hh][e], x[e], acc);
         acc = group_sum<LPR>(acc);
-        if (sub == hh % LPR) zs[hh * 64 + pass * RPP + rl] = acc;
+        if (sub == hh % LPR) zs[hh * TILE + pass * RPP + rl] = acc;
       }
     }
     __syncthreads();
     if (!h0) put_bytes();
-    for (int i = tid; i < min(GMAX, G - h0) * 64; i += 256) {
-      const int h = g * G + h0 + (i >> 6);
+    for (int i = tid; i < min(GMAX, G - h0) * TILE; i += 256) {
+      const int h = g * G + h0 + i / TILE;
       const float x = zs[i], sp = fmaxf(x, 0.f) + log1pf(expf(-fabsf(x)));
-      put_score(h, i & 63, expf(A[h] * sp));
+      put_score(h, i % TILE, expf(A[h] * sp));
     }
   }
 }
@@ -431,11 +438,11 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32_t* __restrict__ slots, T* __restrict__ K,
                                                          T* __restrict__ V, float* __restrict__ z, int n_rows) {
-  constexpr int LPR = D / 8, RPP = 256 / LPR, NP = 64 / RPP;
+  constexpr int TILE = tile_size(D * sizeof(T)), LPR = D / 8, RPP = 256 / LPR, NP = TILE / RPP;
   __shared__ TileRows rows;
-  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * 64;
+  const int g = blockIdx.y, G = c.H_q / c.H_kv, t0 = blockIdx.x * TILE;
   const int tid = threadIdx.x, sub = tid % LPR, rl = tid / LPR;
-  tile_rows(c, slots, t0, n_rows, rows);
+  tile_rows(c, slots, TILE, t0, n_rows, rows);
   __syncthreads();
   uint32_t kc[NP], vc[NP], kb[NP], vb[NP];
 #pragma unroll
@@ -477,8 +484,8 @@ __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32
       put(V + ((size_t)t * c.H_kv + g) * D + 8 * sub, vc[pass], vb[pass]);
     }
   }
-  for (int i = tid; i < G * 64; i += 256) {
-    const int h = g * G + (i >> 6), r = i & 63;
+  for (int i = tid; i < G * TILE; i += 256) {
+    const int h = g * G + i / TILE, r = i % TILE;
     if (t0 + r >= n_rows) continue;
     const char* page = rows.page[r];
     z[(size_t)h * n_rows + t0 + r] = page ? reinterpret_cast<const float*>(page + c.off_z)[((uint32_t)h << c.shift) + rows.place[r]] : -INFINITY;
@@ -489,7 +496,8 @@ template <typename T, int D>
 static void append_t(const dma_cache_shape& s, int n_rows, const void* K, long k_stride, const void* V, long v_stride,
                      const float* W, const float* A, const float* z, const int32_t* slots, void* pages, hipStream_t st) {
   const CacheRef c = cache_ref(s, pages);
-  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)s.H_kv);
+  const int tile = tile_size(s.d * (s.dtype == DMA_F32 ? 4 : 2));
+  const dim3 grid((unsigned)((n_rows + tile - 1) / tile), (unsigned)s.H_kv);
   const int G = s.H_q / s.H_kv;
 #define DMA_APPEND(GM) \
   cache_append_kernel<T, D, GM><<<grid, 256, 0, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
@@ -514,7 +522,8 @@ int launch_cache_append(const dma_cache_shape& s, int n_rows, const void* K, lon
 int launch_cache_read(const dma_cache_shape& s, int n_rows, const int32_t* slots, const void* pages, void* K, void* V,
                       float* z, hipStream_t st) {
   const CacheRef c = cache_ref(s, pages);
-  const dim3 grid((unsigned)((n_rows + 63) / 64), (unsigned)s.H_kv);
+  const int tile = tile_size(s.d * (s.dtype == DMA_F32 ? 4 : 2));
+  const dim3 grid((unsigned)((n_rows + tile - 1) / tile), (unsigned)s.H_kv);
   auto go = [&](auto t) {
     using T = std::remove_pointer_t<decltype(t)>;
     if (s.d == 256) cache_read_kernel<T, 256><<<grid, 256, 0, st>>>(c, slots, (T*)K, (T*)V, z, n_rows);

@@ -86,7 +86,7 @@ __device__ __forceinline__ uint32_t lanes_before(unsigned long long m) {
 
 // ------------------------------------------------------------------ the kept set by one workgroup
 // The chunks of a row go round the waves, R to each; a lane holds its keys in registers (longer rows: in rounds of as many, read
-// again in every pass).  A histogram of 1024 equal bins between the row's smallest and largest key finds the bin of the kk-th best.
+// again in every pass).  A histogram of equal bins between the row's smallest and largest key finds the bin of the kk-th best.
 // Keys before the bin are counted chunk by chunk; those of the bin move to LDS, each wave's to places of its own, where each
 // counts those before it, by key and position, and adds itself to its chunk's count if it is kept.  A scan of the counts says where the
 // chunks' slots go.  (A bin of many keys, ties above all, is narrowed down digit by digit, and the chunks are counted afterwards.)
@@ -94,8 +94,8 @@ __device__ __forceinline__ uint32_t lanes_before(unsigned long long m) {
 // chunks do not depend on the length (the page numbers are on their way before it is known), and nothing goes through an atomic
 // that returns.
 template <int NT> struct SelectShared {
-  static constexpr int REP = 4, BITS = 10, NDIG = 1 << BITS, NW = NT / 64, NEAR = NT / NW;  // keys of a bin that a wave can list
-  __align__(16) uint32_t hist[NDIG * REP];
+  static constexpr int HIST = 4096, NW = NT / 64, NEAR = NT / NW;  // counters; keys of a bin that a wave can list
+  __align__(16) uint32_t hist[HIST];
   __align__(16) uint32_t near[NT];  // entry e of wave w at e * NW + w
   uint32_t near_pos[NT];
   __align__(16) uint32_t kept[256], equal[256];  // per chunk of a round
@@ -103,30 +103,41 @@ template <int NT> struct SelectShared {
   uint32_t st[4];
 };
 
-// The digit at which the running count of the histogram reaches `remaining` (st[0..2]); CLEAR: leaves it cleared.
-template <int NT, bool CLEAR = true> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m, uint32_t remaining) {
-  constexpr int DPT = SelectShared<NT>::NDIG / NT;
+// A histogram has 1024 bins of four counters each, one for every fourth lane (scores share their leading bits: many lanes of a wave
+// count in one bin), or, for rows of more than 4096 keys, 2048 of two: half the keys in a bin then (whole calls, us, 1024 / 2048 bins:
+// lists x keys: 768 x 5461 55.1 / 53.4, 256 x 8192 29.2 / 26.7, 1024 x 4096 49.9 / 50.6, 768 x 1000 18.9 / 19.7).
+struct KeyBins {
+  int bits, shift;  // 2^bits bins of 2^shift counters
+  __device__ __forceinline__ explicit KeyBins(bool fine) : bits(fine ? 11 : 10), shift(fine ? 1 : 2) {}
+  __device__ __forceinline__ uint32_t word(uint32_t bin, int l) const { return (bin << shift) + (l & ((1 << shift) - 1)); }
+};
+
+// The bin at which the running count of the histogram reaches `remaining`, the rank inside it and its count (st[0..2]); CLEAR: leaves
+// the histogram cleared.
+template <int NT, bool CLEAR = true> __device__ __forceinline__ void pick_digit(SelectShared<NT>& m, const KeyBins& bins, uint32_t remaining) {
+  static_assert(SelectShared<NT>::HIST == 8 * NT, "");
   const int tid = threadIdx.x, w = tid >> 6, l = tid & 63;
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
   __syncthreads();
-  uint32_t cn[DPT], sum = 0;  // this thread's digits
-#pragma unroll
-  for (int i = 0; i < DPT; i++) {
-    const uint4 x = hist4[DPT * tid + i];
-    if (CLEAR) hist4[DPT * tid + i] = make_uint4(0, 0, 0, 0);
-    cn[i] = x.x + x.y + x.z + x.w;
-    sum += cn[i];
+  const uint4 x = hist4[2 * tid], y = hist4[2 * tid + 1];
+  if (CLEAR) hist4[2 * tid] = hist4[2 * tid + 1] = make_uint4(0, 0, 0, 0);
+  uint32_t cn[4] = {x.x + x.y, x.z + x.w, y.x + y.y, y.z + y.w};  // this thread's bins: four, or two
+  if (bins.shift == 2) {
+    cn[0] += cn[1];
+    cn[2] += cn[3];
+    cn[1] = cn[3] = 0;
   }
-  const uint32_t inc = wave_scan(sum, 0u, [](uint32_t x, uint32_t y) { return x + y; });
+  const uint32_t sum = cn[0] + cn[1] + cn[2] + cn[3];
+  const uint32_t inc = wave_scan(sum, 0u, [](uint32_t a, uint32_t b) { return a + b; });
   if (l == 63) m.wsum[w][0] = inc;
   __syncthreads();
   uint32_t run = inc - sum;
 #pragma unroll
   for (int i = 0; i < NT / 64; i++) run += i < w ? m.wsum[i][0] : 0u;
 #pragma unroll
-  for (int i = 0; i < DPT; i++) {
-    if (run < remaining && remaining <= run + cn[i]) {  // exactly one digit of one thread
-      m.st[0] = (uint32_t)(DPT * tid + i);
+  for (int i = 0; i < 4; i++) {
+    if (run < remaining && remaining <= run + cn[i]) {  // exactly one bin of one thread
+      m.st[0] = (uint32_t)(4 * tid + i) >> (bins.shift - 1);
       m.st[1] = remaining - run;
       m.st[2] = cn[i];
     }
@@ -147,10 +158,11 @@ __device__ __forceinline__ uint32_t chunk_offsets(const uint32_t* counts, int w,
 template <int NT, int R, int S, bool LONG>
 __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& row, int h, int kk, int32_t* list, SelectShared<NT>& m) {
   using M = SelectShared<NT>;
-  constexpr int NW = M::NW, REP = M::REP, BITS = M::BITS, NDIG = M::NDIG, NEAR = M::NEAR, STEP = 4;
+  constexpr int NW = M::NW, NEAR = M::NEAR, STEP = 4;
   static_assert(NW == 8 && R <= 32 && R % STEP == 0, "");
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
   const char* scores = c.pages + c.off_z + ((size_t)h << c.shift) * 4;
+  const KeyBins bins(n > 4096);
   const int rounds = LONG ? (n + NW * R * 64 - 1) / (NW * R * 64) : 1;
   PageRun<S> run;
   uint32_t key[R];
@@ -199,7 +211,7 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
   uint32_t kmin = NO_KEY, kmax = 0;
   if (!LONG) run.load(c, row, w, NW, l);
-  for (int i = tid; i < NDIG; i += NT) hist4[i] = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < M::HIST / 4; i += NT) hist4[i] = make_uint4(0, 0, 0, 0);
   m.near[tid] = NO_KEY;
   if (tid < 256) m.kept[tid] = 0;
   if (tid == 0) m.st[3] = NO_KEY;
@@ -229,12 +241,12 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
   }
   kmin = (uint32_t)__builtin_amdgcn_readfirstlane((int)kmin);
   const uint32_t range = (uint32_t)__builtin_amdgcn_readfirstlane((int)(kmax - kmin));
-  const int sh0 = max(0, 32 - (range ? __clz((int)range) : 32) - BITS);  // (key - kmin) >> sh0 < NDIG
+  const int sh0 = max(0, 32 - (range ? __clz((int)range) : 32) - bins.bits);  // (key - kmin) >> sh0 < 2^bits
   // (positions without a key count in the last bin, behind every key of it)
   every([&](uint32_t k32, int) {
-    atomicAdd(&m.hist[min((k32 - kmin) >> sh0, (uint32_t)NDIG - 1) * REP + (l & (REP - 1))], 1u);
+    atomicAdd(&m.hist[bins.word(min((k32 - kmin) >> sh0, (1u << bins.bits) - 1u), l)], 1u);
   });
-  pick_digit<NT>(m, (uint32_t)kk);
+  pick_digit<NT>(m, bins, (uint32_t)kk);
   const uint32_t base = kmin + (m.st[0] << sh0);  // first key of the bin
   const uint32_t width = min(1u << sh0, NO_KEY - base);
   uint32_t need_eq = m.st[1], n_eq = m.st[2], sub = 0;
@@ -324,14 +336,14 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
     }
   }
   for (int sh = sh0; sh > 0;) {  // (at most 22 bits are left: three rounds)
-    const int bits = min(BITS, sh), s2 = sh - bits;
+    const int bits = min(bins.bits, sh), s2 = sh - bits;
     uint32_t from = base;
     asm volatile("" : "+v"(from));  // (the differences of all keys, kept from round to round, would spill)
     every([&](uint32_t k32, int) {
       const uint32_t x = k32 - from;  // (of keys before the bin it wraps round to the far end: never equal to `sub`)
-      if (k32 != NO_KEY && (x >> sh) == sub) atomicAdd(&m.hist[((x >> s2) & ((1u << bits) - 1u)) * REP + (l & (REP - 1))], 1u);
+      if (k32 != NO_KEY && (x >> sh) == sub) atomicAdd(&m.hist[bins.word((x >> s2) & ((1u << bits) - 1u), l)], 1u);
     });
-    pick_digit<NT>(m, need_eq);
+    pick_digit<NT>(m, bins, need_eq);
     sub = (sub << bits) | m.st[0];
     need_eq = m.st[1];
     n_eq = m.st[2];
@@ -426,11 +438,12 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
                                             SelectShared<512>& m) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
   const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
+  const KeyBins bins(false);
   if (slices > SLICES_MAX || part >= slices) return;
   PageRun<S> run;
   slice_pages<S>(c, row, part, run);
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
-  for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+  for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
   // the sample: one key of each of 2048 equal parts of the row, at a place in it that follows no period
   uint32_t sample[SAMPLE / 512], key[SLICE_CHUNKS];
 #pragma unroll
@@ -459,17 +472,17 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
     kmax = max(kmax, m.wsum[i][1]);
   }
   const uint32_t range = kmax - kmin;
-  const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
+  const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - bins.bits);
 #pragma unroll
-  for (int e = 0; e < SAMPLE / 512; e++) atomicAdd(&m.hist[((sample[e] - kmin) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
+  for (int e = 0; e < SAMPLE / 512; e++) atomicAdd(&m.hist[bins.word((sample[e] - kmin) >> sh, l)], 1u);
   const float kept_share = (float)kk / (float)n, middle = kept_share * SAMPLE, off = 3.5f * sqrtf(middle * (1.f - kept_share)) + 3.f;
   uint32_t lo = 0, hi = NO_KEY - 1;
   if (middle - off >= 1.f) {
-    pick_digit<512, false>(m, (uint32_t)(middle - off));
+    pick_digit<512, false>(m, bins, (uint32_t)(middle - off));
     lo = kmin + (m.st[0] << sh);
   }
   if (middle + off < (float)SAMPLE) {
-    pick_digit<512, false>(m, (uint32_t)(middle + off) + 1u);
+    pick_digit<512, false>(m, bins, (uint32_t)(middle + off) + 1u);
     const uint32_t top = (m.st[0] << sh) + ((1u << sh) - 1u);
     hi = top < hi - kmin ? kmin + top : hi;
   }
@@ -515,8 +528,11 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 
 // Workgroups per (row, head): one that selects for a short row, or, SLICED, parts of a long one (a second launch follows).  Not SLICED:
 // the caller's bound says that no row is long; one that is all the same is selected by one workgroup.
-template <int S, bool SLICED>
-__global__ __launch_bounds__(512, 6) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+// WAVES: four workgroups share a compute unit where 64 registers hold what they need (8), at the price of some in scratch, three where
+// they do not (6).  Four are worth it from more lists on than three of each compute unit are (whole calls, us, 6 / 8: 256 lists of
+// 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1).
+template <int S, bool SLICED, int WAVES>
+__global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
   const int pairs = p.n_rows * c.H_q, part = SLICED ? blockIdx.x / pairs : 0, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);
@@ -551,6 +567,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   __shared__ SelectShared<512> m;
   __shared__ __align__(16) uint32_t cand[LISTED];
   const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
+  const KeyBins bins(false);
   const auto add = [](uint32_t x, uint32_t y) { return x + y; };
   if (l >= slices) cnt = make_uint2(0, 0);
   const unsigned long long over = __ballot(cnt.y > (uint32_t)share);
@@ -570,10 +587,10 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   int sh = 0;
   if (found) {
     uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
-    for (int i = tid; i < m.NDIG; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+    for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) *near_all = 0;
     const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.x), range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.y) - lo;
-    sh = max(0, 32 - (range ? __clz((int)range) : 32) - m.BITS);
+    sh = max(0, 32 - (range ? __clz((int)range) : 32) - bins.bits);
     lists([&](uint32_t to, uint32_t have, int s) {
       for (uint32_t i0 = 0; i0 < have; i0 += 256) {
         uint32_t k[4];
@@ -586,8 +603,8 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
     });
     (void)slice_keys<S>(c, row, h, part, run, key);  // (on its way under the search for the threshold)
     __syncthreads();
-    for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[((cand[i] - lo) >> sh) * m.REP + (l & (m.REP - 1))], 1u);
-    pick_digit<512>(m, (uint32_t)kk - better);
+    for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[bins.word((cand[i] - lo) >> sh, l)], 1u);
+    pick_digit<512>(m, bins, (uint32_t)kk - better);
     base = lo + (m.st[0] << sh);
     rank = m.st[1];
     n_near = m.st[2];
@@ -995,14 +1012,18 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
     const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
     const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.parts};
-    auto select = [&](auto width) {
-      constexpr int S = decltype(width)::value;
+    auto select_w = [&](auto width, auto waves) {
+      constexpr int S = decltype(width)::value, W = decltype(waves)::value;
       if (!wk.parts) {
-        cache_select_kernel<S, false><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+        cache_select_kernel<S, false, W><<<pairs, 512, 0, st>>>(c, p, sw, kept);
         return;
       }
-      cache_select_kernel<S, true><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      cache_select_kernel<S, true, W><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
       cache_slice_kernel<S><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+    };
+    auto select = [&](auto width) {
+      if (pairs > 3 * CUS) select_w(width, std::integral_constant<int, 8>{});
+      else select_w(width, std::integral_constant<int, 6>{});
     };
     if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
     else if (s.page_size == 32) select(std::integral_constant<int, 2>{});

@@ -388,6 +388,23 @@ def test_many_rows_of_long_lists(gpu):
     check_rows(cache, q, 4600, rows, cache.decode(q, 4600, req, length))
 
 
+@pytest.mark.parametrize("kind", ["ordinary", "levels", "wide"])
+@pytest.mark.parametrize("ps", [16, 32, 64])
+@pytest.mark.parametrize("n_rows", [24, 25])
+def test_lists_around_three_to_a_compute_unit(gpu, kind, ps, n_rows):
+    """768 and 800 lists, of rows around the length from which on they are sorted into finer bins."""
+    lens, k = (4096, 4097, 300, 4300), 2048
+    cache = GpuCache(gpu, 4, 820, 270, ps, 32, 8, 64)
+    fill(cache, lens, 13, kind)
+    rows = [(i % 4, lens[i % 4] - i // 4) for i in range(n_rows)]
+    q = normal(gpu, 9, n_rows, 32, 64).to(cache.type)
+    req = torch.tensor([b for b, _ in rows], dtype=torch.int32, device=gpu)
+    length = torch.tensor([n for _, n in rows], dtype=torch.int32, device=gpu)
+    got = cache.decode(q, k, req, length)
+    check_kept(cache, k, rows, got[2])
+    check_rows(cache, q[:2], k, rows[:2], (got[0][:2], got[1][:, :2], got[2][:2]))
+
+
 def test_masked_keys_take_no_part(gpu):
     """A key with a score of -infinity counts for nothing, whatever its K and V hold; a row that keeps only such keys is empty."""
     cache = GpuCache(gpu, 2, 8, 4, 16, 2, 1, 128)

@@ -883,14 +883,23 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   }
   const auto add = [](float a, float b) { return a + b; };
   lsum = over_groups<LPG>(lsum, add);
+  const auto across = [](const auto& both) { return __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]); };
+  const auto bits = [](float x) { return __builtin_bit_cast(unsigned, x); };
 #pragma unroll
-  for (int e = 0; e < 32; e++) acc[e] = over_groups<LPG>(acc[e], add);
+  for (int e = 0; e < 16; e++) acc[e] = across(__builtin_amdgcn_permlane32_swap(bits(acc[e]), bits(acc[e + 16]), false, false));
+#pragma unroll
+  for (int e = 0; e < 8; e++) {  // (from here on each row of 16 lanes has sums of its own: a quarter of the channels)
+    acc[e] = across(__builtin_amdgcn_permlane16_swap(bits(acc[e]), bits(acc[e + 8]), false, false));
+    if constexpr (LPG == 2) acc[e] += dpp_move<0x4e>(acc[e]);
+    if constexpr (LPG <= 4) acc[e] += dpp_move<0x124>(acc[e]);
+    acc[e] += dpp_move<0x128>(acc[e]);
+  }
   __shared__ __align__(16) float mo[4][D];
   __shared__ float ml[4][2];
-  if (grp == 0) {
-#pragma unroll
-    for (int e = 0; e < 32; e += 4)
-      *reinterpret_cast<float4*>(&mo[w][32 * sub + e]) = make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
+  if ((l & 15) < LPG) {
+    float4* to = reinterpret_cast<float4*>(&mo[w][32 * sub + 16 * (l >> 5) + 8 * (l >> 4 & 1)]);
+    to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
   }
   if (l == 0) {
     ml[w][0] = m;

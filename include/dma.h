@@ -306,7 +306,7 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
  *   slots        [n_rows] int32: place of a token, page * page_size + place in the page; below 0: none
  *   row_req      [n_rows] int32: request of a row; below 0: none
  *   row_len      [n_rows] int32: keys that a row sees, the first row_len of its request; 0: none
- * n_rows is the capacity of a step's row arrays, not its number of rows, at most 2^30, and may be 0 (nothing is done, or
+ * n_rows is the capacity of a step's row arrays, not its number of rows, at most 2^28, and may be 0 (nothing is done, or
  * enqueued, but by dma_cache_assign).  dtype is the type of K, V, q and o; what the cache holds does not depend on it.
  *
  * A token's K (and V) of one kv-head is held as d codes of 4 bits and d / 32 scale bytes (OCP microscaling, e2m1 with e8m0): channel c

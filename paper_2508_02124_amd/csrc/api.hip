@@ -68,7 +68,7 @@ int check_rows(const dma_cache_shape* s, int32_t n_rows) {
   int rc = check_cache(s);
   if (rc != DMA_OK) return rc;
   if (n_rows < 0) return DMA_EINVAL;
-  return n_rows > CACHE_TOKENS_MAX ? DMA_EUNSUPPORTED : DMA_OK;
+  return n_rows > CACHE_ROWS_MAX ? DMA_EUNSUPPORTED : DMA_OK;
 }
 
 // n_rows rows of `heads` heads, `stride` elements apart
@@ -395,7 +395,7 @@ const char* dma_strerror(int status) {
   switch (status) {
     case DMA_OK: return "ok";
     case DMA_EINVAL: return "invalid argument (null or misaligned pointer, non-positive size, H_q % H_kv != 0)";
-    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, 2^30 tokens)";
+    case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, 2^30 tokens, 2^28 rows)";
     case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes, dma_cache_decode_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
     case DMA_EHIP: return "HIP launch failed";
     default: return "unknown status";

@@ -5,7 +5,8 @@
 namespace dma {
 
 constexpr int CACHE_REQS_MAX = 4096;  // places for requests: their row offsets and page counts wait in LDS (cache_assign_kernel)
-constexpr int CACHE_TOKENS_MAX = 1 << 30;  // of the pool, of a request, of a step (so that a position and a step beyond fit an int)
+constexpr int CACHE_TOKENS_MAX = 1 << 30;  // of the pool, of a request (so that a position and a step beyond fit an int)
+constexpr int CACHE_ROWS_MAX = 1 << 28;    // of a step (a launch has fewer than 2^32 threads: 256 for 32 rows)
 constexpr int FREE_HEADER = 4;        // int32 before the stack of the free list: [0] = number of free pages
 
 struct CacheLayout {

@@ -222,17 +222,17 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
 
 __global__ __launch_bounds__(256) void cache_reset_kernel(int32_t* lens, int32_t* table, int32_t* free_list, int n_reqs,
                                                           int n_pages, size_t entries) {
-  const size_t i = blockIdx.x * (size_t)256 + threadIdx.x;
-  if (i < entries) table[i] = -1;
-  if (i < (size_t)n_reqs) lens[i] = 0;
-  if (i < (size_t)n_pages) free_list[FREE_HEADER + i] = n_pages - 1 - (int)i;  // (the lowest pages are taken first)
-  if (i < FREE_HEADER) free_list[i] = i == 0 ? n_pages : 0;
+  const size_t step = gridDim.x * (size_t)256, i0 = blockIdx.x * (size_t)256 + threadIdx.x;
+  for (size_t i = i0; i < entries; i += step) table[i] = -1;
+  for (size_t i = i0; i < (size_t)n_reqs; i += step) lens[i] = 0;
+  for (size_t i = i0; i < (size_t)n_pages; i += step) free_list[FREE_HEADER + i] = n_pages - 1 - (int)i;  // (the lowest are taken first)
+  if (i0 < FREE_HEADER) free_list[i0] = i0 == 0 ? n_pages : 0;
 }
 
 int launch_cache_reset(const dma_cache_shape& s, int32_t* lens, int32_t* table, int32_t* free_list, hipStream_t st) {
   const size_t entries = (size_t)s.n_reqs * s.max_pages;
-  const size_t n = entries > (size_t)s.n_pages + FREE_HEADER ? entries : (size_t)s.n_pages + FREE_HEADER;
-  cache_reset_kernel<<<(unsigned)((n + 255) / 256), 256, 0, st>>>(lens, table, free_list, s.n_reqs, s.n_pages, entries);
+  const size_t most = entries > (size_t)s.n_pages ? entries : (size_t)s.n_pages, blocks = (most + 255) / 256;
+  cache_reset_kernel<<<(unsigned)(blocks < 64 * CUS ? blocks : 64 * CUS), 256, 0, st>>>(lens, table, free_list, s.n_reqs, s.n_pages, entries);
   return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
 }
 

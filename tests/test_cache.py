@@ -115,7 +115,7 @@ def test_arguments_refused():
 
 
 def test_numbers_of_rows_refused():
-    s, many = shape(), (1 << 30) + 1
+    s, many = shape(), (1 << 28) + 1
     refused(B.DMA_EUNSUPPORTED, B.dma_cache_assign, s, many, *[P] * 9)
     refused(B.DMA_EUNSUPPORTED, B.dma_cache_append, s, many, P, 256, P, 256, P, P, None, P, P)
     refused(B.DMA_EUNSUPPORTED, B.dma_cache_read, s, many, P, P, P, P, P)

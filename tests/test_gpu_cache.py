@@ -65,6 +65,18 @@ def test_sums_that_pass_32_bits(gpu, n_reqs, n_rows):
         check_assign(cache, [int(r.integers(-20, 20)) for _ in range(n_reqs)], n_rows)
 
 
+@pytest.mark.parametrize("n_reqs,n_pages,max_pages,ps", [(3, 2, 1, 16), (60, 5_000_000, 300_000, 16), (4096, 1100, 1100, 32)])
+def test_reset_of_large_tables(gpu, n_reqs, n_pages, max_pages, ps):
+    """More entries than one launch has threads (4,194,304)."""
+    shape = B.make_cache_shape(n_reqs, n_pages, max_pages, ps, 2, 1, 64)
+    lens, table = torch.full((n_reqs,), 5, dtype=torch.int32, device=gpu), torch.full((n_reqs, max_pages), 5, dtype=torch.int32, device=gpu)
+    free = torch.full((B.dma_cache_free_bytes(shape) // 4 + 1,), 5, dtype=torch.int32, device=gpu)
+    B.dma_cache_reset(shape, lens, table, free)
+    assert (lens == 0).all() and (table == -1).all()
+    assert free[:4].tolist() == [n_pages, 0, 0, 0] and free[4 + n_pages:].tolist() == [5] * (len(free) - 4 - n_pages)
+    assert (free[4:4 + n_pages] == torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=gpu)).all()
+
+
 def test_refusals_in_order(gpu):
     cache = GpuCache(gpu, 5, 4, 3, 16, 2, 1, 64)
     assert check_assign(cache, [16, 16, 5, 0, 0], 64) == [0, 0, 0, 0, 0]

@@ -406,7 +406,7 @@ constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hol
 struct SliceWork {
   uint2* counts;  // [pairs][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
   uint2* listed;  // [pairs][LISTED]: key, position
-  uint2* bounds;  // [pairs]: first and last key of the lists
+  uint4* bounds;  // [pairs]: first and last key of the lists; the same, or those of the sample where the lists have no end
   int parts;
 };
 
@@ -432,6 +432,9 @@ __device__ __forceinline__ bool slice_keys(const CacheRef& c, const CacheRow& ro
   return !bad;
 }
 
+// How far from its expected rank in a sample the key at that share of the row may lie: 3.5 standard deviations.
+__device__ __forceinline__ float bracket(float share, float size) { return 3.5f * sqrtf(size * share * (1.f - share)) + 3.f; }
+
 // Counts and lists of one workgroup's slices of a long row.
 template <int S>
 __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& row, int h, int kk, int rh, int part, const SliceWork& sw,
@@ -444,21 +447,31 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
   slice_pages<S>(c, row, part, run);
   uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
   for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
-  // the sample: one key of each of 2048 equal parts of the row, at a place in it that follows no period
-  uint32_t sample[SAMPLE / 512], key[SLICE_CHUNKS];
+  // The sample: one key of each of 2048 equal parts of the row, or of 4096 where the lists would be too long for their share, at a
+  // place in it that follows no period.
+  const float kept_share = (float)kk / (float)n, room = ((float)share - 5.f * sqrtf((float)share)) / SLICE;  // (slices differ)
+  const bool wide = 2.f * bracket(kept_share, SAMPLE) > room * SAMPLE;
+  const int log_n = wide ? 12 : 11;
+  static_assert(SAMPLE == 2048, "");
+  uint32_t sample[SAMPLE / 256], key[SLICE_CHUNKS];
 #pragma unroll
-  for (int e = 0; e < SAMPLE / 512; e++) {
-    const uint32_t i = (uint32_t)(e * 512 + tid), width = (uint32_t)n / SAMPLE;
-    const int j = (int)((unsigned long long)i * (uint32_t)n / SAMPLE) + (int)((i * 2654435761u >> 16) * width >> 16);
+  for (int e = 0; e < SAMPLE / 256; e++) {
+    if (e >= SAMPLE / 512 && !wide) continue;
+    const uint32_t i = (uint32_t)(e * 512 + tid), width = (uint32_t)n >> log_n;
+    const int j = (int)((unsigned long long)i * (uint32_t)n >> log_n) + (int)((i * 2654435761u >> 16) * width >> 16);
     sample[e] = score_key(cache_score(c, cache_slot(c, row, j), h));
   }
   bool good = slice_keys<S>(c, row, h, part, run, key);
   uint32_t kmin = NO_KEY, kmax = 0;
+  auto each = [&](auto f) {
 #pragma unroll
-  for (int e = 0; e < SAMPLE / 512; e++) {
-    kmin = min(kmin, sample[e]);
-    kmax = max(kmax, sample[e]);
-  }
+    for (int e = 0; e < SAMPLE / 256; e++)
+      if (e < SAMPLE / 512 || wide) f(sample[e]);
+  };
+  each([&](uint32_t k) {
+    kmin = min(kmin, k);
+    kmax = max(kmax, k);
+  });
   kmin = last_lane(wave_scan(kmin, NO_KEY, [](uint32_t x, uint32_t y) { return min(x, y); }));
   kmax = last_lane(wave_scan(kmax, 0u, [](uint32_t x, uint32_t y) { return max(x, y); }));
   if (l == 0) {
@@ -473,22 +486,32 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
   }
   const uint32_t range = kmax - kmin;
   const int sh = max(0, 32 - (range ? __clz((int)range) : 32) - bins.bits);
-#pragma unroll
-  for (int e = 0; e < SAMPLE / 512; e++) atomicAdd(&m.hist[bins.word((sample[e] - kmin) >> sh, l)], 1u);
-  const float kept_share = (float)kk / (float)n, middle = kept_share * SAMPLE, off = 3.5f * sqrtf(middle * (1.f - kept_share)) + 3.f;
+  each([&](uint32_t k) { atomicAdd(&m.hist[bins.word((k - kmin) >> sh, l)], 1u); });
+  const float size = (float)(1 << log_n), middle = kept_share * size, off = fminf(bracket(kept_share, size), 0.5f * room * size);
+  // The first (end = 0) or last key of the sample's keys that cannot be told from the one of that rank: those of a bin, or, if these
+  // are so many that the lists would grow by an eighth (wide: a 32nd) of their share, of a 1024th of it.
+  auto key_of_rank = [&](uint32_t rank, uint32_t end) {
+    pick_digit<512, false>(m, bins, rank);
+    const uint32_t digit = m.st[0], left = m.st[1], first = kmin + (digit << sh), crowd = m.st[2];
+    if (sh == 0 || crowd * SLICE <= (uint32_t)share << (wide ? log_n - 5 : log_n - 3)) return first + (end << sh) - end;
+    const int s2 = max(0, sh - bins.bits);
+    __syncthreads();
+    for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
+    __syncthreads();
+    each([&](uint32_t k) {
+      if ((k - kmin) >> sh == digit) atomicAdd(&m.hist[bins.word((k - first) >> s2, l)], 1u);
+    });
+    pick_digit<512>(m, bins, left);
+    const uint32_t found = first + (m.st[0] << s2) + (end << s2) - end;
+    each([&](uint32_t k) { atomicAdd(&m.hist[bins.word((k - kmin) >> sh, l)], 1u); });
+    return found;
+  };
   uint32_t lo = 0, hi = NO_KEY - 1;
-  if (middle - off >= 1.f) {
-    pick_digit<512, false>(m, bins, (uint32_t)(middle - off));
-    lo = kmin + (m.st[0] << sh);
-  }
-  if (middle + off < (float)SAMPLE) {
-    pick_digit<512, false>(m, bins, (uint32_t)(middle + off) + 1u);
-    const uint32_t top = (m.st[0] << sh) + ((1u << sh) - 1u);
-    hi = top < hi - kmin ? kmin + top : hi;
-  }
+  if (middle - off >= 1.f) lo = key_of_rank((uint32_t)(middle - off), 0u);
+  if (middle + off < size) hi = min(key_of_rank((uint32_t)(middle + off) + 1u, 1u), hi);
   lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
   hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
-  if (tid == 0 && part == 0) sw.bounds[rh] = make_uint2(lo, hi);
+  if (tid == 0 && part == 0) sw.bounds[rh] = make_uint4(lo, hi, lo ? lo : kmin, hi == NO_KEY - 1 ? kmax : hi);
   for (int slice = part; slice < slices; slice += sw.parts) {
     if (slice != part) {
       slice_pages<S>(c, row, slice, run);
@@ -530,7 +553,7 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 // the caller's bound says that no row is long; one that is all the same is selected by one workgroup.
 // WAVES: four workgroups share a compute unit where 64 registers hold what they need (8), at the price of some in scratch, three where
 // they do not (6).  Four are worth it from more lists on than three of each compute unit are (whole calls, us, 6 / 8: 256 lists of
-// 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1).
+// 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1; SLICED, 2048 parts of 8192: 115.3 / 115.2).
 template <int S, bool SLICED, int WAVES>
 __global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
   const int pairs = p.n_rows * c.H_q, part = SLICED ? blockIdx.x / pairs : 0, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
@@ -557,7 +580,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   const int pairs = p.n_rows * c.H_q, part = blockIdx.x / pairs, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   uint2 cnt = sw.counts[(size_t)rh * SLICES_MAX + l];  // lane s: of slice s
-  const uint2 bounds = sw.bounds[rh];
+  const uint4 bounds = sw.bounds[rh];
   const CacheRow row = cache_row(c, p, r);
   PageRun<S> run;
   slice_pages<S>(c, row, part, run);
@@ -583,13 +606,16 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   };
   const uint2* listed = sw.listed + (size_t)rh * LISTED;
   uint32_t* near_all = &m.st[3];
-  uint32_t key[SLICE_CHUNKS], base = 0, rank = 0, n_near = NO_KEY;
+  uint32_t key[SLICE_CHUNKS], base = 0, rank = 0, n_near = NO_KEY, digit = 0;
   int sh = 0;
+  // (keys beyond the sample's are in the first or the last bin: bins over all that a list may hold would be too wide for its keys)
+  const uint32_t from = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.z);
+  auto bin = [&](uint32_t k) { return min(__builtin_elementwise_sub_sat(k, from) >> sh, (1u << bins.bits) - 1u); };
   if (found) {
     uint4* hist4 = reinterpret_cast<uint4*>(m.hist);
     for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
     if (tid == 0) *near_all = 0;
-    const uint32_t lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.x), range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.y) - lo;
+    const uint32_t range = (uint32_t)__builtin_amdgcn_readfirstlane((int)bounds.w) - from;
     sh = max(0, 32 - (range ? __clz((int)range) : 32) - bins.bits);
     lists([&](uint32_t to, uint32_t have, int s) {
       for (uint32_t i0 = 0; i0 < have; i0 += 256) {
@@ -603,9 +629,10 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
     });
     (void)slice_keys<S>(c, row, h, part, run, key);  // (on its way under the search for the threshold)
     __syncthreads();
-    for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[bins.word((cand[i] - lo) >> sh, l)], 1u);
+    for (uint32_t i = tid; i < all; i += 512) atomicAdd(&m.hist[bins.word(bin(cand[i]), l)], 1u);
     pick_digit<512>(m, bins, (uint32_t)kk - better);
-    base = lo + (m.st[0] << sh);
+    digit = (uint32_t)__builtin_amdgcn_readfirstlane((int)m.st[0]);
+    base = digit ? from + (digit << sh) : 0u;
     rank = m.st[1];
     n_near = m.st[2];
   }
@@ -621,7 +648,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       const bool there = i0 + l < have;
       const uint32_t k = there ? cand[to + i0 + l] : NO_KEY;
       ahead += (uint32_t)__popcll(__ballot(k < base));
-      if (there && ((k - base) >> sh) == 0) {
+      if (there && bin(k) == digit) {
         const uint32_t e = atomicAdd(near_all, 1u);
         m.near[e] = k;
         m.near_pos[e] = listed[s * share + i0 + l].y;
@@ -990,7 +1017,7 @@ static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   wk.parts = (int)(slices < most ? slices : most < 1 && slices ? 1 : most);
   wk.off_counts = take(wk.parts ? pairs * SLICES_MAX * 8 : 0);
   wk.off_listed = take(wk.parts ? pairs * LISTED * 8 : 0);
-  wk.off_bounds = take(wk.parts ? pairs * 8 : 0);
+  wk.off_bounds = take(wk.parts ? pairs * 16 : 0);
   wk.total = o;
   return wk;
 }
@@ -1023,19 +1050,17 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   if (!all) {
     const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
-    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint2*)(base + wk.off_bounds), wk.parts};
-    auto select_w = [&](auto width, auto waves) {
-      constexpr int S = decltype(width)::value, W = decltype(waves)::value;
-      if (!wk.parts) {
-        cache_select_kernel<S, false, W><<<pairs, 512, 0, st>>>(c, p, sw, kept);
-        return;
-      }
-      cache_select_kernel<S, true, W><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-      cache_slice_kernel<S><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-    };
+    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint4*)(base + wk.off_bounds), wk.parts};
     auto select = [&](auto width) {
-      if (pairs > 3 * CUS) select_w(width, std::integral_constant<int, 8>{});
-      else select_w(width, std::integral_constant<int, 6>{});
+      constexpr int S = decltype(width)::value;
+      if (wk.parts) {
+        cache_select_kernel<S, true, 6><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+        cache_slice_kernel<S><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+      } else if (pairs > 3 * CUS) {
+        cache_select_kernel<S, false, 8><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+      } else {
+        cache_select_kernel<S, false, 6><<<pairs, 512, 0, st>>>(c, p, sw, kept);
+      }
     };
     if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
     else if (s.page_size == 32) select(std::integral_constant<int, 2>{});

@@ -297,6 +297,24 @@ def test_kept_sets_of_long_rows(gpu, kind, lens, k, ps):
     check_kept(cache, k, list(enumerate(lens)), got[2])
 
 
+# Lists of a sample of 4096 keys; windows far smaller than the rows; best keys that share their leading bits, with a few far away.
+@pytest.mark.parametrize("kind", ["ordinary", "wide", "near"])
+@pytest.mark.parametrize("lens,k", [((15500, 12500), 73), ((131072, 131000), 32768), ((524288,), 4096), ((90001,), 45000), ((200000,), 3)])
+def test_lists_of_long_rows(gpu, kind, lens, k):
+    print(f"[case] lists {kind} {lens} k={k}", flush=True)
+    cache = GpuCache(gpu, len(lens), sum(-(-n // 256) for n in lens), -(-max(lens) // 256), 256, 2, 1, 64)
+    fill(cache, lens, 31, "ordinary" if kind == "near" else kind)
+    if kind == "near":
+        for b, n in enumerate(lens):
+            slots = torch.from_numpy(request_slots(cache, b).astype(np.int32)).to(gpu)
+            K, V, z = cache.read(slots)
+            far = torch.arange(n, device=gpu) % 997 == 5
+            z = torch.where(far, torch.tensor(1e-30, device=gpu), 1.0 - 2.0 ** -12 * normal(gpu, 6 + b, 2, n).abs())
+            cache.append(K, V, slots, z=z.contiguous())
+    q = normal(gpu, 5, len(lens), 2, 64).to(cache.type)
+    check_kept(cache, k, list(enumerate(lens)), cache.decode(q, k, None, cache.lens)[2])
+
+
 def test_a_row_of_more_slices_than_are_listed(gpu):
     n, ps = 600000, 256
     cache = GpuCache(gpu, 2, n // ps + 3, n // ps + 2, ps, 1, 1, 64)

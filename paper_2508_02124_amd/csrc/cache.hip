@@ -286,6 +286,17 @@ __device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
   top = max(top, dpp_quad<0x4e>(top));
   return top >= 0x7f800000u ? 255u : (uint32_t)max(2, min(252, (int)((top + 0x200000u) >> 23) - 2));
 }
+// Rows whose K and V are more than this (and bf16) are read past the caches: with the pages they do not fit the last one, of 256 MB, and
+// would only drive each other out.  Rows of 8 heads of 128 channels, us through / past: 65536 from memory 103 / 82, 65536 just made by
+// other kernels, these included, 192 / 183, 49152 (192 MiB) 135 / 130, 40960 (160 MiB) 102 / 111, 16384 48 / 54.  (fp32 ones come in half
+// lines, which then are fetched twice: 5003 rows of 4 heads of 256, in and out, 24.7 / 27.2.  Codes stored past the caches: + 1 us.)
+constexpr size_t APPEND_PAST = (size_t)176 << 20;
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool PAST, typename T> __device__ __forceinline__ void load_row(const T* src, Raw8<T>& r) {
+  if constexpr (PAST) r.x = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src)));
+  else load_raw(src, r);
+}
+
 // The codes of a lane's eight channels, and that byte.
 __device__ __forceinline__ uint32_t quantise8(const Raw8<__bf16>& r, uint32_t& byte) {
   const uint32_t u[4] = {r.x.x, r.x.y, r.x.z, r.x.w};
@@ -342,7 +353,7 @@ __device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __re
 // a copy reaches 4.75), 50 us without a slot to write to.  (A row's pages worked out by each of its lanes, and fp32 values where
 // bf16 ones do, 960 vector instructions instead of 730, took as long; so do heads before rows in the order of the workgroups.  Passes
 // without a row left out: + 3 us, a call of one row as before.)
-template <typename T, int D, int GMAX>
+template <typename T, int D, int GMAX, bool PAST>
 __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* __restrict__ K, long k_stride,
                                                            const T* __restrict__ V, long v_stride,
                                                            const float* __restrict__ W, const float* __restrict__ A,
@@ -360,8 +371,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
 #pragma unroll
   for (int pass = 0; pass < NP; pass++) {
     const long t = min(t0 + pass * RPP + rl, n_rows - 1);
-    load_raw(K + t * k_stride + (long)g * D + 8 * sub, k[pass]);
-    load_raw(V + t * v_stride + (long)g * D + 8 * sub, v[pass]);
+    load_row<PAST>(K + t * k_stride + (long)g * D + 8 * sub, k[pass]);
+    load_row<PAST>(V + t * v_stride + (long)g * D + 8 * sub, v[pass]);
   }
   __syncthreads();
 #pragma unroll
@@ -499,11 +510,13 @@ static void append_t(const dma_cache_shape& s, int n_rows, const void* K, long k
   const int tile = tile_size(s.d * (s.dtype == DMA_F32 ? 4 : 2));
   const dim3 grid((unsigned)((n_rows + tile - 1) / tile), (unsigned)s.H_kv);
   const int G = s.H_q / s.H_kv;
+  const bool past = sizeof(T) == 2 && (size_t)n_rows * s.H_kv * D * 4 > APPEND_PAST;
 #define DMA_APPEND(GM) \
-  cache_append_kernel<T, D, GM><<<grid, 256, 0, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
-  if (G == 1) DMA_APPEND(1);
-  else if (G == 2) DMA_APPEND(2);
-  else DMA_APPEND(4);
+  if (past) cache_append_kernel<T, D, GM, sizeof(T) == 2><<<grid, 256, 0, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows); \
+  else cache_append_kernel<T, D, GM, false><<<grid, 256, 0, st>>>(c, (const T*)K, k_stride, (const T*)V, v_stride, W, A, z, slots, n_rows)
+  if (G == 1) { DMA_APPEND(1); }
+  else if (G == 2) { DMA_APPEND(2); }
+  else { DMA_APPEND(4); }
 #undef DMA_APPEND
 }
 

@@ -148,6 +148,21 @@ def test_values_and_scores(gpu, dtype, H_q, H_kv, d, ps, n):
     assert not (changed & ~own).any()
 
 
+@pytest.mark.parametrize("H_q,H_kv,d,n", [(16, 16, 64, 45101), (32, 16, 128, 22600), (64, 16, 256, 11300), (20, 20, 256, 9100)])
+def test_rows_that_fit_no_cache_level(gpu, H_q, H_kv, d, n):
+    """One call for more than 176 MiB of K and V writes what calls for a quarter of the rows each do."""
+    print(f"[case] large append {H_q}/{H_kv} d={d} n={n}", flush=True)
+    caches = [GpuCache(gpu, 1, n // 64 + 1, n // 64 + 1, 64, H_q, H_kv, d) for _ in range(2)]
+    K, V = normal(gpu, 1, n, H_kv, d).to(torch.bfloat16), normal(gpu, 2, n, H_kv, d).to(torch.bfloat16)
+    W, A = normal(gpu, 3, H_q, d, scale=d ** -0.5), normal(gpu, 4, H_q)
+    slots = torch.randperm(n, generator=torch.Generator().manual_seed(5)).to(torch.int32).to(gpu)
+    assert n * H_kv * d * 4 > 176 << 20
+    caches[0].append(K, V, slots, W, A)
+    for i in range(0, n, n // 4):
+        caches[1].append(K[i:i + n // 4], V[i:i + n // 4], slots[i:i + n // 4].clone(), W, A)
+    assert torch.equal(*[c.pages for c in caches])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_blocks_that_are_not_finite(gpu, dtype):
     cache = GpuCache(gpu, 1, 2, 2, 16, 2, 2, 64, dtype)

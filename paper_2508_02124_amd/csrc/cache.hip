@@ -60,6 +60,9 @@ constexpr int ASSIGN_ROWS = 4096;
 // One workgroup, four requests to a thread.  All that it waits for is one after another -- the lengths, two scans, the pages -- so the
 // sums are formed in registers (data-parallel moves, saturating 32 bits), and the rows take the pages of their tokens from the
 // same place of the stack as the table does, not from the table.
+// Bound by that chain, not by its bytes: 256 requests that grow by a token each 4.4 us alone, of which 2 to 3 are the launch; 777 that
+// change by hundreds of tokens, tens of thousands of pages, 14 us (with 4 MB read and written, 1 us at a copy's rate).  The first
+// form, with sums in LDS and the pages read back from the table, took 9.3 and 28 us a call.
 template <int NT>
 __global__ __launch_bounds__(NT) void cache_assign_kernel(AssignArgs p) {
   constexpr int PER = 4, REQS = NT * PER;
@@ -197,7 +200,8 @@ __global__ __launch_bounds__(NT) void cache_assign_kernel(AssignArgs p) {
   }
 }
 
-// The rows of a step with many of them, from what cache_assign_kernel wrote.
+// The rows of a step with many of them, from what cache_assign_kernel wrote: one a thread, 4.7 us where 777 requests
+// grow by hundreds of tokens (several a thread: 44 instead of 37 us for such a call and the one that takes it back).
 __global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
   __shared__ int32_t first[CACHE_REQS_MAX + 1];
   for (int b = threadIdx.x; b <= p.n_reqs; b += 256) first[b] = p.cu_rows[b];
@@ -349,8 +353,8 @@ __device__ __forceinline__ void tile_rows(const CacheRef& c, const int32_t* __re
 
 // One workgroup per (tile of rows, kv-head).  A row is held by D / 8 lanes; K and V of all rows of the tile are requested before the
 // first is used.  The scores are those of z_kernel, bit for bit: the same sums in the same order.
-// Bound by HBM: 65536 rows of 8 heads of 128 channels, 32 scores each, out of a projection of 48 heads, 81 us for 350 MB (4.3 TB/s;
-// a copy reaches 4.75), 50 us without a slot to write to.  (A row's pages worked out by each of its lanes, and fp32 values where
+// Bound by HBM: 65536 rows of 8 heads of 128 channels, 32 scores each, out of a projection of 48 heads, 82 us for 350 MB (4.3 TB/s;
+// a copy reaches 4.75).  One row: 4.1 us, the latency of slots, rows, sums and two barriers behind a launch.  (A row's pages worked out by each of its lanes, and fp32 values where
 // bf16 ones do, 960 vector instructions instead of 730, took as long; so do heads before rows in the order of the workgroups.  Passes
 // without a row left out: + 3 us, a call of one row as before.)
 template <typename T, int D, int GMAX, bool PAST>
@@ -445,7 +449,9 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
 }
 
 // ------------------------------------------------------------------ rows out of it
-// The same tiles; rows without a slot come back as zeros with a score of -infinity.
+// The same tiles; rows without a slot come back as zeros with a score of -infinity.  Bound by HBM, writes above all: 65536 rows as
+// above 60 us for 355 MB (5.9 TB/s).  (Stores past the caches: 53 instead of 73 us in a row, but the kernel that uses the rows
+// loses more, 141 -> 153 together.  Codes read past them: 65536 rows - 4 us, 20001 of 16 heads of 64 channels + 6.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32_t* __restrict__ slots, T* __restrict__ K,
                                                          T* __restrict__ V, float* __restrict__ z, int n_rows) {

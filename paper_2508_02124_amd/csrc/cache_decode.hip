@@ -92,7 +92,9 @@ __device__ __forceinline__ uint32_t lanes_before(unsigned long long m) {
 // chunks' slots go.  (A bin of many keys, ties above all, is narrowed down digit by digit, and the chunks are counted afterwards.)
 // What bounds it is the chain: the row, its pages, the scores, and six barriers with a few LDS accesses between.  So the
 // chunks do not depend on the length (the page numbers are on their way before it is known), and nothing goes through an atomic
-// that returns.
+// that returns.  48 lists of 5461 keys 10.7 us, 768 of them 17.4 (17 MB of scores, 1 TB/s; its vector instructions alone are 7 us), 1024
+// of 4096 18.6.  24 keys to a lane are as many as the registers of three workgroups hold: 20 took the same for such rows,
+// but cut those of more than 10240 keys into slices, two launches.
 template <int NT> struct SelectShared {
   static constexpr int HIST = 4096, NW = NT / 64, NEAR = NT / NW;  // counters; keys of a bin that a wave can list
   __align__(16) uint32_t hist[HIST];
@@ -399,6 +401,8 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
 // the row has more than SLICES_MAX slices, one workgroup selects alone.
 // A row's slices go round its `parts` workgroups.  How many rows are long the host does not know, so there are only as many parts
 // as keep the chip busy: workgroups that find nothing to do cost 1 ns each.
+// Both launches are chains of loads and barriers again: 32 lists of 65536 keys 11.9 and 10.4 us (8.4 MB each: 0.8 TB/s), against 105 us by
+// one workgroup to a list; with the attention, 256 such lists 115 us.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
 constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS, SLICES_MAX = 64;
 constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together, an equal share for each slice
@@ -493,7 +497,7 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
   auto key_of_rank = [&](uint32_t rank, uint32_t end) {
     pick_digit<512, false>(m, bins, rank);
     const uint32_t digit = m.st[0], left = m.st[1], first = kmin + (digit << sh), crowd = m.st[2];
-    if (sh == 0 || crowd * SLICE <= (uint32_t)share << (wide ? log_n - 5 : log_n - 3)) return first + (end << sh) - end;
+    if (sh == 0 || crowd * SLICE <= (uint32_t)share << (wide ? log_n - 5 : log_n - 3)) return __builtin_elementwise_add_sat(first, (end << sh) - end);
     const int s2 = max(0, sh - bins.bits);
     __syncthreads();
     for (int i = tid; i < m.HIST / 4; i += 512) hist4[i] = make_uint4(0, 0, 0, 0);
@@ -502,7 +506,7 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
       if ((k - kmin) >> sh == digit) atomicAdd(&m.hist[bins.word((k - first) >> s2, l)], 1u);
     });
     pick_digit<512>(m, bins, left);
-    const uint32_t found = first + (m.st[0] << s2) + (end << s2) - end;
+    const uint32_t found = __builtin_elementwise_add_sat(first + (m.st[0] << s2), (end << s2) - end);
     each([&](uint32_t k) { atomicAdd(&m.hist[bins.word((k - kmin) >> sh, l)], 1u); });
     return found;
   };
@@ -770,6 +774,10 @@ template <> struct Query<float> {
 // wave takes 64 keys at a time, all of them requested before the first is used.  Weights are formed with the reference so far; only
 // a score more than 5 above it leads to the wave's maximum and a rescaling (sums in 32 bits hold weights up to e^5 as well as
 // up to 1).  The G heads of a kv-head have the same part of their lists on one XCD at the same time (decode_attend_kernel).
+// Bound by HBM and the vector unit together: 24 rows of 32 heads, 2048 of 5461 keys each, 36 us: 138 MB from HBM, 3.8 TB/s (a third of
+// the scale and score lines for keys that are not kept), and 12.3 M instructions of a wave, 20 us of the four SIMDs.  16 rows of
+// 2 x 32 lists of 1024: 22 us; one row of 32 heads 6 us and 3 of the merge.  Further ahead than one step: + 1 and + 3 us (registers); 16 keys
+// a step: rows of 256 channels + 1, 256 lists of 2048 + 3; a branch around the last, empty request + 0.8.
 // ALL: the window keeps every key that a request can have, so nothing was selected, and the lists are written here.
 template <typename TQ, int D, bool ALL>
 __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows p, const TQ* __restrict__ q, long q_stride,
@@ -950,7 +958,8 @@ __global__ __launch_bounds__(256) void cache_attend_kernel(CacheRef c, CacheRows
   finish(num, den, M);
 }
 
-// The parts of one (row, head) together: o = sum_s o_s e^(M_s - M) / sum_s l_s e^(M_s - M), eight parts requested at a time.
+// The parts of one (row, head) together: o = sum_s o_s e^(M_s - M) / sum_s l_s e^(M_s - M), eight parts requested at a time: 2.8 us,
+// a launch and two loads.
 template <typename TQ, int D>
 __global__ __launch_bounds__(D) void cache_merge_kernel(CacheRef c, CacheRows p, const float* __restrict__ part,
                                                         TQ* __restrict__ o, float* __restrict__ lse, int ch, int nsplit) {

@@ -371,11 +371,10 @@ def test_long_rows_with_outputs(gpu):
         check_rows(cache, q, k, rows, cache.decode(q, k, req, length))
 
 
-@pytest.mark.parametrize("lens", [(900, 5000), (20000, 40)])
-def test_scores_that_are_not_numbers(gpu, lens):
+@pytest.mark.parametrize("lens,k", [((900, 5000), 333), ((20000, 40), 333), ((20000, 900), 10000), ((20000, 16000), 19900)])
+def test_scores_that_are_not_numbers(gpu, lens, k):
     """NaN of any sign and payload among the scores: the lists hold min(k, n) different slots of the row in order of position and
     nothing is written beside them."""
-    k = 333
     cache = GpuCache(gpu, 2, 700, 320, 64, 2, 1, 64)
     fill(cache, lens, 3)
     odd = torch.tensor([0x7fffffff, -1, 0x7fc00000, -0x400000, 0x7f800001, 0x7f800000, -0x800000], dtype=torch.int32).view(torch.float32)

@@ -394,15 +394,16 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
 
 // ------------------------------------------------------------------ the kept set of a long row, by slices
 // Rows of more than SELECT_SHORT keys are cut into slices of SLICE keys.  The first launch takes from a sample of the whole row two
-// keys that the kk-th best very likely lies between (3.5 standard deviations of its rank in the sample to either side); it counts a
+// keys that the kk-th best very likely lies between (3.5 standard deviations of its rank in the sample to either side, or as much as
+// the lists hold; of 4096 keys instead of 2048, 5 us more, if that is less than 3.5 of 2048); it counts a
 // slice's keys that are better and lists those between, with their positions.  The second ranks the listed keys of all slices, a few
 // per cent of the row, for the exact threshold (by key and position: no ties are left), and writes a slice's kept slots behind those
 // of the slices before it.  Where the threshold lies outside after all, or a list is too short for its keys (ties, above all), or
 // the row has more than SLICES_MAX slices, one workgroup selects alone.
 // A row's slices go round its `parts` workgroups.  How many rows are long the host does not know, so there are only as many parts
 // as keep the chip busy: workgroups that find nothing to do cost 1 ns each.
-// Both launches are chains of loads and barriers again: 32 lists of 65536 keys 11.9 and 10.4 us (8.4 MB each: 0.8 TB/s), against 105 us by
-// one workgroup to a list; with the attention, 256 such lists 115 us.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
+// Both launches are chains of loads and barriers again: 32 lists of 65536 keys 11.9 and 10.4 us (8.4 MB each: 0.8 TB/s); whole
+// calls, with one workgroup to a list, 105 us, so 28.7, 256 such lists 115.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
 constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS, SLICES_MAX = 64;
 constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together, an equal share for each slice

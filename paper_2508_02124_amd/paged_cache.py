@@ -76,9 +76,7 @@ class PagedCache:
         """k, v [n, num_kv_heads, head_dim] into their slots [n], with the scores of W [num_heads, head_dim] and A [num_heads], or
         with z [num_heads, n]."""
         s, n = self.shape, slots.numel()
-        self._check("slots", slots, (n,), torch.int32)
-        for name, x in (("k", k), ("v", v)):
-            self._check(name, x, (n, s.H_kv, s.d), self.dtype, whole=False)
+        self._check_values(slots, k, v)
         if (W is None) == (z is None) or (W is None) != (A is None):
             raise ValueError("the scores come from W and A, or are given as z")
         if z is None:
@@ -144,6 +142,12 @@ class PagedCache:
             raise ValueError(f"expected {name} {list(shape)}, got {list(x.shape)}")
         if whole and not x.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
+
+    def _check_values(self, slots, k, v):
+        s, n = self.shape, slots.numel()
+        self._check("slots", slots, (n,), torch.int32)
+        for name, x in (("k", k), ("v", v)):
+            self._check(name, x, (n, s.H_kv, s.d), self.dtype, whole=False)
 
     @staticmethod
     def _aligned(x):

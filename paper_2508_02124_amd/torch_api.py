@@ -170,10 +170,13 @@ class DynamicMaskAttention(torch.nn.Module):
             if W.shape[1] == self.head_dim:
                 cache.append(rows.slots, k, v, W=W, A=A)
             else:                                    # the cross-head scores have an entry point of their own
-                n = v.shape[0]
-                z = torch.empty((self.num_heads, n), dtype=torch.float32, device=v.device)
+                s, n = cache.shape, rows.slots.numel()
+                cache._check_values(rows.slots, k, v)         # (all that append checks: a kernel reads v, W and A before it)
+                cache._check("W", W, (s.H_q, s.H_kv * s.d), torch.float32)
+                cache._check("A", A, (s.H_q,), torch.float32)
+                z = torch.empty((s.H_q, n), dtype=torch.float32, device=v.device)
                 if n:
-                    shape = B.make_shape(n, 1, self.num_heads, self.num_kv_heads, self.head_dim, 1, dtype=_dtype_code(v))
-                    cache._call_with(shape, B.dma_scores_xhead, v.contiguous(), W, A, z)
+                    shape = B.make_shape(n, 1, s.H_q, s.H_kv, s.d, 1, dtype=_dtype_code(v))
+                    cache._call_with(shape, B.dma_scores_xhead, cache._rows(v).contiguous(), cache._aligned(W), A, z)
                 cache.append(rows.slots, k, v, z=z)
             return cache.decode(q, self.keep_window, rows, self.softmax_scale, max_len)[0]

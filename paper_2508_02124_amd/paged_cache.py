@@ -101,14 +101,8 @@ class PagedCache:
         """Attention of q [n, num_heads, head_dim] over the cache: o, lse [num_heads, n] and the kept slots
         [n, num_heads, min(keep_window, longest request)].  rows: the step's (CacheRows), or (row_req, row_len); None: row r
         is request r with all its tokens.  max_len: the most keys that a row sees, where the host knows it (a matter of speed)."""
-        s, n = self.shape, q.shape[0]
-        if max_len:
-            s = B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype, max_len)
-        self._check("q", q, (n, s.H_q, s.d), self.dtype, whole=False)
-        row_req, row_len = (None, self.seq_lens) if rows is None else (rows.row_req, rows.row_len) if isinstance(rows, CacheRows) else rows
-        if rows is not None:
-            self._check("row_req", row_req, (n,), torch.int32)
-            self._check("row_len", row_len, (n,), torch.int32)
+        s, n = self._with_bound(max_len), q.shape[0]
+        row_req, row_len = self._check_queries(q, rows)
         q = self._rows(q)
         o = torch.empty((n, s.H_q, s.d), dtype=self.dtype, device=self.device)
         lse = torch.empty((s.H_q, n), dtype=torch.float32, device=self.device)
@@ -148,6 +142,29 @@ class PagedCache:
         self._check("slots", slots, (n,), torch.int32)
         for name, x in (("k", k), ("v", v)):
             self._check(name, x, (n, s.H_kv, s.d), self.dtype, whole=False)
+
+    def _check_queries(self, q, rows):
+        """row_req and row_len of the rows (see decode)."""
+        n = q.shape[0]
+        self._check("q", q, (n, self.shape.H_q, self.shape.d), self.dtype, whole=False)
+        if rows is None:
+            return None, self.seq_lens
+        row_req, row_len = (rows.row_req, rows.row_len) if isinstance(rows, CacheRows) else rows
+        self._check("row_req", row_req, (n,), torch.int32)
+        self._check("row_len", row_len, (n,), torch.int32)
+        return row_req, row_len
+
+    def _check_decode(self, q, keep_window, rows, softmax_scale=0.0, max_len=0):
+        """Raises what decode would, for a caller that has something to do before it; nothing is allocated or enqueued."""
+        s, n = self._with_bound(max_len), q.shape[0]
+        self._check_queries(q, rows)
+        B.dma_cache_decode(s, 0, keep_window, softmax_scale, None, s.H_q * s.d, *[None] * 8, 0, stream=0)   # (no rows: its other arguments)
+        if (n + 8) * s.H_q * -(-min(int(keep_window), s.max_pages * s.page_size) // 256) >= 1 << 22:
+            raise B.DmaError(B.DMA_EUNSUPPORTED, "dma_cache_decode")
+
+    def _with_bound(self, max_len):
+        s = self.shape
+        return B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype, max_len) if max_len else s
 
     @staticmethod
     def _aligned(x):

@@ -164,9 +164,10 @@ class DynamicMaskAttention(torch.nn.Module):
     def step(self, q, k, v, cache, rows, max_len=0):
         """A decoding step over a paged cache (paged_cache.PagedCache): k, v [n, H_kv, d] of the step's new rows go to their places
         with this module's scores, then q [n, H_q, d] attends from them.  rows: what cache.assign returned; max_len: as for
-        cache.decode.  Without gradients; o [n, H_q, d]."""
+        cache.decode.  Without gradients; o [n, H_q, d].  What cannot be done is refused before the cache is changed."""
         with torch.no_grad():
             W, A = self.W.detach(), self.A.detach()
+            cache._check_decode(q, self.keep_window, rows, self.softmax_scale, max_len)   # (before the rows go in)
             if W.shape[1] == self.head_dim:
                 cache.append(rows.slots, k, v, W=W, A=A)
             else:                                    # the cross-head scores have an entry point of their own

@@ -82,3 +82,35 @@ def test_values_of_the_cross_head_scores(form):
     _, shape, (V, W, A, z) = cache.calls[0]
     assert (shape.T, shape.H_q, shape.H_kv, shape.d) == (n, H_Q, H_KV, D)
     assert V.is_contiguous() and V.data_ptr() % 16 == 0 and torch.equal(V, v) and z.shape == (H_Q, n)
+
+
+@pytest.mark.parametrize("cross_head", [False, True])
+def test_what_decode_refuses_is_refused_before_the_rows_go_in(cross_head):
+    """A step whose attention cannot run leaves the cache as it was."""
+    good = dict(q=values(H_Q), k=values(H_KV), v=values(H_KV), rows=rows())
+    ints = lambda *shape: torch.zeros(shape, dtype=torch.int32)
+    bad = [(ValueError, dict(q=values(H_Q - 1))), (ValueError, dict(q=values(H_Q, n=N + 1))), (TypeError, dict(q=values(H_Q, dtype=torch.float32))),
+           (RuntimeError, dict(q=values(H_Q, device="meta"))), (ValueError, dict(rows=rows()._replace(row_len=ints(N + 1)))),
+           (TypeError, dict(rows=rows()._replace(row_req=ints(N).long()))), (B.DmaError, dict(max_len=-1))]
+    for error, more in bad:
+        cache = Recorded()
+        with pytest.raises(error):
+            module(cross_head).step(**{**good, **more}, cache=cache)
+        assert cache.calls == [], more
+    for more in (dict(keep_window=0), dict(softmax_scale=-1.0), dict(softmax_scale=float("nan"))):
+        cache = Recorded()
+        with pytest.raises(B.DmaError) as e:
+            module(cross_head, **more).step(**good, cache=cache)
+        assert cache.calls == [] and e.value.status == B.DMA_EINVAL
+
+
+def test_rows_and_window_of_a_step():
+    """The limit of dma_cache_decode, (n_rows + 8) * H_q * ceil(window / 256) < 2^22, at both its sides."""
+    cache, window, n = Recorded(), 1 << 21, 120
+    cache.shape = B.make_cache_shape(2, 8, 1 << 18, 16, H_Q, H_KV, D)
+    assert (n + 8) * H_Q * (window // 256) == 1 << 22
+    assert B.dma_cache_decode_bytes(cache.shape, n, window) == 0 < B.dma_cache_decode_bytes(cache.shape, n - 1, window)
+    with pytest.raises(B.DmaError) as e:
+        module(False, keep_window=window).step(values(H_Q, n=n), values(H_KV, n=n), values(H_KV, n=n), cache, rows(n))
+    assert cache.calls == [] and e.value.status == B.DMA_EUNSUPPORTED
+    cache._check_decode(values(H_Q, n=n - 1), window, rows(n - 1))

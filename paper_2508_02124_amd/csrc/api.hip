@@ -383,7 +383,8 @@ int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, fl
   if (n_rows == 0) return DMA_OK;
   if (!q || !pages || !block_table || !row_len || !o || !lse || !kept) return DMA_EINVAL;
   if (!aligned16(q) || !aligned16(pages) || !aligned16(o) || !aligned16(kept) || !aligned16(ws)) return DMA_EINVAL;
-  if (!ws || ws_bytes < cache_decode_bytes(*shape, n_rows, k)) return DMA_EWORKSPACE;
+  const size_t need = cache_decode_bytes(*shape, n_rows, k);
+  if (ws_bytes < need || (need && !ws)) return DMA_EWORKSPACE;  // (no bytes: no address)
   const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->d);
   return launch_cache_decode(*shape, n_rows, k, scale, q, q_stride, pages, block_table, row_req, row_len, o, lse, kept, ws,
                              (hipStream_t)stream);

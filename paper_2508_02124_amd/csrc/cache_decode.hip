@@ -403,16 +403,19 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
 // A row's slices go round its `parts` workgroups.  How many rows are long the host does not know, so there are only as many parts
 // as keep the chip busy: workgroups that find nothing to do cost 1 ns each.
 // Both launches are chains of loads and barriers again: 32 lists of 65536 keys 11.9 and 10.4 us (8.4 MB each: 0.8 TB/s); whole
-// calls, with one workgroup to a list, 105 us, so 28.7, 256 such lists 115.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
+// calls, with one workgroup to a list, 105 us, so 28.7, 256 such lists 112.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
 constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS, SLICES_MAX = 64;
-constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together, an equal share for each slice
+constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together at most, an equal share for each slice
+static_assert(SLICE <= 1 << 16, "");         // (places of 16 bits)
 
 struct SliceWork {
-  uint2* counts;  // [pairs][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
-  uint2* listed;  // [pairs][LISTED]: key, position
+  uint2* counts;  // [pairs of a launch][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
+  uint32_t* keys;    // [pairs][listed]: listed keys
+  uint16_t* places;  // [pairs][listed]: their places in the slice
   uint4* bounds;  // [pairs]: first and last key of the lists; the same, or those of the sample where the lists have no end
-  int parts;
+  int listed, parts;
+  int first, pairs;  // the pairs (row * H_q + head) of this launch
 };
 
 // The keys of a slice, its chunks in turn to the waves (NO_KEY behind the row's end), once slice_pages has asked for its pages.
@@ -442,10 +445,10 @@ __device__ __forceinline__ float bracket(float share, float size) { return 3.5f 
 
 // Counts and lists of one workgroup's slices of a long row.
 template <int S>
-__device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& row, int h, int kk, int rh, int part, const SliceWork& sw,
+__device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& row, int h, int kk, int pair, int part, const SliceWork& sw,
                                             SelectShared<512>& m) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
-  const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
+  const int slices = (n - 1) / SLICE + 1, share = sw.listed / slices;
   const KeyBins bins(false);
   if (slices > SLICES_MAX || part >= slices) return;
   PageRun<S> run;
@@ -516,7 +519,7 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
   if (middle + off < size) hi = min(key_of_rank((uint32_t)(middle + off) + 1u, 1u), hi);
   lo = (uint32_t)__builtin_amdgcn_readfirstlane((int)lo);
   hi = (uint32_t)__builtin_amdgcn_readfirstlane((int)hi);
-  if (tid == 0 && part == 0) sw.bounds[rh] = make_uint4(lo, hi, lo ? lo : kmin, hi == NO_KEY - 1 ? kmax : hi);
+  if (tid == 0 && part == 0) sw.bounds[pair] = make_uint4(lo, hi, lo ? lo : kmin, hi == NO_KEY - 1 ? kmax : hi);
   for (int slice = part; slice < slices; slice += sw.parts) {
     if (slice != part) {
       slice_pages<S>(c, row, slice, run);
@@ -541,16 +544,19 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
       all_better += m.wsum[i][0];
       all += m.wsum[i][1];
     }
-    uint2* listed = sw.listed + (size_t)rh * LISTED + slice * share;
+    const size_t first = (size_t)pair * sw.listed + slice * share;
 #pragma unroll
     for (int u = 0; u < SLICE_CHUNKS; u++) {
       const bool in = key[u] - lo <= hi - lo;
       const unsigned long long b = __ballot(in);
       const uint32_t i = at + lanes_before(b);
-      if (in && i < (uint32_t)share) listed[i] = make_uint2(key[u], (uint32_t)(slice * SLICE + (u * 8 + w) * 64 + l));
+      if (in && i < (uint32_t)share) {
+        sw.keys[first + i] = key[u];
+        sw.places[first + i] = (uint16_t)((u * 8 + w) * 64 + l);
+      }
       at += (uint32_t)__popcll(b);
     }
-    if (tid == 0) sw.counts[(size_t)rh * SLICES_MAX + slice] = make_uint2(all_better, all);
+    if (tid == 0) sw.counts[(size_t)pair * SLICES_MAX + slice] = make_uint2(all_better, all);
   }
 }
 
@@ -561,7 +567,8 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 // 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1; SLICED, 2048 parts of 8192: 115.3 / 115.2).
 template <int S, bool SLICED, int WAVES>
 __global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int pairs = p.n_rows * c.H_q, part = SLICED ? blockIdx.x / pairs : 0, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int part = SLICED ? blockIdx.x / sw.pairs : 0, pair = blockIdx.x - part * sw.pairs, rh = (SLICED ? sw.first : 0) + pair;
+  const int r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);
   const int n = row.n, kk = min(p.k, n), parts = SLICED && n > SELECT_SHORT ? sw.parts : 1;
@@ -576,16 +583,16 @@ __global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, Ca
   }
   __shared__ SelectShared<512> m;
   if (n <= SELECT_SHORT) select_row<512, SELECT_REGS, S, false>(c, row, h, kk, list, m);
-  else if constexpr (SLICED) list_slices<S>(c, row, h, kk, rh, part, sw, m);
+  else if constexpr (SLICED) list_slices<S>(c, row, h, kk, pair, part, sw, m);
   else select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
 }
 
 template <int S>
 __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int pairs = p.n_rows * c.H_q, part = blockIdx.x / pairs, rh = blockIdx.x - part * pairs, r = rh / c.H_q, h = rh - r * c.H_q;
+  const int part = blockIdx.x / sw.pairs, pair = blockIdx.x - part * sw.pairs, rh = sw.first + pair, r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
-  uint2 cnt = sw.counts[(size_t)rh * SLICES_MAX + l];  // lane s: of slice s
-  const uint4 bounds = sw.bounds[rh];
+  uint2 cnt = sw.counts[(size_t)pair * SLICES_MAX + l];  // lane s: of slice s
+  const uint4 bounds = sw.bounds[pair];
   const CacheRow row = cache_row(c, p, r);
   PageRun<S> run;
   slice_pages<S>(c, row, part, run);
@@ -594,7 +601,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   int32_t* list = kept + (size_t)rh * p.kcap;
   __shared__ SelectShared<512> m;
   __shared__ __align__(16) uint32_t cand[LISTED];
-  const int slices = (n - 1) / SLICE + 1, share = LISTED / slices;
+  const int slices = (n - 1) / SLICE + 1, share = sw.listed / slices;
   const KeyBins bins(false);
   const auto add = [](uint32_t x, uint32_t y) { return x + y; };
   if (l >= slices) cnt = make_uint2(0, 0);
@@ -609,7 +616,8 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       f(end - have, have, s);
     }
   };
-  const uint2* listed = sw.listed + (size_t)rh * LISTED;
+  const uint32_t* keys = sw.keys + (size_t)pair * sw.listed;
+  const uint16_t* places = sw.places + (size_t)pair * sw.listed;
   uint32_t* near_all = &m.st[3];
   uint32_t key[SLICE_CHUNKS], base = 0, rank = 0, n_near = NO_KEY, digit = 0;
   int sh = 0;
@@ -626,7 +634,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       for (uint32_t i0 = 0; i0 < have; i0 += 256) {
         uint32_t k[4];
 #pragma unroll
-        for (int e = 0; e < 4; e++) k[e] = listed[s * share + min(i0 + e * 64 + l, have - 1)].x;
+        for (int e = 0; e < 4; e++) k[e] = keys[s * share + min(i0 + e * 64 + l, have - 1)];
 #pragma unroll
         for (int e = 0; e < 4; e++)
           if (i0 + e * 64 + l < have) cand[to + i0 + e * 64 + l] = k[e];
@@ -656,7 +664,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       if (there && bin(k) == digit) {
         const uint32_t e = atomicAdd(near_all, 1u);
         m.near[e] = k;
-        m.near_pos[e] = listed[s * share + i0 + l].y;
+        m.near_pos[e] = (uint32_t)(s * SLICE) + places[s * share + i0 + l];
       }
     }
     if (l == 0) m.equal[s] = ahead;
@@ -1012,10 +1020,18 @@ static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
 
 // The workspace: partial outputs, then, where rows can be long, what the parts of a row tell each other.
 struct DecodeWork {
-  size_t off_counts, off_listed, off_bounds, total;
+  size_t off_counts, off_keys, off_places, off_bounds, total;
   int parts;  // of a long row; 0: no row is long
+  int listed; // keys of a row's lists
+  int pairs;  // (row, head) pairs of a launch
 };
 constexpr int SELECT_WGS = 8 * CUS;  // workgroups that the parts are chosen for
+// The lists of a pair take 48 KiB, and half as much from more than LISTED_PAIRS pairs on; there is room for twice as many of those, and
+// more go through the same room in several launches: 197 MiB at most (8 bytes a key and room for every pair: 0.5 GiB for 256 rows of 32
+// heads, 2 for 1024).  Whole calls of 32 heads, us, room for all / this: 160 rows of 60000 to 130000 keys 1868 / 1995 (short lists
+// take the larger sample), 256 of 14000 to 30000 1143 / 1145, 1024 of 500 to 3000 979 / 991, 256 of which every eighth has 60000
+// keys and the others 3000 608 / 613 (launches of 2048 pairs with whole lists: 799).
+constexpr int LISTED_PAIRS = 4096;
 static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
   const size_t pairs = (size_t)n_rows * s.H_q;
@@ -1023,11 +1039,15 @@ static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   size_t o = nsplit > 1 ? align_up(pairs * nsplit * (s.d + 2) * 4, 256) : 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
   const long cap = (long)s.max_pages * s.page_size, longest = s.max_len > 0 && s.max_len < cap ? s.max_len : cap;
-  const long slices = longest <= SELECT_SHORT || kcap == cap ? 0 : (longest + SLICE - 1) / SLICE, most = SELECT_WGS / (long)pairs;
+  const size_t launches = (pairs + 2 * LISTED_PAIRS - 1) / (2 * LISTED_PAIRS);
+  wk.pairs = (int)((pairs + launches - 1) / launches);
+  const long slices = longest <= SELECT_SHORT || kcap == cap ? 0 : (longest + SLICE - 1) / SLICE, most = SELECT_WGS / (long)wk.pairs;
   wk.parts = (int)(slices < most ? slices : most < 1 && slices ? 1 : most);
-  wk.off_counts = take(wk.parts ? pairs * SLICES_MAX * 8 : 0);
-  wk.off_listed = take(wk.parts ? pairs * LISTED * 8 : 0);
-  wk.off_bounds = take(wk.parts ? pairs * 16 : 0);
+  wk.off_counts = take(wk.parts ? (size_t)wk.pairs * SLICES_MAX * 8 : 0);
+  wk.listed = pairs > LISTED_PAIRS ? LISTED / 2 : LISTED;
+  wk.off_keys = take(wk.parts ? (size_t)wk.pairs * wk.listed * 4 : 0);
+  wk.off_places = take(wk.parts ? (size_t)wk.pairs * wk.listed * 2 : 0);
+  wk.off_bounds = take(wk.parts ? (size_t)wk.pairs * 16 : 0);
   wk.total = o;
   return wk;
 }
@@ -1060,12 +1080,16 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   if (!all) {
     const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
-    const SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint4*)(base + wk.off_bounds), wk.parts};
+    SliceWork sw = {(uint2*)(base + wk.off_counts), (uint32_t*)(base + wk.off_keys), (uint16_t*)(base + wk.off_places),
+                    (uint4*)(base + wk.off_bounds), wk.listed, wk.parts, 0, wk.pairs};
     auto select = [&](auto width) {
       constexpr int S = decltype(width)::value;
       if (wk.parts) {
-        cache_select_kernel<S, true, 6><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
-        cache_slice_kernel<S><<<pairs * wk.parts, 512, 0, st>>>(c, p, sw, kept);
+        for (; sw.first < (int)pairs; sw.first += wk.pairs) {
+          sw.pairs = (int)pairs - sw.first < wk.pairs ? (int)pairs - sw.first : wk.pairs;
+          cache_select_kernel<S, true, 6><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
+          cache_slice_kernel<S><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
+        }
       } else if (pairs > 3 * CUS) {
         cache_select_kernel<S, false, 8><<<pairs, 512, 0, st>>>(c, p, sw, kept);
       } else {

@@ -354,7 +354,8 @@ int dma_cache_reset(const dma_cache_shape* shape, int32_t* seq_lens, int32_t* bl
  *   change     in      [n_reqs]
  *   seq_lens, block_table, free_list   in and out
  *   cu_rows    out     [n_reqs + 1]: the new tokens of request b are the rows cu_rows[b] .. cu_rows[b + 1]
- *   row_req, row_len, slots   out   [n_rows], fully written: -1, 0, -1 for rows behind the last and of requests not served.
+ *   row_req, row_len, slots   out   [n_rows], fully written: -1, 0, -1 for rows behind the last, of requests not served and, should the
+ *                      lists be damaged, of tokens whose page is out of range.
  *                      A row sees the keys up to and with its own token: row_len = its position + 1
  *   status     out     [n_reqs]: 0 served, or why not.  A request that is not served keeps its length and pages; its rows keep
  *                      their places among the rows.  Pages are promised in order of the requests: once one does not find enough,

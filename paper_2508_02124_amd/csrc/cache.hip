@@ -189,9 +189,11 @@ __global__ __launch_bounds__(NT) void cache_assign_kernel(AssignArgs p) {
       if (n >= 0) {
         const int pos = n + (r - first[b]), place = pos >> p.shift, more = place - pages(n);
         const int page = more >= 0 ? stack[(int)have - 1 - (taken[b] + more)] : p.table[(size_t)b * p.max_pages + place];
-        req = b;
-        len = pos + 1;
-        slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+        if ((uint32_t)page < (uint32_t)p.n_pages) {  // (else the lists are damaged, and the row is not there)
+          req = b;
+          len = pos + 1;
+          slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+        }
       }
     }
     p.row_req[r] = req;
@@ -214,9 +216,11 @@ __global__ __launch_bounds__(256) void cache_rows_kernel(AssignArgs p) {
     const int state = p.status[b], pos = p.lens[b] - (first[b + 1] - first[b]) + (r - first[b]);  // (the length has the new tokens)
     if (state == DMA_CACHE_SERVED) {
       const int page = p.table[(size_t)b * p.max_pages + (pos >> p.shift)];
-      req = b;
-      len = pos + 1;
-      slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+      if ((uint32_t)page < (uint32_t)p.n_pages) {
+        req = b;
+        len = pos + 1;
+        slot = (page << p.shift) | (pos & ((1 << p.shift) - 1));
+      }
     }
   }
   p.row_req[r] = req;

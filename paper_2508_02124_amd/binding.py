@@ -277,9 +277,16 @@ def dma_bwd_scores(shape, Q, K, V, O, dO, LSE, z, expiry, mask, cu_seqlens, W, A
 CACHE_SERVED, CACHE_NO_PAGES, CACHE_TOO_LONG, CACHE_NO_ROWS = 0, 1, 2, 3
 
 
+def _i32(x):
+    """x as an int that an int32 holds (ctypes would keep the lowest bits of any other)."""
+    x = int(x)
+    if not -(1 << 31) <= x < 1 << 31:
+        raise OverflowError(f"{x} does not fit 32 bits")
+    return x
+
+
 def make_cache_shape(n_reqs, n_pages, max_pages, page_size, H_q, H_kv, d, dtype=DMA_BF16, max_len=0):
-    return DmaCacheShape(int(n_reqs), int(n_pages), int(max_pages), int(page_size), int(H_q), int(H_kv), int(d), int(dtype),
-                         int(max_len))
+    return DmaCacheShape(*(_i32(x) for x in (n_reqs, n_pages, max_pages, page_size, H_q, H_kv, d, dtype, max_len)))
 
 
 def dma_cache_bytes(shape):
@@ -291,7 +298,7 @@ def dma_cache_free_bytes(shape):
 
 
 def dma_cache_decode_bytes(shape, n_rows, k):
-    return int(lib().dma_cache_decode_bytes(ctypes.byref(shape), int(n_rows), int(k)))
+    return int(lib().dma_cache_decode_bytes(ctypes.byref(shape), _i32(n_rows), _i32(k)))
 
 
 def dma_cache_describe(shape):
@@ -308,24 +315,24 @@ def dma_cache_reset(shape, seq_lens, block_table, free_list, stream=None):
 
 def dma_cache_assign(shape, n_rows, change, seq_lens, block_table, free_list, cu_rows, row_req, row_len, slots, status,
                      stream=None):
-    _check(lib().dma_cache_assign(ctypes.byref(shape), int(n_rows), _ptr(change), _ptr(seq_lens), _ptr(block_table),
+    _check(lib().dma_cache_assign(ctypes.byref(shape), _i32(n_rows), _ptr(change), _ptr(seq_lens), _ptr(block_table),
                                   _ptr(free_list), _ptr(cu_rows), _ptr(row_req), _ptr(row_len), _ptr(slots),
                                   _ptr(status), _stream(stream)), "dma_cache_assign")
 
 
 def dma_cache_append(shape, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, stream=None):
-    _check(lib().dma_cache_append(ctypes.byref(shape), int(n_rows), _ptr(K), int(k_stride), _ptr(V), int(v_stride),
+    _check(lib().dma_cache_append(ctypes.byref(shape), _i32(n_rows), _ptr(K), int(k_stride), _ptr(V), int(v_stride),
                                   _ptr(W), _ptr(A), _ptr(z), _ptr(slots), _ptr(pages), _stream(stream)),
            "dma_cache_append")
 
 
 def dma_cache_read(shape, n_rows, slots, pages, K, V, z, stream=None):
-    _check(lib().dma_cache_read(ctypes.byref(shape), int(n_rows), _ptr(slots), _ptr(pages), _ptr(K), _ptr(V), _ptr(z),
+    _check(lib().dma_cache_read(ctypes.byref(shape), _i32(n_rows), _ptr(slots), _ptr(pages), _ptr(K), _ptr(V), _ptr(z),
                                 _stream(stream)), "dma_cache_read")
 
 
 def dma_cache_decode(shape, n_rows, k, softmax_scale, q, q_stride, pages, block_table, row_req, row_len, o, lse, kept, ws,
                      ws_bytes, stream=None):
-    _check(lib().dma_cache_decode(ctypes.byref(shape), int(n_rows), int(k), float(softmax_scale), _ptr(q), int(q_stride),
+    _check(lib().dma_cache_decode(ctypes.byref(shape), _i32(n_rows), _i32(k), float(softmax_scale), _ptr(q), int(q_stride),
                                   _ptr(pages), _ptr(block_table), _ptr(row_req), _ptr(row_len), _ptr(o), _ptr(lse),
                                   _ptr(kept), _ptr(ws), int(ws_bytes), _stream(stream)), "dma_cache_decode")

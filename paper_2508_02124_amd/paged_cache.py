@@ -101,15 +101,15 @@ class PagedCache:
         """Attention of q [n, num_heads, head_dim] over the cache: o, lse [num_heads, n] and the kept slots
         [n, num_heads, min(keep_window, longest request)].  rows: the step's (CacheRows), or (row_req, row_len); None: row r
         is request r with all its tokens.  max_len: the most keys that a row sees, where the host knows it (a matter of speed)."""
-        s, n = self._with_bound(max_len), q.shape[0]
+        s, n, window = self._with_bound(max_len), q.shape[0], self._window(keep_window)
         row_req, row_len = self._check_queries(q, rows)
         q = self._rows(q)
         o = torch.empty((n, s.H_q, s.d), dtype=self.dtype, device=self.device)
         lse = torch.empty((s.H_q, n), dtype=torch.float32, device=self.device)
-        kept = self._ints(n, s.H_q, min(int(keep_window), s.max_pages * s.page_size))
-        size = B.dma_cache_decode_bytes(s, n, keep_window)
+        kept = self._ints(n, s.H_q, window)
+        size = B.dma_cache_decode_bytes(s, n, window)
         ws = torch.empty(size + 16, dtype=torch.uint8, device=self.device)   # (never empty: its address is passed)
-        self._call_with(s, B.dma_cache_decode, n, keep_window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
+        self._call_with(s, B.dma_cache_decode, n, window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
                    row_len, o, lse, kept, ws, size)
         return o, lse, kept
 
@@ -156,15 +156,22 @@ class PagedCache:
 
     def _check_decode(self, q, keep_window, rows, softmax_scale=0.0, max_len=0):
         """Raises what decode would, for a caller that has something to do before it; nothing is allocated or enqueued."""
-        s, n = self._with_bound(max_len), q.shape[0]
+        s, n, window = self._with_bound(max_len), q.shape[0], self._window(keep_window)
         self._check_queries(q, rows)
-        B.dma_cache_decode(s, 0, keep_window, softmax_scale, None, s.H_q * s.d, *[None] * 8, 0, stream=0)   # (no rows: its other arguments)
-        if (n + 8) * s.H_q * -(-min(int(keep_window), s.max_pages * s.page_size) // 256) >= 1 << 22:
+        B.dma_cache_decode(s, 0, window, softmax_scale, None, s.H_q * s.d, *[None] * 8, 0, stream=0)   # (no rows: its other arguments)
+        if (n + 8) * s.H_q * -(-window // 256) >= 1 << 22:
             raise B.DmaError(B.DMA_EUNSUPPORTED, "dma_cache_decode")
+
+    # (a window or a bound beyond the longest request, of whatever size, is one of just that)
+    def _window(self, keep_window):
+        return min(int(keep_window), self.shape.max_pages * self.shape.page_size)
 
     def _with_bound(self, max_len):
         s = self.shape
-        return B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype, max_len) if max_len else s
+        if not max_len:
+            return s
+        return B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype,
+                                  min(int(max_len), s.max_pages * s.page_size))
 
     @staticmethod
     def _aligned(x):

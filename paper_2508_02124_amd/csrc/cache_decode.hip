@@ -403,18 +403,16 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
 // A row's slices go round its `parts` workgroups.  How many rows are long the host does not know, so there are only as many parts
 // as keep the chip busy: workgroups that find nothing to do cost 1 ns each.
 // Both launches are chains of loads and barriers again: 32 lists of 65536 keys 11.9 and 10.4 us (8.4 MB each: 0.8 TB/s); whole
-// calls, with one workgroup to a list, 105 us, so 28.7, 256 such lists 112.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
+// calls, with one workgroup to a list, 105 us, so 28.6, 256 such lists 116.  One workgroup alone takes 0.2 ms for 131072 keys, 0.7 for 524288.
 constexpr int SELECT_REGS = 24, SELECT_SHORT = 512 * SELECT_REGS;
 constexpr int SLICE_CHUNKS = 16, SLICE = 512 * SLICE_CHUNKS, SLICES_MAX = 64;
 constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hold together at most, an equal share for each slice
-static_assert(SLICE <= 1 << 16, "");         // (places of 16 bits)
 
 struct SliceWork {
   uint2* counts;  // [pairs of a launch][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
-  uint32_t* keys;    // [pairs][listed]: listed keys
-  uint16_t* places;  // [pairs][listed]: their places in the slice
+  uint2* listed;  // [pairs of a launch][room]: key, position
   uint4* bounds;  // [pairs]: first and last key of the lists; the same, or those of the sample where the lists have no end
-  int listed, parts;
+  int room, parts;
   int first, pairs;  // the pairs (row * H_q + head) of this launch
 };
 
@@ -448,7 +446,7 @@ template <int S>
 __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& row, int h, int kk, int pair, int part, const SliceWork& sw,
                                             SelectShared<512>& m) {
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = row.n;
-  const int slices = (n - 1) / SLICE + 1, share = sw.listed / slices;
+  const int slices = (n - 1) / SLICE + 1, share = sw.room / slices;
   const KeyBins bins(false);
   if (slices > SLICES_MAX || part >= slices) return;
   PageRun<S> run;
@@ -544,16 +542,13 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
       all_better += m.wsum[i][0];
       all += m.wsum[i][1];
     }
-    const size_t first = (size_t)pair * sw.listed + slice * share;
+    uint2* listed = sw.listed + (size_t)pair * sw.room + slice * share;
 #pragma unroll
     for (int u = 0; u < SLICE_CHUNKS; u++) {
       const bool in = key[u] - lo <= hi - lo;
       const unsigned long long b = __ballot(in);
       const uint32_t i = at + lanes_before(b);
-      if (in && i < (uint32_t)share) {
-        sw.keys[first + i] = key[u];
-        sw.places[first + i] = (uint16_t)((u * 8 + w) * 64 + l);
-      }
+      if (in && i < (uint32_t)share) listed[i] = make_uint2(key[u], (uint32_t)(slice * SLICE + (u * 8 + w) * 64 + l));
       at += (uint32_t)__popcll(b);
     }
     if (tid == 0) sw.counts[(size_t)pair * SLICES_MAX + slice] = make_uint2(all_better, all);
@@ -601,7 +596,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   int32_t* list = kept + (size_t)rh * p.kcap;
   __shared__ SelectShared<512> m;
   __shared__ __align__(16) uint32_t cand[LISTED];
-  const int slices = (n - 1) / SLICE + 1, share = sw.listed / slices;
+  const int slices = (n - 1) / SLICE + 1, share = sw.room / slices;
   const KeyBins bins(false);
   const auto add = [](uint32_t x, uint32_t y) { return x + y; };
   if (l >= slices) cnt = make_uint2(0, 0);
@@ -616,8 +611,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       f(end - have, have, s);
     }
   };
-  const uint32_t* keys = sw.keys + (size_t)pair * sw.listed;
-  const uint16_t* places = sw.places + (size_t)pair * sw.listed;
+  const uint2* listed = sw.listed + (size_t)pair * sw.room;
   uint32_t* near_all = &m.st[3];
   uint32_t key[SLICE_CHUNKS], base = 0, rank = 0, n_near = NO_KEY, digit = 0;
   int sh = 0;
@@ -634,7 +628,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       for (uint32_t i0 = 0; i0 < have; i0 += 256) {
         uint32_t k[4];
 #pragma unroll
-        for (int e = 0; e < 4; e++) k[e] = keys[s * share + min(i0 + e * 64 + l, have - 1)];
+        for (int e = 0; e < 4; e++) k[e] = listed[s * share + min(i0 + e * 64 + l, have - 1)].x;
 #pragma unroll
         for (int e = 0; e < 4; e++)
           if (i0 + e * 64 + l < have) cand[to + i0 + e * 64 + l] = k[e];
@@ -664,7 +658,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       if (there && bin(k) == digit) {
         const uint32_t e = atomicAdd(near_all, 1u);
         m.near[e] = k;
-        m.near_pos[e] = (uint32_t)(s * SLICE) + places[s * share + i0 + l];
+        m.near_pos[e] = listed[s * share + i0 + l].y;
       }
     }
     if (l == 0) m.equal[s] = ahead;
@@ -1020,17 +1014,19 @@ static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
 
 // The workspace: partial outputs, then, where rows can be long, what the parts of a row tell each other.
 struct DecodeWork {
-  size_t off_counts, off_keys, off_places, off_bounds, total;
+  size_t off_counts, off_listed, off_bounds, total;
   int parts;  // of a long row; 0: no row is long
-  int listed; // keys of a row's lists
+  int room;   // keys of a row's lists
   int pairs;  // (row, head) pairs of a launch
 };
 constexpr int SELECT_WGS = 8 * CUS;  // workgroups that the parts are chosen for
-// The lists of a pair take 48 KiB, and half as much from more than LISTED_PAIRS pairs on; there is room for twice as many of those, and
-// more go through the same room in several launches: 197 MiB at most (8 bytes a key and room for every pair: 0.5 GiB for 256 rows of 32
-// heads, 2 for 1024).  Whole calls of 32 heads, us, room for all / this: 160 rows of 60000 to 130000 keys 1868 / 1995 (short lists
-// take the larger sample), 256 of 14000 to 30000 1143 / 1145, 1024 of 500 to 3000 979 / 991, 256 of which every eighth has 60000
-// keys and the others 3000 608 / 613 (launches of 2048 pairs with whole lists: 799).
+
+// The lists of a pair take 64 KiB, and half as much from more than LISTED_PAIRS pairs on; there is room for twice as many of those, and
+// more go through the same room in several launches: 261 MiB at most (room for every pair: 0.5 GiB for 256 rows of 32 heads, 2 for
+// 1024).  Whole calls of 32 heads, us, room for every pair / this: 160 rows of 20000 to 60000 keys 1044 / 1043, of 60000 to 130000 1871 /
+// 1999 (half lists take the larger sample there), 256 of 14000 to 30000 1143 / 1145, 256 of which every eighth has 60000 keys and the others
+// 3000 608 / 609 (whole lists, launches of 4096 / 2048 pairs: 666 / 799), 1024 of 500 to 3000 983 / 995.  (6 bytes a key, its place in
+// the slice for its position: 196 MiB, but one row of 65536 keys 28.6 / 29.2.)
 constexpr int LISTED_PAIRS = 4096;
 static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
@@ -1044,9 +1040,8 @@ static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
   const long slices = longest <= SELECT_SHORT || kcap == cap ? 0 : (longest + SLICE - 1) / SLICE, most = SELECT_WGS / (long)wk.pairs;
   wk.parts = (int)(slices < most ? slices : most < 1 && slices ? 1 : most);
   wk.off_counts = take(wk.parts ? (size_t)wk.pairs * SLICES_MAX * 8 : 0);
-  wk.listed = pairs > LISTED_PAIRS ? LISTED / 2 : LISTED;
-  wk.off_keys = take(wk.parts ? (size_t)wk.pairs * wk.listed * 4 : 0);
-  wk.off_places = take(wk.parts ? (size_t)wk.pairs * wk.listed * 2 : 0);
+  wk.room = pairs > LISTED_PAIRS ? LISTED / 2 : LISTED;
+  wk.off_listed = take(wk.parts ? (size_t)wk.pairs * wk.room * 8 : 0);
   wk.off_bounds = take(wk.parts ? (size_t)wk.pairs * 16 : 0);
   wk.total = o;
   return wk;
@@ -1080,8 +1075,7 @@ int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale
   if (!all) {
     const DecodeWork wk = decode_work(s, n_rows, k);
     char* base = (char*)ws;
-    SliceWork sw = {(uint2*)(base + wk.off_counts), (uint32_t*)(base + wk.off_keys), (uint16_t*)(base + wk.off_places),
-                    (uint4*)(base + wk.off_bounds), wk.listed, wk.parts, 0, wk.pairs};
+    SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint4*)(base + wk.off_bounds), wk.room, wk.parts, 0, wk.pairs};
     auto select = [&](auto width) {
       constexpr int S = decltype(width)::value;
       if (wk.parts) {

@@ -405,7 +405,8 @@ int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* 
  *   kept     out [n_rows, H_q, min(k, max_pages * page_size)] int32: the slots of the kept keys in order of position, -1 behind
  *                them
  *   ws       dma_cache_decode_bytes(shape, n_rows, k) bytes of scratch (NULL if that is 0); calls that overlap need one each.  At most
- *                261 MiB; it grows with n_rows * H_q up to there where max_len allows rows of more than 12288 keys, else it is below 1 MiB
+ *                261 MiB, reached at 8192 heads of rows where max_len allows rows of more than 12288 keys, else below 1 MiB; more
+ *                rows never need less, so the scratch of the largest step serves all
  * DMA_EUNSUPPORTED where (n_rows + 8) * H_q * ceil(min(k, max_pages * page_size) / 256) reaches 2^22: a whole prompt goes through
  * dma_mask_gen and dma_fwd.
  */

@@ -411,7 +411,7 @@ constexpr int SAMPLE = 2048, LISTED = 8192;  // keys that the lists of a row hol
 struct SliceWork {
   uint2* counts;  // [pairs of a launch][SLICES_MAX]: better keys, listed keys (more than the share: not all are)
   uint2* listed;  // [pairs of a launch][room]: key, position
-  uint4* bounds;  // [pairs]: first and last key of the lists; the same, or those of the sample where the lists have no end
+  uint4* bounds;  // [pairs of a launch]: first and last key of the lists; the same, or those of the sample where the lists have no end
   int room, parts;
   int first, pairs;  // the pairs (row * H_q + head) of this launch
 };
@@ -1022,27 +1022,30 @@ struct DecodeWork {
 constexpr int SELECT_WGS = 8 * CUS;  // workgroups that the parts are chosen for
 
 // The lists of a pair take 64 KiB, and half as much from more than LISTED_PAIRS pairs on; there is room for twice as many of those, and
-// more go through the same room in several launches: 261 MiB at most (room for every pair: 0.5 GiB for 256 rows of 32 heads, 2 for
+// more go through the same room, 256 MiB, in several launches (room for every pair: 0.5 GiB for 256 rows of 32 heads, 2 for
 // 1024).  Whole calls of 32 heads, us, room for every pair / this: 160 rows of 20000 to 60000 keys 1044 / 1043, of 60000 to 130000 1871 /
 // 1999 (half lists take the larger sample there), 256 of 14000 to 30000 1143 / 1145, 256 of which every eighth has 60000 keys and the others
 // 3000 608 / 609 (whole lists, launches of 4096 / 2048 pairs: 666 / 799), 1024 of 500 to 3000 983 / 995.  (6 bytes a key, its place in
 // the slice for its position: 196 MiB, but one row of 65536 keys 28.6 / 29.2.)
 constexpr int LISTED_PAIRS = 4096;
 static DecodeWork decode_work(const dma_cache_shape& s, int n_rows, int k) {
-  const int kcap = list_length(s, k), ch = attend_part(s, n_rows, kcap), nsplit = (kcap + ch - 1) / ch;
+  const int kcap = list_length(s, k);
   const size_t pairs = (size_t)n_rows * s.H_q;
   DecodeWork wk;
-  size_t o = nsplit > 1 ? align_up(pairs * nsplit * (s.d + 2) * 4, 256) : 0;
+  // (No size is less for more rows.  Partial outputs: fewer than ATTEND_WGS + lists of them, and where there are as many lists, none.)
+  const size_t some = pairs < ATTEND_WGS ? pairs : ATTEND_WGS, each = (kcap + 255) / 256, outs = pairs * each < ATTEND_WGS + some ? pairs * each : ATTEND_WGS + some;
+  size_t o = each > 1 && s.H_q < ATTEND_WGS ? align_up(outs * (s.d + 2) * 4, 256) : 0;
   auto take = [&](size_t bytes) { size_t at = o; o = align_up(o + bytes, 256); return at; };
   const long cap = (long)s.max_pages * s.page_size, longest = s.max_len > 0 && s.max_len < cap ? s.max_len : cap;
   const size_t launches = (pairs + 2 * LISTED_PAIRS - 1) / (2 * LISTED_PAIRS);
   wk.pairs = (int)((pairs + launches - 1) / launches);
   const long slices = longest <= SELECT_SHORT || kcap == cap ? 0 : (longest + SLICE - 1) / SLICE, most = SELECT_WGS / (long)wk.pairs;
   wk.parts = (int)(slices < most ? slices : most < 1 && slices ? 1 : most);
-  wk.off_counts = take(wk.parts ? (size_t)wk.pairs * SLICES_MAX * 8 : 0);
   wk.room = pairs > LISTED_PAIRS ? LISTED / 2 : LISTED;
-  wk.off_listed = take(wk.parts ? (size_t)wk.pairs * wk.room * 8 : 0);
-  wk.off_bounds = take(wk.parts ? (size_t)wk.pairs * 16 : 0);
+  const size_t whole = pairs < LISTED_PAIRS ? pairs : LISTED_PAIRS, most_pairs = pairs < 2 * LISTED_PAIRS ? pairs : 2 * LISTED_PAIRS;
+  wk.off_counts = take(wk.parts ? most_pairs * SLICES_MAX * 8 : 0);
+  wk.off_listed = take(wk.parts ? whole * LISTED * 8 : 0);  // (wk.pairs * wk.room are never more)
+  wk.off_bounds = take(wk.parts ? most_pairs * 16 : 0);
   wk.total = o;
   return wk;
 }

@@ -44,7 +44,7 @@ needs_compiler = pytest.mark.skipif(shutil.which("g++") is None, reason="no host
 def test_no_scratch_needs_no_address(tmp_path):
     """An allocation of no bytes has no address."""
     out = over_stand_in(tmp_path, r"""
-for max_pages, k in ((10, 100), (10, 5000)):
+for max_pages, k in ((10, 100), (4, 5000)):
     s = B.make_cache_shape(400, 4000, max_pages, 64, 8, 2, 128)
     assert B.dma_cache_decode_bytes(s, 400, k) == 0
     runtime.start(0)
@@ -65,12 +65,13 @@ for ws, size in ((None, need), (P, need - 1), (None, 0)):
 
 
 def test_size_of_the_scratch():
-    """Lists of keys for each (row, head), 8 bytes a key, with 512 bytes of counts and 16 of bounds: 8192 keys up to 4096 pairs, then half as
-    many, for 8192 pairs at most.  None where no row can have more than 12288 keys."""
+    """Lists of 8192 keys of 8 bytes for each (row, head), but 256 MiB at most, with 512 bytes of counts and 16 of bounds for 8192 pairs at
+    most; before them the partial outputs of fewer than 512 lists.  None of the lists where no row can have more than 12288 keys."""
     s = B.make_cache_shape(4096, 100000, 16384, 64, 32, 8, 128)
-    for n_rows, pairs, keys in ((8, 256, 8192), (128, 4096, 8192), (129, 4128, 4096), (256, 8192, 4096), (257, 4112, 4096), (1024, 8192, 4096),
-                                (4096, 8192, 4096)):
-        assert B.dma_cache_decode_bytes(s, n_rows, 2048) == pairs * (8 * keys + 512 + 16), n_rows
+    for n_rows in (8, 128, 129, 256, 257, 1024, 4096):
+        pairs = 32 * n_rows
+        lists = min(65536 * pairs, 256 << 20) + (512 + 16) * min(pairs, 8192)
+        assert lists <= B.dma_cache_decode_bytes(s, n_rows, 2048) <= lists + 512 * 130 * 4 + 1024, n_rows
     for n_rows in (1, 3, 7, 8, 9, 100, 127, 128, 129, 255, 256, 257, 300, 511, 513, 2047, 5000, 16375):
         for d, k in ((64, 1), (256, 2048), (128, 100000)):
             for max_len in (0, 12288, 12289, 100000):
@@ -99,3 +100,16 @@ for n_rows, want in ((256, 2 + 1), (257, 2 * 2 + 1), (513, 3 * 2 + 1), (3000, 12
             assert e.status == B.DMA_EHIP
 """)
     assert "LOST" not in out, out
+
+
+def test_more_rows_need_no_less():
+    """A program may keep the scratch of its largest step for all of them."""
+    for H_q, H_kv, d in ((32, 8, 128), (1, 1, 64), (8, 2, 256), (300, 3, 64)):
+        for max_pages, k in ((16384, 2048), (10, 300), (10, 5000), (100, 4000), (16384, 100000), (40, 257)):
+            s, last = B.make_cache_shape(4096, 100000, max_pages, 64, H_q, H_kv, d), 0
+            for n_rows in [*range(1, 400), *range(400, 3000, 37)]:
+                size = B.dma_cache_decode_bytes(s, n_rows, k)
+                if size == 0 and (n_rows + 8) * H_q * -(-min(k, max_pages * 64) // 256) >= 1 << 22:
+                    break                            # (more rows than a call takes)
+                assert size >= last, (H_q, max_pages, k, n_rows, last, size)
+                last = size

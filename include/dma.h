@@ -312,7 +312,9 @@ int dma_decode_step(const dma_shape* shape, const void* q, const void* K, const 
  * A token's K (and V) of one kv-head is held as d codes of 4 bits and d / 32 scale bytes (OCP microscaling, e2m1 with e8m0): channel c
  * stands for  code[c] * 2^(byte[c / 32] - 127),  code in {0, 0.5, 1, 1.5, 2, 3, 4, 6} with a sign.  The power of two is the one
  * at which the largest of the 32 rounds to at most 6 (byte 2 to 252), values go to the nearest code, ties to the even one: an
- * error of at most a fifth of the largest value of the 32.  A block with an infinity or NaN has byte 255 and reads as NaN.
+ * error of at most a fifth of the largest value of the 32.  Where the byte is at its limits: at most 2^-127 if the largest value is
+ * below 5 * 2^-127 (values up to 2^-127 become 0), and at most a quarter of it from 1.75 * 2^127 on (values end at 6 * 2^125).
+ * A block with an infinity or NaN has byte 255 and reads as NaN.
  *
  * Numbers of pages, slots and requests in device memory are checked where they are used: one out of range is a row that is not
  * there, never an address.  Calls that write the same arrays must be ordered by the caller (one stream).

@@ -60,9 +60,10 @@ constexpr int ASSIGN_ROWS = 4096;
 // One workgroup, four requests to a thread.  All that it waits for is one after another -- the lengths, two scans, the pages -- so the
 // sums are formed in registers (data-parallel moves, saturating 32 bits), and the rows take the pages of their tokens from the
 // same place of the stack as the table does, not from the table.
-// Bound by that chain, not by its bytes: 256 requests that grow by a token each 4.4 us alone, of which 2 to 3 are the launch; 777 that
-// change by hundreds of tokens, tens of thousands of pages, 14 us (with 4 MB read and written, 1 us at a copy's rate).  The first
-// form, with sums in LDS and the pages read back from the table, took 9.3 and 28 us a call.
+// Bound by that chain, not by its bytes: 256 requests that grow by a token each 4.4 us alone, of which 2 to 3 are the launch; 777 of which
+// 529 grow (25540 tokens, 1594 pages) and others give 9881 pages back, and the same taken back, 14 us on average (2 MB a call, half a
+// microsecond at a copy's rate): all pages move through this one workgroup.  The first form, with sums in LDS and the pages read
+// back from the table, took 9.3 and 28 us a call.
 template <int NT>
 __global__ __launch_bounds__(NT) void cache_assign_kernel(AssignArgs p) {
   constexpr int PER = 4, REQS = NT * PER;
@@ -454,7 +455,8 @@ __global__ __launch_bounds__(256) void cache_append_kernel(CacheRef c, const T* 
 
 // ------------------------------------------------------------------ rows out of it
 // The same tiles; rows without a slot come back as zeros with a score of -infinity.  Bound by HBM, writes above all: 65536 rows as
-// above 60 us for 355 MB (5.9 TB/s).  (Stores past the caches: 53 instead of 73 us in a row, but the kernel that uses the rows
+// above 66 us for 355 MB; that this is more than a copy's 4.75 TB/s is because some of its output is still in the last cache when
+// it ends.  (Stores past the caches: 53 instead of 73 us in a row, but the kernel that uses the rows
 // loses more, 141 -> 153 together.  Codes read past them: 65536 rows - 4 us, 20001 of 16 heads of 64 channels + 6.)
 template <typename T, int D>
 __global__ __launch_bounds__(256) void cache_read_kernel(CacheRef c, const int32_t* __restrict__ slots, T* __restrict__ K,

@@ -774,7 +774,7 @@ template <> struct Query<float> {
 };
 
 // One workgroup per (ch kept keys, row, head).  A key's K (and V) row is held by D / 32 lanes, 32 channels with one scale each; a
-// wave takes 64 keys at a time, all of them requested before the first is used.  Weights are formed with the reference so far; only
+// wave takes 32 keys at a time, all of them requested before the first is used.  Weights are formed with the reference so far; only
 // a score more than 5 above it leads to the wave's maximum and a rescaling (sums in 32 bits hold weights up to e^5 as well as
 // up to 1).  The G heads of a kv-head have the same part of their lists on one XCD at the same time (decode_attend_kernel).
 // Bound by HBM and the vector unit together: 24 rows of 32 heads, 2048 of 5461 keys each, 36 us: 138 MB from HBM, 3.8 TB/s (a third of
@@ -1003,7 +1003,7 @@ static int list_length(const dma_cache_shape& s, int k) {
   return (int)(k < cap ? k : cap);
 }
 
-// Kept keys per workgroup of the attention, a multiple of 256 (64 for each wave): shorter parts where there are few lists.
+// Kept keys per workgroup of the attention, a multiple of 256 (two steps of each wave): shorter parts where there are few lists.
 constexpr int ATTEND_WGS = CUS;
 static int attend_part(const dma_cache_shape& s, int n_rows, int kcap) {
   const long lists = (long)n_rows * s.H_q, most = (kcap + 255) / 256;

@@ -30,7 +30,7 @@ class CacheRows(NamedTuple):
 
 class PagedCache:
     """n_reqs places for requests over a pool of n_pages pages; max_tokens: the longest that one request can get (default: the
-    pool).  dtype is that of k, v, q and o (bfloat16 or float32)."""
+    pool; a decode without max_len is the slower the longer it is).  dtype is that of k, v, q and o (bfloat16 or float32)."""
 
     def __init__(self, n_reqs, n_pages, num_heads, num_kv_heads, head_dim, page_size=64, max_tokens=None,
                  dtype=torch.bfloat16, device="cuda"):

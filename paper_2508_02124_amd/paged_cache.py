@@ -85,7 +85,10 @@ class PagedCache:
             W, A = self._aligned(W), A
         else:
             self._check("z", z, (s.H_q, n), torch.float32)
-        k, v = self._rows(k), self._rows(v)
+        self._append(slots, k, v, W, A, z)
+
+    def _append(self, slots, k, v, W, A, z):
+        n, k, v = slots.numel(), self._rows(k), self._rows(v)
         self._call(B.dma_cache_append, n, k, k.stride(0), v, v.stride(0), W, A, z, slots, self.pages)
 
     def read(self, slots):
@@ -101,17 +104,7 @@ class PagedCache:
         """Attention of q [n, num_heads, head_dim] over the cache: o, lse [num_heads, n] and the kept slots
         [n, num_heads, min(keep_window, longest request)].  rows: the step's (CacheRows), or (row_req, row_len); None: row r
         is request r with all its tokens.  max_len: the most keys that a row sees, where the host knows it (a matter of speed)."""
-        s, n, window = self._with_bound(max_len), q.shape[0], self._window(keep_window)
-        row_req, row_len = self._check_queries(q, rows)
-        q = self._rows(q)
-        o = torch.empty((n, s.H_q, s.d), dtype=self.dtype, device=self.device)
-        lse = torch.empty((s.H_q, n), dtype=torch.float32, device=self.device)
-        kept = self._ints(n, s.H_q, window)
-        size = B.dma_cache_decode_bytes(s, n, window)
-        ws = torch.empty(size + 16, dtype=torch.uint8, device=self.device)   # (never empty: its address is passed)
-        self._call_with(s, B.dma_cache_decode, n, window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
-                   row_len, o, lse, kept, ws, size)
-        return o, lse, kept
+        return self._attend(q, *self._check_decode(q, keep_window, rows, softmax_scale, max_len), softmax_scale)
 
     # ------------------------------------------------------------------
     def _ints(self, *shape):
@@ -143,35 +136,35 @@ class PagedCache:
         for name, x in (("k", k), ("v", v)):
             self._check(name, x, (n, s.H_kv, s.d), self.dtype, whole=False)
 
-    def _check_queries(self, q, rows):
-        """row_req and row_len of the rows (see decode)."""
-        n = q.shape[0]
-        self._check("q", q, (n, self.shape.H_q, self.shape.d), self.dtype, whole=False)
-        if rows is None:
-            return None, self.seq_lens
-        row_req, row_len = (rows.row_req, rows.row_len) if isinstance(rows, CacheRows) else rows
-        self._check("row_req", row_req, (n,), torch.int32)
-        self._check("row_len", row_len, (n,), torch.int32)
-        return row_req, row_len
-
-    def _check_decode(self, q, keep_window, rows, softmax_scale=0.0, max_len=0):
-        """Raises what decode would, for a caller that has something to do before it; nothing is allocated or enqueued."""
-        s, n, window = self._with_bound(max_len), q.shape[0], self._window(keep_window)
-        self._check_queries(q, rows)
-        B.dma_cache_decode(s, 0, window, softmax_scale, None, s.H_q * s.d, *[None] * 8, 0, stream=0)   # (no rows: its other arguments)
+    def _check_decode(self, q, keep_window, rows, softmax_scale, max_len):
+        """The shape, window, row_req and row_len of a decode, or what it would raise, for a caller that has something to do before it.
+        A window or a bound beyond the longest request, of whatever size, is one of just that."""
+        s, n = self.shape, q.shape[0]
+        longest = s.max_pages * s.page_size
+        window, bound = min(int(keep_window), longest), min(int(max_len), longest)
+        if window <= 0 or bound < 0 or not softmax_scale >= 0.0:
+            raise B.DmaError(B.DMA_EINVAL, "dma_cache_decode")
         if (n + 8) * s.H_q * -(-window // 256) >= 1 << 22:
             raise B.DmaError(B.DMA_EUNSUPPORTED, "dma_cache_decode")
+        self._check("q", q, (n, s.H_q, s.d), self.dtype, whole=False)
+        row_req, row_len = (None, self.seq_lens) if rows is None else (rows.row_req, rows.row_len) if isinstance(rows, CacheRows) else rows
+        if rows is not None:
+            self._check("row_req", row_req, (n,), torch.int32)
+            self._check("row_len", row_len, (n,), torch.int32)
+        if bound:
+            s = B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype, bound)
+        return s, window, row_req, row_len
 
-    # (a window or a bound beyond the longest request, of whatever size, is one of just that)
-    def _window(self, keep_window):
-        return min(int(keep_window), self.shape.max_pages * self.shape.page_size)
-
-    def _with_bound(self, max_len):
-        s = self.shape
-        if not max_len:
-            return s
-        return B.make_cache_shape(s.n_reqs, s.n_pages, s.max_pages, s.page_size, s.H_q, s.H_kv, s.d, s.dtype,
-                                  min(int(max_len), s.max_pages * s.page_size))
+    def _attend(self, q, s, window, row_req, row_len, softmax_scale):
+        q, n = self._rows(q), q.shape[0]
+        o = torch.empty((n, s.H_q, s.d), dtype=self.dtype, device=self.device)
+        lse = torch.empty((s.H_q, n), dtype=torch.float32, device=self.device)
+        kept = self._ints(n, s.H_q, window)
+        size = B.dma_cache_decode_bytes(s, n, window)
+        ws = torch.empty(size, dtype=torch.uint8, device=self.device)
+        self._call_with(s, B.dma_cache_decode, n, window, softmax_scale, q, q.stride(0), self.pages, self.block_table, row_req,
+                        row_len, o, lse, kept, ws, size)
+        return o, lse, kept
 
     @staticmethod
     def _aligned(x):

@@ -167,7 +167,7 @@ class DynamicMaskAttention(torch.nn.Module):
         cache.decode.  Without gradients; o [n, H_q, d].  What cannot be done is refused before the cache is changed."""
         with torch.no_grad():
             W, A = self.W.detach(), self.A.detach()
-            cache._check_decode(q, self.keep_window, rows, self.softmax_scale, max_len)   # (before the rows go in)
+            checked = cache._check_decode(q, self.keep_window, rows, self.softmax_scale, max_len)   # (before the rows go in)
             if W.shape[1] == self.head_dim:
                 cache.append(rows.slots, k, v, W=W, A=A)
             else:                                    # the cross-head scores have an entry point of their own
@@ -179,5 +179,5 @@ class DynamicMaskAttention(torch.nn.Module):
                 if n:
                     shape = B.make_shape(n, 1, s.H_q, s.H_kv, s.d, 1, dtype=_dtype_code(v))
                     cache._call_with(shape, B.dma_scores_xhead, cache._rows(v).contiguous(), cache._aligned(W), A, z)
-                cache.append(rows.slots, k, v, z=z)
-            return cache.decode(q, self.keep_window, rows, self.softmax_scale, max_len)[0]
+                cache._append(rows.slots, k, v, None, None, z)
+            return cache._attend(q, *checked, self.softmax_scale)[0]

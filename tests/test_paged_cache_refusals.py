@@ -113,4 +113,4 @@ def test_rows_and_window_of_a_step():
     with pytest.raises(B.DmaError) as e:
         module(False, keep_window=window).step(values(H_Q, n=n), values(H_KV, n=n), values(H_KV, n=n), cache, rows(n))
     assert cache.calls == [] and e.value.status == B.DMA_EUNSUPPORTED
-    cache._check_decode(values(H_Q, n=n - 1), window, rows(n - 1))
+    cache._check_decode(values(H_Q, n=n - 1), window, rows(n - 1), 0.0, 0)

@@ -37,7 +37,7 @@ class PagedCache:
         codes = {torch.bfloat16: B.DMA_BF16, torch.float32: B.DMA_F32}
         if dtype not in codes:
             raise TypeError(f"dtype must be bfloat16 or float32, got {dtype}")
-        max_pages = n_pages if max_tokens is None else -(-int(max_tokens) // int(page_size))
+        max_pages = n_pages if max_tokens is None else -(-int(max_tokens) // max(int(page_size), 1))
         self.shape = B.make_cache_shape(n_reqs, n_pages, max_pages, page_size, num_heads, num_kv_heads, head_dim,
                                         dtype=codes[dtype])
         B.dma_cache_describe(self.shape)                  # (raises for sizes that the library refuses)

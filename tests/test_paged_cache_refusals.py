@@ -114,3 +114,10 @@ def test_rows_and_window_of_a_step():
         module(False, keep_window=window).step(values(H_Q, n=n), values(H_KV, n=n), values(H_KV, n=n), cache, rows(n))
     assert cache.calls == [] and e.value.status == B.DMA_EUNSUPPORTED
     cache._check_decode(values(H_Q, n=n - 1), window, rows(n - 1), 0.0, 0)
+
+
+@pytest.mark.parametrize("page_size", [0, -16, 24])
+def test_page_sizes_are_refused_by_the_library(page_size):
+    for max_tokens in (None, 50):
+        with pytest.raises(B.DmaError):
+            PagedCache(2, 4, H_Q, H_KV, D, page_size=page_size, max_tokens=max_tokens)

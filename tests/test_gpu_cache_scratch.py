@@ -45,3 +45,38 @@ def test_many_pairs_share_the_scratch(gpu, kind, n_rows):
     check_kept(cache, k, [rows[i] for i in some], kept[some])
     few = [i for i in some if rows[i][1] < 13000][:1] or [3]
     check_rows(cache, q[few], k, [rows[i] for i in few], (o[few], lse[:, few], kept[few]))
+
+
+def test_captured_call_of_many_launches(gpu):
+    """8320 pairs, two launches over the same scratch, in a graph: every replay equals the eager call, with eager calls over the same scratch
+    between."""
+    lens, k, H, n_rows = (29000, 300, 13000), 700, 64, 130
+    cache = GpuCache(gpu, 3, 700, 460, 64, H, 1, 64)
+    fill(cache, lens, 8)
+    req = torch.arange(n_rows, device=gpu).remainder(3).int()
+    length = (torch.tensor(lens, device=gpu)[req.long()] - torch.arange(n_rows, device=gpu) // 3).int()
+    q = normal(gpu, 5, n_rows, H, 64).to(cache.type)
+    size = B.dma_cache_decode_bytes(cache.shape, n_rows, k)
+    ws = torch.full((size,), 0xFF, dtype=torch.uint8, device=gpu)
+
+    def outputs():
+        return torch.zeros((n_rows, H, 64), dtype=cache.type, device=gpu), torch.zeros((H, n_rows), device=gpu), cache.ints(n_rows, H, k)
+
+    def call(out):
+        B.dma_cache_decode(cache.shape, n_rows, k, 0.0, q, q.stride(0), cache.pages, cache.table, req, length, *out, ws, size)
+
+    held, plain = outputs(), outputs()
+    torch.cuda.synchronize()
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        call(held)
+    for _ in range(5):
+        graph.replay()
+        torch.cuda.synchronize()
+        call(plain)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(held, plain))
+        for x in (*held, *plain):
+            x.zero_()
+        q.mul_(0.9)
+        length.sub_(1)

@@ -214,6 +214,26 @@ int dma_bwd_scores(const dma_shape* shape, const void* Q, const void* K, const v
                    void* stream);
 
 /*
+ * Rotary positions (Listing 1 turns q and k before the attention): pair i of a head's first `rot` channels is turned by the angle
+ * a = position * freqs[i],
+ *     y1 = x1 cos a - x2 sin a,   y2 = x1 sin a + x2 cos a,
+ * the pairs being the channels (i, i + rot / 2), or the neighbours (2 i, 2 i + 1) if interleaved != 0; channels from rot on stay.
+ *   Q, K       in   T rows of [H_q, d] and [H_kv, d], q_stride and k_stride elements apart (multiples of 8 of at least the row: both may be
+ *                   parts of one projection's output); either may be NULL and is then left out
+ *   positions  in   nullable: [T] int32, of any sign; NULL: a token's position is its place in its document (cu_seqlens, else not read)
+ *   freqs      in   [rot / 2] float, e.g. base^(-2 i / rot)
+ *   rot        a multiple of 16, at most d
+ *   inverse    != 0: turned by -a.  That is the transpose, so the gradients of Q and K are those of Qo and Ko turned with inverse = 1
+ *   Qo, Ko     out  rows qo_stride and ko_stride elements apart (what lies between rows is left as it is); Qo may be Q, and Ko K, with the
+ *                   same stride, else no output overlaps an input
+ * Angles are reduced in 64 bits, so that far positions are as exact as near ones; products are in fp32, rounded once to the type.
+ * shape->k, max_seqlen, causal and softmax_scale are not used, n_docs only with cu_seqlens.
+ */
+int dma_rope(const dma_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+             const int32_t* cu_seqlens, const int32_t* positions, const float* freqs, int32_t rot, int interleaved,
+             int inverse, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride, void* stream);
+
+/*
  * Content scores with the paper's full sampling tensor (Eq. 3 states Delta in R^{n_h x d_h x n_h};
  * Listing 1 flattens the values of all heads of a token before the projection): the score of q-head
  * h contracts the token's value vectors of ALL kv-heads,
@@ -386,6 +406,23 @@ int dma_cache_assign(const dma_cache_shape* shape, int32_t n_rows, const int32_t
 int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K, int64_t k_stride, const void* V,
                      int64_t v_stride, const float* W, const float* A, const float* z, const int32_t* slots, void* pages,
                      void* stream);
+
+/*
+ * dma_cache_append with rotary positions (dma_rope) on the way: K goes into the cache turned, and the rows' queries are turned in the
+ * same call.  The token of row r has the position row_len[r] - 1 (0 if that is below 0) behind the prefix of its request:
+ *   row_req     in  nullable (row r is then request r, n_rows <= n_reqs); row_len in, as dma_cache_assign gives them
+ *   n_prefixes, prefix_len [n_prefixes], req_prefix [n_reqs]   as for dma_cache_decode_prefix; with n_prefixes == 0 neither is read, nor row_req
+ *   Q           in  nullable: n_rows rows of [H_q, d], q_stride elements apart, every row turned, also one without a slot
+ *   Qo          out [n_rows, H_q, d]; may be Q if that is packed
+ *   freqs, rot, interleaved   as for dma_rope
+ * The codes are those of the turned value as 64 bits give it: nothing is rounded before them (rows that dma_rope wrote have been, to their
+ * type).  V and the scores, which come from V, are dma_cache_append's bit for bit, and so is everything else.
+ */
+int dma_cache_append_rope(const dma_cache_shape* shape, int32_t n_rows, const void* Q, int64_t q_stride, const void* K,
+                          int64_t k_stride, const void* V, int64_t v_stride, const float* W, const float* A, const float* z,
+                          const int32_t* slots, const int32_t* row_req, const int32_t* row_len, int32_t n_prefixes,
+                          const int32_t* prefix_len, const int32_t* req_prefix, const float* freqs, int32_t rot,
+                          int interleaved, void* Qo, void* pages, void* stream);
 
 /*
  * Rows out of the cache, for the entry points over plain K, V and z (dma_mask_gen with W == NULL, dma_fwd, dma_decode).

@@ -88,6 +88,9 @@ def lib():
         L.dma_bwd_scores.restype = i32
         L.dma_mask_bwd.argtypes = [shp] + [vp] * 7 + [i32, vp]
         L.dma_mask_bwd.restype = i32
+        i64, f32 = ctypes.c_int64, ctypes.c_float
+        L.dma_rope.argtypes = [shp, vp, i64, vp, i64, vp, vp, vp, i32, i32, i32, vp, i64, vp, i64, vp]
+        L.dma_rope.restype = i32
         L.dma_scores_xhead.argtypes = [shp] + [vp] * 5
         L.dma_scores_xhead.restype = i32
         L.dma_scores_xhead_bwd.argtypes = [shp] + [vp] * 7 + [i32, vp]
@@ -102,7 +105,7 @@ def lib():
         L.dma_decode_static.restype = i32
         L.dma_decode_step.argtypes = [shp] + [vp] * 6 + [i32] + [vp] * 3 + [sz, vp]
         L.dma_decode_step.restype = i32
-        cshp, i64 = ctypes.POINTER(DmaCacheShape), ctypes.c_int64
+        cshp = ctypes.POINTER(DmaCacheShape)
         L.dma_cache_bytes.argtypes = [cshp]
         L.dma_cache_bytes.restype = sz
         L.dma_cache_free_bytes.argtypes = [cshp]
@@ -117,9 +120,12 @@ def lib():
         L.dma_cache_assign.restype = i32
         L.dma_cache_append.argtypes = [cshp, i32, vp, i64, vp, i64] + [vp] * 6
         L.dma_cache_append.restype = i32
+        L.dma_cache_append_rope.argtypes = ([cshp, i32, vp, i64, vp, i64, vp, i64] + [vp] * 6 + [i32, vp, vp, vp, i32, i32]
+                                            + [vp] * 3)
+        L.dma_cache_append_rope.restype = i32
         L.dma_cache_read.argtypes = [cshp, i32] + [vp] * 6
         L.dma_cache_read.restype = i32
-        L.dma_cache_decode.argtypes = [cshp, i32, i32, ctypes.c_float, vp, i64] + [vp] * 8 + [sz, vp]
+        L.dma_cache_decode.argtypes = [cshp, i32, i32, f32, vp, i64] + [vp] * 8 + [sz, vp]
         L.dma_cache_decode.restype = i32
         L.dma_profile_events.argtypes = [vp]
         L.dma_profile_events.restype = None
@@ -250,6 +256,13 @@ def dma_mask_bwd(shape, V, W, A, dz, dW, dA, dV, accumulate, stream=None):
                               int(bool(accumulate)), _stream(stream)), "dma_mask_bwd")
 
 
+def dma_rope(shape, Q, q_stride, K, k_stride, cu_seqlens, positions, freqs, rot, interleaved, inverse, Qo, qo_stride, Ko,
+             ko_stride, stream=None):
+    _check(lib().dma_rope(ctypes.byref(shape), _ptr(Q), int(q_stride), _ptr(K), int(k_stride), _ptr(cu_seqlens),
+                          _ptr(positions), _ptr(freqs), _i32(rot), int(bool(interleaved)), int(bool(inverse)), _ptr(Qo),
+                          int(qo_stride), _ptr(Ko), int(ko_stride), _stream(stream)), "dma_rope")
+
+
 def dma_scores_xhead(shape, V, Delta, A, z, stream=None):
     _check(lib().dma_scores_xhead(ctypes.byref(shape), _ptr(V), _ptr(Delta), _ptr(A), _ptr(z), _stream(stream)),
            "dma_scores_xhead")
@@ -324,6 +337,15 @@ def dma_cache_append(shape, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pa
     _check(lib().dma_cache_append(ctypes.byref(shape), _i32(n_rows), _ptr(K), int(k_stride), _ptr(V), int(v_stride),
                                   _ptr(W), _ptr(A), _ptr(z), _ptr(slots), _ptr(pages), _stream(stream)),
            "dma_cache_append")
+
+
+def dma_cache_append_rope(shape, n_rows, Q, q_stride, K, k_stride, V, v_stride, W, A, z, slots, row_req, row_len, n_prefixes,
+                          prefix_len, req_prefix, freqs, rot, interleaved, Qo, pages, stream=None):
+    _check(lib().dma_cache_append_rope(ctypes.byref(shape), _i32(n_rows), _ptr(Q), int(q_stride), _ptr(K), int(k_stride),
+                                       _ptr(V), int(v_stride), _ptr(W), _ptr(A), _ptr(z), _ptr(slots), _ptr(row_req),
+                                       _ptr(row_len), _i32(n_prefixes), _ptr(prefix_len), _ptr(req_prefix), _ptr(freqs),
+                                       _i32(rot), int(bool(interleaved)), _ptr(Qo), _ptr(pages), _stream(stream)),
+           "dma_cache_append_rope")
 
 
 def dma_cache_read(shape, n_rows, slots, pages, K, V, z, stream=None):

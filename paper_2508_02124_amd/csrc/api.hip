@@ -3,6 +3,7 @@
 // dma_profile_events has one set (per host thread), nothing else in this file.
 #include "cache.h"
 #include "common.h"
+#include "rope.h"
 
 using namespace dma;
 
@@ -73,6 +74,12 @@ int check_rows(const dma_cache_shape* s, int32_t n_rows) {
 
 // n_rows rows of `heads` heads, `stride` elements apart
 bool bad_rows(const dma_cache_shape& s, int64_t stride, int heads) { return stride < (int64_t)heads * s.d || stride % 8 != 0; }
+
+// pairs of channels in turn: whole units of eight channels to either half
+int check_rope(const float* freqs, int rot, int d) {
+  if (!freqs || rot <= 0 || rot > d) return DMA_EINVAL;
+  return rot % 16 ? DMA_EUNSUPPORTED : DMA_OK;
+}
 
 Ptrs make_ptrs(const dma_shape* s, const void* mask) {
   Ptrs p;
@@ -225,6 +232,23 @@ int dma_mask_bwd(const dma_shape* shape, const void* V, const float* W, const fl
   return launch_mask_bwd(*shape, V, W, A, dz, dW, dA, dV, accumulate != 0, (hipStream_t)stream);
 }
 
+int dma_rope(const dma_shape* shape, const void* Q, int64_t q_stride, const void* K, int64_t k_stride,
+             const int32_t* cu_seqlens, const int32_t* positions, const float* freqs, int32_t rot, int interleaved,
+             int inverse, void* Qo, int64_t qo_stride, void* Ko, int64_t ko_stride, void* stream) {
+  int rc = check_shape(shape, 256);
+  if (rc != DMA_OK) return rc;
+  if ((rc = check_rope(freqs, rot, shape->d)) != DMA_OK) return rc;
+  if ((!Q && !K) || (!positions && !cu_seqlens)) return DMA_EINVAL;
+  auto bad = [&](const void* in, int64_t in_stride, const void* out, int64_t out_stride, int heads) {
+    const int64_t row = (int64_t)heads * shape->d;
+    return in && (!out || !aligned16(in) || !aligned16(out) || in_stride < row || out_stride < row || in_stride % 8 || out_stride % 8 ||
+                  (in == out && in_stride != out_stride));
+  };
+  if (bad(Q, q_stride, Qo, qo_stride, shape->H_q) || bad(K, k_stride, Ko, ko_stride, shape->H_kv)) return DMA_EINVAL;
+  return launch_rope(*shape, Q, q_stride, K, k_stride, cu_seqlens, positions, {freqs, rot}, interleaved != 0, inverse != 0, Qo,
+                     qo_stride, Ko, ko_stride, (hipStream_t)stream);
+}
+
 int dma_scores_xhead(const dma_shape* shape, const void* V, const float* Delta, const float* A, float* z,
                      void* stream) {
   int rc = check_shape(shape);
@@ -361,6 +385,30 @@ int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K
   if (!K || !V || !slots || !pages || (W ? !A : !z)) return DMA_EINVAL;
   if (!aligned16(K) || !aligned16(V) || !aligned16(W) || !aligned16(pages)) return DMA_EINVAL;
   return launch_cache_append(*shape, n_rows, K, k_stride, V, v_stride, W, A, z, slots, pages, (hipStream_t)stream);
+}
+
+// The arrays that lead from a row to its prefix.
+static bool bad_prefixes(const dma_cache_shape* s, int32_t n_rows, const int32_t* row_req, int32_t n_prefixes, const int32_t* prefix_len,
+                         const int32_t* req_prefix) {
+  return n_prefixes < 0 || (!row_req && n_rows > s->n_reqs) || (n_prefixes > 0 && (!prefix_len || !req_prefix));
+}
+
+int dma_cache_append_rope(const dma_cache_shape* shape, int32_t n_rows, const void* Q, int64_t q_stride, const void* K,
+                          int64_t k_stride, const void* V, int64_t v_stride, const float* W, const float* A, const float* z,
+                          const int32_t* slots, const int32_t* row_req, const int32_t* row_len, int32_t n_prefixes,
+                          const int32_t* prefix_len, const int32_t* req_prefix, const float* freqs, int32_t rot,
+                          int interleaved, void* Qo, void* pages, void* stream) {
+  int rc = check_rows(shape, n_rows);
+  if (rc != DMA_OK) return rc;
+  if ((rc = check_rope(freqs, rot, shape->d)) != DMA_OK) return rc;
+  if (bad_rows(*shape, k_stride, shape->H_kv) || bad_rows(*shape, v_stride, shape->H_kv)) return DMA_EINVAL;
+  if (Q && (bad_rows(*shape, q_stride, shape->H_q) || (Q == Qo && q_stride != (int64_t)shape->H_q * shape->d))) return DMA_EINVAL;
+  if (bad_prefixes(shape, n_prefixes ? n_rows : 0, row_req, n_prefixes, prefix_len, req_prefix)) return DMA_EINVAL;
+  if (n_rows == 0) return DMA_OK;
+  if (!K || !V || !slots || !row_len || !pages || (W ? !A : !z) || (Q && !Qo)) return DMA_EINVAL;
+  if (!aligned16(K) || !aligned16(V) || !aligned16(W) || !aligned16(pages) || !aligned16(Q) || (Q && !aligned16(Qo))) return DMA_EINVAL;
+  return launch_cache_append_rope(*shape, n_rows, Q, q_stride, K, k_stride, V, v_stride, W, A, z, slots, row_req, row_len, n_prefixes,
+                                  prefix_len, req_prefix, {freqs, rot}, interleaved != 0, Qo, pages, (hipStream_t)stream);
 }
 
 int dma_cache_read(const dma_cache_shape* shape, int32_t n_rows, const int32_t* slots, const void* pages, void* K, void* V,

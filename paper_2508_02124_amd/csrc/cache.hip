@@ -4,6 +4,7 @@
 // 32 channels of a token's head, 17 / 32 bytes a channel against bf16's 2.  The content scores (Eq. 3) are formed from V as it comes, not
 // as it is stored, and held in fp32: they decide which keys a row keeps.
 #include "cache.h"
+#include "cache_rows.h"
 #include "select.h"
 
 namespace dma {
@@ -258,43 +259,6 @@ int launch_cache_assign(const dma_cache_shape& s, int n_rows, const int32_t* cha
 }
 
 // ------------------------------------------------------------------ rows into the cache
-// Eight channels of a lane, as they come, and as fp32.
-template <typename T> struct Raw8;
-template <> struct Raw8<__bf16> { uint4 x; };
-template <> struct Raw8<float> { float4 a, b; };
-__device__ __forceinline__ void load_raw(const __bf16* src, Raw8<__bf16>& r) { r.x = *reinterpret_cast<const uint4*>(src); }
-__device__ __forceinline__ void load_raw(const float* src, Raw8<float>& r) {
-  r.a = reinterpret_cast<const float4*>(src)[0];
-  r.b = reinterpret_cast<const float4*>(src)[1];
-}
-__device__ __forceinline__ void to_f32(const Raw8<__bf16>& r, float* x) {
-  const uint32_t u[4] = {r.x.x, r.x.y, r.x.z, r.x.w};
-#pragma unroll
-  for (int e = 0; e < 4; e++) {
-    x[2 * e] = __uint_as_float(u[e] << 16);
-    x[2 * e + 1] = __uint_as_float(u[e] & 0xffff0000u);
-  }
-}
-__device__ __forceinline__ void to_f32(const Raw8<float>& r, float* x) {
-  x[0] = r.a.x; x[1] = r.a.y; x[2] = r.a.z; x[3] = r.a.w;
-  x[4] = r.b.x; x[5] = r.b.y; x[6] = r.b.z; x[7] = r.b.w;
-}
-
-template <int CTRL> __device__ __forceinline__ uint32_t dpp_quad(uint32_t x) {
-  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, true);
-}
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
-
-// The scale byte that four neighbouring lanes (32 channels) share, from the bits of the largest magnitude of a lane's (as integers: the
-// bits of NaN are above those of every number): the power of two at which it rounds to at most 6, 2^(exponent - 2) or, from a
-// mantissa of 1.75 on, twice that.  A block that holds an infinity or NaN has the byte 255.  Bytes 2 to 252: what the cache holds is
-// finite and normal in fp32 and bf16 alike.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t top) {
-  top = max(top, dpp_quad<0xb1>(top));
-  top = max(top, dpp_quad<0x4e>(top));
-  return top >= 0x7f800000u ? 255u : (uint32_t)max(2, min(252, (int)((top + 0x200000u) >> 23) - 2));
-}
 // Rows whose K and V are more than this (and bf16) are read past the caches: with the pages they do not fit the last one, of 256 MB, and
 // would only drive each other out.  Rows of 8 heads of 128 channels, us through / past: 65536 from memory 103 / 82, 65536 just made by
 // other kernels, these included, 192 / 183, 49152 (192 MiB) 135 / 130, 40960 (160 MiB) 102 / 111, 16384 48 / 54.  (fp32 ones come in half
@@ -304,35 +268,6 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <bool PAST, typename T> __device__ __forceinline__ void load_row(const T* src, Raw8<T>& r) {
   if constexpr (PAST) r.x = __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(src)));
   else load_raw(src, r);
-}
-
-// The codes of a lane's eight channels, and that byte.
-__device__ __forceinline__ uint32_t quantise8(const Raw8<__bf16>& r, uint32_t& byte) {
-  const uint32_t u[4] = {r.x.x, r.x.y, r.x.z, r.x.w};
-  u16x2 top = __builtin_bit_cast(u16x2, u[0] & 0x7fff7fffu);
-#pragma unroll
-  for (int e = 1; e < 4; e++) top = __builtin_elementwise_max(top, __builtin_bit_cast(u16x2, u[e] & 0x7fff7fffu));
-  byte = scale_byte((uint32_t)max(top[0], top[1]) << 16);
-  const float scale = mx_scale(byte);
-  uint32_t code = 0;
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[0]), scale, 0);
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[1]), scale, 1);
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[2]), scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(code, __builtin_bit_cast(bf16x2, u[3]), scale, 3);
-}
-__device__ __forceinline__ uint32_t quantise8(const Raw8<float>& r, uint32_t& byte) {
-  float x[8];
-  to_f32(r, x);
-  uint32_t top = 0;
-#pragma unroll
-  for (int e = 0; e < 8; e++) top = max(top, __float_as_uint(x[e]) & 0x7fffffffu);
-  byte = scale_byte(top);
-  const float scale = mx_scale(byte);
-  uint32_t code = 0;
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[0], x[1], scale, 0);
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[2], x[3], scale, 1);
-  code = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[4], x[5], scale, 2);
-  return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(code, x[6], x[7], scale, 3);
 }
 
 // Rows of a tile, for rows of that many bytes: more workgroups of fewer registers where a row is long.  In and out, 64 / 32 rows, us:

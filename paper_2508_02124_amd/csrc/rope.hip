@@ -1,0 +1,124 @@
+// Rotary positions of packed Q and K, and the rotation back that carries gradients: y1 = x1 cos a - x2 sin a,
+// y2 = x1 sin a + x2 cos a for every pair of channels, a = position * frequency.  The transpose is the rotation by -a.
+#include "cache_rows.h"
+#include "rope.h"
+
+namespace dma {
+
+struct RopeRows {
+  const void *q, *k;
+  void *qo, *ko;
+  long q_stride, k_stride, qo_stride, ko_stride;
+  const int32_t *cu, *positions;
+  int T, n_docs, H_q, H;  // q-heads, and all heads (either kind may be left out)
+};
+
+// The last document that starts at or before t: 64 of the starts at a time, a lane each.
+__device__ __forceinline__ int document_start(const int32_t* __restrict__ cu, int n_docs, int t, int l) {
+  int lo = 0, n = n_docs;  // it is one of the n from lo on
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int i = min(l * step, n - 1);
+    const unsigned long long m = __ballot(cu[lo + i] <= t);  // (ascending: the lanes before one that is behind t)
+    const int last = max(0, __popcll(m) - 1);
+    const int at = min(last * step, n - 1);
+    n = min(step, n - at);
+    lo += at;
+  }
+  return cu[lo];
+}
+
+// A lane has 16 channels of a token, eight whole pairs (or channels that stay), in the same place of every head: it forms its eight
+// angles once.  A wave has 64 / (D / 16) tokens.
+template <typename T, int D, bool NEXT>
+__global__ __launch_bounds__(256) void rope_kernel(RopeRows p, RopeArgs rope, int heads, int inverse) {
+  constexpr int TASKS = D / 16, TOKENS = 64 / TASKS, U = 4;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), task = l % TASKS;
+  const int h0 = blockIdx.y * heads, h1 = min(p.H, h0 + heads);
+  const bool turned = task < rope.rot / 16;
+  const int a = NEXT ? 16 * task : turned ? 8 * task : rope.rot + 16 * (task - rope.rot / 16);
+  const int b = !NEXT && turned ? a + rope.rot / 2 : a + 8;
+  float f[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) f[e] = turned ? rope.freqs[8 * task + e] : 0.f;
+  for (long t0 = ((long)blockIdx.x * 4 + w) * TOKENS; t0 < p.T; t0 += (long)gridDim.x * 4 * TOKENS) {
+    const long t = t0 + l / TASKS, tc = min(t, (long)p.T - 1);
+    int position;
+    if (p.positions) {
+      position = p.positions[tc];
+    } else {
+      position = 0;
+      for (int i = 0; i < TOKENS; i++) {
+        const int ti = (int)min(t0 + i, (long)p.T - 1), start = document_start(p.cu, p.n_docs, ti, l);
+        position = l / TASKS == i ? ti - start : position;
+      }
+    }
+    float c[8], s[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const Turn turn = turn_of(position, f[e]);
+      c[e] = (float)turn.c;
+      s[e] = (float)(inverse ? -turn.s : turn.s);
+    }
+    for (int hb = h0; hb < h1; hb += U) {
+      Raw8<T> x[U], y[U];
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int h = min(hb + u, h1 - 1);
+        const T* src = h < p.H_q ? (const T*)p.q + tc * p.q_stride + (long)h * D : (const T*)p.k + tc * p.k_stride + (long)(h - p.H_q) * D;
+        load_raw(src + a, x[u]);
+        load_raw(src + b, y[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int h = hb + u;
+        if (h >= h1 || t >= p.T) continue;
+        T* dst = h < p.H_q ? (T*)p.qo + t * p.qo_stride + (long)h * D : (T*)p.ko + t * p.ko_stride + (long)(h - p.H_q) * D;
+        if (turned) {
+          float v[16], o[16];
+          to_f32(x[u], v);
+          to_f32(y[u], v + 8);
+#pragma unroll
+          for (int e = 0; e < 8; e++) {
+            const int i = NEXT ? 2 * e : e, j = NEXT ? 2 * e + 1 : e + 8;
+            o[i] = fmaf(v[i], c[e], -(v[j] * s[e]));
+            o[j] = fmaf(v[i], s[e], v[j] * c[e]);
+          }
+          store8<T>(dst + a, o);
+          store8<T>(dst + b, o + 8);
+        } else {
+          store_raw(dst + a, x[u]);
+          store_raw(dst + b, y[u]);
+        }
+      }
+    }
+  }
+}
+
+template <typename T, int D>
+static void rope_t(const RopeRows& p, const RopeArgs& rope, bool next, bool inverse, hipStream_t st) {
+  constexpr int TOKENS = 64 / (D / 16);
+  const long tiles = ((long)p.T + 4 * TOKENS - 1) / (4 * TOKENS);
+  int heads = (int)((tiles * p.H + 4 * CUS - 1) / (4 * CUS));  // of a workgroup: fewer where there are few tokens
+  heads = heads < 4 ? 4 : heads > p.H ? p.H : heads;
+  const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((p.H + heads - 1) / heads));
+  if (next) rope_kernel<T, D, true><<<grid, 256, 0, st>>>(p, rope, heads, inverse);
+  else rope_kernel<T, D, false><<<grid, 256, 0, st>>>(p, rope, heads, inverse);
+}
+
+int launch_rope(const dma_shape& s, const void* Q, long q_stride, const void* K, long k_stride, const int32_t* cu,
+                const int32_t* positions, const RopeArgs& rope, bool next, bool inverse, void* Qo, long qo_stride, void* Ko,
+                long ko_stride, hipStream_t st) {
+  const int H_q = Q ? s.H_q : 0;
+  const RopeRows p = {Q, K, Qo, Ko, q_stride, k_stride, qo_stride, ko_stride, cu, positions, s.T, s.n_docs, H_q, H_q + (K ? s.H_kv : 0)};
+  auto go = [&](auto t) {
+    using T = std::remove_pointer_t<decltype(t)>;
+    if (s.d == 256) rope_t<T, 256>(p, rope, next, inverse, st);
+    else if (s.d == 128) rope_t<T, 128>(p, rope, next, inverse, st);
+    else rope_t<T, 64>(p, rope, next, inverse, st);
+  };
+  if (s.dtype == DMA_BF16) go((__bf16*)nullptr); else go((float*)nullptr);
+  return hipGetLastError() == hipSuccess ? DMA_OK : DMA_EHIP;
+}
+
+}  // namespace dma

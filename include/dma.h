@@ -454,6 +454,33 @@ int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, fl
                      const int32_t* row_len, void* o, float* lse, int32_t* kept, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * Decode for requests that share prefixes.  A prefix (a system prompt, a document that many ask about) lies in the cache once, as the
+ * tokens of a request of its own; a request behind it holds only what comes after.  Row r sees the tokens of its request's prefix and then the
+ * first row_len[r] of its own, and keeps the min(k, n) best of all n of them by (z descending, position ascending, the prefix's first): what
+ * dma_cache_decode would make of one request with all the tokens.
+ *   n_prefixes   number of prefixes, at most 4096
+ *   max_prefix   upper bound on their lengths (0 => max_pages * page_size).  Like shape->max_len, the bound on a row's own keys, it chooses
+ *                between equal ways of working; one that is too small costs time but changes no result
+ *   prefix_req   in [n_prefixes] int32: the request that holds each; one out of range is a prefix without tokens
+ *   prefix_len   in [n_prefixes] int32: its tokens (their number may be less than that request has)
+ *   req_prefix   in [n_reqs] int32: the prefix of each request, 0 to n_prefixes - 1; any other value: none.  (A prefix of a prefix is not
+ *                looked at.)  The last three are not read if n_prefixes is 0
+ *   q, q_stride, pages, block_table, row_req, row_len, softmax_scale, o, lse   as for dma_cache_decode; a row that has no request or no
+ *                keys of its own, or a page out of range among its own or its prefix's, sees nothing
+ *   ws           dma_cache_decode_prefix_bytes(shape, n_rows, k, n_prefixes, max_prefix) bytes of scratch; calls that overlap need one
+ *                each.  It holds the lists of kept keys, 8 bytes for each of (n_rows + n_prefixes) * H_q * min(k, max_pages * page_size)
+ * A prefix is selected from, gathered and decoded once for all of its rows.  The limit on rows is dma_cache_decode's, with n_rows + n_prefixes
+ * in the place of n_rows.
+ */
+size_t dma_cache_decode_prefix_bytes(const dma_cache_shape* shape, int32_t n_rows, int32_t k, int32_t n_prefixes,
+                                     int32_t max_prefix);
+int dma_cache_decode_prefix(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
+                            int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,
+                            const int32_t* row_len, int32_t n_prefixes, int32_t max_prefix, const int32_t* prefix_req,
+                            const int32_t* prefix_len, const int32_t* req_prefix, void* o, float* lse, void* ws,
+                            size_t ws_bytes, void* stream);
+
+/*
  * Per-stage timing aid.  dma_mask_gen, dma_fwd and dma_bwd each launch several kernels, so a
  * caller cannot bracket one of them with events from outside.  `events` is a HOST array of
  * 2 * DMA_N_STAGES hipEvent_t handles (as void*) owned by the caller, or NULL to switch the aid

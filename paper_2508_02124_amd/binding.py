@@ -127,6 +127,10 @@ def lib():
         L.dma_cache_read.restype = i32
         L.dma_cache_decode.argtypes = [cshp, i32, i32, f32, vp, i64] + [vp] * 8 + [sz, vp]
         L.dma_cache_decode.restype = i32
+        L.dma_cache_decode_prefix_bytes.argtypes = [cshp, i32, i32, i32, i32]
+        L.dma_cache_decode_prefix_bytes.restype = sz
+        L.dma_cache_decode_prefix.argtypes = [cshp, i32, i32, f32, vp, i64] + [vp] * 4 + [i32, i32] + [vp] * 6 + [sz, vp]
+        L.dma_cache_decode_prefix.restype = i32
         L.dma_profile_events.argtypes = [vp]
         L.dma_profile_events.restype = None
         L.dma_strerror.argtypes = [i32]
@@ -358,3 +362,16 @@ def dma_cache_decode(shape, n_rows, k, softmax_scale, q, q_stride, pages, block_
     _check(lib().dma_cache_decode(ctypes.byref(shape), _i32(n_rows), _i32(k), float(softmax_scale), _ptr(q), int(q_stride),
                                   _ptr(pages), _ptr(block_table), _ptr(row_req), _ptr(row_len), _ptr(o), _ptr(lse),
                                   _ptr(kept), _ptr(ws), int(ws_bytes), _stream(stream)), "dma_cache_decode")
+
+
+def dma_cache_decode_prefix_bytes(shape, n_rows, k, n_prefixes, max_prefix=0):
+    return int(lib().dma_cache_decode_prefix_bytes(ctypes.byref(shape), _i32(n_rows), _i32(k), _i32(n_prefixes), _i32(max_prefix)))
+
+
+def dma_cache_decode_prefix(shape, n_rows, k, softmax_scale, q, q_stride, pages, block_table, row_req, row_len, n_prefixes,
+                            max_prefix, prefix_req, prefix_len, req_prefix, o, lse, ws, ws_bytes, stream=None):
+    _check(lib().dma_cache_decode_prefix(ctypes.byref(shape), _i32(n_rows), _i32(k), float(softmax_scale), _ptr(q),
+                                         int(q_stride), _ptr(pages), _ptr(block_table), _ptr(row_req), _ptr(row_len),
+                                         _i32(n_prefixes), _i32(max_prefix), _ptr(prefix_req), _ptr(prefix_len),
+                                         _ptr(req_prefix), _ptr(o), _ptr(lse), _ptr(ws), int(ws_bytes), _stream(stream)),
+           "dma_cache_decode_prefix")

@@ -438,6 +438,39 @@ int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, fl
                              (hipStream_t)stream);
 }
 
+// (more prefixes than there can be requests have no use)
+static int check_decode_prefix(const dma_cache_shape* shape, int32_t n_rows, int32_t k, int32_t n_prefixes, int32_t max_prefix) {
+  int rc = check_rows(shape, n_rows);
+  if (rc != DMA_OK) return rc;
+  if (n_prefixes < 0 || max_prefix < 0) return DMA_EINVAL;
+  if (n_prefixes > CACHE_REQS_MAX) return DMA_EUNSUPPORTED;
+  return check_cache_decode(shape, n_rows + n_prefixes, k);
+}
+
+size_t dma_cache_decode_prefix_bytes(const dma_cache_shape* shape, int32_t n_rows, int32_t k, int32_t n_prefixes,
+                                     int32_t max_prefix) {
+  if (check_decode_prefix(shape, n_rows, k, n_prefixes, max_prefix) != DMA_OK) return 0;
+  return cache_decode_prefix_bytes(*shape, n_rows, k, n_prefixes, max_prefix);
+}
+
+int dma_cache_decode_prefix(const dma_cache_shape* shape, int32_t n_rows, int32_t k, float softmax_scale, const void* q,
+                            int64_t q_stride, const void* pages, const int32_t* block_table, const int32_t* row_req,
+                            const int32_t* row_len, int32_t n_prefixes, int32_t max_prefix, const int32_t* prefix_req,
+                            const int32_t* prefix_len, const int32_t* req_prefix, void* o, float* lse, void* ws,
+                            size_t ws_bytes, void* stream) {
+  int rc = check_decode_prefix(shape, n_rows, k, n_prefixes, max_prefix);
+  if (rc != DMA_OK) return rc;
+  if (softmax_scale < 0.f || softmax_scale != softmax_scale || bad_rows(*shape, q_stride, shape->H_q)) return DMA_EINVAL;
+  if (bad_prefixes(shape, n_rows, row_req, n_prefixes, prefix_len, req_prefix) || (n_prefixes > 0 && !prefix_req)) return DMA_EINVAL;
+  if (n_rows == 0) return DMA_OK;
+  if (!q || !pages || !block_table || !row_len || !o || !lse) return DMA_EINVAL;
+  if (!aligned16(q) || !aligned16(pages) || !aligned16(o) || !aligned16(ws)) return DMA_EINVAL;
+  if (!ws || ws_bytes < cache_decode_prefix_bytes(*shape, n_rows, k, n_prefixes, max_prefix)) return DMA_EWORKSPACE;
+  const float scale = softmax_scale > 0.f ? softmax_scale : 1.0f / sqrtf((float)shape->d);
+  return launch_cache_decode_prefix(*shape, n_rows, k, scale, q, q_stride, pages, block_table, row_req, row_len, n_prefixes,
+                                    max_prefix, prefix_req, prefix_len, req_prefix, o, lse, ws, (hipStream_t)stream);
+}
+
 void dma_profile_events(void** events) { dma::g_stage_events = events; }
 
 const char* dma_strerror(int status) {
@@ -445,7 +478,7 @@ const char* dma_strerror(int status) {
     case DMA_OK: return "ok";
     case DMA_EINVAL: return "invalid argument (null or misaligned pointer, non-positive size, H_q % H_kv != 0)";
     case DMA_EUNSUPPORTED: return "unsupported configuration (d must be 64, 128 or 256 -- cross-head scores: 64 or 128 --, dtype bf16 or f32; cross-head scores: at most 32 q-heads; bf16 attention: Q, K, V at most 4 GiB each, fewer than 2^24 tokens; paged cache: pages of 16 to 256 tokens, at most 4096 requests, 2^30 tokens, 2^28 rows)";
-    case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes, dma_cache_decode_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
+    case DMA_EWORKSPACE: return "workspace missing or too small (dma_workspace_bytes, dma_decode_kept_bytes, dma_cache_decode_bytes, dma_cache_decode_prefix_bytes), or the shape needs more than the library-owned scratch of dma_decode_static";
     case DMA_EHIP: return "HIP launch failed";
     default: return "unknown status";
   }

@@ -59,5 +59,10 @@ size_t cache_decode_bytes(const dma_cache_shape& s, int n_rows, int k);
 int launch_cache_decode(const dma_cache_shape& s, int n_rows, int k, float scale, const void* q, long q_stride,
                         const void* pages, const int32_t* table, const int32_t* row_req, const int32_t* row_len, void* o,
                         float* lse, int32_t* kept, void* ws, hipStream_t st);
+size_t cache_decode_prefix_bytes(const dma_cache_shape& s, int n_rows, int k, int n_prefixes, int max_prefix);
+int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, float scale, const void* q, long q_stride,
+                               const void* pages, const int32_t* table, const int32_t* row_req, const int32_t* row_len,
+                               int n_prefixes, int max_prefix, const int32_t* prefix_req, const int32_t* prefix_len,
+                               const int32_t* req_prefix, void* o, float* lse, void* ws, hipStream_t st);
 
 }  // namespace dma

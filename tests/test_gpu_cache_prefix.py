@@ -1,0 +1,275 @@
+"""dma_cache_decode_prefix on the GPU against the oracle's plain loops over all of a row's keys, prefix first."""
+from __future__ import annotations
+
+import numpy as np
+import pytest
+import torch
+
+from cache_harness import GpuCache, f64, normal
+from oracle import cache_oracle as co
+from paper_2508_02124_amd import binding as B
+from test_gpu_cache import fill, request_slots
+
+pytestmark = pytest.mark.gpu
+
+
+def ints(dev, values):
+    return torch.tensor(values, dtype=torch.int32, device=dev)
+
+
+class Shared:
+    """A cache whose first requests hold prefixes (their lengths `pre`) and whose others have `lens` tokens of their own behind prefix
+    of[i] (-1: none)."""
+
+    def __init__(self, dev, pre, lens, of, ps, H_q, H_kv, d, dtype="bf16", z="ordinary", seed=31):
+        every = list(pre) + list(lens)
+        self.pre, self.lens, self.of, self.n_pre = list(pre), list(lens), list(of), len(pre)
+        self.cache = GpuCache(dev, len(every), sum(-(-n // ps) for n in every) + 2, -(-max(every) // ps), ps, H_q, H_kv, d, dtype)
+        fill(self.cache, every, seed, z)
+        self.req_prefix = ints(dev, [-1] * self.n_pre + self.of)
+        self.prefix_req, self.prefix_len = ints(dev, list(range(self.n_pre))), ints(dev, self.pre)
+        self.held = {}
+
+    def row(self, i, n):
+        """(request, length) of request i of those behind prefixes"""
+        return self.n_pre + i, n
+
+    def decode(self, q, k, req, length, scale=0.0, max_prefix=0, n_pre=None, table=None, stream=None):
+        c, n = self.cache, q.shape[0]
+        n_pre = self.n_pre if n_pre is None else n_pre
+        o = torch.full((n, c.H_q, c.d), float("nan"), dtype=c.type, device=c.dev)
+        lse = torch.full((c.H_q, n), float("nan"), device=c.dev)
+        size = B.dma_cache_decode_prefix_bytes(c.shape, n, k, n_pre, max_prefix)
+        ws = torch.full((size + 256,), 0xFF, dtype=torch.uint8, device=c.dev)
+        B.dma_cache_decode_prefix(c.shape, n, k, scale, q, q.stride(0), c.pages, c.table if table is None else table, req, length, n_pre,
+                                  max_prefix, self.prefix_req, self.prefix_len, self.req_prefix, o, lse, ws, size, stream)
+        assert (ws[size:] == 0xFF).all()
+        return o, lse
+
+    def values(self, b, n):
+        """K, V, z of the first n tokens of request b, as the cache holds them"""
+        if b not in self.held:
+            t = torch.from_numpy(request_slots(self.cache, b).astype(np.int32)).to(self.cache.dev)
+            c = self.cache
+            self.held[b] = tuple(f64(x) for x in c.read(t)) if len(t) else (np.zeros((0, c.H_kv, c.d)), np.zeros((0, c.H_kv, c.d)), np.zeros((c.H_q, 0)))
+        K, V, z = self.held[b]
+        return K[:n], V[:n], z[:, :n]
+
+    def keys(self, b, n):
+        """What a row of request b with n keys of its own sees."""
+        p = int(self.req_prefix[b]) if 0 <= b < self.cache.n_reqs else -1
+        parts = []
+        if n > 0 and 0 <= p < self.n_pre:
+            parts.append(self.values(int(self.prefix_req[p]), int(self.prefix_len[p])))
+        parts.append(self.values(b if 0 <= b < self.cache.n_reqs else 0, n))
+        return [np.concatenate(x, axis) for x, axis in zip(zip(*parts), (0, 0, 1))]
+
+    def check(self, q, k, rows, got, scale=None):
+        """The bound of test_gpu_cache.check_rows; a weight is also split into two terms of 8 bits (three for fp32 values): 2^-16 (2^-24)
+        of it at most."""
+        c = self.cache
+        o, lse = f64(got[0]), f64(got[1])
+        scale = c.d ** -0.5 if scale is None else scale
+        half, u, split = torch.finfo(c.type).eps / 2, 2.0 ** -24, 2.0 ** -16 if c.type == torch.bfloat16 else 2.0 ** -24
+        for r, (b, n) in enumerate(rows):
+            K, V, z = self.keys(b, n)
+            ro, rl, rk = co.decode_row(f64(q)[r], K, V, z, k, scale)
+            for h in range(c.H_q):
+                if np.isneginf(rl[h]):
+                    assert np.isneginf(lse[h, r]) and (o[r, h] == 0).all(), (r, h)
+                    continue
+                g, use = h // (c.H_q // c.H_kv), rk[h][~np.isneginf(z[h, rk[h]])]
+                zu = z[h, use]
+                p = np.exp(K[use, g] @ f64(q)[r, h] * scale + zu - rl[h])
+                E = (c.d + 4) * u * (np.abs(K[use, g]) @ np.abs(f64(q)[r, h]) * scale + np.where(zu > -1e30, np.abs(zu), 0.0)).max()
+                w = 2 * E + 2.0 ** -20 + (len(use) + 16) * u
+                bound = (w + split) * (p @ np.abs(V[use, g])) + half * np.abs(ro[h]) * (1 + w + split)
+                assert (np.abs(o[r, h] - ro[h]) <= bound + 1e-37).all(), (r, h, np.abs(o[r, h] - ro[h]).max(), bound.min())
+                assert abs(lse[h, r] - rl[h]) <= w + 2.0 ** -22 * abs(rl[h]), (r, h, lse[h, r], rl[h])
+
+
+CASES = [  # prefixes, own lengths, window
+    ((16,), (1, 15, 16, 17), 8), ((1, 257), (40, 1, 3, 255, 256), 64), ((1023,), (3, 700), 5000), ((31, 0, 33), (5, 6, 7, 8), 32),
+    ((4100,), (515, 90), 1024), ((2049, 513), (1025, 2), 1)]
+
+
+@pytest.mark.parametrize("kind", ["ordinary", "equal", "levels", "outlier", "wide", "signed", "masked"])
+@pytest.mark.parametrize("pre,lens,k", CASES)
+def test_kept_sets_and_outputs(gpu, kind, pre, lens, k):
+    print(f"[case] prefix {kind} {pre} {lens} k={k}", flush=True)
+    of = [(i * 7 + 1) % (len(pre) + 1) - 1 for i in range(len(lens))]
+    s = Shared(gpu, pre, lens, of, 16 if max(pre) < 2000 else 64, 4, 2, 64, z=kind)
+    rows = [s.row(i, n) for i, n in enumerate(lens)]
+    q = normal(gpu, 5, len(rows), 4, 64).to(s.cache.type)
+    got = s.decode(q, k, ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows]))
+    s.check(q, k, rows, got)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("H_q,H_kv,d,ps", [(3, 1, 64, 16), (8, 2, 128, 32), (6, 6, 256, 64), (16, 1, 128, 128), (5, 5, 64, 256)])
+def test_heads_types_and_drafts(gpu, dtype, H_q, H_kv, d, ps):
+    """Several rows of a request, rows that see nothing, requests without a prefix, queries inside a projection's output, a scale of their
+    own, a prefix shorter than the request that holds it."""
+    print(f"[case] prefix {dtype} {H_q}/{H_kv} d={d} ps={ps}", flush=True)
+    s = Shared(gpu, (700, 130), (290, 1, 33, 0, 64), (0, 1, -1, 0, 0), ps, H_q, H_kv, d, dtype, seed=77)
+    s.prefix_len[1] = 99
+    rows = [s.row(0, 290), s.row(0, 289), s.row(0, 100), s.row(1, 1), (-1, 9), s.row(2, 33), s.row(2, 0), s.row(3, 0), s.row(4, 64), s.row(4, 1),
+            (0, 700), (99, 5)]
+    fused = normal(gpu, 6, len(rows), H_q + 2 * H_kv, d).to(s.cache.type)
+    q = fused[:, :H_q]
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    seen = [(b, n if 0 <= b < 7 else 0) for b, n in rows]
+    for k, scale in ((300, 0.0), (1000, 0.25), (720, 0.0)):
+        s.check(q, k, seen, s.decode(q, k, req, length, scale), scale or None)
+
+
+@pytest.mark.parametrize("n_rows", [1, 2, 15, 31, 32, 33, 64, 65, 100, 200])
+def test_numbers_of_rows(gpu, n_rows):
+    """Groups of a prefix of every size, in no order among the rows."""
+    print(f"[case] prefix rows {n_rows}", flush=True)
+    rng = np.random.default_rng(n_rows)
+    lens, of = [int(x) for x in rng.integers(1, 60, n_rows)], [int(x) for x in rng.integers(-1, 3, n_rows)]
+    if n_rows > 60:
+        of = [0 if x < 2 else x for x in of]
+    s = Shared(gpu, (520, 77, 300), lens, of, 16, 4, 2, 64, seed=n_rows)
+    order = rng.permutation(n_rows)
+    rows = [s.row(int(i), lens[i]) for i in order]
+    q = normal(gpu, 5, n_rows, 4, 64).to(s.cache.type)
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    for k in (50, 400):
+        got = s.decode(q, k, req, length)
+        s.check(q, k, rows, got)
+    # a row's result does not depend on who else is there
+    one = s.decode(q[-1:], k, req[-1:], length[-1:])
+    assert torch.equal(one[1][:, 0], got[1][:, -1]) or (one[1][:, 0] - got[1][:, -1]).abs().max() < 1e-5
+
+
+@pytest.mark.parametrize("kind", ["ordinary", "levels", "equal"])
+@pytest.mark.parametrize("pre,lens,k", [((30000,), (13000, 100, 20), 1500), ((12289, 12288), (12289, 5), 12300), ((70001,), (3, 4), 9000),
+                                        ((20000,), (16000,), 30080)])
+def test_long_prefixes_and_long_rows(gpu, kind, pre, lens, k):
+    print(f"[case] prefix long {kind} {pre} {lens} k={k}", flush=True)
+    s = Shared(gpu, pre, lens, [i % len(pre) for i in range(len(lens))], 64, 2, 1, 64, z=kind, seed=8)
+    rows = [s.row(i, n) for i, n in enumerate(lens)] + [s.row(0, 1)]
+    q = normal(gpu, 5, len(rows), 2, 64).to(s.cache.type)
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    for max_prefix, max_len in ((0, 0), (max(pre), max(lens)), (7, 7)):   # (bounds that hold, none, and bounds that do not hold)
+        s.cache.shape.max_len = max_len
+        s.check(q, k, rows, s.decode(q, k, req, length, max_prefix=max_prefix))
+
+
+def test_no_prefixes_and_rows_without_a_list_of_requests(gpu):
+    s = Shared(gpu, (100,), (60, 17, 5), (0, 0, -1), 16, 4, 2, 128)
+    q = normal(gpu, 5, 4, 4, 128).to(s.cache.type)
+    rows = [(b, n) for b, n in enumerate([100, 60, 17, 5])]
+    got = s.decode(q, 40, None, s.cache.lens)                   # row r is request r: also the one that holds the prefix
+    s.check(q, 40, rows, got)
+    plain = s.cache.decode(q, 40, None, s.cache.lens)
+    s.prefix_req = s.prefix_len = s.req_prefix = None
+    o, lse = s.decode(q, 40, None, s.cache.lens, n_pre=0)
+    half = torch.finfo(torch.bfloat16).eps
+    assert (o.float() - plain[0].float()).abs().max() <= half * plain[0].float().abs().max() and torch.allclose(lse, plain[1], atol=1e-5, rtol=0)
+
+
+def test_masked_keys_and_numbers_that_are_none(gpu):
+    """A key that a row does not keep, or whose score is -infinity, counts for nothing, whatever its K and V hold; one that it keeps makes
+    the channels of its block NaN, for the rows that keep it."""
+    pre, own, ps, H_q, d = 40, (20, 3, 1), 16, 2, 128
+    s = Shared(gpu, (pre,), own, (0, 0, 0), ps, H_q, 1, d)
+    c = s.cache
+    at = lambda b: torch.from_numpy(request_slots(c, b).astype(np.int32)).to(gpu)
+    z = torch.linspace(2.0, 1.0, pre, device=gpu).expand(H_q, pre).contiguous()     # the prefix's keys in falling order
+    K, V = normal(gpu, 1, pre, 1, d).to(c.type), normal(gpu, 2, pre, 1, d).to(c.type)
+    K[5], V[5], V[6], K[7] = float("nan"), float("inf"), float("nan"), float("inf")
+    z[:, 5:8] = -float("inf")
+    V[30, 0, 40] = float("nan")                                                     # channels 32 to 63
+    K[33] = float("inf")                                                            # all of a row that keeps it
+    c.append(K, V, at(0), z=z)
+    for b, n in enumerate(own):
+        c.append(normal(gpu, 3, n, 1, d).to(c.type), normal(gpu, 4, n, 1, d).to(c.type), at(1 + b), z=torch.full((H_q, n), 5.0, device=gpu))
+    q = normal(gpu, 4, 3, H_q, d).to(c.type)
+    req, length = ints(gpu, [1, 2, 3]), ints(gpu, own)
+    # window 30: prefix keys by rank 0 .. (three of the 40 are out of the ranking's front): row 0 keeps 10, row 1 27, row 2 29
+    o, lse = (f64(x) for x in s.decode(q, 30, req, length))
+    kept = {0: 10, 1: 27, 2: 29}
+    ranked = [j for j in range(pre) if not 5 <= j < 8]
+    for r in range(3):
+        mine = ranked[:kept[r]]
+        nan = np.zeros(d, bool)
+        nan[32:64] = 30 in mine
+        assert (np.isnan(o[r]) == nan[None]).all() and np.isfinite(lse[:, r]).all(), r
+    o, lse = (f64(x) for x in s.decode(q, 36, req, length))       # row 0 keeps 16 of them, the others 33 and 35 with key 30 and key 33
+    assert np.isfinite(o[0]).all() and np.isnan(o[1:]).all() and np.isnan(lse[:, 1:]).all() and np.isfinite(lse[:, 0]).all()
+    z[1] = -float("inf")                                          # head 1: the prefix is masked; then the own keys too
+    c.append(K, V, at(0), z=z)
+    o, lse = (f64(x) for x in s.decode(q, 12, req, length))
+    assert np.isfinite(o).all() and np.isfinite(lse).all()
+    gone = torch.full((H_q, 1), -float("inf"), device=gpu)
+    c.append(normal(gpu, 3, 1, 1, d).to(c.type), normal(gpu, 4, 1, 1, d).to(c.type), at(3), z=gone)
+    o, lse = (f64(x) for x in s.decode(q, 12, req, length))
+    assert np.isneginf(lse[1, 2]) and (o[2, 1] == 0).all() and np.isfinite(lse[0]).all() and np.isfinite(o).all()
+
+
+def test_pages_and_prefixes_that_are_not_there(gpu):
+    s = Shared(gpu, (48, 33, 20), (16, 17, 5, 9, 4), (0, 1, 2, 0, 1), 16, 2, 1, 64)
+    s.req_prefix = ints(gpu, [-1] * 3 + [0, 1, 2, 3, -9])         # (requests 3 and 4: prefixes out of range)
+    s.of = [0, 1, 2, -1, -1]
+    table = s.cache.table.clone()
+    table[1, 1], table[3, 0] = 2 ** 31 - 1, -7                    # a page of prefix 1; the only page of the first request
+    rows = [s.row(i, n) for i, n in enumerate(s.lens)]
+    q = normal(gpu, 5, 5, 2, 64).to(s.cache.type)
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    for k in (10, 100):
+        o, lse = s.decode(q, k, req, length, table=table)
+        for r in (0, 1):
+            assert (o[r] == 0).all() and torch.isneginf(lse[:, r]).all(), r
+        s.check(q[2:], k, rows[2:], (o[2:], lse[:, 2:]))
+        # prefixes of requests that are not there, or of lengths that are none, have no tokens
+        s.prefix_req = ints(gpu, [-1, 99, 2])
+        s.prefix_len = ints(gpu, [48, 33, -5])
+        o, lse = s.decode(q, k, req, length)
+        plain = s.cache.decode(q, k, req, length)
+        assert torch.allclose(lse, plain[1], atol=1e-5, rtol=0)
+        s.prefix_req, s.prefix_len = ints(gpu, [0, 1, 2]), ints(gpu, [48, 33, 20])
+        # a length beyond the table ends with it
+        s.prefix_len[0] = 2 ** 31 - 1
+        whole = s.decode(q[3:4] * 0 + q[:1], k, ints(gpu, [3]), ints(gpu, [16]))
+        s.prefix_len[0] = 48
+        s.check(q[:1], k, [s.row(0, 16)], whole)
+
+
+def test_another_stream_and_captured_calls(gpu):
+    """Two captured calls with scratch of their own, replayed in turn with eager ones between them."""
+    s = Shared(gpu, (700, 90), [9 + i for i in range(40)], [i % 3 - 1 for i in range(40)], 16, 4, 2, 128)
+    rows = [s.row(i, 9 + i) for i in range(40)]
+    q, k = normal(gpu, 5, 40, 4, 128).to(s.cache.type), 200
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    ref = s.decode(q, k, req, length)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        got = s.decode(q, k, req, length)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    assert torch.equal(got[0], ref[0]) and torch.equal(got[1], ref[1])
+    c = s.cache
+    size = B.dma_cache_decode_prefix_bytes(c.shape, 40, k, 2, 0)
+    sets = [(torch.zeros_like(ref[0]), torch.zeros_like(ref[1]), torch.zeros(size, dtype=torch.uint8, device=gpu)) for _ in range(2)]
+    call = lambda o, lse, ws: B.dma_cache_decode_prefix(c.shape, 40, k, 0.0, q, q.stride(0), c.pages, c.table, req, length, 2, 0, s.prefix_req,
+                                                        s.prefix_len, s.req_prefix, o, lse, ws, size)
+    graphs = []
+    for x in sets:
+        graphs.append(torch.cuda.CUDAGraph())
+        torch.cuda.synchronize()
+        with torch.cuda.graph(graphs[-1]):
+            call(*x)
+    for i in range(4):
+        q.copy_(normal(gpu, 50 + i, 40, 4, 128).to(s.cache.type))
+        length -= i % 2
+        s.req_prefix[2 + i] = i % 2
+        ref = s.decode(q, k, req, length)
+        for graph, x in zip(graphs, sets):
+            x[0].zero_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(x[0], ref[0]) and torch.equal(x[1], ref[1])

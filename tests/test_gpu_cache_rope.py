@@ -7,8 +7,8 @@ import torch
 
 from oracle import cache_oracle as co, rope_oracle as ro
 from paper_2508_02124_amd import binding as B
-from tests.cache_harness import GpuCache, f64, normal
-from tests.test_gpu_rope import bound, frequencies
+from cache_harness import GpuCache, f64, normal
+from test_gpu_rope import bound, frequencies
 
 pytestmark = pytest.mark.gpu
 

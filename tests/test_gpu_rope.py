@@ -12,7 +12,7 @@ import torch
 
 from oracle import rope_oracle as ro
 from paper_2508_02124_amd import binding as B
-from tests.cache_harness import f64, normal
+from cache_harness import f64, normal
 
 pytestmark = pytest.mark.gpu
 TYPES = {"bf16": (torch.bfloat16, B.DMA_BF16), "f32": (torch.float32, B.DMA_F32)}

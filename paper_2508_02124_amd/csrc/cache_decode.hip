@@ -5,6 +5,41 @@
 
 namespace dma {
 
+// ------------------------------------------------------------------ the kept sets
+template <int S, bool SLICED, int WAVES>
+__global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+  select_block<S, SLICED, false>(c, p, sw, kept, nullptr, (int)blockIdx.x);
+}
+
+template <int S>
+__global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
+  slice_block<S, false>(c, p, sw, kept, nullptr, (int)blockIdx.x);
+}
+
+static void launch_select(const dma_cache_shape& s, const CacheRef& c, const CacheRows& p, const SelectWork& wk, void* ws, int32_t* kept,
+                          hipStream_t st) {
+  const int pairs = p.n_rows * s.H_q;
+  char* base = (char*)ws;
+  SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint4*)(base + wk.off_bounds), wk.room, wk.parts, 0, wk.pairs};
+  auto select = [&](auto width) {
+    constexpr int S = decltype(width)::value;
+    if (wk.parts) {
+      for (; sw.first < pairs; sw.first += wk.pairs) {
+        sw.pairs = pairs - sw.first < wk.pairs ? pairs - sw.first : wk.pairs;
+        cache_select_kernel<S, true, 6><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
+        cache_slice_kernel<S><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
+      }
+    } else if (pairs > 3 * CUS) {
+      cache_select_kernel<S, false, 8><<<(unsigned)pairs, 512, 0, st>>>(c, p, sw, kept);
+    } else {
+      cache_select_kernel<S, false, 6><<<(unsigned)pairs, 512, 0, st>>>(c, p, sw, kept);
+    }
+  };
+  if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
+  else if (s.page_size == 32) select(std::integral_constant<int, 2>{});
+  else select(std::integral_constant<int, 4>{});
+}
+
 // ------------------------------------------------------------------ attention over a part of the list
 // One workgroup per (ch kept keys, row, head).  A key's K (and V) row is held by D / 32 lanes, 32 channels with one scale each; a
 // wave takes 32 keys at a time, all of them requested before the first is used.  Weights are formed with the reference so far; only

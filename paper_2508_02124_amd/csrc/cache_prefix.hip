@@ -1,198 +1,761 @@
 // Decode over the paged 4-bit cache for requests that share prefixes: a row's keys are those of its prefix, then its request's own, and it
 // keeps the min(k, n) best of all of them by (score descending, position ascending).
 //
-// The min(k, P) best of a prefix are listed once for each of its heads, the min(k, m) best of a row's own keys for each row.  What a row
-// keeps are the k best of the two lists together: a cut through each of them.
+// The min(k, P) best of a prefix are listed once for each of its heads; what a row keeps are the k best of that list and its own keys
+// together, a cut through both.  So a prefix is selected from once, and its listed K and V are gathered and decoded once for 32 rows: they are
+// the columns of two matrix products whose weights each row masks by its own cut.  Four launches (five behind long prefixes):
+//   prefix_select_kernel (prefix_slice_kernel)   the lists, and the rows in order of their prefixes
+//   prefix_row_kernel                            a row's cut, and attention to its own keys
+//   prefix_tile_kernel                           attention to the prefix, joined with the row's own
+//   prefix_merge_kernel                          only where the lists are long: the parts of a list together
 #include "cache_attend.h"
 #include "cache_select.h"
 
 namespace dma {
 
-struct PrefixRows {
-  CacheRows own, pre;  // the rows, and the prefixes as rows of their requests
-  const int32_t* req_prefix;
-  const int32_t *list_own, *list_pre;  // [rows or prefixes][H_q][kcap]
-};
+constexpr int TILE_ROWS = 32;
 
-// What a row sees: its own keys (0: no row) and those of its prefix.
+// What a row sees: its own keys (0: no row) and the prefix (-1: none) with its keys, and its request.
 struct PrefixRow {
-  int own, pre, prefix;
+  int own, pre, prefix, req;
 };
-__device__ __forceinline__ PrefixRow prefix_row(const CacheRef& c, const PrefixRows& p, int r) {
-  PrefixRow row = {cache_row(c, p.own, r).n, 0, 0};
-  const int req = p.own.row_req ? p.own.row_req[r] : r;
-  const int prefix = row.own > 0 && p.pre.n_rows ? p.req_prefix[req] : -1;  // (own > 0: the request is in range)
-  if ((uint32_t)prefix < (uint32_t)p.pre.n_rows) {
-    row.prefix = prefix;
-    row.pre = cache_row(c, p.pre, prefix).n;
-  }
-  return row;
-}
-
-// The last key that a row keeps of either list: those before it in (key, place in the list) order, and itself.
+// Rows of one prefix: order[start] .. order[start + count - 1] (count 0: behind the last tile).
+struct PrefixTile {
+  int prefix, start, count, pre;
+};
+// The keys that a row keeps of a list: those before `key`, and those equal to it up to place `last`.
 struct Cut {
   uint32_t key;
-  int pre, own;  // of the keys equal to it, those up to this place of the list (-1: none)
+  int last;
 };
 
-// One workgroup per (row, head): digit by digit, the key at which the lists' common count reaches k; among equal keys the prefix's are first.
-__global__ __launch_bounds__(256) void prefix_cut_kernel(CacheRef c, PrefixRows p, Cut* __restrict__ cuts) {
-  __shared__ uint32_t hist[256];
-  __shared__ uint32_t st[2];
-  __shared__ uint32_t wsum[4];
-  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, tid = threadIdx.x, l = tid & 63, w = tid >> 6;
-  const PrefixRow row = prefix_row(c, p, r);
-  const int k = p.own.k, n_pre = min(k, row.pre), n_own = min(k, row.own);
-  const int32_t* own = p.list_own + (size_t)rh * p.own.kcap;
-  const int32_t* pre = p.list_pre + ((size_t)row.prefix * c.H_q + h) * p.own.kcap;
-  auto key = [&](const int32_t* list, int i) { return score_key(cache_score(c, (uint32_t)list[i], h)); };
-  Cut cut = {NO_KEY, -1, -1};
-  if ((long)n_pre + n_own > k) {
-    uint32_t prefix = 0, need = (uint32_t)k;
-    for (int shift = 24; shift >= 0; shift -= 8) {
-      hist[tid] = 0;
-      __syncthreads();
-      const auto count = [&](uint32_t x) {
-        if (shift == 24 || x >> (shift + 8) == prefix) atomicAdd(&hist[x >> shift & 255u], 1u);
-      };
-      for (int i = tid; i < n_pre; i += 256) count(key(pre, i));
-      for (int i = tid; i < n_own; i += 256) count(key(own, i));
-      __syncthreads();
-      if (tid == 0) {
-        uint32_t run = 0, d = 0;
-        while (run + hist[d] < need) run += hist[d++];
-        st[0] = d;
-        st[1] = need - run;
+struct PrefixArgs {
+  CacheRows own, pre;  // the rows, and the prefixes as rows of the requests that hold them
+  const int32_t* req_prefix;
+  PrefixRow* rows;
+  int32_t* order;
+  PrefixTile* tiles;
+  int32_t *list_pre, *list_own;    // [prefixes or rows][H_q][kcap]
+  uint32_t *keys_pre, *keys_own;   // the listed keys
+  Cut* cuts;                       // [rows][H_q], of the prefix's list
+  float *part_own, *part_pre;      // [rows][H_q] and [rows][H_q][nsplit] of D sums, their reference and their weight
+  int max_tiles, nsplit;
+};
+
+// ------------------------------------------------------------------ the rows by prefix
+// One workgroup: what each row sees, and the rows of each prefix together, in tiles.  (A row's result does not depend on its place in a
+// tile, so the order inside a prefix may be any.)
+__device__ __forceinline__ void group_rows(const CacheRef& c, const PrefixArgs& p) {
+  __shared__ uint32_t cursor[CACHE_REQS_MAX];  // rows of a prefix, then the place of the next one
+  __shared__ uint32_t wsum[8][2];
+  const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, n_prefixes = p.pre.n_rows;
+  constexpr int PER = CACHE_REQS_MAX / 512;
+  for (int i = tid; i < n_prefixes; i += 512) cursor[i] = 0;
+  __syncthreads();
+  for (int r = tid; r < p.own.n_rows; r += 512) {
+    const int req = p.own.row_req ? p.own.row_req[r] : r;
+    PrefixRow row = {cache_row(c, p.own, r).n, 0, -1, req};
+    if (n_prefixes && row.own > 0) {  // (the request is in range)
+      const int prefix = p.req_prefix[req];
+      if ((uint32_t)prefix < (uint32_t)n_prefixes) row.pre = cache_row(c, p.pre, prefix).n;
+      if (row.pre > 0) {
+        row.prefix = prefix;
+        atomicAdd(&cursor[prefix], 1u);
       }
-      __syncthreads();
-      prefix = prefix << 8 | st[0];
-      need = st[1];
-      __syncthreads();
     }
-    cut.key = prefix;
-    // the place of the need-th key equal to it, through the prefix's list and then the row's own
-    uint32_t seen = 0;
-    auto walk = [&](const int32_t* list, int n) {
-      int last = -1;
-      for (int i0 = 0; i0 < n && seen < need; i0 += 256) {
-        const bool eq = i0 + tid < n && key(list, i0 + tid) == cut.key;
-        const unsigned long long m = __ballot(eq);
-        if (l == 0) wsum[w] = (uint32_t)__popcll(m);
-        __syncthreads();
-        uint32_t at = seen;
-        for (int i = 0; i < w; i++) at += wsum[i];
-        at += lanes_before(m);
-        if (eq && at + 1 <= need) last = i0 + tid;
-        seen += wsum[0] + wsum[1] + wsum[2] + wsum[3];
-        __syncthreads();
-      }
-      const int best = (int)last_lane(wave_scan((uint32_t)(last + 1), 0u, [](uint32_t a, uint32_t b) { return max(a, b); }));
-      if (l == 0) wsum[w] = (uint32_t)best;
-      __syncthreads();
-      const int all = (int)max(max(wsum[0], wsum[1]), max(wsum[2], wsum[3])) - 1;
-      __syncthreads();
-      return all;
-    };
-    cut.pre = walk(pre, n_pre);
-    cut.own = walk(own, n_own);
+    p.rows[r] = row;
   }
-  if (tid == 0) cuts[rh] = cut;
+  __syncthreads();
+  if (!n_prefixes) return;
+  uint32_t count[PER], rows = 0, tiles = 0;
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int i = tid * PER + e;
+    count[e] = i < n_prefixes ? cursor[i] : 0u;
+    rows += count[e];
+    tiles += (count[e] + TILE_ROWS - 1) / TILE_ROWS;
+  }
+  const auto add = [](uint32_t a, uint32_t b) { return a + b; };
+  uint32_t row0 = wave_scan(rows, 0u, add), tile0 = wave_scan(tiles, 0u, add);
+  if (l == 63) {
+    wsum[w][0] = row0;
+    wsum[w][1] = tile0;
+  }
+  __syncthreads();
+  row0 -= rows;
+  tile0 -= tiles;
+  uint32_t all_tiles = 0;
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    row0 += i < w ? wsum[i][0] : 0u;
+    tile0 += i < w ? wsum[i][1] : 0u;
+    all_tiles += wsum[i][1];
+  }
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int i = tid * PER + e;
+    if (i >= n_prefixes) break;
+    const int pre = count[e] ? cache_row(c, p.pre, i).n : 0;
+    for (uint32_t a = 0; a < count[e]; a += TILE_ROWS)
+      p.tiles[tile0++] = {i, (int)(row0 + a), (int)min(count[e] - a, (uint32_t)TILE_ROWS), pre};
+    cursor[i] = row0;
+    row0 += count[e];
+  }
+  for (int i = (int)all_tiles + tid; i < p.max_tiles; i += 512) p.tiles[i] = {0, 0, 0, 0};
+  __syncthreads();
+  for (int r = tid; r < p.own.n_rows; r += 512) {
+    const int prefix = p.rows[r].prefix;  // (this thread wrote it)
+    if (prefix >= 0) p.order[atomicAdd(&cursor[prefix], 1u)] = r;
+  }
 }
 
-// One workgroup per (row, head), over both lists; the form of cache_attend_kernel.
-template <typename TQ, int D>
-__global__ __launch_bounds__(256) void prefix_attend_kernel(CacheRef c, PrefixRows p, const Cut* __restrict__ cuts,
-                                                            const TQ* __restrict__ q, long q_stride, TQ* __restrict__ o,
-                                                            float* __restrict__ lse, float scale) {
-  constexpr int LPG = D / 32, NG = 64 / LPG;
-  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, g = h / (c.H_q / c.H_kv);
-  const int tid = threadIdx.x, w = tid >> 6, l = tid & 63, sub = l % LPG, grp = l / LPG;
-  const PrefixRow row = prefix_row(c, p, r);
-  const int k = p.own.k, n_pre = min(k, row.pre), n_own = min(k, row.own);
-  const int32_t* own = p.list_own + (size_t)rh * p.own.kcap;
-  const int32_t* pre = p.list_pre + ((size_t)row.prefix * c.H_q + h) * p.own.kcap;
-  const Cut cut = cuts[rh];
-  const bool bad = (n_own > 0 && own[0] < 0) || (n_pre > 0 && pre[0] < 0);  // a page is out of range: the row sees nothing
+// ------------------------------------------------------------------ the lists
+struct SelectSet {
+  CacheRows rows;
+  SliceWork sw;
+  int32_t* list;
+  uint32_t* keys;
+  int wgs;
+};
+
+// The prefixes' lists, and, where rows may have many keys of their own, theirs.  GROUP: the first workgroup orders the rows.
+template <int S, bool SLICED, bool GROUP>
+__global__ __launch_bounds__(512, 6) void prefix_select_kernel(CacheRef c, PrefixArgs p, SelectSet a, SelectSet b) {
+  int block = (int)blockIdx.x - (GROUP ? 1 : 0);
+  if (GROUP && block < 0) {
+    group_rows(c, p);
+    return;
+  }
+  const bool first = block < a.wgs;
+  if (!first) block -= a.wgs;
+  const CacheRows rows = first ? a.rows : b.rows;
+  const SliceWork sw = first ? a.sw : b.sw;
+  select_block<S, SLICED, true, true>(c, rows, sw, first ? a.list : b.list, first ? a.keys : b.keys, block);
+}
+template <int S>
+__global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, SelectSet a, SelectSet b) {
+  int block = (int)blockIdx.x;
+  const bool first = block < a.wgs;
+  if (!first) block -= a.wgs;
+  const CacheRows rows = first ? a.rows : b.rows;
+  const SliceWork sw = first ? a.sw : b.sw;
+  slice_block<S, true>(c, rows, sw, first ? a.list : b.list, first ? a.keys : b.keys, block);
+}
+
+// ------------------------------------------------------------------ a row's cut, and its own keys
+constexpr int OWN_DIRECT = 2048;  // rows of at most so many keys of their own need no list of them
+
+// NW waves per (row, head).  All keys wait in registers, 64 of the prefix's list or of the row's own to each (longer ones are read again in
+// every pass).  A key that exactly k lie before is looked for by halving between the smallest and the largest: counts are ballots, so a step
+// is a comparison for each register; about log2 of the number of keys are needed (scores that are equal there take all bits, then the
+// places are halved).  LISTED: the row's own keys come from a list of the best of them.
+template <typename TQ, int D, int NW, bool LISTED>
+__global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
+                                                             TQ* __restrict__ o, float* __restrict__ lse, float scale) {
+  constexpr int RC = NW == 1 ? 32 : 16, RO = NW == 1 ? 16 : 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
+  __shared__ uint32_t ids[NW][RO * 64];
+  __shared__ uint32_t sums[2][NW];
+  __shared__ __align__(16) float mo[NW][D];
+  __shared__ float ml[NW][2];
+  const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
+  if (unit >= p.own.n_rows * c.H_kv) return;
+  const int r = unit / c.H_kv, g = unit - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
+  const PrefixRow info = p.rows[r];
+  const int k = p.own.k, n_own = LISTED ? min(k, info.own) : info.own, n_pre = min(k, info.pre);
+  const bool whole = info.prefix < 0;  // (no prefix: the output is complete here)
+  auto finish = [&](int t, float num, float den, float M) {
+    if (whole) {
+      o[(size_t)rh * D + t] = TQ(den == 0.f ? 0.f : num / den);
+      if (t == 0) lse[(size_t)h * p.own.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
+    } else {
+      float* out = p.part_own + (size_t)rh * (D + 2);
+      out[t] = num;
+      if (t == 0) {
+        out[D] = M;
+        out[D + 1] = den;
+      }
+    }
+  };
+  if (n_own <= 0) {
+    for (int t = tid; t < D; t += 64 * NW) finish(t, 0.f, 0.f, -INFINITY);
+    return;
+  }
   Query<TQ> qv;
   qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
-  float m = -INFINITY, lsum = 0.f, acc[32];
+  const int32_t* pages = p.own.table + (size_t)info.req * c.max_pages;
+  const int32_t* list = p.list_own + (size_t)rh * p.own.kcap;
+  const size_t at_pre = ((size_t)max(info.prefix, 0) * c.H_q + h) * p.pre.kcap;
+  const uint32_t* keys_pre = p.keys_pre + at_pre;
+  const int first_pre = n_pre > 0 ? p.list_pre[at_pre] : 0, first_own = LISTED ? list[0] : 0;
+  const int rounds_c = (n_pre + 64 * NW * RC - 1) / (64 * NW * RC), rounds_o = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
+  uint32_t kc[RC], ko[RO], id[RO];
+  bool bad = first_pre < 0 || first_own < 0;  // (a page is out of range: the list says so)
+  auto place_c = [&](int round, int u) { return ((round * RC + u) * NW + w) * 64 + l; };
+  auto place_o = [&](int round, int u) { return ((round * RO + u) * NW + w) * 64 + l; };
+  auto fetch_c = [&](int round) {
 #pragma unroll
-  for (int e = 0; e < 32; e++) acc[e] = 0.f;
-  const long n = bad || !n_own ? 0 : (long)n_pre + n_own;
-  for (long i0 = (long)w * NG; i0 < n; i0 += 4 * NG) {
-    const long i = i0 + grp;
-    const bool of_pre = i < n_pre;
-    const int at = (int)(of_pre ? i : i - n_pre);
-    const uint32_t id = i < n ? (uint32_t)(of_pre ? pre : own)[at] : 0xffffffffu;
-    const uint32_t slot = id < c.n_slots ? id : 0u, place = cache_place(c, slot);
-    const char* page = cache_page(c, slot);
-    const size_t at_g = ((size_t)g << c.shift) + place;
-    const uint4* codes = reinterpret_cast<const uint4*>(page + at_g * D + 16 * sub);
-    const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + c.off_scales + at_g * (D / 16) + sub);
-    const uint4 kr = codes[0], vr = codes[LPG];
-    const float z = reinterpret_cast<const float*>(page + c.off_z)[((size_t)h << c.shift) + place], ks = mx_scale(scales[0]);
-    const uint32_t key = score_key(z);
-    const bool there = id < c.n_slots && z != -INFINITY && (key < cut.key || (key == cut.key && at <= (of_pre ? cut.pre : cut.own)));
-    float s = qv.template dot8<0>(kr.x, ks, 0.f);
-    s = qv.template dot8<1>(kr.y, ks, s);
-    s = qv.template dot8<2>(kr.z, ks, s);
-    s = lanes_sum<LPG>(qv.template dot8<3>(kr.w, ks, s));
-    s = there ? fmaf(s, scale, z) : -INFINITY;
-    const float top = fmaxf(m, over_groups<LPG>(s, [](float a, float b) { return fmaxf(a, b); }));
-    const float ref = top == -INFINITY ? 0.f : top, alpha = weight(m, ref), pv = weight(s, ref), vs = there ? mx_scale(scales[LPG]) : 0.f;
-    m = top;
-    lsum = fmaf(lsum, alpha, pv);
-    const uint32_t code[4] = {vr.x, vr.y, vr.z, vr.w};
+    for (int u = 0; u < RC; u++) {
+      const int i = place_c(round, u);
+      kc[u] = i - l < n_pre ? keys_pre[min(i, n_pre - 1)] : NO_KEY;
+      kc[u] = i < n_pre ? kc[u] : NO_KEY;
+    }
+  };
+  auto fetch_o = [&](int round) {
 #pragma unroll
-    for (int i4 = 0; i4 < 4; i4++) {
-      static_for<4>([&](auto b) {
-        constexpr int Bp = decltype(b)::value;
-        const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i4], vs, Bp);
-        acc[8 * i4 + 2 * Bp] = fmaf(acc[8 * i4 + 2 * Bp], alpha, pv * v[0]);
-        acc[8 * i4 + 2 * Bp + 1] = fmaf(acc[8 * i4 + 2 * Bp + 1], alpha, pv * v[1]);
-      });
+    for (int u = 0; u < RO; u++) {
+      const int i = place_o(round, u), j = min(i, n_own - 1);
+      ko[u] = NO_KEY;
+      id[u] = 0xffffffffu;
+      if (i - l < n_own) {
+        if constexpr (LISTED) {
+          id[u] = (uint32_t)list[j];
+          ko[u] = p.keys_own[(size_t)rh * p.own.kcap + j];
+        } else {
+          const uint32_t page = (uint32_t)pages[j >> c.shift];
+          id[u] = page < (uint32_t)c.n_pages ? page << c.shift | ((uint32_t)j & ((1u << c.shift) - 1u)) : 0xffffffffu;
+        }
+      }
+    }
+    if constexpr (!LISTED) {
+#pragma unroll
+      for (int u = 0; u < RO; u++)
+        if (place_o(round, u) - l < n_own) {
+          bad |= id[u] == 0xffffffffu;
+          ko[u] = score_key(cache_score(c, id[u], h));
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < RO; u++) ko[u] = place_o(round, u) < n_own ? ko[u] : NO_KEY;
+  };
+  fetch_o(0);
+  const bool selects = (long)n_pre + n_own > k;
+  if (selects && n_pre) fetch_c(0);
+  // f(key, place in its list, whether that is the prefix's) for all of this wave's keys
+  auto every = [&](auto f) {
+    for (int round = 0; round < rounds_c; round++) {
+      if (rounds_c > 1) fetch_c(round);
+#pragma unroll
+      for (int u0 = 0; u0 < RC; u0 += 4)
+        if (place_c(round, u0) - l < n_pre) {
+#pragma unroll
+          for (int u = u0; u < u0 + 4; u++) f(kc[u], place_c(round, u), true);
+        }
+    }
+    for (int round = 0; round < rounds_o; round++) {
+      if (rounds_o > 1) fetch_o(round);
+#pragma unroll
+      for (int u0 = 0; u0 < RO; u0 += 4)
+        if (place_o(round, u0) - l < n_own) {
+#pragma unroll
+          for (int u = u0; u < u0 + 4; u++) f(ko[u], place_o(round, u), false);
+        }
+    }
+  };
+  int turn = 0;
+  auto over_waves = [&](uint32_t x, auto op) {
+    if constexpr (NW > 1) {
+      turn ^= 1;
+      if (l == 0) sums[turn][w] = x;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < NW; i++) x = i == 0 ? sums[turn][0] : op(x, sums[turn][i]);
+    }
+    return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
+  };
+  const auto add = [](uint32_t a, uint32_t b) { return a + b; };
+  auto count = [&](auto pred) {
+    uint32_t n = 0;
+    every([&](uint32_t key, int place, bool pre) { n += (uint32_t)__popcll(__ballot(pred(key, place, pre))); });
+    return over_waves(n, add);
+  };
+  uint32_t cut_key = NO_KEY;
+  int cut_pre = -1, cut_own = -1;  // of the keys equal to cut_key, those up to these places are kept
+  if (selects) {
+    uint32_t lo = NO_KEY, hi = 0;
+    every([&](uint32_t key, int, bool pre) {
+      lo = min(lo, key);
+      if (pre || n_pre < k) hi = max(hi, key == NO_KEY ? 0u : key);  // (k of the prefix: the worst of them bounds the cut)
+    });
+    lo = last_lane(wave_scan(lo, NO_KEY, [](uint32_t a, uint32_t b) { return min(a, b); }));
+    hi = last_lane(wave_scan(hi, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }));
+    lo = over_waves(lo, [](uint32_t a, uint32_t b) { return min(a, b); });
+    hi = over_waves(hi, [](uint32_t a, uint32_t b) { return max(a, b); }) + 1u;
+    // fewer than k keys are before lo, at least k before hi
+    uint32_t before_lo = 0, before_hi = count([&](uint32_t key, int, bool) { return key < hi; });
+    while (before_hi != (uint32_t)k && hi - lo > 1u) {
+      const uint32_t mid = lo + (hi - lo) / 2, n = count([&](uint32_t key, int, bool) { return key < mid; });
+      if (n < (uint32_t)k) {
+        lo = mid;
+        before_lo = n;
+      } else {
+        hi = mid;
+        before_hi = n;
+      }
+    }
+    if (before_hi == (uint32_t)k) {
+      cut_key = hi;
+    } else {  // keys equal to lo: the prefix's are first
+      cut_key = lo;
+      const uint32_t need = (uint32_t)k - before_lo;
+      long from = 0, upto = (long)n_pre + n_own;  // fewer than `need` of them are before place `from`, at least as many before `upto`
+      while (upto - from > 1) {
+        const long mid = (from + upto) / 2;
+        const uint32_t n = count([&](uint32_t key, int place, bool pre) { return key == cut_key && (pre ? (long)place : (long)n_pre + place) < mid; });
+        if (n < need) from = mid; else upto = mid;
+      }
+      cut_pre = (int)min(upto, (long)n_pre) - 1;
+      cut_own = (int)(upto - n_pre) - 1;
     }
   }
-  const auto add = [](float a, float b) { return a + b; };
-  lsum = over_groups<LPG>(lsum, add);
-  __shared__ float mo[4][D], ml[4][2];
+  // (a page out of range: nothing is kept)
+  const bool gone = over_waves(__ballot(bad) ? 1u : 0u, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
+  if (!whole && tid == 0) p.cuts[rh] = gone ? Cut{0u, -1} : Cut{cut_key, cut_pre};
+  if (gone) {
+    for (int t = tid; t < D; t += 64 * NW) finish(t, 0.f, 0.f, -INFINITY);
+    return;
+  }
+  // Attention to the kept ones, each wave to its own; the form of cache_attend_kernel.
+  const uint32_t k_off = ((uint32_t)g << c.shift) * D + 16 * sub, z_off = c.off_z + ((uint32_t)h << c.shift) * 4;
+  const uint32_t b_off = c.off_scales + ((uint32_t)g << c.shift) * (D / 16) + sub, page_bytes = (uint32_t)c.page_bytes;
+  float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f, acc[32];
 #pragma unroll
-  for (int e = 0; e < 32; e++) {
-    acc[e] = over_groups<LPG>(acc[e], add);
-    if (grp == 0) mo[w][32 * sub + e] = acc[e];
+  for (int e = 0; e < 32; e++) acc[e] = 0.f;
+  struct Keys {
+    uint4 kr[U], vr[U];
+    uint32_t kb[U], vb[U];
+    float s[U];
+    uint32_t there;
+  };
+  auto take = [&](Keys& x) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float sc = mx_scale(x.kb[u]), zb = x.there >> u & 1 ? x.s[u] : -INFINITY;
+      float s = qv.template dot8<0>(x.kr[u].x, sc, 0.f);
+      s = qv.template dot8<1>(x.kr[u].y, sc, s);
+      s = qv.template dot8<2>(x.kr[u].z, sc, s);
+      s = lanes_sum<LPG>(qv.template dot8<3>(x.kr[u].w, sc, s));
+      x.s[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
+      top = fmaxf(top, x.s[u]);
+    }
+    if (__ballot(top > limit)) {
+      top = fmaxf(m, over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); }));
+      const float alpha = weight(m, top);
+      m = ref = top;
+      limit = top + 5.f;
+      lsum *= alpha;
+#pragma unroll
+      for (int e = 0; e < 32; e++) acc[e] *= alpha;
+    }
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float pv = weight(x.s[u], ref), sc = x.s[u] == -INFINITY ? 0.f : mx_scale(x.vb[u]);
+      lsum += pv;
+      const uint32_t code[4] = {x.vr[u].x, x.vr[u].y, x.vr[u].z, x.vr[u].w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        static_for<4>([&](auto b) {
+          constexpr int B = decltype(b)::value;
+          const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], sc, B);
+          acc[8 * i + 2 * B] = fmaf(pv, v[0], acc[8 * i + 2 * B]);
+          acc[8 * i + 2 * B + 1] = fmaf(pv, v[1], acc[8 * i + 2 * B + 1]);
+        });
+      }
+    }
+  };
+  for (int round = 0; round < rounds_o; round++) {
+    if (rounds_o > 1) fetch_o(round);
+    int n = 0;
+#pragma unroll
+    for (int u = 0; u < RO; u++)
+      if (place_o(round, u) - l < n_own) {
+        const bool keep = ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_o(round, u) <= cut_own);
+        const unsigned long long b = __ballot(keep);
+        if (keep) ids[w][n + (int)lanes_before(b)] = id[u];
+        n += (int)__popcll(b);
+      }
+    asm volatile("" ::: "memory");  // (a wave's LDS accesses are in order: it reads what it wrote)
+    int i0 = 0;
+    auto fetch = [&](Keys& x) {
+      x.there = 0;
+#pragma unroll
+      for (int u = 0; u < U; u++) {
+        const int i = i0 + u * NG + grp;
+        const bool there = i < n;
+        const uint32_t slot = there ? ids[w][min(i, RO * 64 - 1)] : 0u, place = cache_place(c, slot);
+        const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
+        const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
+        const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (b_off + place * (D / 16)));
+        x.kr[u] = codes[0];
+        x.vr[u] = codes[LPG];
+        x.kb[u] = scales[0];
+        x.vb[u] = scales[LPG];
+        x.s[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
+        x.there |= there ? 1u << u : 0u;
+      }
+      i0 += KEYS;
+    };
+    if (n > 0) {
+      Keys even, odd;
+      fetch(even);
+#pragma unroll 1
+      for (;;) {
+        const bool more = i0 < n;
+        fetch(odd);
+        take(even);
+        if (!more) break;
+        const bool again = i0 < n;
+        fetch(even);
+        take(odd);
+        if (!again) break;
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+  lsum = over_groups<LPG>(lsum, [](float a, float b) { return a + b; });
+  const auto across = [](const auto& both) { return __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]); };
+  const auto bits = [](float x) { return __builtin_bit_cast(unsigned, x); };
+#pragma unroll
+  for (int e = 0; e < 16; e++) acc[e] = across(__builtin_amdgcn_permlane32_swap(bits(acc[e]), bits(acc[e + 16]), false, false));
+#pragma unroll
+  for (int e = 0; e < 8; e++) {  // (from here on each row of 16 lanes has sums of its own: a quarter of the channels)
+    acc[e] = across(__builtin_amdgcn_permlane16_swap(bits(acc[e]), bits(acc[e + 8]), false, false));
+    if constexpr (LPG == 2) acc[e] += dpp_move<0x4e>(acc[e]);
+    if constexpr (LPG <= 4) acc[e] += dpp_move<0x124>(acc[e]);
+    acc[e] += dpp_move<0x128>(acc[e]);
+  }
+  if ((l & 15) < LPG) {
+    float4* to = reinterpret_cast<float4*>(&mo[w][32 * sub + 16 * (l >> 5) + 8 * (l >> 4 & 1)]);
+    to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
   }
   if (l == 0) {
     ml[w][0] = m;
     ml[w][1] = lsum;
   }
   __syncthreads();
-  if (tid >= D) return;
-  const float M = fmaxf(fmaxf(ml[0][0], ml[1][0]), fmaxf(ml[2][0], ml[3][0])), mr = M == -INFINITY ? 0.f : M;
-  float num = 0.f, den = 0.f;
+  float M = -INFINITY;
 #pragma unroll
-  for (int i = 0; i < 4; i++) {
-    const float w8 = weight(ml[i][0], mr);
-    num = fmaf(mo[i][tid], w8, num);
-    den = fmaf(ml[i][1], w8, den);
+  for (int i = 0; i < NW; i++) M = fmaxf(M, ml[i][0]);
+  const float mr = M == -INFINITY ? 0.f : M;
+  for (int t = tid; t < D; t += 64 * NW) {
+    float num = 0.f, den = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; i++) {
+      const float w8 = weight(ml[i][0], mr);
+      num = fmaf(mo[i][t], w8, num);
+      den = fmaf(ml[i][1], w8, den);
+    }
+    finish(t, num, den, M);
   }
-  o[(size_t)rh * D + tid] = TQ(den == 0.f ? 0.f : num / den);
-  if (tid == 0) lse[(size_t)h * p.own.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
 }
 
-struct PrefixWork {
-  size_t off_pre, off_own, off_cuts, total;
-  SelectWork pre, own;
+// ------------------------------------------------------------------ the prefix, for 32 rows at a time
+// x as a sum of bf16 values, the next one each time (of what is left).
+template <int N> struct Terms {
+  bf16x8 t[N];
+  __device__ __forceinline__ void split(int i, float x) {
+#pragma unroll
+    for (int n = 0; n < N; n++) {
+      t[n][i] = (__bf16)x;
+      x -= (float)t[n][i];
+    }
+  }
 };
+
+// Joins the weighted sums of parts with references of their own.
+struct Joined {
+  float M, num, den;
+  __device__ __forceinline__ void add(float m, float n, float d) {
+    const float top = fmaxf(M, m), ref = top == -INFINITY ? 0.f : top, a = weight(M, ref), b = weight(m, ref);
+    M = top;
+    num = num * a + n * b;
+    den = den * a + d * b;
+  }
+};
+
+// One workgroup per (tile of 32 rows, head, part of the list); a wave takes 32 listed keys at a time.  Their K rows go from memory to the A operand
+// of S^T = K Q^T (a lane has half a row; which channel is which product's does not matter, as long as Q has them in the same places), the
+// rows' queries are the B operand.  A row is then a column of S^T, in two lanes, which mask it by the row's cut and form the weights with a
+// reference of the row's own.  Its weights are the B operand of O^T += V^T P^T as they lie; V goes through LDS to be transposed.  What the cache
+// holds is exact in bf16; the weights, and fp32 queries, are sums of bf16 terms (two terms of a weight: off by 2^-16 of it; one term, 2^-8,
+// would show beside the rounding of the output; three for fp32, 2^-24).
+template <typename TQ, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
+                                                              TQ* __restrict__ o, float* __restrict__ lse, float scale) {
+  constexpr bool F32 = sizeof(TQ) == 4;
+  constexpr int KS = D / 16, CB = D / 32, NQ = D / 64, NTQ = F32 ? 3 : 1, NTP = F32 ? 3 : 2, PITCH = D + 4;
+  constexpr int TILE_BYTES = 32 * D * 2, OUT_BYTES = 32 * PITCH * 4;
+  __shared__ __align__(16) char mem[NW * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES)];  // a V tile of each wave; in the end its sums
+  __shared__ __align__(16) uint32_t s_key[NW][32];
+  __shared__ __align__(16) float ml[NW][2][32];
+  __shared__ uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers
+  __shared__ uint32_t row_nan[32];
+  const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
+  const int per = p.max_tiles * c.H_kv, sp = unit / per, tg = unit - sp * per;
+  if (sp >= p.nsplit) return;
+  const int t = tg / c.H_kv, g = tg - t * c.H_kv, h = g * G + idx % G;
+  const PrefixTile tile = p.tiles[t];
+  if (tile.count == 0) return;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = l & 31, hh = l >> 5;
+  const int n_keys = min(p.pre.k, tile.pre), step = p.nsplit * NW * 32;
+  const size_t at_pre = ((size_t)tile.prefix * c.H_q + h) * p.pre.kcap;
+  const int32_t* list = p.list_pre + at_pre;
+  const uint32_t* keys = p.keys_pre + at_pre;
+  uint16_t* vt = reinterpret_cast<uint16_t*>(mem + w * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES));
+  int j0 = (sp * NW + w) * 32;
+  uint32_t id = (uint32_t)list[min(j0 + n, n_keys - 1)], key = keys[min(j0 + n, n_keys - 1)];
+  const int row = p.order[tile.start + min(n, tile.count - 1)];
+  if (tid < 32) row_nan[tid] = 0;
+  struct Raw {
+    uint4 k[NQ], v[NQ];
+    uint32_t kb, vb, key;
+  };
+  const uint32_t page_bytes = (uint32_t)c.page_bytes;
+  auto load_bytes = [&](const char* src) -> uint32_t {
+    if constexpr (D == 256) return *reinterpret_cast<const uint32_t*>(src);
+    if constexpr (D == 128) return *reinterpret_cast<const uint16_t*>(src);
+    return *reinterpret_cast<const uint8_t*>(src);
+  };
+  // the keys at j0, and the ids of those behind them
+  auto fetch = [&](Raw& x) {
+    const bool there = j0 + n < n_keys && id < c.n_slots;
+    const uint32_t slot = there ? id : 0u, place = cache_place(c, slot), at = ((uint32_t)g << c.shift) + place;
+    const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
+    const uint4* codes = reinterpret_cast<const uint4*>(page + at * D) + NQ * hh;
+    const char* bytes = page + (c.off_scales + at * (D / 16) + hh * (D / 64));
+#pragma unroll
+    for (int i = 0; i < NQ; i++) {
+      x.k[i] = codes[i];
+      x.v[i] = codes[i + 2 * NQ];
+    }
+    x.kb = load_bytes(bytes);
+    x.vb = load_bytes(bytes + D / 32);
+    x.key = there ? key : NO_KEY;
+    j0 += step;
+    id = (uint32_t)list[min(j0 + n, n_keys - 1)];
+    key = keys[min(j0 + n, n_keys - 1)];
+  };
+  Raw cur;
+  const bool any = j0 < n_keys;
+  int at0 = j0;
+  if (any) fetch(cur);
+  const Cut cut = n < tile.count ? p.cuts[(size_t)row * c.H_q + h] : Cut{0u, -1};
+  // channel 8 s + e of this half of the row: the lane's part of product s
+  Terms<NTQ> qf[KS];
+  {
+    const TQ* src = q + (size_t)row * q_stride + (size_t)h * D + hh * (D / 2);
+#pragma unroll
+    for (int s = 0; s < KS; s++) {
+      if constexpr (F32) {
+#pragma unroll
+        for (int e = 0; e < 8; e++) qf[s].split(e, (float)src[8 * s + e]);
+      } else {
+        qf[s].t[0] = *reinterpret_cast<const bf16x8*>(src + 8 * s);
+      }
+    }
+  }
+  FragOffsets<D> fo;
+  fo.init(l);
+  float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f;
+  uint32_t nan = 0;
+  f32x16 acc[CB];
+#pragma unroll
+  for (int b = 0; b < CB; b++)
+#pragma unroll
+    for (int v = 0; v < 16; v++) acc[b][v] = 0.f;
+  __syncthreads();
+  while (at0 < n_keys) {
+    Raw next;
+    if (j0 < n_keys) fetch(next); else j0 += step;
+    const float z = key_value(cur.key);
+    const bool counts = cur.key != NO_KEY && z != -INFINITY;
+    // V to LDS, a half row of a lane; blocks that are no numbers, and keys that count for nothing, as zeros
+    uint32_t nans = 0;
+#pragma unroll
+    for (int b = 0; b < NQ; b++) {
+      const uint32_t byte = cur.vb >> (8 * b) & 255u;
+      nans |= byte == 255u && counts ? 1u << (NQ * hh + b) : 0u;
+      const float sc = counts && byte != 255u ? mx_scale(byte) : 0.f;
+      const uint32_t code[4] = {cur.v[b].x, cur.v[b].y, cur.v[b].z, cur.v[b].w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        uint4 out;
+        out.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 0));
+        out.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 1));
+        out.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 2));
+        out.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 3));
+        *reinterpret_cast<uint4*>(vt + TileLayout<D>::off(n, (D / 16) * hh + 4 * b + i)) = out;
+      }
+    }
+    if (hh == 0) s_key[w][n] = cur.key;
+    const bool some_nan = __ballot(nans != 0) != 0;
+    if (some_nan) {
+      const uint32_t other = __builtin_amdgcn_permlane32_swap(nans, nans, false, false)[0] | __builtin_amdgcn_permlane32_swap(nans, nans, false, false)[1];
+      if (hh == 0) s_nan[w][n] = other;
+    }
+    asm volatile("" ::: "memory");  // (a wave's LDS accesses are in order: it reads what it wrote)
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; v++) s[v] = 0.f;
+#pragma unroll
+    for (int b = 0; b < NQ; b++) {
+      const float sc = mx_scale(cur.kb >> (8 * b) & 255u);
+      const uint32_t code[4] = {cur.k[b].x, cur.k[b].y, cur.k[b].z, cur.k[b].w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        uint4 a;
+        a.x = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 0));
+        a.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 1));
+        a.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 2));
+        a.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 3));
+#pragma unroll
+        for (int x = NTQ - 1; x >= 0; x--) s = mfma32(__builtin_bit_cast(bf16x8, a), qf[4 * b + i].t[x], s);
+      }
+    }
+    // this lane's keys: 8 (v / 4) + 4 hh + v % 4
+    float top = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < 4; b++) {
+      const uint4 kk = *reinterpret_cast<const uint4*>(&s_key[w][8 * b + 4 * hh]);
+      const uint32_t ks[4] = {kk.x, kk.y, kk.z, kk.w};
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        const float zz = key_value(ks[e]);
+        const bool keep = ks[e] < cut.key || (ks[e] == cut.key && at0 + 8 * b + 4 * hh + e <= cut.last);
+        const float x = keep && zz != -INFINITY && ks[e] != NO_KEY ? fmaf(s[4 * b + e], scale, zz) : -INFINITY;
+        s[4 * b + e] = x;
+        top = fmaxf(top, x);
+      }
+    }
+    if (some_nan) {
+#pragma unroll
+      for (int v = 0; v < 16; v++) nan |= s[v] == -INFINITY ? 0u : s_nan[w][8 * (v / 4) + 4 * hh + v % 4];
+    }
+    top = half_swap_max(top);
+    if (__ballot(top > limit)) {
+      const float now = top > limit ? top : m, alpha = top > limit ? weight(m, now) : 1.f;
+      ref = top > limit ? now : ref;
+      limit = top > limit ? now + 5.f : limit;
+      m = now;
+      lsum *= alpha;
+#pragma unroll
+      for (int b = 0; b < CB; b++)
+#pragma unroll
+        for (int v = 0; v < 16; v++) acc[b][v] *= alpha;
+    }
+    Terms<NTP> pf[2];
+#pragma unroll
+    for (int v = 0; v < 16; v++) {
+      const float pv = weight(s[v], ref);
+      lsum += pv;
+      pf[v / 8].split(v % 8, pv);
+    }
+#pragma unroll
+    for (int x = 0; x < 2; x++)
+#pragma unroll
+      for (int b = 0; b < CB; b++) {
+        const bf16x8 vf = fo.tr_frag(vt, 16 * x, b);
+#pragma unroll
+        for (int y = NTP - 1; y >= 0; y--) acc[b] = mfma32(vf, pf[x].t[y], acc[b]);
+      }
+    asm volatile("" ::: "memory");
+    cur = next;
+    at0 += step;
+  }
+  lsum = half_swap_sum(lsum);
+  if (nan) atomicOr(&row_nan[n], nan);
+  __syncthreads();  // (the tiles have been read)
+  if (hh == 0) {
+    ml[w][0][n] = m;
+    ml[w][1][n] = lsum;
+  }
+  float* out = reinterpret_cast<float*>(vt) + n * PITCH;
+#pragma unroll
+  for (int b = 0; b < CB; b++)
+#pragma unroll
+    for (int v = 0; v < 16; v += 4)
+      *reinterpret_cast<float4*>(out + 32 * b + 2 * v + 4 * hh) = make_float4(acc[b][v], acc[b][v + 1], acc[b][v + 2], acc[b][v + 3]);
+  __syncthreads();
+  for (int i = tid; i < tile.count * D; i += 64 * NW) {
+    const int rr = i / D, ch = i % D, r = p.order[tile.start + rr];
+    const size_t rh = (size_t)r * c.H_q + h;
+    float M = -INFINITY, num = 0.f, den = 0.f;
+#pragma unroll
+    for (int x = 0; x < NW; x++) M = fmaxf(M, ml[x][0][rr]);
+    const float mr = M == -INFINITY ? 0.f : M;
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const float w8 = weight(ml[x][0][rr], mr);
+      num = fmaf(reinterpret_cast<const float*>(mem + x * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES))[rr * PITCH + ch], w8, num);
+      den = fmaf(ml[x][1][rr], w8, den);
+    }
+    if (row_nan[rr] >> (ch / 32) & 1) num = NAN;
+    if (p.nsplit == 1) {
+      const float* own = p.part_own + rh * (D + 2);
+      Joined j = {M, num, den};
+      j.add(own[D], own[ch], own[D + 1]);
+      o[rh * D + ch] = TQ(j.den == 0.f ? 0.f : j.num / j.den);
+      if (ch == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
+    } else {
+      float* to = p.part_pre + (rh * p.nsplit + sp) * (D + 2);
+      to[ch] = num;
+      if (ch == 0) {
+        to[D] = M;
+        to[D + 1] = den;
+      }
+    }
+  }
+}
+
+// The parts of a row's prefix and its own keys together.
+template <typename TQ, int D>
+__global__ __launch_bounds__(D) void prefix_merge_kernel(CacheRef c, PrefixArgs p, TQ* __restrict__ o, float* __restrict__ lse) {
+  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, t = threadIdx.x;
+  if (p.rows[r].prefix < 0) return;  // (complete already)
+  const float* own = p.part_own + (size_t)rh * (D + 2);
+  Joined j = {own[D], own[t], own[D + 1]};
+  for (int i = 0; i < p.nsplit; i++) {
+    const float* x = p.part_pre + ((size_t)rh * p.nsplit + i) * (D + 2);
+    j.add(x[D], x[t], x[D + 1]);
+  }
+  o[(size_t)rh * D + t] = TQ(j.den == 0.f ? 0.f : j.num / j.den);
+  if (t == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
+}
+
+// ------------------------------------------------------------------ host side
+struct PrefixWork {
+  size_t off_rows, off_order, off_tiles, off_list_pre, off_keys_pre, off_list_own, off_keys_own, off_cuts, off_part_own, off_part_pre, total;
+  SelectWork pre, own;
+  bool listed;
+  int max_tiles, nsplit;
+};
+constexpr int tile_waves(int d) { return d == 256 ? 4 : 8; }
 static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n_prefixes, int max_prefix) {
   const int kcap = list_length(s, k);
+  const long cap = (long)s.max_pages * s.page_size;
   const size_t pairs = (size_t)n_rows * s.H_q, pre_pairs = (size_t)n_prefixes * s.H_q;
   PrefixWork wk = {};
   auto take = [&](size_t bytes) { size_t at = wk.total; wk.total = align_up(at + bytes, 256); return at; };
-  wk.off_pre = take(pre_pairs * kcap * 4);
-  wk.off_own = take(pairs * kcap * 4);
+  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > OWN_DIRECT;
+  const long groups = n_prefixes < n_rows ? n_prefixes : n_rows;
+  wk.max_tiles = n_prefixes ? (int)((n_rows + (TILE_ROWS - 1) * groups) / TILE_ROWS) : 0;
+  // a wave takes at most 16 steps of the list: longer ones are cut into parts
+  const int per = 16 * 32 * tile_waves(s.d);
+  wk.nsplit = (kcap + per - 1) / per;
+  wk.off_rows = take((size_t)n_rows * sizeof(PrefixRow));
+  wk.off_order = take((size_t)n_rows * 4);
+  wk.off_tiles = take((size_t)wk.max_tiles * sizeof(PrefixTile));
   wk.off_cuts = take(pairs * sizeof(Cut));
+  wk.off_part_own = take(pairs * (s.d + 2) * 4);
+  wk.off_part_pre = take(n_prefixes && wk.nsplit > 1 ? pairs * wk.nsplit * (s.d + 2) * 4 : 0);
+  wk.off_list_pre = take(pre_pairs * kcap * 4);
+  wk.off_keys_pre = take(pre_pairs * kcap * 4);
+  wk.off_list_own = take(wk.listed ? pairs * kcap * 4 : 0);
+  wk.off_keys_own = take(wk.listed ? pairs * kcap * 4 : 0);
   if (n_prefixes) wk.pre = select_work(s, pre_pairs, kcap, max_prefix, wk.total);
-  wk.own = select_work(s, pairs, kcap, s.max_len, wk.total);
+  if (wk.listed) wk.own = select_work(s, pairs, kcap, s.max_len, wk.total);
   return wk;
 }
 
@@ -208,19 +771,65 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
   const PrefixWork wk = prefix_work(s, n_rows, k, n_prefixes, max_prefix);
   const int kcap = list_length(s, k);
   char* base = (char*)ws;
-  int32_t *list_pre = (int32_t*)(base + wk.off_pre), *list_own = (int32_t*)(base + wk.off_own);
-  Cut* cuts = (Cut*)(base + wk.off_cuts);
-  const PrefixRows p = {{table, row_req, row_len, n_rows, k, kcap}, {table, prefix_req, prefix_len, n_prefixes, k, kcap}, req_prefix,
-                        list_own, list_pre};
-  if (n_prefixes) launch_select(s, c, p.pre, wk.pre, ws, list_pre, st);
-  launch_select(s, c, p.own, wk.own, ws, list_own, st);
-  const unsigned pairs = (unsigned)(n_rows * s.H_q);
-  prefix_cut_kernel<<<pairs, 256, 0, st>>>(c, p, cuts);
+  const PrefixArgs p = {{table, row_req, row_len, n_rows, k, kcap}, {table, prefix_req, prefix_len, n_prefixes, k, kcap}, req_prefix,
+                        (PrefixRow*)(base + wk.off_rows), (int32_t*)(base + wk.off_order), (PrefixTile*)(base + wk.off_tiles),
+                        (int32_t*)(base + wk.off_list_pre), (int32_t*)(base + wk.off_list_own), (uint32_t*)(base + wk.off_keys_pre),
+                        (uint32_t*)(base + wk.off_keys_own), (Cut*)(base + wk.off_cuts), (float*)(base + wk.off_part_own),
+                        (float*)(base + wk.off_part_pre), wk.max_tiles, wk.nsplit};
+  const int pairs = n_rows * s.H_q;
+  // the lists: prefixes first, rows behind them; more pairs than a launch has room for take several
+  auto set_of = [&](const CacheRows& rows, const SelectWork& w, int32_t* list, uint32_t* keys, bool used) {
+    SelectSet x = {rows, {(uint2*)(base + w.off_counts), (uint2*)(base + w.off_listed), (uint4*)(base + w.off_bounds), w.room, w.parts, 0, w.pairs},
+                   list, keys, 0};
+    if (!used) x.sw.pairs = x.sw.parts = 0;
+    return x;
+  };
+  SelectSet a = set_of(p.pre, wk.pre, p.list_pre, p.keys_pre, n_prefixes > 0), b = set_of(p.own, wk.own, p.list_own, p.keys_own, wk.listed);
+  const bool sliced = wk.pre.parts > 0 || wk.own.parts > 0;
+  auto select = [&](auto width) {
+    constexpr int S = decltype(width)::value;
+    bool group = true;
+    const int pre_pairs = n_prefixes * s.H_q;
+    auto left = [](SelectSet& x, int all, int per) {  // pairs of this launch
+      x.sw.pairs = all - x.sw.first < per ? all - x.sw.first : per;
+      x.wgs = x.sw.pairs * (x.sw.parts ? x.sw.parts : 1);
+    };
+    for (;;) {
+      if (n_prefixes) left(a, pre_pairs, wk.pre.pairs);
+      if (wk.listed) left(b, pairs, wk.own.pairs);
+      const unsigned wgs = (unsigned)(a.wgs + b.wgs);
+      if (group) {
+        if (sliced) prefix_select_kernel<S, true, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
+        else prefix_select_kernel<S, false, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
+      } else if (wgs) {
+        if (sliced) prefix_select_kernel<S, true, false><<<wgs, 512, 0, st>>>(c, p, a, b);
+        else prefix_select_kernel<S, false, false><<<wgs, 512, 0, st>>>(c, p, a, b);
+      }
+      SelectSet a2 = a, b2 = b;
+      if (!a.sw.parts) a2.wgs = 0;
+      if (!b.sw.parts) b2.wgs = 0;
+      if (a2.wgs + b2.wgs) prefix_slice_kernel<S><<<(unsigned)(a2.wgs + b2.wgs), 512, 0, st>>>(c, a2, b2);
+      group = false;
+      a.sw.first += a.sw.pairs;
+      b.sw.first += b.sw.pairs;
+      if (a.sw.first >= (n_prefixes ? pre_pairs : 0) && b.sw.first >= (wk.listed ? pairs : 0)) break;
+    }
+  };
+  if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
+  else if (s.page_size == 32) select(std::integral_constant<int, 2>{});
+  else select(std::integral_constant<int, 4>{});
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
   auto go = [&](auto t, auto width) {
     using T = std::remove_pointer_t<decltype(t)>;
-    constexpr int D = decltype(width)::value;
-    prefix_attend_kernel<T, D><<<pairs, 256, 0, st>>>(c, p, cuts, (const T*)q, q_stride, (T*)o, lse, scale);
+    constexpr int D = decltype(width)::value, NW = tile_waves(D);
+    const int G = s.H_q / s.H_kv;
+    const unsigned grid = (unsigned)(((long)n_rows * s.H_kv + 7) / 8 * 8 * G);
+    if (wk.listed) prefix_row_kernel<T, D, 4, true><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    else prefix_row_kernel<T, D, 4, false><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    if (!n_prefixes) return;
+    const unsigned tiles = (unsigned)(((long)wk.max_tiles * s.H_kv * wk.nsplit + 7) / 8 * 8 * G);
+    prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    if (wk.nsplit > 1) prefix_merge_kernel<T, D><<<(unsigned)pairs, D, 0, st>>>(c, p, (T*)o, lse);
   };
   auto types = [&](auto width) {
     if (s.dtype == DMA_BF16) go((__bf16*)nullptr, width); else go((float*)nullptr, width);

@@ -159,8 +159,9 @@ __device__ __forceinline__ uint32_t chunk_offsets(const uint32_t* counts, int w,
   return inc - sum + (i > 0 ? x.x : 0u) + (i > 1 ? x.y : 0u) + (i > 2 ? x.z : 0u);
 }
 
-template <int NT, int R, int S, bool LONG>
-__device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& row, int h, int kk, int32_t* list, SelectShared<NT>& m) {
+// KEYS: the listed keys go to `keys`, at the same places.
+template <int NT, int R, int S, bool LONG, bool KEYS>
+__device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& row, int h, int kk, int32_t* list, uint32_t* keys, SelectShared<NT>& m) {
   using M = SelectShared<NT>;
   constexpr int NW = M::NW, NEAR = M::NEAR, STEP = 4;
   static_assert(NW == 8 && R <= 32 && R % STEP == 0, "");
@@ -266,7 +267,11 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
         for (int u = u0; u < u0 + STEP; u++) {
           const unsigned long long k = __ballot(keeps(key[u], u));
           const int32_t x = run.slot(c, chunk(round, u), u, l);
-          if (keeps(key[u], u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(k)] = x;
+          if (keeps(key[u], u)) {
+            const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(k);
+            list[to] = x;
+            if constexpr (KEYS) keys[to] = key[u];
+          }
         }
         __builtin_amdgcn_sched_barrier(0);
       }
@@ -384,7 +389,11 @@ __device__ __forceinline__ void select_row(const CacheRef& c, const CacheRow& ro
           const uint32_t first = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2));
           const uint32_t eq = (uint32_t)__builtin_amdgcn_readlane((int)at_eq, 2 * u + (w >> 2)) + lanes_before(em);  // equal ones before
           const int32_t x = run.slot(c, chunk(round, u), u, l);
-          if (k32 < thr || (k32 == thr && eq < need_eq)) list[first + lanes_before(bm) + min(eq, need_eq)] = x;
+          if (k32 < thr || (k32 == thr && eq < need_eq)) {
+            const uint32_t to = first + lanes_before(bm) + min(eq, need_eq);
+            list[to] = x;
+            if constexpr (KEYS) keys[to] = k32;
+          }
         }
       });
     }
@@ -562,31 +571,41 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 // WAVES: four workgroups share a compute unit where 64 registers hold what they need (8), at the price of some in scratch, three where
 // they do not (6).  Four are worth it from more lists on than three of each compute unit are (whole calls, us, 6 / 8: 256 lists of
 // 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1; SLICED, 2048 parts of 8192: 115.3 / 115.2).
-template <int S, bool SLICED, int WAVES>
-__global__ __launch_bounds__(512, WAVES) void cache_select_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int part = SLICED ? blockIdx.x / sw.pairs : 0, pair = blockIdx.x - part * sw.pairs, rh = (SLICED ? sw.first : 0) + pair;
+// EITHER: the launch is for rows in slices, but these may be none (no parts: there is no room for what slices tell each other).
+template <int S, bool SLICED, bool KEYS, bool EITHER = false>
+__device__ __forceinline__ void select_block(const CacheRef& c, const CacheRows& p, const SliceWork& sw, int32_t* kept, uint32_t* keys, int block) {
+  const int part = SLICED ? block / sw.pairs : 0, pair = block - part * sw.pairs, rh = (SLICED ? sw.first : 0) + pair;
   const int r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);
-  const int n = row.n, kk = min(p.k, n), parts = SLICED && n > SELECT_SHORT ? sw.parts : 1;
+  const bool slices = SLICED && (!EITHER || sw.parts);
+  const int n = row.n, kk = min(p.k, n), parts = slices && n > SELECT_SHORT ? sw.parts : 1;
   if (part && n <= SELECT_SHORT) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
   if (kk == n) {  // (a page out of range anywhere: none is kept)
     bool bad = false;
     for (long long j = tid; j << c.shift < n; j += 512) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;
     const int there = __syncthreads_or(bad) ? 0 : n;
-    for (long long j = part * 512 + tid; j < p.kcap; j += parts * 512) list[j] = j < there ? (int32_t)cache_slot(c, row, (int)j) : -1;
+    for (long long j = part * 512 + tid; j < (KEYS ? n : p.kcap); j += parts * 512) {
+      const int32_t slot = j < there ? (int32_t)cache_slot(c, row, (int)j) : -1;
+      list[j] = slot;
+      if constexpr (KEYS) keys[(size_t)rh * p.kcap + j] = score_key(cache_score(c, (uint32_t)slot, h));
+    }
     return;
   }
   __shared__ SelectShared<512> m;
-  if (n <= SELECT_SHORT) select_row<512, SELECT_REGS, S, false>(c, row, h, kk, list, m);
-  else if constexpr (SLICED) list_slices<S>(c, row, h, kk, pair, part, sw, m);
-  else select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
+  keys += KEYS ? (size_t)rh * p.kcap : 0;
+  if (n <= SELECT_SHORT) select_row<512, SELECT_REGS, S, false, KEYS>(c, row, h, kk, list, keys, m);
+  else if (slices) {
+    if constexpr (SLICED) list_slices<S>(c, row, h, kk, pair, part, sw, m);
+  } else if constexpr (!SLICED || EITHER) {
+    select_row<512, SELECT_REGS, S, true, KEYS>(c, row, h, kk, list, keys, m);
+  }
 }
 
-template <int S>
-__global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRows p, SliceWork sw, int32_t* kept) {
-  const int part = blockIdx.x / sw.pairs, pair = blockIdx.x - part * sw.pairs, rh = sw.first + pair, r = rh / c.H_q, h = rh - r * c.H_q;
+template <int S, bool KEYS>
+__device__ __forceinline__ void slice_block(const CacheRef& c, const CacheRows& p, const SliceWork& sw, int32_t* kept, uint32_t* keys, int block) {
+  const int part = block / sw.pairs, pair = block - part * sw.pairs, rh = sw.first + pair, r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   uint2 cnt = sw.counts[(size_t)pair * SLICES_MAX + l];  // lane s: of slice s
   const uint4 bounds = sw.bounds[pair];
@@ -596,6 +615,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   const int n = row.n, kk = min(p.k, n);
   if (n <= SELECT_SHORT || part * SLICE >= n || kk == n) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
+  keys += KEYS ? (size_t)rh * p.kcap : 0;
   __shared__ SelectShared<512> m;
   __shared__ __align__(16) uint32_t cand[LISTED];
   const int slices = (n - 1) / SLICE + 1, share = sw.room / slices;
@@ -647,7 +667,7 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
   }
   if (n_near > 512) {  // (ties, or nothing found at all)
     __syncthreads();
-    if (part == 0) select_row<512, SELECT_REGS, S, true>(c, row, h, kk, list, m);
+    if (part == 0) select_row<512, SELECT_REGS, S, true, KEYS>(c, row, h, kk, list, keys, m);
     return;
   }
   // The bin's keys with their positions (again from the lists); kept keys of every slice that are before the bin (m.equal).
@@ -708,7 +728,11 @@ __global__ __launch_bounds__(512, 4) void cache_slice_kernel(CacheRef c, CacheRo
       for (int u = 0; u < SLICE_CHUNKS; u++) {
         const unsigned long long b = __ballot(keeps(u));
         const int32_t slot = run.slot(c, slice * SLICE + (u * 8 + w) * 64, u, l);
-        if (keeps(u)) list[(uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b)] = slot;
+        if (keeps(u)) {
+          const uint32_t to = (uint32_t)__builtin_amdgcn_readlane((int)at, 2 * u + (w >> 2)) + lanes_before(b);
+          list[to] = slot;
+          if constexpr (KEYS) keys[to] = key[u];
+        }
         if (u % 4 == 3) __builtin_amdgcn_sched_barrier(0);  // (addresses of all chunks at once would spill)
       }
     };
@@ -753,30 +777,6 @@ inline SelectWork select_work(const dma_cache_shape& s, size_t pairs, int kcap, 
   wk.off_listed = take(wk.parts ? whole * LISTED * 8 : 0);  // (wk.pairs * wk.room are never more)
   wk.off_bounds = take(wk.parts ? most_pairs * 16 : 0);
   return wk;
-}
-
-inline void launch_select(const dma_cache_shape& s, const CacheRef& c, const CacheRows& p, const SelectWork& wk, void* ws, int32_t* kept,
-                          hipStream_t st) {
-  const int pairs = p.n_rows * s.H_q;
-  char* base = (char*)ws;
-  SliceWork sw = {(uint2*)(base + wk.off_counts), (uint2*)(base + wk.off_listed), (uint4*)(base + wk.off_bounds), wk.room, wk.parts, 0, wk.pairs};
-  auto select = [&](auto width) {
-    constexpr int S = decltype(width)::value;
-    if (wk.parts) {
-      for (; sw.first < pairs; sw.first += wk.pairs) {
-        sw.pairs = pairs - sw.first < wk.pairs ? pairs - sw.first : wk.pairs;
-        cache_select_kernel<S, true, 6><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
-        cache_slice_kernel<S><<<(unsigned)(sw.pairs * wk.parts), 512, 0, st>>>(c, p, sw, kept);
-      }
-    } else if (pairs > 3 * CUS) {
-      cache_select_kernel<S, false, 8><<<(unsigned)pairs, 512, 0, st>>>(c, p, sw, kept);
-    } else {
-      cache_select_kernel<S, false, 6><<<(unsigned)pairs, 512, 0, st>>>(c, p, sw, kept);
-    }
-  };
-  if (s.page_size >= 64) select(std::integral_constant<int, 1>{});
-  else if (s.page_size == 32) select(std::integral_constant<int, 2>{});
-  else select(std::integral_constant<int, 4>{});
 }
 
 }  // namespace

@@ -38,7 +38,7 @@ struct PrefixArgs {
   int32_t *list_pre, *list_own;    // [prefixes or rows][H_q][kcap]
   uint32_t *keys_pre, *keys_own;   // the listed keys
   Cut* cuts;                       // [rows][H_q], of the prefix's list
-  float *part_own, *part_pre;      // [rows][H_q] and [rows][H_q][nsplit] of D sums, their reference and their weight
+  float *part_own, *part_pre;      // [rows][H_q] of D sums, their reference and their weight; [rows][H_q][nsplit] of the same and two more
   int max_tiles, nsplit;
 };
 
@@ -150,9 +150,9 @@ constexpr int OWN_DIRECT = 2048;  // rows of at most so many keys of their own n
 // is a comparison for each register; about log2 of the number of keys are needed (scores that are equal there take all bits, then the
 // places are halved).  LISTED: the row's own keys come from a list of the best of them.
 template <typename TQ, int D, int NW, bool LISTED>
-__global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
+__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 || NW < 4 ? 3 : 4) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
                                                              TQ* __restrict__ o, float* __restrict__ lse, float scale) {
-  constexpr int RC = NW == 1 ? 32 : 16, RO = NW == 1 ? 16 : 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
+  constexpr int RC = NW < 4 ? 32 : 16, RO = NW < 4 ? 16 : 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
   __shared__ uint32_t ids[NW][RO * 64];
   __shared__ uint32_t sums[2][NW];
   __shared__ __align__(16) float mo[NW][D];
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
   const PrefixRow info = p.rows[r];
   const int k = p.own.k, n_own = LISTED ? min(k, info.own) : info.own, n_pre = min(k, info.pre);
   const bool whole = info.prefix < 0;  // (no prefix: the output is complete here)
-  auto finish = [&](int t, float num, float den, float M) {
+  auto finish = [&](int t, float num, float den, float M) __attribute__((always_inline)) {
     if (whole) {
       o[(size_t)rh * D + t] = TQ(den == 0.f ? 0.f : num / den);
       if (t == 0) lse[(size_t)h * p.own.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
@@ -188,72 +188,91 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
   const size_t at_pre = ((size_t)max(info.prefix, 0) * c.H_q + h) * p.pre.kcap;
   const uint32_t* keys_pre = p.keys_pre + at_pre;
   const int first_pre = n_pre > 0 ? p.list_pre[at_pre] : 0, first_own = LISTED ? list[0] : 0;
-  const int rounds_c = (n_pre + 64 * NW * RC - 1) / (64 * NW * RC), rounds_o = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
+  const int rounds_o = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
   uint32_t kc[RC], ko[RO], id[RO];
   bool bad = first_pre < 0 || first_own < 0;  // (a page is out of range: the list says so)
-  auto place_c = [&](int round, int u) { return ((round * RC + u) * NW + w) * 64 + l; };
-  auto place_o = [&](int round, int u) { return ((round * RO + u) * NW + w) * 64 + l; };
-  auto fetch_c = [&](int round) {
+  auto place_of = [&](int u) { return (u * NW + w) * 64 + l; };
+  // (all loads of four registers are on their way before the first is used: places behind the end read the last one)
+  auto fetch_c = [&]() __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < RC; u++) {
-      const int i = place_c(round, u);
-      kc[u] = i - l < n_pre ? keys_pre[min(i, n_pre - 1)] : NO_KEY;
-      kc[u] = i < n_pre ? kc[u] : NO_KEY;
+    for (int u0 = 0; u0 < RC; u0 += 4) {
+#pragma unroll
+      for (int u = u0; u < u0 + 4; u++) kc[u] = NO_KEY;
+      if (u0 * NW * 64 < n_pre) {
+#pragma unroll
+        for (int u = u0; u < u0 + 4; u++) kc[u] = keys_pre[min(place_of(u), n_pre - 1)];
+      }
     }
-  };
-  auto fetch_o = [&](int round) {
 #pragma unroll
-    for (int u = 0; u < RO; u++) {
-      const int i = place_o(round, u), j = min(i, n_own - 1);
-      ko[u] = NO_KEY;
-      id[u] = 0xffffffffu;
-      if (i - l < n_own) {
-        if constexpr (LISTED) {
-          id[u] = (uint32_t)list[j];
-          ko[u] = p.keys_own[(size_t)rh * p.own.kcap + j];
-        } else {
-          const uint32_t page = (uint32_t)pages[j >> c.shift];
-          id[u] = page < (uint32_t)c.n_pages ? page << c.shift | ((uint32_t)j & ((1u << c.shift) - 1u)) : 0xffffffffu;
+    for (int u = 0; u < RC; u++) kc[u] = place_of(u) < n_pre ? kc[u] : NO_KEY;
+  };
+  // slot of the own key at place j, of that page, and where its score is
+  auto slot_of = [&](uint32_t page, int j) __attribute__((always_inline)) {
+    const bool out = page >= (uint32_t)c.n_pages;
+    bad |= out;
+    return (out ? 0u : page << c.shift) | ((uint32_t)j & ((1u << c.shift) - 1u));
+  };
+  auto score_at = [&](uint32_t slot) __attribute__((always_inline)) {
+    return reinterpret_cast<const float*>(cache_page(c, slot) + c.off_z) + ((size_t)h << c.shift) + cache_place(c, slot);
+  };
+  auto fetch_o = [&](int round) __attribute__((always_inline)) {
+#pragma unroll
+    for (int u0 = 0; u0 < RO; u0 += 4) {
+#pragma unroll
+      for (int u = u0; u < u0 + 4; u++) {
+        ko[u] = NO_KEY;
+        id[u] = 0;
+      }
+      if ((round * RO + u0) * NW * 64 < n_own) {
+#pragma unroll
+        for (int u = u0; u < u0 + 4; u++) {
+          const int j = min(place_of(round * RO + u), n_own - 1);
+          if constexpr (LISTED) {
+            id[u] = (uint32_t)list[j];
+            ko[u] = p.keys_own[(size_t)rh * p.own.kcap + j];
+          } else {
+            id[u] = (uint32_t)pages[j >> c.shift];
+          }
         }
       }
     }
     if constexpr (!LISTED) {
 #pragma unroll
-      for (int u = 0; u < RO; u++)
-        if (place_o(round, u) - l < n_own) {
-          bad |= id[u] == 0xffffffffu;
-          ko[u] = score_key(cache_score(c, id[u], h));
+      for (int u0 = 0; u0 < RO; u0 += 4)
+        if ((round * RO + u0) * NW * 64 < n_own) {
+#pragma unroll
+          for (int u = u0; u < u0 + 4; u++) {
+            const int j = min(place_of(round * RO + u), n_own - 1);
+            id[u] = slot_of(id[u], j);
+            ko[u] = __float_as_uint(*score_at(id[u]));
+          }
         }
     }
 #pragma unroll
-    for (int u = 0; u < RO; u++) ko[u] = place_o(round, u) < n_own ? ko[u] : NO_KEY;
+    for (int u = 0; u < RO; u++)
+      ko[u] = place_of(round * RO + u) >= n_own ? NO_KEY : LISTED ? ko[u] : score_key(__uint_as_float(ko[u]));
   };
   fetch_o(0);
+  if (!LISTED && rounds_o > 1)
+    for (int j = tid; (long)j << c.shift < n_own; j += 64 * NW) bad |= (uint32_t)pages[j] >= (uint32_t)c.n_pages;
   const bool selects = (long)n_pre + n_own > k;
-  if (selects && n_pre) fetch_c(0);
-  // f(key, place in its list, whether that is the prefix's) for all of this wave's keys
-  auto every = [&](auto f) {
-    for (int round = 0; round < rounds_c; round++) {
-      if (rounds_c > 1) fetch_c(round);
+  if (selects) fetch_c();
+  // f(key, place in its list, whether that is the prefix's) for all of this wave's keys; what the registers do not hold is read again
+  auto every = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-      for (int u0 = 0; u0 < RC; u0 += 4)
-        if (place_c(round, u0) - l < n_pre) {
+    for (int u = 0; u < RC; u++) f(kc[u], place_of(u), true);
 #pragma unroll
-          for (int u = u0; u < u0 + 4; u++) f(kc[u], place_c(round, u), true);
-        }
-    }
-    for (int round = 0; round < rounds_o; round++) {
-      if (rounds_o > 1) fetch_o(round);
-#pragma unroll
-      for (int u0 = 0; u0 < RO; u0 += 4)
-        if (place_o(round, u0) - l < n_own) {
-#pragma unroll
-          for (int u = u0; u < u0 + 4; u++) f(ko[u], place_o(round, u), false);
-        }
+    for (int u = 0; u < RO; u++) f(ko[u], place_of(u), false);
+#pragma unroll 1
+    for (int i = place_of(RC); i < n_pre; i += NW * 64) f(keys_pre[i], i, true);
+#pragma unroll 1
+    for (int i = place_of(RO); i < n_own; i += NW * 64) {
+      if constexpr (LISTED) f(p.keys_own[(size_t)rh * p.own.kcap + i], i, false);
+      else f(score_key(*score_at(slot_of((uint32_t)pages[i >> c.shift], i))), i, false);
     }
   };
   int turn = 0;
-  auto over_waves = [&](uint32_t x, auto op) {
+  auto over_waves = [&](uint32_t x, auto op) __attribute__((always_inline)) {
     if constexpr (NW > 1) {
       turn ^= 1;
       if (l == 0) sums[turn][w] = x;
@@ -264,45 +283,46 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
   };
   const auto add = [](uint32_t a, uint32_t b) { return a + b; };
-  auto count = [&](auto pred) {
-    uint32_t n = 0;
-    every([&](uint32_t key, int place, bool pre) { n += (uint32_t)__popcll(__ballot(pred(key, place, pre))); });
-    return over_waves(n, add);
-  };
+  const auto sum_lanes = [&](uint32_t x) __attribute__((always_inline)) { return over_waves(last_lane(wave_scan(x, 0u, add)), add); };
   uint32_t cut_key = NO_KEY;
   int cut_pre = -1, cut_own = -1;  // of the keys equal to cut_key, those up to these places are kept
   if (selects) {
-    uint32_t lo = NO_KEY, hi = 0;
-    every([&](uint32_t key, int, bool pre) {
-      lo = min(lo, key);
-      if (pre || n_pre < k) hi = max(hi, key == NO_KEY ? 0u : key);  // (k of the prefix: the worst of them bounds the cut)
+    uint32_t least = NO_KEY, most = 0;
+    every([&](uint32_t key, int, bool pre) __attribute__((always_inline)) {
+      least = min(least, key);
+      if (pre || n_pre < k) most = max(most, key + 1u);  // (k of the prefix: the worst of them bounds the cut; NO_KEY + 1 is 0)
     });
-    lo = last_lane(wave_scan(lo, NO_KEY, [](uint32_t a, uint32_t b) { return min(a, b); }));
-    hi = last_lane(wave_scan(hi, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }));
-    lo = over_waves(lo, [](uint32_t a, uint32_t b) { return min(a, b); });
-    hi = over_waves(hi, [](uint32_t a, uint32_t b) { return max(a, b); }) + 1u;
+    least = last_lane(wave_scan(least, NO_KEY, [](uint32_t a, uint32_t b) { return min(a, b); }));
+    most = last_lane(wave_scan(most, 0u, [](uint32_t a, uint32_t b) { return max(a, b); }));
     // fewer than k keys are before lo, at least k before hi
-    uint32_t before_lo = 0, before_hi = count([&](uint32_t key, int, bool) { return key < hi; });
-    while (before_hi != (uint32_t)k && hi - lo > 1u) {
-      const uint32_t mid = lo + (hi - lo) / 2, n = count([&](uint32_t key, int, bool) { return key < mid; });
+    uint32_t lo = over_waves(least, [](uint32_t a, uint32_t b) { return min(a, b); });
+    uint32_t hi = over_waves(most, [](uint32_t a, uint32_t b) { return max(a, b); });
+    uint32_t probe = hi, before_lo = 0;
+    for (;;) {
+      uint32_t n = 0;
+      every([&](uint32_t key, int, bool) __attribute__((always_inline)) { n += key < probe; });
+      n = sum_lanes(n);
+      if (n == (uint32_t)k) break;  // exactly the keys before `probe`
       if (n < (uint32_t)k) {
-        lo = mid;
+        lo = probe;
         before_lo = n;
       } else {
-        hi = mid;
-        before_hi = n;
+        hi = probe;
       }
+      if (hi - lo <= 1u) break;
+      probe = lo + (hi - lo) / 2;
     }
-    if (before_hi == (uint32_t)k) {
-      cut_key = hi;
-    } else {  // keys equal to lo: the prefix's are first
+    cut_key = probe;
+    if (hi - lo <= 1u) {  // keys equal to lo are on both sides: the prefix's are first
       cut_key = lo;
       const uint32_t need = (uint32_t)k - before_lo;
       long from = 0, upto = (long)n_pre + n_own;  // fewer than `need` of them are before place `from`, at least as many before `upto`
       while (upto - from > 1) {
-        const long mid = (from + upto) / 2;
-        const uint32_t n = count([&](uint32_t key, int place, bool pre) { return key == cut_key && (pre ? (long)place : (long)n_pre + place) < mid; });
-        if (n < need) from = mid; else upto = mid;
+        const long middle = (from + upto) / 2;
+        const int before_pre = (int)min(middle, (long)n_pre), before_own = (int)(middle - before_pre);
+        uint32_t n = 0;
+        every([&](uint32_t key, int place, bool pre) __attribute__((always_inline)) { n += (key == lo) & (place < (pre ? before_pre : before_own)); });
+        if (sum_lanes(n) < need) from = middle; else upto = middle;
       }
       cut_pre = (int)min(upto, (long)n_pre) - 1;
       cut_own = (int)(upto - n_pre) - 1;
@@ -327,7 +347,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
     float s[U];
     uint32_t there;
   };
-  auto take = [&](Keys& x) {
+  auto take = [&](Keys& x) __attribute__((always_inline)) {
     float top = -INFINITY;
 #pragma unroll
     for (int u = 0; u < U; u++) {
@@ -365,19 +385,19 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
     }
   };
   for (int round = 0; round < rounds_o; round++) {
-    if (rounds_o > 1) fetch_o(round);
+    if (round) fetch_o(round);
     int n = 0;
 #pragma unroll
     for (int u = 0; u < RO; u++)
-      if (place_o(round, u) - l < n_own) {
-        const bool keep = ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_o(round, u) <= cut_own);
+      if ((round * RO + u) * NW * 64 < n_own) {
+        const bool keep = ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_of(round * RO + u) <= cut_own);
         const unsigned long long b = __ballot(keep);
         if (keep) ids[w][n + (int)lanes_before(b)] = id[u];
         n += (int)__popcll(b);
       }
     asm volatile("" ::: "memory");  // (a wave's LDS accesses are in order: it reads what it wrote)
     int i0 = 0;
-    auto fetch = [&](Keys& x) {
+    auto fetch = [&](Keys& x) __attribute__((always_inline)) {
       x.there = 0;
 #pragma unroll
       for (int u = 0; u < U; u++) {
@@ -402,11 +422,11 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
 #pragma unroll 1
       for (;;) {
         const bool more = i0 < n;
-        fetch(odd);
+        if (more) fetch(odd);
         take(even);
         if (!more) break;
         const bool again = i0 < n;
-        fetch(even);
+        if (again) fetch(even);
         take(odd);
         if (!again) break;
       }
@@ -452,14 +472,21 @@ __global__ __launch_bounds__(64 * NW) void prefix_row_kernel(CacheRef c, PrefixA
 }
 
 // ------------------------------------------------------------------ the prefix, for 32 rows at a time
-// x as a sum of bf16 values, the next one each time (of what is left).
+// Two values, x and y, as sums of bf16 ones: each term is what is left, rounded.
 template <int N> struct Terms {
   bf16x8 t[N];
-  __device__ __forceinline__ void split(int i, float x) {
+  __device__ __forceinline__ void split(int i, float x, float y) {  // (i even)
 #pragma unroll
     for (int n = 0; n < N; n++) {
-      t[n][i] = (__bf16)x;
-      x -= (float)t[n][i];
+      typedef float f32x2 __attribute__((ext_vector_type(2)));
+      const bf16x2 both = __builtin_convertvector((f32x2){x, y}, bf16x2);
+      t[n][i] = both[0];
+      t[n][i + 1] = both[1];
+      if (n + 1 < N) {
+        const uint32_t bits = __builtin_bit_cast(uint32_t, both);
+        x -= __uint_as_float(bits << 16);
+        y -= __uint_as_float(bits & 0xffff0000u);
+      }
     }
   }
 };
@@ -475,6 +502,14 @@ struct Joined {
   }
 };
 
+__device__ __forceinline__ void store4(__bf16* dst, const float* x) {
+  bf16x4 v;
+#pragma unroll
+  for (int e = 0; e < 4; e++) v[e] = (__bf16)x[e];
+  *reinterpret_cast<bf16x4*>(dst) = v;
+}
+__device__ __forceinline__ void store4(float* dst, const float* x) { *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]); }
+
 // One workgroup per (tile of 32 rows, head, part of the list); a wave takes 32 listed keys at a time.  Their K rows go from memory to the A operand
 // of S^T = K Q^T (a lane has half a row; which channel is which product's does not matter, as long as Q has them in the same places), the
 // rows' queries are the B operand.  A row is then a column of S^T, in two lanes, which mask it by the row's cut and form the weights with a
@@ -489,9 +524,11 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   constexpr int TILE_BYTES = 32 * D * 2, OUT_BYTES = 32 * PITCH * 4;
   __shared__ __align__(16) char mem[NW * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES)];  // a V tile of each wave; in the end its sums
   __shared__ __align__(16) uint32_t s_key[NW][32];
+  __shared__ __align__(16) float s_z[NW][32];
   __shared__ __align__(16) float ml[NW][2][32];
-  __shared__ uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers
+  __shared__ __align__(16) uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers
   __shared__ uint32_t row_nan[32];
+  __shared__ float wave_weight[NW][32], row_sum[2][32];
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   const int per = p.max_tiles * c.H_kv, sp = unit / per, tg = unit - sp * per;
   if (sp >= p.nsplit) return;
@@ -550,7 +587,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
     for (int s = 0; s < KS; s++) {
       if constexpr (F32) {
 #pragma unroll
-        for (int e = 0; e < 8; e++) qf[s].split(e, (float)src[8 * s + e]);
+        for (int e = 0; e < 8; e += 2) qf[s].split(e, (float)src[8 * s + e], (float)src[8 * s + e + 1]);
       } else {
         qf[s].t[0] = *reinterpret_cast<const bf16x8*>(src + 8 * s);
       }
@@ -589,7 +626,10 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
         *reinterpret_cast<uint4*>(vt + TileLayout<D>::off(n, (D / 16) * hh + 4 * b + i)) = out;
       }
     }
-    if (hh == 0) s_key[w][n] = cur.key;
+    if (hh == 0) {
+      s_key[w][n] = counts ? cur.key : NO_KEY;  // (one that counts for nothing is behind every cut)
+      s_z[w][n] = z;
+    }
     const bool some_nan = __ballot(nans != 0) != 0;
     if (some_nan) {
       const uint32_t other = __builtin_amdgcn_permlane32_swap(nans, nans, false, false)[0] | __builtin_amdgcn_permlane32_swap(nans, nans, false, false)[1];
@@ -614,24 +654,33 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
         for (int x = NTQ - 1; x >= 0; x--) s = mfma32(__builtin_bit_cast(bf16x8, a), qf[4 * b + i].t[x], s);
       }
     }
-    // this lane's keys: 8 (v / 4) + 4 hh + v % 4
+    // this lane's keys: 8 (v / 4) + 4 hh + v % 4; the row keeps those before its cut, and where it falls among equal ones in this tile, those
+    // up to its place
+    const uint32_t bound = cut.last >= at0 + 31 ? cut.key + 1u : cut.key;
+    const bool among = __ballot(cut.last >= at0 && cut.last < at0 + 31) != 0;
     float top = -INFINITY;
 #pragma unroll
     for (int b = 0; b < 4; b++) {
       const uint4 kk = *reinterpret_cast<const uint4*>(&s_key[w][8 * b + 4 * hh]);
+      const float4 zz = *reinterpret_cast<const float4*>(&s_z[w][8 * b + 4 * hh]);
       const uint32_t ks[4] = {kk.x, kk.y, kk.z, kk.w};
+      const float zs[4] = {zz.x, zz.y, zz.z, zz.w};
 #pragma unroll
       for (int e = 0; e < 4; e++) {
-        const float zz = key_value(ks[e]);
-        const bool keep = ks[e] < cut.key || (ks[e] == cut.key && at0 + 8 * b + 4 * hh + e <= cut.last);
-        const float x = keep && zz != -INFINITY && ks[e] != NO_KEY ? fmaf(s[4 * b + e], scale, zz) : -INFINITY;
-        s[4 * b + e] = x;
-        top = fmaxf(top, x);
+        const float x = fmaf(s[4 * b + e], scale, zs[e]);
+        bool keep = ks[e] < bound;
+        if (among) keep = keep | ((ks[e] == cut.key) & (at0 + 8 * b + 4 * hh + e <= cut.last) & (ks[e] != NO_KEY));
+        s[4 * b + e] = keep ? x : -INFINITY;
+        top = fmaxf(top, s[4 * b + e]);
       }
     }
     if (some_nan) {
 #pragma unroll
-      for (int v = 0; v < 16; v++) nan |= s[v] == -INFINITY ? 0u : s_nan[w][8 * (v / 4) + 4 * hh + v % 4];
+      for (int b = 0; b < 4; b++) {
+        const uint4 nn = *reinterpret_cast<const uint4*>(&s_nan[w][8 * b + 4 * hh]);
+        nan |= (s[4 * b] == -INFINITY ? 0u : nn.x) | (s[4 * b + 1] == -INFINITY ? 0u : nn.y) | (s[4 * b + 2] == -INFINITY ? 0u : nn.z) |
+               (s[4 * b + 3] == -INFINITY ? 0u : nn.w);
+      }
     }
     top = half_swap_max(top);
     if (__ballot(top > limit)) {
@@ -647,10 +696,10 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
     }
     Terms<NTP> pf[2];
 #pragma unroll
-    for (int v = 0; v < 16; v++) {
-      const float pv = weight(s[v], ref);
-      lsum += pv;
-      pf[v / 8].split(v % 8, pv);
+    for (int v = 0; v < 16; v += 2) {
+      const float pv = weight(s[v], ref), pw = weight(s[v + 1], ref);
+      lsum += pv + pw;
+      pf[v / 8].split(v % 8, pv, pw);
     }
 #pragma unroll
     for (int x = 0; x < 2; x++)
@@ -678,29 +727,54 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
     for (int v = 0; v < 16; v += 4)
       *reinterpret_cast<float4*>(out + 32 * b + 2 * v + 4 * hh) = make_float4(acc[b][v], acc[b][v + 1], acc[b][v + 2], acc[b][v + 3]);
   __syncthreads();
-  for (int i = tid; i < tile.count * D; i += 64 * NW) {
-    const int rr = i / D, ch = i % D, r = p.order[tile.start + rr];
-    const size_t rh = (size_t)r * c.H_q + h;
-    float M = -INFINITY, num = 0.f, den = 0.f;
+  // each wave's weight of a row, then four channels of a row to a thread
+  if (tid < 32) {
+    float M = -INFINITY, den = 0.f;
 #pragma unroll
-    for (int x = 0; x < NW; x++) M = fmaxf(M, ml[x][0][rr]);
+    for (int x = 0; x < NW; x++) M = fmaxf(M, ml[x][0][tid]);
     const float mr = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int x = 0; x < NW; x++) {
-      const float w8 = weight(ml[x][0][rr], mr);
-      num = fmaf(reinterpret_cast<const float*>(mem + x * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES))[rr * PITCH + ch], w8, num);
-      den = fmaf(ml[x][1][rr], w8, den);
+      const float w8 = weight(ml[x][0][tid], mr);
+      den = fmaf(ml[x][1][tid], w8, den);
+      wave_weight[x][tid] = w8;
     }
-    if (row_nan[rr] >> (ch / 32) & 1) num = NAN;
+    row_sum[0][tid] = M;
+    row_sum[1][tid] = den;
+  }
+  __syncthreads();
+  constexpr int QUADS = D / 4, PER_PASS = 64 * NW / QUADS;
+  const int ch = tid % QUADS * 4;
+  for (int rr = tid / QUADS; rr < tile.count; rr += PER_PASS) {
+    const int r = p.order[tile.start + rr];
+    const size_t rh = (size_t)r * c.H_q + h;
+    float num[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < NW; x++) {
+      const float4 v = *reinterpret_cast<const float4*>(mem + x * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES) + (rr * PITCH + ch) * 4);
+      const float w8 = wave_weight[x][rr];
+      num[0] = fmaf(v.x, w8, num[0]);
+      num[1] = fmaf(v.y, w8, num[1]);
+      num[2] = fmaf(v.z, w8, num[2]);
+      num[3] = fmaf(v.w, w8, num[3]);
+    }
+    if (row_nan[rr] >> (ch / 32) & 1) num[0] = num[1] = num[2] = num[3] = NAN;
+    const float M = row_sum[0][rr], den = row_sum[1][rr];
     if (p.nsplit == 1) {
       const float* own = p.part_own + rh * (D + 2);
-      Joined j = {M, num, den};
-      j.add(own[D], own[ch], own[D + 1]);
-      o[rh * D + ch] = TQ(j.den == 0.f ? 0.f : j.num / j.den);
+      const float own_m = own[D], own_den = own[D + 1];
+      Joined j = {};
+#pragma unroll
+      for (int e = 0; e < 4; e++) {
+        j = {M, num[e], den};
+        j.add(own_m, own[ch + e], own_den);
+        num[e] = j.den == 0.f ? 0.f : j.num / j.den;
+      }
+      store4(o + rh * D + ch, num);
       if (ch == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
     } else {
-      float* to = p.part_pre + (rh * p.nsplit + sp) * (D + 2);
-      to[ch] = num;
+      float* to = p.part_pre + (rh * p.nsplit + sp) * (D + 4);
+      *reinterpret_cast<float4*>(to + ch) = make_float4(num[0], num[1], num[2], num[3]);
       if (ch == 0) {
         to[D] = M;
         to[D + 1] = den;
@@ -710,16 +784,27 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
 }
 
 // The parts of a row's prefix and its own keys together.
+// (Eight parts are requested at a time; those behind the last are the last again.)
 template <typename TQ, int D>
 __global__ __launch_bounds__(D) void prefix_merge_kernel(CacheRef c, PrefixArgs p, TQ* __restrict__ o, float* __restrict__ lse) {
   const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, t = threadIdx.x;
-  if (p.rows[r].prefix < 0) return;  // (complete already)
-  const float* own = p.part_own + (size_t)rh * (D + 2);
+  const float *own = p.part_own + (size_t)rh * (D + 2), *pre = p.part_pre + (size_t)rh * p.nsplit * (D + 4);
+  const bool whole = p.rows[r].prefix < 0;  // (complete already)
   Joined j = {own[D], own[t], own[D + 1]};
-  for (int i = 0; i < p.nsplit; i++) {
-    const float* x = p.part_pre + ((size_t)rh * p.nsplit + i) * (D + 2);
-    j.add(x[D], x[t], x[D + 1]);
+  for (int i0 = 0; i0 < p.nsplit; i0 += 8) {
+    float m[8], n[8], d[8];
+#pragma unroll
+    for (int u = 0; u < 8; u++) {
+      const float* x = pre + (size_t)min(i0 + u, p.nsplit - 1) * (D + 4);
+      m[u] = x[D];
+      n[u] = x[t];
+      d[u] = x[D + 1];
+    }
+#pragma unroll
+    for (int u = 0; u < 8; u++)
+      if (i0 + u < p.nsplit) j.add(m[u], n[u], d[u]);
   }
+  if (whole) return;
   o[(size_t)rh * D + t] = TQ(j.den == 0.f ? 0.f : j.num / j.den);
   if (t == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
 }
@@ -741,15 +826,17 @@ static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n
   wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > OWN_DIRECT;
   const long groups = n_prefixes < n_rows ? n_prefixes : n_rows;
   wk.max_tiles = n_prefixes ? (int)((n_rows + (TILE_ROWS - 1) * groups) / TILE_ROWS) : 0;
-  // a wave takes at most 16 steps of the list: longer ones are cut into parts
-  const int per = 16 * 32 * tile_waves(s.d);
-  wk.nsplit = (kcap + per - 1) / per;
+  // parts of the lists: so many that every compute unit has one, as long as a wave has a step to take
+  const long per = 32 * tile_waves(s.d), most = (kcap + per - 1) / per, want = wk.max_tiles ? CUS / ((long)wk.max_tiles * s.H_q) : 1;
+  wk.nsplit = (int)(want < 1 ? 1 : want > most ? most : want);
   wk.off_rows = take((size_t)n_rows * sizeof(PrefixRow));
   wk.off_order = take((size_t)n_rows * 4);
   wk.off_tiles = take((size_t)wk.max_tiles * sizeof(PrefixTile));
   wk.off_cuts = take(pairs * sizeof(Cut));
   wk.off_part_own = take(pairs * (s.d + 2) * 4);
-  wk.off_part_pre = take(n_prefixes && wk.nsplit > 1 ? pairs * wk.nsplit * (s.d + 2) * 4 : 0);
+  // (there are at least n_rows / 32 tiles, so nsplit parts of all pairs are at most 32 * CUS: room that never is less for more rows)
+  const size_t parts = pairs * most < TILE_ROWS * CUS ? pairs * most : TILE_ROWS * CUS;
+  wk.off_part_pre = take(n_prefixes && most > 1 ? parts * (s.d + 4) * 4 : 0);
   wk.off_list_pre = take(pre_pairs * kcap * 4);
   wk.off_keys_pre = take(pre_pairs * kcap * 4);
   wk.off_list_own = take(wk.listed ? pairs * kcap * 4 : 0);
@@ -824,8 +911,16 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
     constexpr int D = decltype(width)::value, NW = tile_waves(D);
     const int G = s.H_q / s.H_kv;
     const unsigned grid = (unsigned)(((long)n_rows * s.H_kv + 7) / 8 * 8 * G);
-    if (wk.listed) prefix_row_kernel<T, D, 4, true><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
-    else prefix_row_kernel<T, D, 4, false><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    auto row = [&](auto waves, auto listed) {
+      constexpr int W = decltype(waves)::value;
+      prefix_row_kernel<T, D, W, decltype(listed)::value><<<grid, 64 * W, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    };
+    auto rows = [&](auto waves) {
+      if (wk.listed) row(waves, std::true_type{}); else row(waves, std::false_type{});
+    };
+    if (pairs < 4 * CUS) rows(std::integral_constant<int, 4>{});
+    else if (kcap <= 2048 && !wk.listed && s.max_len <= 1024) row(std::integral_constant<int, 1>{}, std::false_type{});
+    else rows(std::integral_constant<int, 2>{});
     if (!n_prefixes) return;
     const unsigned tiles = (unsigned)(((long)wk.max_tiles * s.H_kv * wk.nsplit + 7) / 8 * 8 * G);
     prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);

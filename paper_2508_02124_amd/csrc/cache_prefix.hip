@@ -146,13 +146,13 @@ __global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, Select
 constexpr int OWN_DIRECT = 2048;  // rows of at most so many keys of their own need no list of them
 
 // NW waves per (row, head).  All keys wait in registers, 64 of the prefix's list or of the row's own to each (longer ones are read again in
-// every pass).  A key that exactly k lie before is looked for by halving between the smallest and the largest: counts are ballots, so a step
-// is a comparison for each register; about log2 of the number of keys are needed (scores that are equal there take all bits, then the
-// places are halved).  LISTED: the row's own keys come from a list of the best of them.
+// every pass).  A key that exactly k lie before is looked for between the smallest and the largest: where a straight line through the counts
+// at both ends has it, and every third time half way.  A pass is two instructions for each register, and about seven are needed (halving alone: 13;
+// scores that are equal there take all bits, then the places are halved).  LISTED: the row's own keys come from a list of the best of them.
 template <typename TQ, int D, int NW, bool LISTED>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 || NW < 4 ? 3 : 4) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
+__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
                                                              TQ* __restrict__ o, float* __restrict__ lse, float scale) {
-  constexpr int RC = NW < 4 ? 32 : 16, RO = NW < 4 ? 16 : 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
+  constexpr int RC = 16, RO = 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
   __shared__ uint32_t ids[NW][RO * 64];
   __shared__ uint32_t sums[2][NW];
   __shared__ __align__(16) float mo[NW][D];
@@ -260,9 +260,17 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 || NW < 4 ?
   // f(key, place in its list, whether that is the prefix's) for all of this wave's keys; what the registers do not hold is read again
   auto every = [&](auto f) __attribute__((always_inline)) {
 #pragma unroll
-    for (int u = 0; u < RC; u++) f(kc[u], place_of(u), true);
+    for (int u0 = 0; u0 < RC; u0 += 8)
+      if (u0 * NW * 64 < n_pre) {
 #pragma unroll
-    for (int u = 0; u < RO; u++) f(ko[u], place_of(u), false);
+        for (int u = u0; u < u0 + 8; u++) f(kc[u], place_of(u), true);
+      }
+#pragma unroll
+    for (int u0 = 0; u0 < RO; u0 += 8)
+      if (u0 * NW * 64 < n_own) {
+#pragma unroll
+        for (int u = u0; u < u0 + 8; u++) f(ko[u], place_of(u), false);
+      }
 #pragma unroll 1
     for (int i = place_of(RC); i < n_pre; i += NW * 64) f(keys_pre[i], i, true);
 #pragma unroll 1
@@ -297,8 +305,8 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 || NW < 4 ?
     // fewer than k keys are before lo, at least k before hi
     uint32_t lo = over_waves(least, [](uint32_t a, uint32_t b) { return min(a, b); });
     uint32_t hi = over_waves(most, [](uint32_t a, uint32_t b) { return max(a, b); });
-    uint32_t probe = hi, before_lo = 0;
-    for (;;) {
+    uint32_t probe = hi, before_lo = 0, before_hi = 0;
+    for (int step = 1;; step++) {
       uint32_t n = 0;
       every([&](uint32_t key, int, bool) __attribute__((always_inline)) { n += key < probe; });
       n = sum_lanes(n);
@@ -308,9 +316,12 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 || NW < 4 ?
         before_lo = n;
       } else {
         hi = probe;
+        before_hi = n;
       }
       if (hi - lo <= 1u) break;
-      probe = lo + (hi - lo) / 2;
+      const float share = (float)((uint32_t)k - before_lo) / (float)(before_hi - before_lo);
+      const uint32_t ahead = step % 3 ? (uint32_t)((float)(hi - lo) * share) : (hi - lo) / 2;
+      probe = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lo + min(max(ahead, 1u), hi - lo - 1u)));
     }
     cut_key = probe;
     if (hi - lo <= 1u) {  // keys equal to lo are on both sides: the prefix's are first
@@ -918,9 +929,8 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
     auto rows = [&](auto waves) {
       if (wk.listed) row(waves, std::true_type{}); else row(waves, std::false_type{});
     };
-    if (pairs < 4 * CUS) rows(std::integral_constant<int, 4>{});
-    else if (kcap <= 2048 && !wk.listed && s.max_len <= 1024) row(std::integral_constant<int, 1>{}, std::false_type{});
-    else rows(std::integral_constant<int, 2>{});
+    if (pairs < 4 * CUS || kcap > 2048 || wk.listed || s.max_len > 1024) rows(std::integral_constant<int, 4>{});
+    else row(std::integral_constant<int, 2>{}, std::false_type{});
     if (!n_prefixes) return;
     const unsigned tiles = (unsigned)(((long)wk.max_tiles * s.H_kv * wk.nsplit + 7) / 8 * 8 * G);
     prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);

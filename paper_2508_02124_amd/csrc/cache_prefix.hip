@@ -5,9 +5,9 @@
 // together, a cut through both.  So a prefix is selected from once, and its listed K and V are gathered and decoded once for 32 rows: they are
 // the columns of two matrix products whose weights each row masks by its own cut.  Four launches (five behind long prefixes):
 //   prefix_select_kernel (prefix_slice_kernel)   the lists, and the rows in order of their prefixes
-//   prefix_row_kernel                            a row's cut, and attention to its own keys
-//   prefix_tile_kernel                           attention to the prefix, joined with the row's own
-//   prefix_merge_kernel                          only where the lists are long: the parts of a list together
+//   prefix_cut_kernel                            a row's cut, and which of its own keys it keeps
+//   prefix_tile_kernel                           attention to the prefixes, in parts
+//   prefix_own_kernel                            attention to a row's own keys, joined with the parts
 #include "cache_attend.h"
 #include "cache_select.h"
 
@@ -23,10 +23,11 @@ struct PrefixRow {
 struct PrefixTile {
   int prefix, start, count, pre;
 };
-// The keys that a row keeps of a list: those before `key`, and those equal to it up to place `last`.
+// What a row keeps: of the prefix's list the keys before `key`, and those equal to it up to place `last`; of its own the `count` that
+// are listed (-1: a page is out of range, the row sees nothing).
 struct Cut {
   uint32_t key;
-  int last;
+  int last, count, unused;
 };
 
 struct PrefixArgs {
@@ -37,9 +38,10 @@ struct PrefixArgs {
   PrefixTile* tiles;
   int32_t *list_pre, *list_own;    // [prefixes or rows][H_q][kcap]
   uint32_t *keys_pre, *keys_own;   // the listed keys
-  Cut* cuts;                       // [rows][H_q], of the prefix's list
-  float *part_own, *part_pre;      // [rows][H_q] of D sums, their reference and their weight; [rows][H_q][nsplit] of the same and two more
+  Cut* cuts;                       // [rows][H_q]
+  float* part;                     // [rows][H_q][nsplit]: D sums over a part of the prefix's list, their reference, their weight, and two more
   int max_tiles, nsplit;
+  bool listed;                     // rows of more than k keys of their own have lists of them
 };
 
 // ------------------------------------------------------------------ the rows by prefix
@@ -118,7 +120,7 @@ struct SelectSet {
   int wgs;
 };
 
-// The prefixes' lists, and, where rows may have many keys of their own, theirs.  GROUP: the first workgroup orders the rows.
+// The prefixes' lists, and those of rows with more than k keys of their own.  GROUP: the first workgroup orders the rows.
 template <int S, bool SLICED, bool GROUP>
 __global__ __launch_bounds__(512, 6) void prefix_select_kernel(CacheRef c, PrefixArgs p, SelectSet a, SelectSet b) {
   int block = (int)blockIdx.x - (GROUP ? 1 : 0);
@@ -130,7 +132,7 @@ __global__ __launch_bounds__(512, 6) void prefix_select_kernel(CacheRef c, Prefi
   if (!first) block -= a.wgs;
   const CacheRows rows = first ? a.rows : b.rows;
   const SliceWork sw = first ? a.sw : b.sw;
-  select_block<S, SLICED, true, true>(c, rows, sw, first ? a.list : b.list, first ? a.keys : b.keys, block);
+  select_block<S, SLICED, true, true>(c, rows, sw, first ? a.list : b.list, first ? a.keys : b.keys, block, first);
 }
 template <int S>
 __global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, SelectSet a, SelectSet b) {
@@ -142,55 +144,38 @@ __global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, Select
   slice_block<S, true>(c, rows, sw, first ? a.list : b.list, first ? a.keys : b.keys, block);
 }
 
-// ------------------------------------------------------------------ a row's cut, and its own keys
-constexpr int OWN_DIRECT = 2048;  // rows of at most so many keys of their own need no list of them
-
-// NW waves per (row, head).  All keys wait in registers, 64 of the prefix's list or of the row's own to each (longer ones are read again in
-// every pass).  A key that exactly k lie before is looked for between the smallest and the largest: where a straight line through the counts
+// ------------------------------------------------------------------ a row's cut
+// NW waves per (row, head).  All keys wait in registers, 64 of the prefix's list or of the row's own to each (what these do not hold is read again
+// in every pass).  A key that exactly k lie before is looked for between the smallest and the largest: where a straight line through the counts
 // at both ends has it, and every third time half way.  A pass is two instructions for each register, and about seven are needed (halving alone: 13;
-// scores that are equal there take all bits, then the places are halved).  LISTED: the row's own keys come from a list of the best of them.
-template <typename TQ, int D, int NW, bool LISTED>
-__global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) void prefix_row_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
-                                                             TQ* __restrict__ o, float* __restrict__ lse, float scale) {
-  constexpr int RC = 16, RO = 8, LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG;
-  __shared__ uint32_t ids[NW][RO * 64];
+// scores that are equal there take all bits, then the places are halved).  Counts are kept in the lanes and summed once a pass: one ballot a
+// register needed three scalar instructions, which four SIMDs share (64 rows of 32 heads, 2048 + 400 keys: 83 us instead of 26).
+// A row with more than k keys of its own has a list of the best of them, unless the caller's bound says that there are none; else they are
+// read where they are.
+template <int NW>
+__global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixArgs p) {
+  constexpr int RC = 16, RO = 8;
   __shared__ uint32_t sums[2][NW];
-  __shared__ __align__(16) float mo[NW][D];
-  __shared__ float ml[NW][2];
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   if (unit >= p.own.n_rows * c.H_kv) return;
   const int r = unit / c.H_kv, g = unit - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
   const PrefixRow info = p.rows[r];
-  const int k = p.own.k, n_own = LISTED ? min(k, info.own) : info.own, n_pre = min(k, info.pre);
-  const bool whole = info.prefix < 0;  // (no prefix: the output is complete here)
-  auto finish = [&](int t, float num, float den, float M) __attribute__((always_inline)) {
-    if (whole) {
-      o[(size_t)rh * D + t] = TQ(den == 0.f ? 0.f : num / den);
-      if (t == 0) lse[(size_t)h * p.own.n_rows + r] = den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(den), LN2, M);
-    } else {
-      float* out = p.part_own + (size_t)rh * (D + 2);
-      out[t] = num;
-      if (t == 0) {
-        out[D] = M;
-        out[D + 1] = den;
-      }
-    }
-  };
+  const int k = p.own.k, n_pre = min(k, info.pre);
+  const bool listed = p.listed && info.own > k;
+  const int n_own = listed ? k : info.own;
   if (n_own <= 0) {
-    for (int t = tid; t < D; t += 64 * NW) finish(t, 0.f, 0.f, -INFINITY);
+    if (tid == 0) p.cuts[rh] = {0u, -1, 0, 0};
     return;
   }
-  Query<TQ> qv;
-  qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
   const int32_t* pages = p.own.table + (size_t)info.req * c.max_pages;
-  const int32_t* list = p.list_own + (size_t)rh * p.own.kcap;
+  int32_t* list = p.list_own + (size_t)rh * p.own.kcap;
+  const uint32_t* keys_own = p.keys_own + (size_t)rh * p.own.kcap;
   const size_t at_pre = ((size_t)max(info.prefix, 0) * c.H_q + h) * p.pre.kcap;
   const uint32_t* keys_pre = p.keys_pre + at_pre;
-  const int first_pre = n_pre > 0 ? p.list_pre[at_pre] : 0, first_own = LISTED ? list[0] : 0;
-  const int rounds_o = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
+  const int first_pre = n_pre > 0 ? p.list_pre[at_pre] : 0;
   uint32_t kc[RC], ko[RO], id[RO];
-  bool bad = first_pre < 0 || first_own < 0;  // (a page is out of range: the list says so)
+  bool bad = first_pre < 0 || (listed && list[0] < 0);  // (a page is out of range: the list says so)
   auto place_of = [&](int u) { return (u * NW + w) * 64 + l; };
   // (all loads of four registers are on their way before the first is used: places behind the end read the last one)
   auto fetch_c = [&]() __attribute__((always_inline)) {
@@ -227,16 +212,16 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) vo
 #pragma unroll
         for (int u = u0; u < u0 + 4; u++) {
           const int j = min(place_of(round * RO + u), n_own - 1);
-          if constexpr (LISTED) {
+          if (listed) {
             id[u] = (uint32_t)list[j];
-            ko[u] = p.keys_own[(size_t)rh * p.own.kcap + j];
+            ko[u] = keys_own[j];
           } else {
             id[u] = (uint32_t)pages[j >> c.shift];
           }
         }
       }
     }
-    if constexpr (!LISTED) {
+    if (!listed) {
 #pragma unroll
       for (int u0 = 0; u0 < RO; u0 += 4)
         if ((round * RO + u0) * NW * 64 < n_own) {
@@ -250,10 +235,11 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) vo
     }
 #pragma unroll
     for (int u = 0; u < RO; u++)
-      ko[u] = place_of(round * RO + u) >= n_own ? NO_KEY : LISTED ? ko[u] : score_key(__uint_as_float(ko[u]));
+      ko[u] = place_of(round * RO + u) >= n_own ? NO_KEY : listed ? ko[u] : score_key(__uint_as_float(ko[u]));
   };
   fetch_o(0);
-  if (!LISTED && rounds_o > 1)
+  const int rounds = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
+  if (!listed && rounds > 1)
     for (int j = tid; (long)j << c.shift < n_own; j += 64 * NW) bad |= (uint32_t)pages[j] >= (uint32_t)c.n_pages;
   const bool selects = (long)n_pre + n_own > k;
   if (selects) fetch_c();
@@ -275,8 +261,7 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) vo
     for (int i = place_of(RC); i < n_pre; i += NW * 64) f(keys_pre[i], i, true);
 #pragma unroll 1
     for (int i = place_of(RO); i < n_own; i += NW * 64) {
-      if constexpr (LISTED) f(p.keys_own[(size_t)rh * p.own.kcap + i], i, false);
-      else f(score_key(*score_at(slot_of((uint32_t)pages[i >> c.shift], i))), i, false);
+      f(listed ? keys_own[i] : score_key(*score_at(slot_of((uint32_t)pages[i >> c.shift], i))), i, false);
     }
   };
   int turn = 0;
@@ -339,147 +324,39 @@ __global__ __launch_bounds__(64 * NW, D == 256 ? 2 : sizeof(TQ) == 4 ? 3 : 4) vo
       cut_own = (int)(upto - n_pre) - 1;
     }
   }
-  // (a page out of range: nothing is kept)
   const bool gone = over_waves(__ballot(bad) ? 1u : 0u, [](uint32_t a, uint32_t b) { return a | b; }) != 0;
-  if (!whole && tid == 0) p.cuts[rh] = gone ? Cut{0u, -1} : Cut{cut_key, cut_pre};
-  if (gone) {
-    for (int t = tid; t < D; t += 64 * NW) finish(t, 0.f, 0.f, -INFINITY);
-    return;
-  }
-  // Attention to the kept ones, each wave to its own; the form of cache_attend_kernel.
-  const uint32_t k_off = ((uint32_t)g << c.shift) * D + 16 * sub, z_off = c.off_z + ((uint32_t)h << c.shift) * 4;
-  const uint32_t b_off = c.off_scales + ((uint32_t)g << c.shift) * (D / 16) + sub, page_bytes = (uint32_t)c.page_bytes;
-  float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f, acc[32];
-#pragma unroll
-  for (int e = 0; e < 32; e++) acc[e] = 0.f;
-  struct Keys {
-    uint4 kr[U], vr[U];
-    uint32_t kb[U], vb[U];
-    float s[U];
-    uint32_t there;
-  };
-  auto take = [&](Keys& x) __attribute__((always_inline)) {
-    float top = -INFINITY;
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const float sc = mx_scale(x.kb[u]), zb = x.there >> u & 1 ? x.s[u] : -INFINITY;
-      float s = qv.template dot8<0>(x.kr[u].x, sc, 0.f);
-      s = qv.template dot8<1>(x.kr[u].y, sc, s);
-      s = qv.template dot8<2>(x.kr[u].z, sc, s);
-      s = lanes_sum<LPG>(qv.template dot8<3>(x.kr[u].w, sc, s));
-      x.s[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
-      top = fmaxf(top, x.s[u]);
-    }
-    if (__ballot(top > limit)) {
-      top = fmaxf(m, over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); }));
-      const float alpha = weight(m, top);
-      m = ref = top;
-      limit = top + 5.f;
-      lsum *= alpha;
-#pragma unroll
-      for (int e = 0; e < 32; e++) acc[e] *= alpha;
-    }
-#pragma unroll
-    for (int u = 0; u < U; u++) {
-      const float pv = weight(x.s[u], ref), sc = x.s[u] == -INFINITY ? 0.f : mx_scale(x.vb[u]);
-      lsum += pv;
-      const uint32_t code[4] = {x.vr[u].x, x.vr[u].y, x.vr[u].z, x.vr[u].w};
-#pragma unroll
-      for (int i = 0; i < 4; i++) {
-        static_for<4>([&](auto b) {
-          constexpr int B = decltype(b)::value;
-          const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], sc, B);
-          acc[8 * i + 2 * B] = fmaf(pv, v[0], acc[8 * i + 2 * B]);
-          acc[8 * i + 2 * B + 1] = fmaf(pv, v[1], acc[8 * i + 2 * B + 1]);
-        });
-      }
-    }
-  };
-  for (int round = 0; round < rounds_o; round++) {
-    if (round) fetch_o(round);
-    int n = 0;
-#pragma unroll
-    for (int u = 0; u < RO; u++)
-      if ((round * RO + u) * NW * 64 < n_own) {
-        const bool keep = ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_of(round * RO + u) <= cut_own);
-        const unsigned long long b = __ballot(keep);
-        if (keep) ids[w][n + (int)lanes_before(b)] = id[u];
-        n += (int)__popcll(b);
-      }
-    asm volatile("" ::: "memory");  // (a wave's LDS accesses are in order: it reads what it wrote)
-    int i0 = 0;
-    auto fetch = [&](Keys& x) __attribute__((always_inline)) {
-      x.there = 0;
-#pragma unroll
-      for (int u = 0; u < U; u++) {
-        const int i = i0 + u * NG + grp;
-        const bool there = i < n;
-        const uint32_t slot = there ? ids[w][min(i, RO * 64 - 1)] : 0u, place = cache_place(c, slot);
-        const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
-        const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
-        const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (b_off + place * (D / 16)));
-        x.kr[u] = codes[0];
-        x.vr[u] = codes[LPG];
-        x.kb[u] = scales[0];
-        x.vb[u] = scales[LPG];
-        x.s[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
-        x.there |= there ? 1u << u : 0u;
-      }
-      i0 += KEYS;
-    };
-    if (n > 0) {
-      Keys even, odd;
-      fetch(even);
+  // the slots of its own keys that are kept, wave by wave behind one another (all are in registers before one is written)
+  uint32_t total = 0;
 #pragma unroll 1
-      for (;;) {
-        const bool more = i0 < n;
-        if (more) fetch(odd);
-        take(even);
-        if (!more) break;
-        const bool again = i0 < n;
-        if (again) fetch(even);
-        take(odd);
-        if (!again) break;
+  for (int round = 0; round < rounds && !gone; round++) {
+    if (round) fetch_o(round);
+    uint32_t mine = 0;
+    unsigned long long kept[RO];
+#pragma unroll
+    for (int u = 0; u < RO; u++) {
+      kept[u] = __ballot(ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_of(round * RO + u) <= cut_own));
+      mine += (uint32_t)__popcll(kept[u]);
+    }
+    uint32_t at = total, all = mine;
+    if constexpr (NW > 1) {
+      turn ^= 1;
+      if (l == 0) sums[turn][w] = mine;
+      __syncthreads();
+      all = 0;
+#pragma unroll
+      for (int i = 0; i < NW; i++) {
+        at += i < w ? sums[turn][i] : 0u;
+        all += sums[turn][i];
       }
     }
-    asm volatile("" ::: "memory");
-  }
-  lsum = over_groups<LPG>(lsum, [](float a, float b) { return a + b; });
-  const auto across = [](const auto& both) { return __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]); };
-  const auto bits = [](float x) { return __builtin_bit_cast(unsigned, x); };
 #pragma unroll
-  for (int e = 0; e < 16; e++) acc[e] = across(__builtin_amdgcn_permlane32_swap(bits(acc[e]), bits(acc[e + 16]), false, false));
-#pragma unroll
-  for (int e = 0; e < 8; e++) {  // (from here on each row of 16 lanes has sums of its own: a quarter of the channels)
-    acc[e] = across(__builtin_amdgcn_permlane16_swap(bits(acc[e]), bits(acc[e + 8]), false, false));
-    if constexpr (LPG == 2) acc[e] += dpp_move<0x4e>(acc[e]);
-    if constexpr (LPG <= 4) acc[e] += dpp_move<0x124>(acc[e]);
-    acc[e] += dpp_move<0x128>(acc[e]);
-  }
-  if ((l & 15) < LPG) {
-    float4* to = reinterpret_cast<float4*>(&mo[w][32 * sub + 16 * (l >> 5) + 8 * (l >> 4 & 1)]);
-    to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
-    to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
-  }
-  if (l == 0) {
-    ml[w][0] = m;
-    ml[w][1] = lsum;
-  }
-  __syncthreads();
-  float M = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < NW; i++) M = fmaxf(M, ml[i][0]);
-  const float mr = M == -INFINITY ? 0.f : M;
-  for (int t = tid; t < D; t += 64 * NW) {
-    float num = 0.f, den = 0.f;
-#pragma unroll
-    for (int i = 0; i < NW; i++) {
-      const float w8 = weight(ml[i][0], mr);
-      num = fmaf(mo[i][t], w8, num);
-      den = fmaf(ml[i][1], w8, den);
+    for (int u = 0; u < RO; u++) {
+      if (kept[u] >> l & 1) list[at + lanes_before(kept[u])] = (int32_t)id[u];
+      at += (uint32_t)__popcll(kept[u]);
     }
-    finish(t, num, den, M);
+    total += all;
   }
+  if (tid == 0) p.cuts[rh] = {cut_key, cut_pre, gone ? -1 : (int)total, 0};
 }
 
 // ------------------------------------------------------------------ the prefix, for 32 rows at a time
@@ -513,14 +390,6 @@ struct Joined {
   }
 };
 
-__device__ __forceinline__ void store4(__bf16* dst, const float* x) {
-  bf16x4 v;
-#pragma unroll
-  for (int e = 0; e < 4; e++) v[e] = (__bf16)x[e];
-  *reinterpret_cast<bf16x4*>(dst) = v;
-}
-__device__ __forceinline__ void store4(float* dst, const float* x) { *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]); }
-
 // One workgroup per (tile of 32 rows, head, part of the list); a wave takes 32 listed keys at a time.  Their K rows go from memory to the A operand
 // of S^T = K Q^T (a lane has half a row; which channel is which product's does not matter, as long as Q has them in the same places), the
 // rows' queries are the B operand.  A row is then a column of S^T, in two lanes, which mask it by the row's cut and form the weights with a
@@ -528,8 +397,7 @@ __device__ __forceinline__ void store4(float* dst, const float* x) { *reinterpre
 // holds is exact in bf16; the weights, and fp32 queries, are sums of bf16 terms (two terms of a weight: off by 2^-16 of it; one term, 2^-8,
 // would show beside the rounding of the output; three for fp32, 2^-24).
 template <typename TQ, int D, int NW>
-__global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
-                                                              TQ* __restrict__ o, float* __restrict__ lse, float scale) {
+__global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride, float scale) {
   constexpr bool F32 = sizeof(TQ) == 4;
   constexpr int KS = D / 16, CB = D / 32, NQ = D / 64, NTQ = F32 ? 3 : 1, NTP = F32 ? 3 : 2, PITCH = D + 4;
   constexpr int TILE_BYTES = 32 * D * 2, OUT_BYTES = 32 * PITCH * 4;
@@ -589,7 +457,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   const bool any = j0 < n_keys;
   int at0 = j0;
   if (any) fetch(cur);
-  const Cut cut = n < tile.count ? p.cuts[(size_t)row * c.H_q + h] : Cut{0u, -1};
+  const Cut cut = n < tile.count ? p.cuts[(size_t)row * c.H_q + h] : Cut{0u, -1, 0, 0};
   // channel 8 s + e of this half of the row: the lane's part of product s
   Terms<NTQ> qf[KS];
   {
@@ -770,59 +638,191 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
       num[3] = fmaf(v.w, w8, num[3]);
     }
     if (row_nan[rr] >> (ch / 32) & 1) num[0] = num[1] = num[2] = num[3] = NAN;
-    const float M = row_sum[0][rr], den = row_sum[1][rr];
-    if (p.nsplit == 1) {
-      const float* own = p.part_own + rh * (D + 2);
-      const float own_m = own[D], own_den = own[D + 1];
-      Joined j = {};
-#pragma unroll
-      for (int e = 0; e < 4; e++) {
-        j = {M, num[e], den};
-        j.add(own_m, own[ch + e], own_den);
-        num[e] = j.den == 0.f ? 0.f : j.num / j.den;
-      }
-      store4(o + rh * D + ch, num);
-      if (ch == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
-    } else {
-      float* to = p.part_pre + (rh * p.nsplit + sp) * (D + 4);
-      *reinterpret_cast<float4*>(to + ch) = make_float4(num[0], num[1], num[2], num[3]);
-      if (ch == 0) {
-        to[D] = M;
-        to[D + 1] = den;
-      }
-    }
+    float* to = p.part + (rh * p.nsplit + sp) * (D + 4);
+    *reinterpret_cast<float4*>(to + ch) = make_float4(num[0], num[1], num[2], num[3]);
+    if (ch == 0) *reinterpret_cast<float2*>(to + D) = make_float2(row_sum[0][rr], row_sum[1][rr]);
   }
 }
 
-// The parts of a row's prefix and its own keys together.
-// (Eight parts are requested at a time; those behind the last are the last again.)
-template <typename TQ, int D>
-__global__ __launch_bounds__(D) void prefix_merge_kernel(CacheRef c, PrefixArgs p, TQ* __restrict__ o, float* __restrict__ lse) {
-  const int rh = blockIdx.x, r = rh / c.H_q, h = rh - r * c.H_q, t = threadIdx.x;
-  const float *own = p.part_own + (size_t)rh * (D + 2), *pre = p.part_pre + (size_t)rh * p.nsplit * (D + 4);
-  const bool whole = p.rows[r].prefix < 0;  // (complete already)
-  Joined j = {own[D], own[t], own[D + 1]};
-  for (int i0 = 0; i0 < p.nsplit; i0 += 8) {
-    float m[8], n[8], d[8];
+// ------------------------------------------------------------------ a row's own keys, and all of it together
+// NW waves per (row, head), 32 of the listed keys to a wave at a time, in the form of cache_attend_kernel.  The parts of the prefix are
+// requested first and joined last.
+template <typename TQ, int D, int NW>
+__global__ __launch_bounds__(64 * NW) void prefix_own_kernel(CacheRef c, PrefixArgs p, const TQ* __restrict__ q, long q_stride,
+                                                             TQ* __restrict__ o, float* __restrict__ lse, float scale) {
+  constexpr int LPG = D / 32, NG = 64 / LPG, KEYS = 32, U = KEYS / NG, PER = (D + 64 * NW - 1) / (64 * NW), PARTS = 4;
+  __shared__ __align__(16) float mo[NW][D];
+  __shared__ float ml[NW][2];
+  const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
+  if (unit >= p.own.n_rows * c.H_kv) return;
+  const int r = unit / c.H_kv, g = unit - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, sub = l % LPG, grp = l / LPG;
+  const int32_t* list = p.list_own + (size_t)rh * p.own.kcap;
+  uint32_t id[U];
+  int i0 = w * KEYS;
 #pragma unroll
-    for (int u = 0; u < 8; u++) {
-      const float* x = pre + (size_t)min(i0 + u, p.nsplit - 1) * (D + 4);
-      m[u] = x[D];
-      n[u] = x[t];
-      d[u] = x[D + 1];
+  for (int u = 0; u < U; u++) id[u] = (uint32_t)list[min(i0 + u * NG + grp, p.own.kcap - 1)];  // (before their number is known)
+  const float* parts = p.part + (size_t)rh * p.nsplit * (D + 4);
+  float part_m[PARTS], part_den[PARTS], part_num[PARTS][PER];
+  const int n_parts = p.pre.n_rows ? p.nsplit : 0;
+  auto request = [&](int first) __attribute__((always_inline)) {
+    if (n_parts)
+#pragma unroll
+      for (int i = 0; i < PARTS; i++) {
+        const float* x = parts + (size_t)min(first + i, n_parts - 1) * (D + 4);
+        part_m[i] = x[D];
+        part_den[i] = x[D + 1];
+#pragma unroll
+        for (int e = 0; e < PER; e++) part_num[i][e] = x[min(tid + e * 64 * NW, D - 1)];
+      }
+  };
+  request(0);
+  Query<TQ> qv;
+  qv.load(q + (size_t)r * q_stride + (size_t)h * D + 32 * sub);
+  const int count = p.cuts[rh].count, prefix = p.rows[r].prefix;
+  // Attention to the kept ones, each wave to its own; the form of cache_attend_kernel.
+  const uint32_t k_off = ((uint32_t)g << c.shift) * D + 16 * sub, z_off = c.off_z + ((uint32_t)h << c.shift) * 4;
+  const uint32_t b_off = c.off_scales + ((uint32_t)g << c.shift) * (D / 16) + sub, page_bytes = (uint32_t)c.page_bytes;
+  float m = -INFINITY, ref = 0.f, limit = -INFINITY, lsum = 0.f, acc[32];
+#pragma unroll
+  for (int e = 0; e < 32; e++) acc[e] = 0.f;
+  struct Keys {
+    uint4 kr[U], vr[U];
+    uint32_t kb[U], vb[U];
+    float s[U];
+    uint32_t there;
+  };
+  auto take = [&](Keys& x) __attribute__((always_inline)) {
+    float top = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const float sc = mx_scale(x.kb[u]), zb = x.there >> u & 1 ? x.s[u] : -INFINITY;
+      float s = qv.template dot8<0>(x.kr[u].x, sc, 0.f);
+      s = qv.template dot8<1>(x.kr[u].y, sc, s);
+      s = qv.template dot8<2>(x.kr[u].z, sc, s);
+      s = lanes_sum<LPG>(qv.template dot8<3>(x.kr[u].w, sc, s));
+      x.s[u] = zb == -INFINITY ? -INFINITY : fmaf(s, scale, zb);  // (whatever such a key holds)
+      top = fmaxf(top, x.s[u]);
+    }
+    if (__ballot(top > limit)) {
+      top = fmaxf(m, over_groups<LPG>(top, [](float a, float b) { return fmaxf(a, b); }));
+      const float alpha = weight(m, top);
+      m = ref = top;
+      limit = top + 5.f;
+      lsum *= alpha;
+#pragma unroll
+      for (int e = 0; e < 32; e++) acc[e] *= alpha;
     }
 #pragma unroll
-    for (int u = 0; u < 8; u++)
-      if (i0 + u < p.nsplit) j.add(m[u], n[u], d[u]);
+    for (int u = 0; u < U; u++) {
+      const float pv = weight(x.s[u], ref), sc = x.s[u] == -INFINITY ? 0.f : mx_scale(x.vb[u]);
+      lsum += pv;
+      const uint32_t code[4] = {x.vr[u].x, x.vr[u].y, x.vr[u].z, x.vr[u].w};
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        static_for<4>([&](auto b) {
+          constexpr int B = decltype(b)::value;
+          const auto v = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(code[i], sc, B);
+          acc[8 * i + 2 * B] = fmaf(pv, v[0], acc[8 * i + 2 * B]);
+          acc[8 * i + 2 * B + 1] = fmaf(pv, v[1], acc[8 * i + 2 * B + 1]);
+        });
+      }
+    }
+  };
+  auto fetch = [&](Keys& x) __attribute__((always_inline)) {  // the keys at i0 (in id), and the ids of those behind them
+    x.there = 0;
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const bool there = i0 + u * NG + grp < count;
+      const uint32_t slot = there ? id[u] : 0u, place = cache_place(c, slot);
+      const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
+      const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
+      const uint8_t* scales = reinterpret_cast<const uint8_t*>(page + (b_off + place * (D / 16)));
+      x.kr[u] = codes[0];
+      x.vr[u] = codes[LPG];
+      x.kb[u] = scales[0];
+      x.vb[u] = scales[LPG];
+      x.s[u] = *reinterpret_cast<const float*>(page + (z_off + place * 4));
+      x.there |= there ? 1u << u : 0u;
+    }
+    i0 += NW * KEYS;
+#pragma unroll
+    for (int u = 0; u < U; u++) id[u] = (uint32_t)list[min(i0 + u * NG + grp, p.own.kcap - 1)];
+  };
+  if (i0 < count) {
+    Keys even, odd;
+    fetch(even);
+#pragma unroll 1
+    for (;;) {
+      const bool more = i0 < count;
+      if (more) fetch(odd);
+      take(even);
+      if (!more) break;
+      const bool again = i0 < count;
+      if (again) fetch(even);
+      take(odd);
+      if (!again) break;
+    }
   }
-  if (whole) return;
-  o[(size_t)rh * D + t] = TQ(j.den == 0.f ? 0.f : j.num / j.den);
-  if (t == 0) lse[(size_t)h * p.own.n_rows + r] = j.den == 0.f ? -INFINITY : fmaf(__builtin_amdgcn_logf(j.den), LN2, j.M);
+  lsum = over_groups<LPG>(lsum, [](float a, float b) { return a + b; });
+  const auto across = [](const auto& both) { return __builtin_bit_cast(float, (unsigned)both[0]) + __builtin_bit_cast(float, (unsigned)both[1]); };
+  const auto bits = [](float x) { return __builtin_bit_cast(unsigned, x); };
+#pragma unroll
+  for (int e = 0; e < 16; e++) acc[e] = across(__builtin_amdgcn_permlane32_swap(bits(acc[e]), bits(acc[e + 16]), false, false));
+#pragma unroll
+  for (int e = 0; e < 8; e++) {  // (from here on each row of 16 lanes has sums of its own: a quarter of the channels)
+    acc[e] = across(__builtin_amdgcn_permlane16_swap(bits(acc[e]), bits(acc[e + 8]), false, false));
+    if constexpr (LPG == 2) acc[e] += dpp_move<0x4e>(acc[e]);
+    if constexpr (LPG <= 4) acc[e] += dpp_move<0x124>(acc[e]);
+    acc[e] += dpp_move<0x128>(acc[e]);
+  }
+  if ((l & 15) < LPG) {
+    float4* to = reinterpret_cast<float4*>(&mo[w][32 * sub + 16 * (l >> 5) + 8 * (l >> 4 & 1)]);
+    to[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+    to[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
+  }
+  if (l == 0) {
+    ml[w][0] = m;
+    ml[w][1] = lsum;
+  }
+  __syncthreads();
+  float M = -INFINITY, den = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; i++) M = fmaxf(M, ml[i][0]);
+  const float mr = M == -INFINITY ? 0.f : M;
+#pragma unroll
+  for (int i = 0; i < NW; i++) den = fmaf(ml[i][1], weight(ml[i][0], mr), den);
+  Joined j[PER];
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    float num = 0.f;
+#pragma unroll
+    for (int i = 0; i < NW; i++) num = fmaf(mo[i][min(tid + e * 64 * NW, D - 1)], weight(ml[i][0], mr), num);
+    j[e] = {M, num, den};
+  }
+  if (prefix >= 0)
+    for (int first = 0; first < n_parts; first += PARTS) {
+      if (first) request(first);
+#pragma unroll
+      for (int i = 0; i < PARTS; i++)
+        if (first + i < n_parts) {
+#pragma unroll
+          for (int e = 0; e < PER; e++) j[e].add(part_m[i], part_num[i][e], part_den[i]);
+        }
+    }
+#pragma unroll
+  for (int e = 0; e < PER; e++) {
+    const int t = tid + e * 64 * NW;
+    if (t >= D) break;
+    const bool none = count < 0 || j[e].den == 0.f;  // (a page is out of range, or no key took part)
+    o[(size_t)rh * D + t] = TQ(none ? 0.f : j[e].num / j[e].den);
+    if (t == 0) lse[(size_t)h * p.own.n_rows + r] = none ? -INFINITY : fmaf(__builtin_amdgcn_logf(j[e].den), LN2, j[e].M);
+  }
 }
 
 // ------------------------------------------------------------------ host side
 struct PrefixWork {
-  size_t off_rows, off_order, off_tiles, off_list_pre, off_keys_pre, off_list_own, off_keys_own, off_cuts, off_part_own, off_part_pre, total;
+  size_t off_rows, off_order, off_tiles, off_list_pre, off_keys_pre, off_list_own, off_keys_own, off_cuts, off_part, total;
   SelectWork pre, own;
   bool listed;
   int max_tiles, nsplit;
@@ -834,7 +834,7 @@ static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n
   const size_t pairs = (size_t)n_rows * s.H_q, pre_pairs = (size_t)n_prefixes * s.H_q;
   PrefixWork wk = {};
   auto take = [&](size_t bytes) { size_t at = wk.total; wk.total = align_up(at + bytes, 256); return at; };
-  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > OWN_DIRECT;
+  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > k;
   const long groups = n_prefixes < n_rows ? n_prefixes : n_rows;
   wk.max_tiles = n_prefixes ? (int)((n_rows + (TILE_ROWS - 1) * groups) / TILE_ROWS) : 0;
   // parts of the lists: so many that every compute unit has one, as long as a wave has a step to take
@@ -844,13 +844,12 @@ static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n
   wk.off_order = take((size_t)n_rows * 4);
   wk.off_tiles = take((size_t)wk.max_tiles * sizeof(PrefixTile));
   wk.off_cuts = take(pairs * sizeof(Cut));
-  wk.off_part_own = take(pairs * (s.d + 2) * 4);
-  // (there are at least n_rows / 32 tiles, so nsplit parts of all pairs are at most 32 * CUS: room that never is less for more rows)
-  const size_t parts = pairs * most < TILE_ROWS * CUS ? pairs * most : TILE_ROWS * CUS;
-  wk.off_part_pre = take(n_prefixes && most > 1 ? parts * (s.d + 4) * 4 : 0);
+  // (there are at least n_rows / 32 tiles, so several parts of each pair are at most 32 * CUS: room that never is less for more rows)
+  const size_t parts = pairs * most < TILE_ROWS * CUS ? pairs * most : pairs > TILE_ROWS * CUS ? pairs : TILE_ROWS * CUS;
+  wk.off_part = take(n_prefixes ? parts * (s.d + 4) * 4 : 0);
   wk.off_list_pre = take(pre_pairs * kcap * 4);
   wk.off_keys_pre = take(pre_pairs * kcap * 4);
-  wk.off_list_own = take(wk.listed ? pairs * kcap * 4 : 0);
+  wk.off_list_own = take(pairs * kcap * 4);
   wk.off_keys_own = take(wk.listed ? pairs * kcap * 4 : 0);
   if (n_prefixes) wk.pre = select_work(s, pre_pairs, kcap, max_prefix, wk.total);
   if (wk.listed) wk.own = select_work(s, pairs, kcap, s.max_len, wk.total);
@@ -872,8 +871,7 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
   const PrefixArgs p = {{table, row_req, row_len, n_rows, k, kcap}, {table, prefix_req, prefix_len, n_prefixes, k, kcap}, req_prefix,
                         (PrefixRow*)(base + wk.off_rows), (int32_t*)(base + wk.off_order), (PrefixTile*)(base + wk.off_tiles),
                         (int32_t*)(base + wk.off_list_pre), (int32_t*)(base + wk.off_list_own), (uint32_t*)(base + wk.off_keys_pre),
-                        (uint32_t*)(base + wk.off_keys_own), (Cut*)(base + wk.off_cuts), (float*)(base + wk.off_part_own),
-                        (float*)(base + wk.off_part_pre), wk.max_tiles, wk.nsplit};
+                        (uint32_t*)(base + wk.off_keys_own), (Cut*)(base + wk.off_cuts), (float*)(base + wk.off_part), wk.max_tiles, wk.nsplit, wk.listed};
   const int pairs = n_rows * s.H_q;
   // the lists: prefixes first, rows behind them; more pairs than a launch has room for take several
   auto set_of = [&](const CacheRows& rows, const SelectWork& w, int32_t* list, uint32_t* keys, bool used) {
@@ -917,24 +915,20 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
   else if (s.page_size == 32) select(std::integral_constant<int, 2>{});
   else select(std::integral_constant<int, 4>{});
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
+  const int G = s.H_q / s.H_kv;
+  const unsigned grid = (unsigned)(((long)n_rows * s.H_kv + 7) / 8 * 8 * G);
+  const bool many = pairs >= 4 * CUS;  // (row, head) pairs: two waves to each, else four
+  if (many) prefix_cut_kernel<2><<<grid, 128, 0, st>>>(c, p);
+  else prefix_cut_kernel<4><<<grid, 256, 0, st>>>(c, p);
   auto go = [&](auto t, auto width) {
     using T = std::remove_pointer_t<decltype(t)>;
     constexpr int D = decltype(width)::value, NW = tile_waves(D);
-    const int G = s.H_q / s.H_kv;
-    const unsigned grid = (unsigned)(((long)n_rows * s.H_kv + 7) / 8 * 8 * G);
-    auto row = [&](auto waves, auto listed) {
-      constexpr int W = decltype(waves)::value;
-      prefix_row_kernel<T, D, W, decltype(listed)::value><<<grid, 64 * W, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
-    };
-    auto rows = [&](auto waves) {
-      if (wk.listed) row(waves, std::true_type{}); else row(waves, std::false_type{});
-    };
-    if (pairs < 4 * CUS || kcap > 2048 || wk.listed || s.max_len > 1024) rows(std::integral_constant<int, 4>{});
-    else row(std::integral_constant<int, 2>{}, std::false_type{});
-    if (!n_prefixes) return;
-    const unsigned tiles = (unsigned)(((long)wk.max_tiles * s.H_kv * wk.nsplit + 7) / 8 * 8 * G);
-    prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
-    if (wk.nsplit > 1) prefix_merge_kernel<T, D><<<(unsigned)pairs, D, 0, st>>>(c, p, (T*)o, lse);
+    if (n_prefixes) {
+      const unsigned tiles = (unsigned)(((long)wk.max_tiles * s.H_kv * wk.nsplit + 7) / 8 * 8 * G);
+      prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, scale);
+    }
+    if (many) prefix_own_kernel<T, D, 2><<<grid, 128, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    else prefix_own_kernel<T, D, 4><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
   };
   auto types = [&](auto width) {
     if (s.dtype == DMA_BF16) go((__bf16*)nullptr, width); else go((float*)nullptr, width);

@@ -571,9 +571,10 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 // WAVES: four workgroups share a compute unit where 64 registers hold what they need (8), at the price of some in scratch, three where
 // they do not (6).  Four are worth it from more lists on than three of each compute unit are (whole calls, us, 6 / 8: 256 lists of
 // 8192 keys 26.7 / 27.1, 768 of 5461 53.4 / 54.2, 1024 of 4096 50.6 / 48.9, 2048 of 4096 79.0 / 78.1; SLICED, 2048 parts of 8192: 115.3 / 115.2).
-// EITHER: the launch is for rows in slices, but these may be none (no parts: there is no room for what slices tell each other).
+// Not `whole`: rows that keep all their keys get no list.  EITHER: the launch is for rows in slices, but these may be none (no parts: there is no room for what slices tell each other).
 template <int S, bool SLICED, bool KEYS, bool EITHER = false>
-__device__ __forceinline__ void select_block(const CacheRef& c, const CacheRows& p, const SliceWork& sw, int32_t* kept, uint32_t* keys, int block) {
+__device__ __forceinline__ void select_block(const CacheRef& c, const CacheRows& p, const SliceWork& sw, int32_t* kept, uint32_t* keys, int block,
+                                             bool whole = true) {
   const int part = SLICED ? block / sw.pairs : 0, pair = block - part * sw.pairs, rh = (SLICED ? sw.first : 0) + pair;
   const int r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x;
@@ -582,6 +583,7 @@ __device__ __forceinline__ void select_block(const CacheRef& c, const CacheRows&
   const int n = row.n, kk = min(p.k, n), parts = slices && n > SELECT_SHORT ? sw.parts : 1;
   if (part && n <= SELECT_SHORT) return;
   int32_t* list = kept + (size_t)rh * p.kcap;
+  if (kk == n && !whole) return;
   if (kk == n) {  // (a page out of range anywhere: none is kept)
     bool bad = false;
     for (long long j = tid; j << c.shift < n; j += 512) bad |= (uint32_t)row.pages[j] >= (uint32_t)c.n_pages;

@@ -179,17 +179,19 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
   auto place_of = [&](int u) { return (u * NW + w) * 64 + l; };
   // (all loads of four registers are on their way before the first is used: places behind the end read the last one)
   auto fetch_c = [&]() __attribute__((always_inline)) {
-#pragma unroll
-    for (int u0 = 0; u0 < RC; u0 += 4) {
-#pragma unroll
-      for (int u = u0; u < u0 + 4; u++) kc[u] = NO_KEY;
-      if (u0 * NW * 64 < n_pre) {
-#pragma unroll
-        for (int u = u0; u < u0 + 4; u++) kc[u] = keys_pre[min(place_of(u), n_pre - 1)];
-      }
-    }
-#pragma unroll
-    for (int u = 0; u < RC; u++) kc[u] = place_of(u) < n_pre ? kc[u] : NO_KEY;
+    static_for<RC / 4>([&](auto quad) __attribute__((always_inline)) {
+      constexpr int U0 = 4 * decltype(quad)::value;
+      static_for<4>([&](auto e) __attribute__((always_inline)) { kc[U0 + decltype(e)::value] = NO_KEY; });
+      if (U0 * NW * 64 < n_pre)
+        static_for<4>([&](auto e) __attribute__((always_inline)) {
+          constexpr int X = U0 + decltype(e)::value;
+          kc[X] = keys_pre[min(place_of(X), n_pre - 1)];
+        });
+    });
+    static_for<RC>([&](auto u) __attribute__((always_inline)) {
+      constexpr int X = decltype(u)::value;
+      kc[X] = place_of(X) < n_pre ? kc[X] : NO_KEY;
+    });
   };
   // slot of the own key at place j, of that page, and where its score is
   auto slot_of = [&](uint32_t page, int j) __attribute__((always_inline)) {
@@ -201,41 +203,38 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     return reinterpret_cast<const float*>(cache_page(c, slot) + c.off_z) + ((size_t)h << c.shift) + cache_place(c, slot);
   };
   auto fetch_o = [&](int round) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u0 = 0; u0 < RO; u0 += 4) {
-#pragma unroll
-      for (int u = u0; u < u0 + 4; u++) {
-        ko[u] = NO_KEY;
-        id[u] = 0;
-      }
-      if ((round * RO + u0) * NW * 64 < n_own) {
-#pragma unroll
-        for (int u = u0; u < u0 + 4; u++) {
-          const int j = min(place_of(round * RO + u), n_own - 1);
-          if (listed) {
-            id[u] = (uint32_t)list[j];
-            ko[u] = keys_own[j];
-          } else {
-            id[u] = (uint32_t)pages[j >> c.shift];
-          }
-        }
-      }
+    auto each = [&](auto f) __attribute__((always_inline)) {  // f(index, place) of the registers that hold something, four at a time
+      static_for<RO / 4>([&](auto quad) __attribute__((always_inline)) {
+        constexpr int U0 = 4 * decltype(quad)::value;
+        if ((round * RO + U0) * NW * 64 < n_own)
+          static_for<4>([&](auto e) __attribute__((always_inline)) {
+            constexpr int X = U0 + decltype(e)::value;
+            f(std::integral_constant<int, X>{}, min(place_of(round * RO + X), n_own - 1));
+          });
+      });
+    };
+    static_for<RO>([&](auto u) __attribute__((always_inline)) {
+      ko[decltype(u)::value] = NO_KEY;
+      id[decltype(u)::value] = 0;
+    });
+    if (listed) {
+      each([&](auto u, int j) __attribute__((always_inline)) {
+        id[decltype(u)::value] = (uint32_t)list[j];
+        ko[decltype(u)::value] = keys_own[j];
+      });
+    } else {
+      each([&](auto u, int j) __attribute__((always_inline)) { id[decltype(u)::value] = (uint32_t)pages[j >> c.shift]; });
+      each([&](auto u, int j) __attribute__((always_inline)) {
+        constexpr int X = decltype(u)::value;
+        id[X] = slot_of(id[X], j);
+        ko[X] = __float_as_uint(*score_at(id[X]));
+      });
+      static_for<RO>([&](auto u) __attribute__((always_inline)) { ko[decltype(u)::value] = score_key(__uint_as_float(ko[decltype(u)::value])); });
     }
-    if (!listed) {
-#pragma unroll
-      for (int u0 = 0; u0 < RO; u0 += 4)
-        if ((round * RO + u0) * NW * 64 < n_own) {
-#pragma unroll
-          for (int u = u0; u < u0 + 4; u++) {
-            const int j = min(place_of(round * RO + u), n_own - 1);
-            id[u] = slot_of(id[u], j);
-            ko[u] = __float_as_uint(*score_at(id[u]));
-          }
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < RO; u++)
-      ko[u] = place_of(round * RO + u) >= n_own ? NO_KEY : listed ? ko[u] : score_key(__uint_as_float(ko[u]));
+    static_for<RO>([&](auto u) __attribute__((always_inline)) {
+      constexpr int X = decltype(u)::value;
+      ko[X] = place_of(round * RO + X) < n_own ? ko[X] : NO_KEY;
+    });
   };
   fetch_o(0);
   const int rounds = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
@@ -245,18 +244,15 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
   if (selects) fetch_c();
   // f(key, place in its list, whether that is the prefix's) for all of this wave's keys; what the registers do not hold is read again
   auto every = [&](auto f) __attribute__((always_inline)) {
-#pragma unroll
-    for (int u0 = 0; u0 < RC; u0 += 8)
-      if (u0 * NW * 64 < n_pre) {
-#pragma unroll
-        for (int u = u0; u < u0 + 8; u++) f(kc[u], place_of(u), true);
-      }
-#pragma unroll
-    for (int u0 = 0; u0 < RO; u0 += 8)
-      if (u0 * NW * 64 < n_own) {
-#pragma unroll
-        for (int u = u0; u < u0 + 8; u++) f(ko[u], place_of(u), false);
-      }
+    static_for<RC / 8>([&](auto eight) __attribute__((always_inline)) {
+      constexpr int U0 = 8 * decltype(eight)::value;
+      if (U0 * NW * 64 < n_pre)
+        static_for<8>([&](auto e) __attribute__((always_inline)) { f(kc[U0 + decltype(e)::value], place_of(U0 + decltype(e)::value), true); });
+    });
+    static_for<RO / 8>([&](auto eight) __attribute__((always_inline)) {
+      constexpr int U0 = 8 * decltype(eight)::value;
+      static_for<8>([&](auto e) __attribute__((always_inline)) { f(ko[U0 + decltype(e)::value], place_of(U0 + decltype(e)::value), false); });
+    });
 #pragma unroll 1
     for (int i = place_of(RC); i < n_pre; i += NW * 64) f(keys_pre[i], i, true);
 #pragma unroll 1
@@ -304,7 +300,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
         before_hi = n;
       }
       if (hi - lo <= 1u) break;
-      const float share = (float)((uint32_t)k - before_lo) / (float)(before_hi - before_lo);
+      const float share = (float)((uint32_t)k - before_lo) * __builtin_amdgcn_rcpf((float)(before_hi - before_lo));
       const uint32_t ahead = step % 3 ? (uint32_t)((float)(hi - lo) * share) : (hi - lo) / 2;
       probe = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lo + min(max(ahead, 1u), hi - lo - 1u)));
     }
@@ -332,11 +328,11 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     if (round) fetch_o(round);
     uint32_t mine = 0;
     unsigned long long kept[RO];
-#pragma unroll
-    for (int u = 0; u < RO; u++) {
-      kept[u] = __ballot(ko[u] < cut_key || (ko[u] == cut_key && ko[u] != NO_KEY && place_of(round * RO + u) <= cut_own));
-      mine += (uint32_t)__popcll(kept[u]);
-    }
+    static_for<RO>([&](auto u) __attribute__((always_inline)) {
+      constexpr int X = decltype(u)::value;
+      kept[X] = __ballot(ko[X] < cut_key || (ko[X] == cut_key && ko[X] != NO_KEY && place_of(round * RO + X) <= cut_own));
+      mine += (uint32_t)__popcll(kept[X]);
+    });
     uint32_t at = total, all = mine;
     if constexpr (NW > 1) {
       turn ^= 1;
@@ -349,11 +345,11 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
         all += sums[turn][i];
       }
     }
-#pragma unroll
-    for (int u = 0; u < RO; u++) {
-      if (kept[u] >> l & 1) list[at + lanes_before(kept[u])] = (int32_t)id[u];
-      at += (uint32_t)__popcll(kept[u]);
-    }
+    static_for<RO>([&](auto u) __attribute__((always_inline)) {
+      constexpr int X = decltype(u)::value;
+      if (kept[X] >> l & 1) list[at + lanes_before(kept[X])] = (int32_t)id[X];
+      at += (uint32_t)__popcll(kept[X]);
+    });
     total += all;
   }
   if (tid == 0) p.cuts[rh] = {cut_key, cut_pre, gone ? -1 : (int)total, 0};

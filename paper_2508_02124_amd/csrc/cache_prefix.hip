@@ -146,20 +146,23 @@ __global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, Select
 
 // ------------------------------------------------------------------ a row's cut
 // NW waves per (row, head).  All keys wait in registers, 64 of the prefix's list or of the row's own to each (what these do not hold is read again
-// in every pass).  A key that exactly k lie before is looked for between the smallest and the largest: where a straight line through the counts
-// at both ends has it, and every third time half way.  A pass is two instructions for each register, and about seven are needed (halving alone: 13;
-// scores that are equal there take all bits, then the places are halved).  Counts are kept in the lanes and summed once a pass: one ballot a
-// register needed three scalar instructions, which four SIMDs share (64 rows of 32 heads, 2048 + 400 keys: 83 us instead of 26).
+// in every pass).  The cut is looked for between the smallest and the largest key: a pass counts the keys before two probes, to either side of where a
+// straight line through the counts at both ends has it (every third pass at thirds), until 64 keys are left, which are ranked; or a
+// probe has exactly k before it; or only equal keys are left, whose places are then halved.  About three passes, six at most on scores of the usual kinds.
+// (Halving alone took 13, one probe 7 and up to 17 -- the slowest row is what a launch takes.)  Counts are kept in the lanes and summed once a pass:
+// one ballot a register needed three scalar instructions, which four SIMDs share (64 rows of 32 heads, 2048 + 400 keys: 83 us instead of 26).
 // A row with more than k keys of its own has a list of the best of them, unless the caller's bound says that there are none; else they are
 // read where they are.
 template <int NW>
 __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixArgs p) {
   constexpr int RC = 16, RO = 8;
-  __shared__ uint32_t sums[2][NW];
+  constexpr uint32_t NEAR = 64;  // keys that a wave ranks, a lane each
+  __shared__ uint32_t sums[4][NW], near[NEAR], near_at[NEAR], n_near;
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   if (unit >= p.own.n_rows * c.H_kv) return;
   const int r = unit / c.H_kv, g = unit - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
+  if (tid == 0) n_near = 0;  // (barriers lie between)
   const PrefixRow info = p.rows[r];
   const int k = p.own.k, n_pre = min(k, info.pre);
   const bool listed = p.listed && info.own > k;
@@ -272,7 +275,6 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     return (uint32_t)__builtin_amdgcn_readfirstlane((int)x);
   };
   const auto add = [](uint32_t a, uint32_t b) { return a + b; };
-  const auto sum_lanes = [&](uint32_t x) __attribute__((always_inline)) { return over_waves(last_lane(wave_scan(x, 0u, add)), add); };
   uint32_t cut_key = NO_KEY;
   int cut_pre = -1, cut_own = -1;  // of the keys equal to cut_key, those up to these places are kept
   if (selects) {
@@ -286,35 +288,86 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     // fewer than k keys are before lo, at least k before hi
     uint32_t lo = over_waves(least, [](uint32_t a, uint32_t b) { return min(a, b); });
     uint32_t hi = over_waves(most, [](uint32_t a, uint32_t b) { return max(a, b); });
-    uint32_t probe = hi, before_lo = 0, before_hi = 0;
+    uint32_t before_lo = 0, before_hi = NO_KEY, first = hi - min((hi - lo) / 16, hi - lo - 1u), second = hi;
+    bool found = false;
     for (int step = 1;; step++) {
-      uint32_t n = 0;
-      every([&](uint32_t key, int, bool) __attribute__((always_inline)) { n += key < probe; });
-      n = sum_lanes(n);
-      if (n == (uint32_t)k) break;  // exactly the keys before `probe`
-      if (n < (uint32_t)k) {
-        lo = probe;
-        before_lo = n;
-      } else {
-        hi = probe;
-        before_hi = n;
+      uint32_t n = 0, m = 0;
+      every([&](uint32_t key, int, bool) __attribute__((always_inline)) {
+        n += key < first;
+        m += key < second;
+      });
+      n = last_lane(wave_scan(n, 0u, add));
+      m = last_lane(wave_scan(m, 0u, add));
+      turn ^= 1;
+      if (l == 0) {
+        sums[turn][w] = n;
+        sums[2 + turn][w] = m;
       }
-      if (hi - lo <= 1u) break;
-      const float share = (float)((uint32_t)k - before_lo) * __builtin_amdgcn_rcpf((float)(before_hi - before_lo));
-      const uint32_t ahead = step % 3 ? (uint32_t)((float)(hi - lo) * share) : (hi - lo) / 2;
-      probe = (uint32_t)__builtin_amdgcn_readfirstlane((int)(lo + min(max(ahead, 1u), hi - lo - 1u)));
+      __syncthreads();
+      n = m = 0;
+#pragma unroll
+      for (int i = 0; i < NW; i++) {
+        n += sums[turn][i];
+        m += sums[2 + turn][i];
+      }
+      n = (uint32_t)__builtin_amdgcn_readfirstlane((int)n);
+      m = (uint32_t)__builtin_amdgcn_readfirstlane((int)m);
+      found = n == (uint32_t)k || m == (uint32_t)k;
+      if (found) {  // exactly the keys before it
+        cut_key = n == (uint32_t)k ? first : second;
+        break;
+      }
+      if (n > (uint32_t)k) {
+        hi = first;
+        before_hi = n;
+      } else {
+        const bool beyond = m < (uint32_t)k;
+        lo = beyond ? second : first;
+        before_lo = beyond ? m : n;
+        hi = beyond ? hi : second;
+        before_hi = beyond ? before_hi : m;
+      }
+      const uint32_t width = hi - lo, left = before_hi - before_lo;
+      if (width <= 1u || left <= NEAR) break;
+      const float each = __builtin_amdgcn_rcpf((float)left), share = (float)((uint32_t)k - before_lo) * each;
+      const float off = step % 3 ? (__builtin_amdgcn_sqrtf((float)left) + 1.f) * each : 1.f / 6.f, at = step % 3 ? share : 0.5f;
+      auto probe = [&](float x) {
+        const uint32_t ahead = (uint32_t)((float)width * fmaxf(x, 0.f));
+        return (uint32_t)__builtin_amdgcn_readfirstlane((int)(lo + min(max(ahead, 1u), width - 1u)));
+      };
+      first = probe(at - off);
+      second = probe(at + off);
     }
-    cut_key = probe;
-    if (hi - lo <= 1u) {  // keys equal to lo are on both sides: the prefix's are first
+    const uint32_t need = (uint32_t)k - before_lo, left = before_hi - before_lo;  // the need-th of the left ones is the last that is kept
+    if (!found && left <= NEAR) {
+      every([&](uint32_t key, int place, bool pre) __attribute__((always_inline)) {
+        if (key - lo < hi - lo) {
+          const uint32_t i = atomicAdd(&n_near, 1u);
+          near[i] = key;
+          near_at[i] = (uint32_t)place + (pre ? 0u : (uint32_t)n_pre);
+        }
+      });
+      __syncthreads();
+      const uint32_t key = l < (int)left ? near[l] : NO_KEY, at = l < (int)left ? near_at[l] : NO_KEY;
+      uint32_t rank = 0;
+      for (int i = 0; i < (int)left; i++) {
+        const uint32_t x = (uint32_t)__builtin_amdgcn_readlane((int)key, i), y = (uint32_t)__builtin_amdgcn_readlane((int)at, i);
+        rank += (x < key) | ((x == key) & (y < at));
+      }
+      const int last = (int)__builtin_ctzll(__ballot(rank == need - 1u && l < (int)left));
+      cut_key = (uint32_t)__builtin_amdgcn_readlane((int)key, last);
+      const int place = __builtin_amdgcn_readlane((int)at, last);
+      cut_pre = min(place, n_pre - 1);
+      cut_own = place - n_pre;
+    } else if (!found) {  // keys equal to lo are on both sides: the prefix's are first
       cut_key = lo;
-      const uint32_t need = (uint32_t)k - before_lo;
       long from = 0, upto = (long)n_pre + n_own;  // fewer than `need` of them are before place `from`, at least as many before `upto`
       while (upto - from > 1) {
         const long middle = (from + upto) / 2;
         const int before_pre = (int)min(middle, (long)n_pre), before_own = (int)(middle - before_pre);
         uint32_t n = 0;
         every([&](uint32_t key, int place, bool pre) __attribute__((always_inline)) { n += (key == lo) & (place < (pre ? before_pre : before_own)); });
-        if (sum_lanes(n) < need) from = middle; else upto = middle;
+        if (over_waves(last_lane(wave_scan(n, 0u, add)), add) < need) from = middle; else upto = middle;
       }
       cut_pre = (int)min(upto, (long)n_pre) - 1;
       cut_own = (int)(upto - n_pre) - 1;

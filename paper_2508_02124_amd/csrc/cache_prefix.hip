@@ -19,9 +19,10 @@ constexpr int TILE_ROWS = 32;
 struct PrefixRow {
   int own, pre, prefix, req;
 };
-// Rows of one prefix: order[start] .. order[start + count - 1] (count 0: behind the last tile).
+// Rows of one prefix (count 0: behind the last tile; only that many of the rows are there).
 struct PrefixTile {
-  int prefix, start, count, pre;
+  int prefix, count, pre, unused;
+  int rows[TILE_ROWS];
 };
 // What a row keeps: of the prefix's list the keys before `key`, and those equal to it up to place `last`; of its own the `count` that
 // are listed (-1: a page is out of range, the row sees nothing).
@@ -34,7 +35,6 @@ struct PrefixArgs {
   CacheRows own, pre;  // the rows, and the prefixes as rows of the requests that hold them
   const int32_t* req_prefix;
   PrefixRow* rows;
-  int32_t* order;
   PrefixTile* tiles;
   int32_t *list_pre, *list_own;    // [prefixes or rows][H_q][kcap]
   uint32_t *keys_pre, *keys_own;   // the listed keys
@@ -48,8 +48,8 @@ struct PrefixArgs {
 // One workgroup: what each row sees, and the rows of each prefix together, in tiles.  (A row's result does not depend on its place in a
 // tile, so the order inside a prefix may be any.)
 __device__ __forceinline__ void group_rows(const CacheRef& c, const PrefixArgs& p) {
-  __shared__ uint32_t cursor[CACHE_REQS_MAX];  // rows of a prefix, then the place of the next one
-  __shared__ uint32_t wsum[8][2];
+  __shared__ uint32_t cursor[CACHE_REQS_MAX];  // rows of a prefix, then the place of the next one: tile * 32 + row in it
+  __shared__ uint32_t wsum[8];
   const int tid = threadIdx.x, l = tid & 63, w = tid >> 6, n_prefixes = p.pre.n_rows;
   constexpr int PER = CACHE_REQS_MAX / 512;
   for (int i = tid; i < n_prefixes; i += 512) cursor[i] = 0;
@@ -69,45 +69,44 @@ __device__ __forceinline__ void group_rows(const CacheRef& c, const PrefixArgs& 
   }
   __syncthreads();
   if (!n_prefixes) return;
-  uint32_t count[PER], rows = 0, tiles = 0;
+  uint32_t count[PER], tiles = 0;
 #pragma unroll
   for (int e = 0; e < PER; e++) {
     const int i = tid * PER + e;
     count[e] = i < n_prefixes ? cursor[i] : 0u;
-    rows += count[e];
     tiles += (count[e] + TILE_ROWS - 1) / TILE_ROWS;
   }
-  const auto add = [](uint32_t a, uint32_t b) { return a + b; };
-  uint32_t row0 = wave_scan(rows, 0u, add), tile0 = wave_scan(tiles, 0u, add);
-  if (l == 63) {
-    wsum[w][0] = row0;
-    wsum[w][1] = tile0;
-  }
+  uint32_t tile0 = wave_scan(tiles, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+  if (l == 63) wsum[w] = tile0;
   __syncthreads();
-  row0 -= rows;
   tile0 -= tiles;
   uint32_t all_tiles = 0;
 #pragma unroll
   for (int i = 0; i < 8; i++) {
-    row0 += i < w ? wsum[i][0] : 0u;
-    tile0 += i < w ? wsum[i][1] : 0u;
-    all_tiles += wsum[i][1];
+    tile0 += i < w ? wsum[i] : 0u;
+    all_tiles += wsum[i];
   }
 #pragma unroll
   for (int e = 0; e < PER; e++) {
     const int i = tid * PER + e;
     if (i >= n_prefixes) break;
     const int pre = count[e] ? cache_row(c, p.pre, i).n : 0;
-    for (uint32_t a = 0; a < count[e]; a += TILE_ROWS)
-      p.tiles[tile0++] = {i, (int)(row0 + a), (int)min(count[e] - a, (uint32_t)TILE_ROWS), pre};
-    cursor[i] = row0;
-    row0 += count[e];
+    cursor[i] = tile0 * TILE_ROWS;
+    for (uint32_t a = 0; a < count[e]; a += TILE_ROWS, tile0++) {
+      PrefixTile& t = p.tiles[tile0];
+      t.prefix = i;
+      t.count = (int)min(count[e] - a, (uint32_t)TILE_ROWS);
+      t.pre = pre;
+    }
   }
-  for (int i = (int)all_tiles + tid; i < p.max_tiles; i += 512) p.tiles[i] = {0, 0, 0, 0};
+  for (int i = (int)all_tiles + tid; i < p.max_tiles; i += 512) p.tiles[i].count = 0;
   __syncthreads();
   for (int r = tid; r < p.own.n_rows; r += 512) {
     const int prefix = p.rows[r].prefix;  // (this thread wrote it)
-    if (prefix >= 0) p.order[atomicAdd(&cursor[prefix], 1u)] = r;
+    if (prefix >= 0) {
+      const uint32_t at = atomicAdd(&cursor[prefix], 1u);
+      p.tiles[at / TILE_ROWS].rows[at % TILE_ROWS] = r;
+    }
   }
 }
 
@@ -456,12 +455,15 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   __shared__ __align__(16) float ml[NW][2][32];
   __shared__ __align__(16) uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers
   __shared__ uint32_t row_nan[32];
+  __shared__ int tile_row[32];
   __shared__ float wave_weight[NW][32], row_sum[2][32];
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   const int per = p.max_tiles * c.H_kv, sp = unit / per, tg = unit - sp * per;
   if (sp >= p.nsplit) return;
   const int t = tg / c.H_kv, g = tg - t * c.H_kv, h = g * G + idx % G;
-  const PrefixTile tile = p.tiles[t];
+  const PrefixTile* tp = p.tiles + t;
+  const int listed_row = tp->rows[threadIdx.x & 31];  // (with the tile's head, not behind it)
+  const struct { int prefix, count, pre; } tile = {tp->prefix, tp->count, tp->pre};
   if (tile.count == 0) return;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63, n = l & 31, hh = l >> 5;
   const int n_keys = min(p.pre.k, tile.pre), step = p.nsplit * NW * 32;
@@ -471,7 +473,9 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   uint16_t* vt = reinterpret_cast<uint16_t*>(mem + w * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES));
   int j0 = (sp * NW + w) * 32;
   uint32_t id = (uint32_t)list[min(j0 + n, n_keys - 1)], key = keys[min(j0 + n, n_keys - 1)];
-  const int row = p.order[tile.start + min(n, tile.count - 1)];
+  const int first_row = __builtin_amdgcn_readfirstlane(listed_row);  // (with all lanes there: in a branch it would be the first of that branch)
+  const int row = n < tile.count ? listed_row : first_row;
+  if (tid < 32) tile_row[tid] = row;
   if (tid < 32) row_nan[tid] = 0;
   struct Raw {
     uint4 k[NQ], v[NQ];
@@ -674,7 +678,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   constexpr int QUADS = D / 4, PER_PASS = 64 * NW / QUADS;
   const int ch = tid % QUADS * 4;
   for (int rr = tid / QUADS; rr < tile.count; rr += PER_PASS) {
-    const int r = p.order[tile.start + rr];
+    const int r = tile_row[rr];
     const size_t rh = (size_t)r * c.H_q + h;
     float num[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -871,11 +875,14 @@ __global__ __launch_bounds__(64 * NW) void prefix_own_kernel(CacheRef c, PrefixA
 
 // ------------------------------------------------------------------ host side
 struct PrefixWork {
-  size_t off_rows, off_order, off_tiles, off_list_pre, off_keys_pre, off_list_own, off_keys_own, off_cuts, off_part, total;
+  size_t off_rows, off_tiles, off_list_pre, off_keys_pre, off_list_own, off_keys_own, off_cuts, off_part, total;
   SelectWork pre, own;
   bool listed;
   int max_tiles, nsplit;
 };
+// A row of at most so many keys of its own needs no list of the best of them for its cut (40 requests x 5 rows of 500 keys, window 512, 16
+// heads: the lists' launch 13 -> 21 us with them).
+constexpr int OWN_DIRECT = 2048;
 constexpr int tile_waves(int d) { return d == 256 ? 4 : 8; }
 static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n_prefixes, int max_prefix) {
   const int kcap = list_length(s, k);
@@ -883,14 +890,13 @@ static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n
   const size_t pairs = (size_t)n_rows * s.H_q, pre_pairs = (size_t)n_prefixes * s.H_q;
   PrefixWork wk = {};
   auto take = [&](size_t bytes) { size_t at = wk.total; wk.total = align_up(at + bytes, 256); return at; };
-  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > k;
+  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > (k > OWN_DIRECT ? k : OWN_DIRECT);
   const long groups = n_prefixes < n_rows ? n_prefixes : n_rows;
   wk.max_tiles = n_prefixes ? (int)((n_rows + (TILE_ROWS - 1) * groups) / TILE_ROWS) : 0;
   // parts of the lists: so many that every compute unit has one, as long as a wave has a step to take
   const long per = 32 * tile_waves(s.d), most = (kcap + per - 1) / per, want = wk.max_tiles ? CUS / ((long)wk.max_tiles * s.H_q) : 1;
   wk.nsplit = (int)(want < 1 ? 1 : want > most ? most : want);
   wk.off_rows = take((size_t)n_rows * sizeof(PrefixRow));
-  wk.off_order = take((size_t)n_rows * 4);
   wk.off_tiles = take((size_t)wk.max_tiles * sizeof(PrefixTile));
   wk.off_cuts = take(pairs * sizeof(Cut));
   // (there are at least n_rows / 32 tiles, so several parts of each pair are at most 32 * CUS: room that never is less for more rows)
@@ -918,7 +924,7 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
   const int kcap = list_length(s, k);
   char* base = (char*)ws;
   const PrefixArgs p = {{table, row_req, row_len, n_rows, k, kcap}, {table, prefix_req, prefix_len, n_prefixes, k, kcap}, req_prefix,
-                        (PrefixRow*)(base + wk.off_rows), (int32_t*)(base + wk.off_order), (PrefixTile*)(base + wk.off_tiles),
+                        (PrefixRow*)(base + wk.off_rows), (PrefixTile*)(base + wk.off_tiles),
                         (int32_t*)(base + wk.off_list_pre), (int32_t*)(base + wk.off_list_own), (uint32_t*)(base + wk.off_keys_pre),
                         (uint32_t*)(base + wk.off_keys_own), (Cut*)(base + wk.off_cuts), (float*)(base + wk.off_part), wk.max_tiles, wk.nsplit, wk.listed};
   const int pairs = n_rows * s.H_q;

@@ -449,14 +449,13 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   constexpr bool F32 = sizeof(TQ) == 4;
   constexpr int KS = D / 16, CB = D / 32, NQ = D / 64, NTQ = F32 ? 3 : 1, NTP = F32 ? 3 : 2, PITCH = D + 4;
   constexpr int TILE_BYTES = 32 * D * 2, OUT_BYTES = 32 * PITCH * 4;
-  __shared__ __align__(16) char mem[NW * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES)];  // a V tile of each wave; in the end its sums
+  constexpr int WAVE_BYTES = TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES;
+  __shared__ __align__(16) char mem[NW * WAVE_BYTES];  // a V tile of each wave; in the end its sums
   __shared__ __align__(16) uint32_t s_key[NW][32];
   __shared__ __align__(16) float s_z[NW][32];
   __shared__ __align__(16) float ml[NW][2][32];
-  __shared__ __align__(16) uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers
-  __shared__ uint32_t row_nan[32];
+  __shared__ __align__(16) uint32_t s_nan[NW][32];  // blocks of a key's V that are no numbers; in the end, of a row's sums
   __shared__ int tile_row[32];
-  __shared__ float wave_weight[NW][32], row_sum[2][32];
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   const int per = p.max_tiles * c.H_kv, sp = unit / per, tg = unit - sp * per;
   if (sp >= p.nsplit) return;
@@ -470,13 +469,12 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   const size_t at_pre = ((size_t)tile.prefix * c.H_q + h) * p.pre.kcap;
   const int32_t* list = p.list_pre + at_pre;
   const uint32_t* keys = p.keys_pre + at_pre;
-  uint16_t* vt = reinterpret_cast<uint16_t*>(mem + w * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES));
+  uint16_t* vt = reinterpret_cast<uint16_t*>(mem + w * WAVE_BYTES);
   int j0 = (sp * NW + w) * 32;
   uint32_t id = (uint32_t)list[min(j0 + n, n_keys - 1)], key = keys[min(j0 + n, n_keys - 1)];
   const int first_row = __builtin_amdgcn_readfirstlane(listed_row);  // (with all lanes there: in a branch it would be the first of that branch)
   const int row = n < tile.count ? listed_row : first_row;
   if (tid < 32) tile_row[tid] = row;
-  if (tid < 32) row_nan[tid] = 0;
   struct Raw {
     uint4 k[NQ], v[NQ];
     uint32_t kb, vb, key;
@@ -534,7 +532,6 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   for (int b = 0; b < CB; b++)
 #pragma unroll
     for (int v = 0; v < 16; v++) acc[b][v] = 0.f;
-  __syncthreads();
   while (at0 < n_keys) {
     Raw next;
     if (j0 < n_keys) fetch(next); else j0 += step;
@@ -646,54 +643,48 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
     at0 += step;
   }
   lsum = half_swap_sum(lsum);
-  if (nan) atomicOr(&row_nan[n], nan);
-  __syncthreads();  // (the tiles have been read)
+  {
+    const auto both = __builtin_amdgcn_permlane32_swap(nan, nan, false, false);
+    nan = both[0] | both[1];
+  }
   if (hh == 0) {
     ml[w][0][n] = m;
     ml[w][1][n] = lsum;
+    s_nan[w][n] = nan;
   }
-  float* out = reinterpret_cast<float*>(vt) + n * PITCH;
+  asm volatile("" ::: "memory");
+  float* out = reinterpret_cast<float*>(vt) + n * PITCH;  // (over the wave's own tile, which it has read)
 #pragma unroll
   for (int b = 0; b < CB; b++)
 #pragma unroll
     for (int v = 0; v < 16; v += 4)
       *reinterpret_cast<float4*>(out + 32 * b + 2 * v + 4 * hh) = make_float4(acc[b][v], acc[b][v + 1], acc[b][v + 2], acc[b][v + 3]);
   __syncthreads();
-  // each wave's weight of a row, then four channels of a row to a thread
-  if (tid < 32) {
-    float M = -INFINITY, den = 0.f;
-#pragma unroll
-    for (int x = 0; x < NW; x++) M = fmaxf(M, ml[x][0][tid]);
-    const float mr = M == -INFINITY ? 0.f : M;
-#pragma unroll
-    for (int x = 0; x < NW; x++) {
-      const float w8 = weight(ml[x][0][tid], mr);
-      den = fmaf(ml[x][1][tid], w8, den);
-      wave_weight[x][tid] = w8;
-    }
-    row_sum[0][tid] = M;
-    row_sum[1][tid] = den;
-  }
-  __syncthreads();
+  // four channels of a row to a thread
   constexpr int QUADS = D / 4, PER_PASS = 64 * NW / QUADS;
   const int ch = tid % QUADS * 4;
   for (int rr = tid / QUADS; rr < tile.count; rr += PER_PASS) {
-    const int r = tile_row[rr];
-    const size_t rh = (size_t)r * c.H_q + h;
-    float num[4] = {0.f, 0.f, 0.f, 0.f};
+    const size_t rh = (size_t)tile_row[rr] * c.H_q + h;
+    float M = -INFINITY, den = 0.f, num[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t nans = 0;
+#pragma unroll
+    for (int x = 0; x < NW; x++) M = fmaxf(M, ml[x][0][rr]);
+    const float mr = M == -INFINITY ? 0.f : M;
 #pragma unroll
     for (int x = 0; x < NW; x++) {
-      const float4 v = *reinterpret_cast<const float4*>(mem + x * (TILE_BYTES > OUT_BYTES ? TILE_BYTES : OUT_BYTES) + (rr * PITCH + ch) * 4);
-      const float w8 = wave_weight[x][rr];
+      const float4 v = *reinterpret_cast<const float4*>(mem + x * WAVE_BYTES + (rr * PITCH + ch) * 4);
+      const float w8 = weight(ml[x][0][rr], mr);
+      den = fmaf(ml[x][1][rr], w8, den);
       num[0] = fmaf(v.x, w8, num[0]);
       num[1] = fmaf(v.y, w8, num[1]);
       num[2] = fmaf(v.z, w8, num[2]);
       num[3] = fmaf(v.w, w8, num[3]);
+      nans |= s_nan[x][rr];
     }
-    if (row_nan[rr] >> (ch / 32) & 1) num[0] = num[1] = num[2] = num[3] = NAN;
+    if (nans >> (ch / 32) & 1) num[0] = num[1] = num[2] = num[3] = NAN;
     float* to = p.part + (rh * p.nsplit + sp) * (D + 4);
     *reinterpret_cast<float4*>(to + ch) = make_float4(num[0], num[1], num[2], num[3]);
-    if (ch == 0) *reinterpret_cast<float2*>(to + D) = make_float2(row_sum[0][rr], row_sum[1][rr]);
+    if (ch == 0) *reinterpret_cast<float2*>(to + D) = make_float2(M, den);
   }
 }
 

@@ -19,6 +19,7 @@ import math
 import torch
 
 from . import binding as B
+from .paged_cache import PagedCache
 
 
 def _dtype_code(t):
@@ -122,6 +123,54 @@ def dynamic_mask_attention(Q, K, V, W, A, cu_seqlens, k, max_seqlen=0, softmax_s
     return DynamicMaskAttentionFunction.apply(Q, K, V, W, A, cu_seqlens, k, max_seqlen, softmax_scale, bias)
 
 
+def rotary_freqs(dim, base=10000.0, device=None):
+    """base^(-2 i / dim) for the dim / 2 pairs of dim rotated channels (float32)."""
+    i = torch.arange(dim // 2, dtype=torch.float64, device=device)
+    return (float(base) ** (-2.0 * i / dim)).float()
+
+
+class RotaryFunction(torch.autograd.Function):
+    """Q and K turned to their positions, or back (dma_rope); their gradients go the other way.  Differentiable in Q and K, any number of times."""
+
+    @staticmethod
+    def forward(ctx, Q, K, freqs, cu_seqlens, positions, interleaved, inverse):
+        T = Q.shape[0]
+        for name, t in (("Q", Q), ("K", K), ("freqs", freqs), ("cu_seqlens", cu_seqlens), ("positions", positions)):
+            if t is not None and not t.is_cuda:
+                raise RuntimeError(f"{name} must live on the GPU: this library has no CPU path")
+            if t is not None and t.device != Q.device:
+                raise RuntimeError(f"{name} must be on {Q.device}, got {t.device}")
+        if Q.dim() != 3 or K.dim() != 3 or K.shape[0] != T or K.shape[2] != Q.shape[2]:
+            raise ValueError("expected Q [T, H_q, d] and K [T, H_kv, d]")
+        if (cu_seqlens is None) == (positions is None):
+            raise ValueError("positions are those in the documents of cu_seqlens, or given: one of the two")
+        if positions is not None and positions.shape != (T,):
+            raise ValueError(f"expected positions [{T}], got {list(positions.shape)}")
+        if K.dtype != Q.dtype or freqs.dtype != torch.float32 or freqs.dim() != 1 or (cu_seqlens if positions is None else positions).dtype != torch.int32:
+            raise TypeError("Q and K must share one dtype, freqs [m] be float32, cu_seqlens or positions int32")
+        freqs, cu_seqlens, positions = (None if t is None else t.contiguous() for t in (freqs, cu_seqlens, positions))
+        shape = B.make_shape(T, 1 if cu_seqlens is None else cu_seqlens.numel() - 1, Q.shape[1], K.shape[1], Q.shape[2], 1, dtype=_dtype_code(Q))
+        Qi, Ki = PagedCache._rows(Q), PagedCache._rows(K)     # (where they lie, if rows can be read there)
+        Qo, Ko = (torch.empty(x.shape, dtype=x.dtype, device=x.device) for x in (Q, K))
+        with torch.cuda.device(Q.device):
+            B.dma_rope(shape, Qi, Qi.stride(0), Ki, Ki.stride(0), cu_seqlens, positions, freqs, 2 * freqs.numel(), interleaved, inverse, Qo,
+                       Qo.stride(0), Ko, Ko.stride(0))
+        ctx.save_for_backward(freqs, cu_seqlens, positions)
+        ctx.way = bool(interleaved), not inverse
+        return Qo, Ko
+
+    @staticmethod
+    def backward(ctx, dQ, dK):
+        return (*RotaryFunction.apply(dQ, dK, *ctx.saved_tensors, *ctx.way), None, None, None, None, None)
+
+
+def rotary(Q, K, freqs, cu_seqlens=None, positions=None, interleaved=False):
+    """Q [T, H_q, d] and K [T, H_kv, d] with their first 2 * len(freqs) channels turned in pairs, pair i by position * freqs[i]: the
+    channels (i, i + len(freqs)), or (2 i, 2 i + 1) if interleaved.  A token's position is its place in its document (cu_seqlens), or
+    positions [T] (int32).  Differentiable in Q and K, which may be parts of one projection's output."""
+    return RotaryFunction.apply(Q, K, freqs, cu_seqlens, positions, interleaved, False)
+
+
 class DynamicMaskAttention(torch.nn.Module):
     """The attention core of a DMA layer (the part between the QKV projections and the output
     projection).  Parameters: the score projection `W` [H_q, d] (the paper's Delta taken per head;
@@ -130,11 +179,12 @@ class DynamicMaskAttention(torch.nn.Module):
     keeps the initial scores in (0, 1) and close together.
 
     forward(q, k, v): [B, L, H, d] batches (each sequence its own document), or packed [T, H, d]
-    tensors with cu_seqlens.
+    tensors with cu_seqlens.  rotary_dim > 0: q and k are turned to their positions first (rotary), in that many
+    channels; positions [T] (int32, [B, L] with batches) replace those in the documents.
     """
 
     def __init__(self, num_heads, num_kv_heads, head_dim, keep_window, softmax_scale=None, device=None,
-                 cross_head=False):
+                 cross_head=False, rotary_dim=0, rotary_base=10000.0, rotary_interleaved=False):
         super().__init__()
         if num_heads % num_kv_heads:
             raise ValueError("num_heads must be a multiple of num_kv_heads")
@@ -144,32 +194,50 @@ class DynamicMaskAttention(torch.nn.Module):
         fan_in = head_dim * (num_kv_heads if cross_head else 1)   # cross_head: the full Delta of Eq. 3
         self.W = torch.nn.Parameter(torch.randn(num_heads, fan_in, dtype=torch.float32, device=device)
                                     / math.sqrt(fan_in))
+        if rotary_dim % 16 or not 0 <= rotary_dim <= head_dim:
+            raise ValueError("rotary_dim must be a multiple of 16 of at most head_dim")
+        self.rotary_interleaved = bool(rotary_interleaved)
+        freqs = rotary_freqs(rotary_dim, rotary_base, device) if rotary_dim else None
+        self.register_buffer("rotary_freqs", freqs, persistent=False)
         self.A = torch.nn.Parameter(torch.full((num_heads,), -1.0, dtype=torch.float32, device=device))
 
-    def forward(self, q, k, v, cu_seqlens=None, max_seqlen=0):
+    def forward(self, q, k, v, cu_seqlens=None, max_seqlen=0, positions=None):
         if q.dim() == 4:
             if cu_seqlens is not None:
                 raise ValueError("cu_seqlens goes with packed [T, H, d] inputs")
             Bsz, L = q.shape[0], q.shape[1]
             cu = torch.arange(0, (Bsz + 1) * L, L, dtype=torch.int32, device=q.device)
-            o = dynamic_mask_attention(q.reshape(Bsz * L, *q.shape[2:]), k.reshape(Bsz * L, *k.shape[2:]),
-                                       v.reshape(Bsz * L, *v.shape[2:]), self.W, self.A, cu,
-                                       self.keep_window, L, self.softmax_scale)
+            packed = (x.reshape(Bsz * L, *x.shape[2:]) for x in (q, k, v))
+            o = self._attend(*packed, cu, L, None if positions is None else positions.reshape(-1))
             return o.view(Bsz, L, *q.shape[2:])
         if cu_seqlens is None:
             raise ValueError("packed inputs need cu_seqlens")
+        return self._attend(q, k, v, cu_seqlens, max_seqlen, positions)
+
+    def _attend(self, q, k, v, cu_seqlens, max_seqlen, positions):
+        if self.rotary_freqs is not None:
+            q, k = rotary(q, k, self.rotary_freqs, cu_seqlens if positions is None else None, positions, self.rotary_interleaved)
+        elif positions is not None:
+            raise ValueError("positions go with rotary_dim")
         return dynamic_mask_attention(q, k, v, self.W, self.A, cu_seqlens, self.keep_window, max_seqlen,
                                       self.softmax_scale)
 
-    def step(self, q, k, v, cache, rows, max_len=0):
+    def step(self, q, k, v, cache, rows, max_len=0, prefixes=None, max_prefix=0):
         """A decoding step over a paged cache (paged_cache.PagedCache): k, v [n, H_kv, d] of the step's new rows go to their places
         with this module's scores, then q [n, H_q, d] attends from them.  rows: what cache.assign returned; max_len: as for
-        cache.decode.  Without gradients; o [n, H_q, d].  What cannot be done is refused before the cache is changed."""
+        cache.decode; prefixes, max_prefix: as for cache.decode_prefix.  With rotary_dim, k and q are turned on the way, to their places in
+        the requests, behind the prefixes.  Without gradients; o [n, H_q, d].  What cannot be done is refused before the cache is changed."""
         with torch.no_grad():
             W, A = self.W.detach(), self.A.detach()
-            checked = cache._check_decode(q, self.keep_window, rows, self.softmax_scale, max_len)   # (before the rows go in)
+            checked = cache._check_decode(q, self.keep_window, rows, self.softmax_scale, max_len, prefixes, max_prefix)   # (before the rows go in)
+            freqs = self.rotary_freqs
+            if freqs is not None:
+                cache._check_rotary(rows, q, freqs, prefixes)
             if W.shape[1] == self.head_dim:
-                cache.append(rows.slots, k, v, W=W, A=A)
+                if freqs is None:
+                    cache.append(rows.slots, k, v, W=W, A=A)
+                else:
+                    q = cache.append_rotary(rows, q, k, v, freqs, W=W, A=A, prefixes=prefixes, interleaved=self.rotary_interleaved)
             else:                                    # the cross-head scores have an entry point of their own
                 s, n = cache.shape, rows.slots.numel()
                 cache._check_values(rows.slots, k, v)         # (all that append checks: a kernel reads v, W and A before it)
@@ -179,5 +247,10 @@ class DynamicMaskAttention(torch.nn.Module):
                 if n:
                     shape = B.make_shape(n, 1, s.H_q, s.H_kv, s.d, 1, dtype=_dtype_code(v))
                     cache._call_with(shape, B.dma_scores_xhead, cache._rows(v).contiguous(), cache._aligned(W), A, z)
-                cache._append(rows.slots, k, v, None, None, z)
+                if freqs is None:
+                    cache._append(rows.slots, k, v, None, None, z)
+                else:
+                    q = cache._append_rotary(rows, q, k, v, freqs, None, None, z, prefixes, self.rotary_interleaved)
+            if prefixes is not None:
+                return cache._attend_prefix(q, *checked, self.softmax_scale, prefixes, max_prefix)[0]
             return cache._attend(q, *checked, self.softmax_scale)[0]

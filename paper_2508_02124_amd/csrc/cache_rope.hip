@@ -77,7 +77,7 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
     const long cap = (long)c.max_pages << c.shift;
     if ((uint32_t)prefix < (uint32_t)p.n_prefixes) position = max(position, 0l) + max(0l, min((long)p.prefix_len[prefix], cap));
   }
-  position = max(0l, position);
+  position = max(0l, min(position, 0x7fffffffl));
   const bool turned = sub < 2 * half, first = sub < half;
   const int other = !NEXT && turned ? (first ? l + half : l - half) : l;
   // its angles: of the eight pairs that the two lanes have halves of, or of the lane's own four

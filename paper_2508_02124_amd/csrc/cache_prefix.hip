@@ -156,12 +156,12 @@ template <int NW>
 __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixArgs p) {
   constexpr int RC = 16, RO = 8;
   constexpr uint32_t NEAR = 64;  // keys that a wave ranks, a lane each
-  __shared__ uint32_t sums[4][NW], near[NEAR], near_at[NEAR], n_near;
+  __shared__ uint32_t sums[4][NW], n_near[NW];
+  __shared__ unsigned long long near[NW][NEAR];  // key and place
   const int G = c.H_q / c.H_kv, idx = (int)(blockIdx.x >> 3), unit = (idx / G) * 8 + (int)(blockIdx.x & 7);
   if (unit >= p.own.n_rows * c.H_kv) return;
   const int r = unit / c.H_kv, g = unit - r * c.H_kv, h = g * G + idx % G, rh = r * c.H_q + h;
   const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), l = tid & 63;
-  if (tid == 0) n_near = 0;  // (barriers lie between)
   const PrefixRow info = p.rows[r];
   const int k = p.own.k, n_pre = min(k, info.pre);
   const bool listed = p.listed && info.own > k;
@@ -189,10 +189,6 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
           constexpr int X = U0 + decltype(e)::value;
           kc[X] = keys_pre[min(place_of(X), n_pre - 1)];
         });
-    });
-    static_for<RC>([&](auto u) __attribute__((always_inline)) {
-      constexpr int X = decltype(u)::value;
-      kc[X] = place_of(X) < n_pre ? kc[X] : NO_KEY;
     });
   };
   // slot of the own key at place j, of that page, and where its score is
@@ -238,12 +234,17 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
       ko[X] = place_of(round * RO + X) < n_own ? ko[X] : NO_KEY;
     });
   };
+  const bool selects = (long)n_pre + n_own > k;
+  if (selects) fetch_c();  // (on their way while the pages of the row's own keys lead to their scores)
   fetch_o(0);
+  if (selects)
+    static_for<RC>([&](auto u) __attribute__((always_inline)) {
+      constexpr int X = decltype(u)::value;
+      kc[X] = place_of(X) < n_pre ? kc[X] : NO_KEY;
+    });
   const int rounds = (n_own + 64 * NW * RO - 1) / (64 * NW * RO);
   if (!listed && rounds > 1)
     for (int j = tid; (long)j << c.shift < n_own; j += 64 * NW) bad |= (uint32_t)pages[j] >= (uint32_t)c.n_pages;
-  const bool selects = (long)n_pre + n_own > k;
-  if (selects) fetch_c();
   // f(key, place in its list, whether that is the prefix's) for all of this wave's keys; what the registers do not hold is read again
   auto every = [&](auto f) __attribute__((always_inline)) {
     static_for<RC / 8>([&](auto eight) __attribute__((always_inline)) {
@@ -253,13 +254,19 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     });
     static_for<RO / 8>([&](auto eight) __attribute__((always_inline)) {
       constexpr int U0 = 8 * decltype(eight)::value;
-      static_for<8>([&](auto e) __attribute__((always_inline)) { f(ko[U0 + decltype(e)::value], place_of(U0 + decltype(e)::value), false); });
+      if (U0 * NW * 64 < n_own)
+        static_for<8>([&](auto e) __attribute__((always_inline)) { f(ko[U0 + decltype(e)::value], place_of(U0 + decltype(e)::value), false); });
     });
 #pragma unroll 1
-    for (int i = place_of(RC); i < n_pre; i += NW * 64) f(keys_pre[i], i, true);
+    for (int i0 = place_of(RC) - l; i0 < n_pre; i0 += NW * 64) {  // (all lanes stay: f may count over them)
+      const uint32_t key = keys_pre[min(i0 + l, n_pre - 1)];
+      f(i0 + l < n_pre ? key : NO_KEY, i0 + l, true);
+    }
 #pragma unroll 1
-    for (int i = place_of(RO); i < n_own; i += NW * 64) {
-      f(listed ? keys_own[i] : score_key(*score_at(slot_of((uint32_t)pages[i >> c.shift], i))), i, false);
+    for (int i0 = place_of(RO) - l; i0 < n_own; i0 += NW * 64) {
+      const int i = min(i0 + l, n_own - 1);
+      const uint32_t key = listed ? keys_own[i] : score_key(*score_at(slot_of((uint32_t)pages[i >> c.shift], i)));
+      f(i0 + l < n_own ? key : NO_KEY, i0 + l, false);
     }
   };
   int turn = 0;
@@ -339,23 +346,39 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     }
     const uint32_t need = (uint32_t)k - before_lo, left = before_hi - before_lo;  // the need-th of the left ones is the last that is kept
     if (!found && left <= NEAR) {
+      // each wave lists its own of them; a lane then takes one, and counts those before it
+      uint32_t mine = 0;
       every([&](uint32_t key, int place, bool pre) __attribute__((always_inline)) {
-        if (key - lo < hi - lo) {
-          const uint32_t i = atomicAdd(&n_near, 1u);
-          near[i] = key;
-          near_at[i] = (uint32_t)place + (pre ? 0u : (uint32_t)n_pre);
+        const unsigned long long in = __ballot(key - lo < hi - lo);
+        if (in) {
+          if (key - lo < hi - lo) near[w][mine + lanes_before(in)] = (unsigned long long)key << 32 | ((uint32_t)place + (pre ? 0u : (uint32_t)n_pre));
+          mine += (uint32_t)__popcll(in);
         }
       });
+      if (l == 0) n_near[w] = mine;
       __syncthreads();
-      const uint32_t key = l < (int)left ? near[l] : NO_KEY, at = l < (int)left ? near_at[l] : NO_KEY;
-      uint32_t rank = 0;
-      for (int i = 0; i < (int)left; i++) {
-        const uint32_t x = (uint32_t)__builtin_amdgcn_readlane((int)key, i), y = (uint32_t)__builtin_amdgcn_readlane((int)at, i);
-        rank += (x < key) | ((x == key) & (y < at));
+      unsigned long long one = ~0ull;
+      uint32_t at = (uint32_t)l, rank = 0;
+#pragma unroll
+      for (int i = 0; i < NW; i++) {
+        const uint32_t have = n_near[i];
+        if (at < have) one = near[i][at];
+        at = at < have ? 1u << 30 : at - have;  // (taken, or further on)
       }
-      const int last = (int)__builtin_ctzll(__ballot(rank == need - 1u && l < (int)left));
-      cut_key = (uint32_t)__builtin_amdgcn_readlane((int)key, last);
-      const int place = __builtin_amdgcn_readlane((int)at, last);
+#pragma unroll
+      for (int i = 0; i < NW; i++) {
+        const uint32_t have = n_near[i];
+        for (uint32_t j = 0; j < have; j += 4) {
+          unsigned long long other[4];
+#pragma unroll
+          for (int e = 0; e < 4; e++) other[e] = near[i][min(j + e, NEAR - 1u)];
+#pragma unroll
+          for (int e = 0; e < 4; e++) rank += j + e < have && other[e] < one;
+        }
+      }
+      const int last = (int)__builtin_ctzll(__ballot(rank == need - 1u && one != ~0ull));
+      cut_key = (uint32_t)__builtin_amdgcn_readlane((int)(one >> 32), last);
+      const int place = __builtin_amdgcn_readlane((int)(uint32_t)one, last);
       cut_pre = min(place, n_pre - 1);
       cut_own = place - n_pre;
     } else if (!found) {  // keys equal to lo are on both sides: the prefix's are first
@@ -399,7 +422,8 @@ __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixA
     }
     static_for<RO>([&](auto u) __attribute__((always_inline)) {
       constexpr int X = decltype(u)::value;
-      if (kept[X] >> l & 1) list[at + lanes_before(kept[X])] = (int32_t)id[X];
+      const uint32_t to = at + lanes_before(kept[X]);
+      if (kept[X] >> l & 1 && to < (uint32_t)p.own.kcap) list[to] = (int32_t)id[X];  // (there are never more than k)
       at += (uint32_t)__popcll(kept[X]);
     });
     total += all;

@@ -28,51 +28,52 @@ __device__ __forceinline__ int document_start(const int32_t* __restrict__ cu, in
   return cu[lo];
 }
 
-// A lane has 16 channels of a token, eight whole pairs (or channels that stay), in the same place of every head: it forms its eight
-// angles once.  A wave has 64 / (D / 16) tokens.
+// A wave has a token: a lane 16 channels, eight whole pairs (or channels that stay), of every 64 / (D / 16)-th head, so that a load of the wave
+// covers whole heads in a row.  The lanes of one place in the heads share their eight angles: each forms 8 / heads of them (or, with
+// more than eight heads at a time, one that others form too), and takes the rest from the others.
 template <typename T, int D, bool NEXT>
 __global__ __launch_bounds__(256) void rope_kernel(RopeRows p, RopeArgs rope, int heads, int inverse) {
-  constexpr int TASKS = D / 16, TOKENS = 64 / TASKS, U = 4;
-  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), task = l % TASKS;
+  constexpr int TASKS = D / 16, HEADS = 64 / TASKS, OWN = HEADS < 8 ? 8 / HEADS : 1, U = 5;
+  const int l = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), task = l % TASKS, hs = l / TASKS;
   const int h0 = blockIdx.y * heads, h1 = min(p.H, h0 + heads);
   const bool turned = task < rope.rot / 16;
   const int a = NEXT ? 16 * task : turned ? 8 * task : rope.rot + 16 * (task - rope.rot / 16);
   const int b = !NEXT && turned ? a + rope.rot / 2 : a + 8;
-  float f[8];
+  float f[OWN];
 #pragma unroll
-  for (int e = 0; e < 8; e++) f[e] = turned ? rope.freqs[8 * task + e] : 0.f;
-  for (long t0 = ((long)blockIdx.x * 4 + w) * TOKENS; t0 < p.T; t0 += (long)gridDim.x * 4 * TOKENS) {
-    const long t = t0 + l / TASKS, tc = min(t, (long)p.T - 1);
-    int position;
-    if (p.positions) {
-      position = p.positions[tc];
-    } else {
-      position = 0;
-      for (int i = 0; i < TOKENS; i++) {
-        const int ti = (int)min(t0 + i, (long)p.T - 1), start = document_start(p.cu, p.n_docs, ti, l);
-        position = l / TASKS == i ? ti - start : position;
-      }
-    }
-    float c[8], s[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const Turn turn = turn_of(position, f[e]);
-      c[e] = (float)turn.c;
-      s[e] = (float)(inverse ? -turn.s : turn.s);
-    }
-    for (int hb = h0; hb < h1; hb += U) {
-      Raw8<T> x[U], y[U];
+  for (int e = 0; e < OWN; e++) f[e] = turned ? rope.freqs[8 * task + (OWN * hs + e) % 8] : 0.f;
+  for (long t = (long)blockIdx.x * 4 + w; t < p.T; t += (long)gridDim.x * 4) {
+    const int position = p.positions ? p.positions[t] : (int)t - document_start(p.cu, p.n_docs, (int)t, l);
+    Raw8<T> x[U], y[U];
+    auto load = [&](int hb) __attribute__((always_inline)) {
 #pragma unroll
       for (int u = 0; u < U; u++) {
-        const int h = min(hb + u, h1 - 1);
-        const T* src = h < p.H_q ? (const T*)p.q + tc * p.q_stride + (long)h * D : (const T*)p.k + tc * p.k_stride + (long)(h - p.H_q) * D;
+        const int h = min(hb + u * HEADS + hs, h1 - 1);
+        const T* src = h < p.H_q ? (const T*)p.q + t * p.q_stride + (long)h * D : (const T*)p.k + t * p.k_stride + (long)(h - p.H_q) * D;
         load_raw(src + a, x[u]);
         load_raw(src + b, y[u]);
       }
+    };
+    load(h0);  // (on their way under the angles)
+    float c[8], s[8];
+    {
+      Turn turn[OWN];
+#pragma unroll
+      for (int e = 0; e < OWN; e++) turn[e] = turn_of(position, f[e]);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int lane = ((e / OWN) * TASKS + task) * 4;
+        c[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(lane, __float_as_int((float)turn[e % OWN].c)));
+        s[e] = __int_as_float(__builtin_amdgcn_ds_bpermute(lane, __float_as_int((float)turn[e % OWN].s)));
+        s[e] = inverse ? -s[e] : s[e];
+      }
+    }
+    for (int hb = h0; hb < h1; hb += U * HEADS) {
+      if (hb != h0) load(hb);
 #pragma unroll
       for (int u = 0; u < U; u++) {
-        const int h = hb + u;
-        if (h >= h1 || t >= p.T) continue;
+        const int h = hb + u * HEADS + hs;
+        if (h >= h1) continue;
         T* dst = h < p.H_q ? (T*)p.qo + t * p.qo_stride + (long)h * D : (T*)p.ko + t * p.ko_stride + (long)(h - p.H_q) * D;
         if (turned) {
           float v[16], o[16];
@@ -97,10 +98,11 @@ __global__ __launch_bounds__(256) void rope_kernel(RopeRows p, RopeArgs rope, in
 
 template <typename T, int D>
 static void rope_t(const RopeRows& p, const RopeArgs& rope, bool next, bool inverse, hipStream_t st) {
-  constexpr int TOKENS = 64 / (D / 16);
-  const long tiles = ((long)p.T + 4 * TOKENS - 1) / (4 * TOKENS);
-  int heads = (int)((tiles * p.H + 4 * CUS - 1) / (4 * CUS));  // of a workgroup: fewer where there are few tokens
-  heads = heads < 4 ? 4 : heads > p.H ? p.H : heads;
+  constexpr int HEADS = 64 / (D / 16);
+  const long tiles = ((long)p.T + 3) / 4;
+  int heads = (int)((tiles * p.H + 4 * CUS - 1) / (4 * CUS));  // of a workgroup: fewer where there are few tokens, whole rounds of a wave
+  heads = (heads + HEADS - 1) / HEADS * HEADS;
+  heads = heads > p.H ? p.H : heads;
   const dim3 grid((unsigned)(tiles < (1 << 20) ? tiles : 1 << 20), (unsigned)((p.H + heads - 1) / heads));
   if (next) rope_kernel<T, D, true><<<grid, 256, 0, st>>>(p, rope, heads, inverse);
   else rope_kernel<T, D, false><<<grid, 256, 0, st>>>(p, rope, heads, inverse);

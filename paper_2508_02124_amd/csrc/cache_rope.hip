@@ -13,6 +13,7 @@ struct AppendRows {
   const float *W, *A, *z;
   const int32_t *slots, *row_req, *row_len, *prefix_len, *req_prefix;
   int n_rows, n_prefixes;
+  int first;  // row of this launch
 };
 
 // A value of 64 bits in 32: the nearer of its two neighbours with an odd last bit, unless it is a value of 32 bits itself.  What is rounded
@@ -55,19 +56,23 @@ __device__ __forceinline__ double from_lane(double x, int lane) {
   return __hiloint2double((int)from_lane((uint32_t)__double2hiint(x), lane), (int)from_lane((uint32_t)__double2loint(x), lane));
 }
 
-// A row is held by D / 8 lanes of a wave, eight channels each, the same place of every head.  Pairs half a rotation apart lie in two lanes:
-// each forms the angles of four of its eight pairs and gives the other the rest, and the heads' values are exchanged the same way.  A wave goes
-// through `heads` kv-heads, their q-heads and their scores; nothing is shared between waves.
+// A wave has a row: D / 8 lanes a head, eight channels each, 64 / (D / 8) heads at a time, so that a load of the wave covers whole heads in a
+// row.  The angles are the same in every head: each lane forms one (two at 256 channels) and takes the others of its pairs from the lanes that
+// have them.  Pairs half a rotation apart lie in two lanes, which exchange their values.  Nothing is shared between waves.
 template <typename T, int D, bool NEXT>
 __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, AppendRows p, RopeArgs rope, int heads) {
-  constexpr int LPR = D / 8, ROWS = 64 / LPR, GMAX = 4;
-  const int tid = threadIdx.x, l = tid & 63, sub = l % LPR, half = rope.rot / 16;  // lanes of half the turned channels
-  const long t = ((long)blockIdx.x * 4 + (tid >> 6)) * ROWS + l / LPR;
-  const bool there = t < p.n_rows;
-  const int r = (int)(there ? t : p.n_rows - 1), G = c.H_q / c.H_kv;
-  const int g0 = blockIdx.y * heads, g1 = min(c.H_kv, g0 + heads);
+  constexpr int LPR = D / 8, HEADS = 64 / LPR, GMAX = 4, PAIRS = NEXT ? 4 : 8, FORMERS = NEXT ? HEADS : 2 * HEADS;
+  constexpr int OWN = PAIRS > FORMERS ? PAIRS / FORMERS : 1;
+  const int tid = threadIdx.x, l = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), sub = l % LPR, hs = l / LPR;
+  const int half = rope.rot / 16;  // lanes of half the turned channels of a head
+  const int G = c.H_q / c.H_kv, g0 = blockIdx.y * heads, g1 = min(c.H_kv, g0 + heads);
+  const bool turned = sub < 2 * half, first = sub < half;
+  const int unit = first || NEXT ? sub : sub - half, other = !NEXT && turned ? (first ? l + half : l - half) : l;
+  const long t = (long)p.first + (long)blockIdx.x * 4 + w;
+  if (t >= p.n_rows) return;
+  const int r = (int)t;
   // the row's place and position
-  const uint32_t slot = there ? (uint32_t)p.slots[r] : 0xffffffffu;
+  const uint32_t slot = (uint32_t)p.slots[r];
   char* page = slot < c.n_slots ? cache_page(c, slot) : nullptr;
   const uint32_t place = cache_place(c, slot);
   long position = p.row_len[r] - 1;
@@ -78,41 +83,34 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
     if ((uint32_t)prefix < (uint32_t)p.n_prefixes) position = max(position, 0l) + max(0l, min((long)p.prefix_len[prefix], cap));
   }
   position = max(0l, min(position, 0x7fffffffl));
-  const bool turned = sub < 2 * half, first = sub < half;
-  const int other = !NEXT && turned ? (first ? l + half : l - half) : l;
-  // its angles: of the eight pairs that the two lanes have halves of, or of the lane's own four
-  constexpr int PAIRS = NEXT ? 4 : 8;
-  double cs[PAIRS], sn[PAIRS];
-  {
-    const int pair = NEXT ? 4 * sub : 8 * (first ? sub : sub - half) + (first ? 0 : 4);
-    Turn turn[4];
-#pragma unroll
-    for (int e = 0; e < 4; e++) turn[e] = turn_of((int)position, turned ? rope.freqs[pair + e] : 0.f);
-#pragma unroll
-    for (int e = 0; e < 4; e++) {
-      if constexpr (NEXT) {
-        cs[e] = turn[e].c;
-        sn[e] = turn[e].s;
-      } else {
-        const double oc = from_lane(turn[e].c, other), os = from_lane(turn[e].s, other);
-        cs[e] = first ? turn[e].c : oc;
-        sn[e] = first ? turn[e].s : os;
-        cs[e + 4] = first ? oc : turn[e].c;
-        sn[e + 4] = first ? os : turn[e].s;
-      }
-    }
-  }
-  if (!NEXT && !first) {  // (the second of a pair: y2 = x2 cos a + x1 sin a)
-#pragma unroll
-    for (int e = 0; e < PAIRS; e++) sn[e] = -sn[e];
-  }
-  auto load = [&](const void* base, long stride, int h) {
+  auto load = [&](const void* base, long stride, int h) __attribute__((always_inline)) {
     Raw8<T> x;
     load_raw((const T*)base + (long)r * stride + (long)h * D + 8 * sub, x);
     return x;
   };
-  for (int g = g0; g < g1; g++) {
-    const Raw8<T> k = load(p.k, p.k_stride, g), v = load(p.v, p.v_stride, g);
+  Raw8<T> k = load(p.k, p.k_stride, min(g0 + hs, g1 - 1)), v = load(p.v, p.v_stride, min(g0 + hs, g1 - 1));
+  double cs[PAIRS], sn[PAIRS];
+  {
+    const int former = NEXT || first ? hs : HEADS + hs;
+    Turn turn[OWN];
+#pragma unroll
+    for (int e = 0; e < OWN; e++) turn[e] = turn_of((int)position, turned ? rope.freqs[PAIRS * unit + (OWN * former + e) % PAIRS] : 0.f);
+#pragma unroll
+    for (int e = 0; e < PAIRS; e++) {
+      constexpr int PER = OWN;
+      const int from = e / PER, lane = !turned ? l : from < HEADS ? from * LPR + unit : (from - HEADS) * LPR + unit + half;
+      cs[e] = from_lane(turn[e % PER].c, lane);
+      sn[e] = from_lane(turn[e % PER].s, lane);
+      if (!NEXT && !first) sn[e] = -sn[e];  // (the second of a pair: y2 = x2 cos a + x1 sin a)
+    }
+  }
+  for (int gb = g0; gb < g1; gb += HEADS) {
+    const int g = min(gb + hs, g1 - 1);
+    const bool mine = page && gb + hs < g1;
+    if (gb != g0) {
+      k = load(p.k, p.k_stride, g);
+      v = load(p.v, p.v_stride, g);
+    }
     float x[8], y[8];
     double turned_k[8];
     to_f32(k, x);
@@ -132,7 +130,7 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
     uint32_t kb, vb;
     const uint32_t kc = quantise8(turned_k, kb), vc = quantise8(v, vb);
     const uint32_t at = ((uint32_t)g << c.shift) + place;
-    if (page) {
+    if (mine) {
       uint32_t* codes = reinterpret_cast<uint32_t*>(page + (at * D + 4 * sub));
       codes[0] = kc;
       codes[LPR] = vc;
@@ -147,11 +145,11 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
     };
     if (!p.W) {
       for (int h = sub; h < G; h += LPR)
-        if (page) put_score(g * G + h, p.z[(size_t)(g * G + h) * p.n_rows + r]);
+        if (mine) put_score(g * G + h, p.z[(size_t)(g * G + h) * p.n_rows + r]);
     } else {  // the scores of z_kernel, bit for bit: the same sums in the same order
       to_f32(v, x);
       for (int h0 = 0; h0 < G; h0 += GMAX) {
-        float mine = 0.f;
+        float own = 0.f;
 #pragma unroll
         for (int hh = 0; hh < GMAX; hh++) {
           Raw8<float> raw;
@@ -161,48 +159,66 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
 #pragma unroll
           for (int e = 0; e < 8; e++) acc = fmaf(wv[e], x[e], acc);
           acc = group_sum<LPR>(acc);
-          mine = sub == hh ? acc : mine;
+          own = sub == hh ? acc : own;
         }
-        if (sub < min(GMAX, G - h0) && page) {
+        if (sub < min(GMAX, G - h0) && mine) {
           const int h = g * G + h0 + sub;
-          const float sp = fmaxf(mine, 0.f) + log1pf(expf(-fabsf(mine)));
+          const float sp = fmaxf(own, 0.f) + log1pf(expf(-fabsf(own)));
           put_score(h, expf(p.A[h] * sp));
         }
       }
     }
-    if (!p.q) continue;
-    for (int h = g * G; h < (g + 1) * G; h++) {
-      const Raw8<T> q = load(p.q, p.q_stride, h);
+  }
+  if (!p.q) return;
+  float cf[PAIRS], sf[PAIRS];
+#pragma unroll
+  for (int e = 0; e < PAIRS; e++) {
+    cf[e] = (float)cs[e];
+    sf[e] = (float)sn[e];
+  }
+  constexpr int U = sizeof(T) == 4 ? 2 : 4;
+  const int h1 = g1 * G;
+  for (int hb = g0 * G; hb < h1; hb += U * HEADS) {
+    Raw8<T> q[U];
+#pragma unroll
+    for (int u = 0; u < U; u++) q[u] = load(p.q, p.q_stride, min(hb + u * HEADS + hs, h1 - 1));
+#pragma unroll
+    for (int u = 0; u < U; u++) {
+      const int h = hb + u * HEADS + hs;
       T* dst = (T*)p.qo + ((long)r * c.H_q + h) * D + 8 * sub;
-      float o[8];
-      to_f32(q, x);
+      float x[8], y[8], o[8];
+      to_f32(q[u], x);
       if constexpr (NEXT) {
 #pragma unroll
         for (int e = 0; e < 4; e++) {
-          o[2 * e] = fmaf(x[2 * e], (float)cs[e], -(x[2 * e + 1] * (float)sn[e]));
-          o[2 * e + 1] = fmaf(x[2 * e], (float)sn[e], x[2 * e + 1] * (float)cs[e]);
+          o[2 * e] = fmaf(x[2 * e], cf[e], -(x[2 * e + 1] * sf[e]));
+          o[2 * e + 1] = fmaf(x[2 * e], sf[e], x[2 * e + 1] * cf[e]);
         }
       } else {
-        to_f32(from_lane(q, other), y);
+        to_f32(from_lane(q[u], other), y);
 #pragma unroll
-        for (int e = 0; e < 8; e++) o[e] = fmaf(x[e], (float)cs[e], -(y[e] * (float)sn[e]));
+        for (int e = 0; e < 8; e++) o[e] = fmaf(x[e], cf[e], -(y[e] * sf[e]));
       }
-      if (!there) continue;
+      if (h >= h1) continue;
       if (turned) store8<T>(dst, o);
-      else store_raw(dst, q);
+      else store_raw(dst, q[u]);
     }
   }
 }
 
+// (2^22 rows to a launch: it has fewer than 2^32 threads)
 template <typename T, int D>
-static void append_rope_t(const CacheRef& c, const AppendRows& p, const RopeArgs& rope, bool next, hipStream_t st) {
-  constexpr int ROWS = 64 / (D / 8) * 4;
-  const long tiles = ((long)p.n_rows + ROWS - 1) / ROWS;
-  long heads = tiles * c.H_kv / (4 * CUS);  // kv-heads of a workgroup: one where there are few rows
-  heads = heads < 1 ? 1 : heads > c.H_kv ? c.H_kv : heads;
-  const dim3 grid((unsigned)tiles, (unsigned)((c.H_kv + heads - 1) / heads));
-  if (next) cache_append_rope_kernel<T, D, true><<<grid, 256, 0, st>>>(c, p, rope, (int)heads);
-  else cache_append_rope_kernel<T, D, false><<<grid, 256, 0, st>>>(c, p, rope, (int)heads);
+static void append_rope_t(const CacheRef& c, AppendRows p, const RopeArgs& rope, bool next, hipStream_t st) {
+  constexpr int HEADS = 64 / (D / 8), MOST = 1 << 22;
+  for (; p.first < p.n_rows; p.first += MOST) {
+    const int rows = p.n_rows - p.first < MOST ? p.n_rows - p.first : MOST, tiles = (rows + 3) / 4;
+    long heads = (long)tiles * c.H_kv / (4 * CUS);  // kv-heads of a workgroup: one round of a wave where there are few rows
+    heads = (heads + HEADS - 1) / HEADS * HEADS;
+    heads = heads < HEADS ? HEADS : heads > c.H_kv ? c.H_kv : heads;
+    const dim3 grid((unsigned)tiles, (unsigned)((c.H_kv + heads - 1) / heads));
+    if (next) cache_append_rope_kernel<T, D, true><<<grid, 256, 0, st>>>(c, p, rope, (int)heads);
+    else cache_append_rope_kernel<T, D, false><<<grid, 256, 0, st>>>(c, p, rope, (int)heads);
+  }
 }
 
 int launch_cache_append_rope(const dma_cache_shape& s, int n_rows, const void* Q, long q_stride, const void* K, long k_stride,
@@ -210,7 +226,7 @@ int launch_cache_append_rope(const dma_cache_shape& s, int n_rows, const void* Q
                              const int32_t* row_req, const int32_t* row_len, int n_prefixes, const int32_t* prefix_len,
                              const int32_t* req_prefix, const RopeArgs& rope, bool next, void* Qo, void* pages, hipStream_t st) {
   const CacheRef c = cache_ref(s, pages);
-  const AppendRows p = {Q, K, V, Qo, q_stride, k_stride, v_stride, W, A, z, slots, row_req, row_len, prefix_len, req_prefix, n_rows, n_prefixes};
+  const AppendRows p = {Q, K, V, Qo, q_stride, k_stride, v_stride, W, A, z, slots, row_req, row_len, prefix_len, req_prefix, n_rows, n_prefixes, 0};
   auto go = [&](auto t) {
     using T = std::remove_pointer_t<decltype(t)>;
     if (s.d == 256) append_rope_t<T, 256>(c, p, rope, next, st);

@@ -273,3 +273,57 @@ def test_another_stream_and_captured_calls(gpu):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(x[0], ref[0]) and torch.equal(x[1], ref[1])
+
+
+def test_scores_that_are_not_numbers(gpu):
+    """NaN or +infinity among a prefix's scores: rows that keep such a key are NaN, rows that do not are as without it."""
+    s = Shared(gpu, (300, 100), (7, 9, 30), (0, 1, 1), 16, 2, 1, 64)
+    c = s.cache
+    at = torch.from_numpy(request_slots(c, 0).astype(np.int32)).to(gpu)
+    K, V, z = c.read(at)
+    q, req, length = normal(gpu, 5, 3, 2, 64).to(c.type), ints(gpu, [2, 3, 4]), ints(gpu, [7, 9, 30])
+    ref = s.decode(q, 50, req, length)
+    for bad in (float("inf"), float("nan"), -float("nan")):
+        zz = z.clone()
+        zz[1, 200] = bad
+        c.append(K, V, at, z=zz)
+        for k in (50, 400):
+            o, lse = s.decode(q, k, req, length)
+            mine = torch.isnan(o[0, 1]).all() and torch.isnan(lse[1, 0])
+            # (a NaN of one sign ranks as the best score, of the other as the worst: kept by a window of everything)
+            assert mine or (k == 50 and not np.isinf(bad) and torch.isfinite(o[0, 1]).all())
+            assert torch.isfinite(o[0, 0]).all() and torch.isfinite(o[1:]).all() and torch.isfinite(lse[:, 1:]).all()
+            if k == 50:
+                assert torch.equal(o[1:], ref[0][1:])
+
+
+def test_a_prefix_to_each_row(gpu):
+    """More prefixes than rows that have them, some without tokens, some twice."""
+    pre = [int(x) for x in np.random.default_rng(4).integers(0, 90, 40)]
+    lens, of = [1 + i % 7 for i in range(20)], [(i * 11) % 43 for i in range(20)]
+    s = Shared(gpu, pre, lens, [x if x < 40 else -1 for x in of], 16, 2, 2, 64)
+    s.prefix_req[5] = s.prefix_req[11]
+    s.prefix_len[5] = s.prefix_len[11]
+    rows = [s.row(i, n) for i, n in enumerate(lens)]
+    q = normal(gpu, 5, 20, 2, 64).to(s.cache.type)
+    for k in (20, 1000):
+        s.check(q, k, rows, s.decode(q, k, ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])))
+
+
+def test_offsets_beyond_four_gigabytes(gpu):
+    n_pages = 8000
+    s = Shared(gpu, (1,), (1,), (0,), 256, 8, 8, 256)
+    c = s.cache
+    c.shape = B.make_cache_shape(2, n_pages, 4, 256, 8, 8, 256)
+    assert B.dma_cache_bytes(c.shape) > 1 << 32
+    c.pages, c.cap = torch.empty(B.dma_cache_bytes(c.shape), dtype=torch.uint8, device=gpu), 1024
+    c.table = ints(gpu, [[7999, 0, 7990, -1], [7998, 1, -1, -1]])
+    c.model = co.Pages(2, n_pages, 4, 256)
+    c.model.tables, c.model.lens = [[7999, 0, 7990], [7998, 1]], [700, 300]
+    for b, n in ((0, 700), (1, 300)):
+        K, V = normal(gpu, 1 + b, n, 8, 256).to(c.type), normal(gpu, 3 + b, n, 8, 256).to(c.type)
+        c.append(K, V, torch.from_numpy(request_slots(c, b).astype(np.int32)).to(gpu), z=torch.rand((8, n), device=gpu))
+    s.prefix_len[0] = 700
+    q = normal(gpu, 4, 2, 8, 256).to(c.type)
+    for k in (300, 1000):
+        s.check(q, k, [(1, 300), (1, 41)], s.decode(q, k, ints(gpu, [1, 1]), ints(gpu, [300, 41])))

@@ -133,3 +133,18 @@ def test_graph_replays(gpu):
         torch.cuda.synchronize()
         assert torch.equal(outs[0], outs[1])
         assert all(torch.equal(a, b) for a, b in zip(cache.read(slots), eager.read(slots)))
+
+
+def test_more_rows_than_a_launch_takes(gpu):
+    n, d, ps = (1 << 22) + 21, 64, 256
+    cache = GpuCache(gpu, 1, n // ps + 2, n // ps + 2, ps, 1, 1, d)
+    K = normal(gpu, 1, 512, 1, d, dtype=torch.bfloat16).repeat(n // 512 + 1, 1, 1)[:n]
+    freqs, slots = frequencies(gpu, d, 500000.0), torch.arange(n, device=gpu).int()
+    length, z = slots + 1, torch.rand((1, n), device=gpu)
+    q = torch.full((n + 3, 1, d), 5.0, dtype=torch.bfloat16, device=gpu)
+    B.dma_cache_append_rope(cache.shape, n, K, d, K, d, K, d, None, None, z, slots, None, length, 0, None, None, freqs, d, True, q, cache.pages)
+    at = torch.cat((torch.arange(0, 1 << 22, 99991), torch.arange((1 << 22) - 9, n))).to(gpu)
+    k, v, zz = cache.read(slots[at])
+    ref, size = ro.rotate(f64(K[at]), at.cpu().numpy(), freqs.cpu().numpy(), True)
+    assert (f64(k) == co.quantise(ref)).all() and (f64(v) == co.quantise(f64(K[at]))).all() and torch.equal(zz, z[:, at])
+    assert (np.abs(f64(q[at]) - ref) <= bound(ref, size, "bf16")).all() and (q[n:] == 5).all()

@@ -135,3 +135,16 @@ def test_other_stream_and_graph(gpu):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, ref)
+
+
+def test_more_tokens_than_a_launch_takes(gpu):
+    """2^22 + 37 tokens: the last ones are turned, to their own positions, and nothing behind them is written."""
+    T, d = (1 << 22) + 37, 64
+    x = normal(gpu, 1, 1024, 1, d, dtype=torch.bfloat16).repeat(T // 1024 + 1, 1, 1)[:T]
+    y = torch.full((T + 5, 1, d), 3.0, dtype=torch.bfloat16, device=gpu)
+    freqs, cu = frequencies(gpu, d, 500000.0), torch.tensor([0, 1 << 22, T], dtype=torch.int32, device=gpu)
+    B.dma_rope(B.make_shape(T, 2, 1, 1, d, 1), x, d, None, 0, cu, None, freqs, d, False, False, y, d, None, 0)
+    at = torch.cat((torch.arange(0, 1 << 22, 99991), torch.arange((1 << 22) - 9, T))).to(gpu)
+    positions = torch.where(at < 1 << 22, at, at - (1 << 22)).cpu().numpy()
+    check(y[at], x[at], positions, freqs, "bf16", False, False)
+    assert (y[T:] == 3).all()

@@ -75,7 +75,7 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
   const uint32_t slot = (uint32_t)p.slots[r];
   char* page = slot < c.n_slots ? cache_page(c, slot) : nullptr;
   const uint32_t place = cache_place(c, slot);
-  long position = p.row_len[r] - 1;
+  long position = (long)p.row_len[r] - 1;
   if (p.n_prefixes) {
     const int req = p.row_req ? p.row_req[r] : r;
     const int prefix = (uint32_t)req < (uint32_t)c.n_reqs ? p.req_prefix[req] : -1;

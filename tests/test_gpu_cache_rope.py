@@ -148,3 +148,20 @@ def test_more_rows_than_a_launch_takes(gpu):
     ref, size = ro.rotate(f64(K[at]), at.cpu().numpy(), freqs.cpu().numpy(), True)
     assert (f64(k) == co.quantise(ref)).all() and (f64(v) == co.quantise(f64(K[at]))).all() and torch.equal(zz, z[:, at])
     assert (np.abs(f64(q[at]) - ref) <= bound(ref, size, "bf16")).all() and (q[n:] == 5).all()
+
+
+def test_lengths_at_the_ends_of_their_type(gpu):
+    """Below 1: position 0, behind a prefix the prefix's length; the largest: at most 2^31 - 1, also behind a prefix."""
+    n, d, low, high = 6, 64, -2 ** 31, 2 ** 31 - 1
+    cache = GpuCache(gpu, n, 4, 4, 16, 2, 1, d, "f32")
+    freqs, slots = frequencies(gpu, d), torch.arange(n, device=gpu).int()
+    q, K = normal(gpu, 1, n, 2, d), normal(gpu, 2, n, 1, d)
+    W, A = normal(gpu, 3, 2, d), normal(gpu, 4, 2)
+    length, of = ints(gpu, [low, low, high, high, 0, -5]), ints(gpu, [-1, 0, -1, 0, 1, 1])
+    out = torch.empty_like(q)
+    B.dma_cache_append_rope(cache.shape, n, q, 2 * d, K, d, K, d, W, A, None, slots, None, length, 2, ints(gpu, [37, low]), of, freqs, d, False, out,
+                            cache.pages)
+    at = [0, 37, high - 1, min(high - 1 + 37, high), 0, 0]
+    ref, size = ro.rotate(f64(q), at, freqs.cpu().numpy(), False)
+    assert (np.abs(f64(out) - ref) <= bound(ref, size, "f32")).all()
+    assert (f64(cache.read(slots)[0]) == co.quantise(ro.rotate(f64(K), at, freqs.cpu().numpy(), False)[0])).all()

@@ -126,7 +126,10 @@ class PagedCache:
         a sequence or int32 tensor [n_reqs]).  length: their tokens; left out: all that those requests have now."""
         ints = lambda x: x if isinstance(x, torch.Tensor) else torch.tensor([int(i) for i in x], dtype=torch.int32, device=self.device)
         req, of = ints(req), ints(of)
-        length = self.seq_lens[req.long()] if length is None else ints(length)
+        if length is None:   # (a request that is not there holds nothing)
+            length = self.seq_lens[req.long().clamp(0, self.shape.n_reqs - 1)].where((req >= 0) & (req < self.shape.n_reqs), 0).int()
+        else:
+            length = ints(length)
         shared = CachePrefixes(req, length, of)
         self._check_prefixes(shared)
         return shared

@@ -125,8 +125,8 @@ def dynamic_mask_attention(Q, K, V, W, A, cu_seqlens, k, max_seqlen=0, softmax_s
 
 def rotary_freqs(dim, base=10000.0, device=None):
     """base^(-2 i / dim) for the dim / 2 pairs of dim rotated channels (float32)."""
-    i = torch.arange(dim // 2, dtype=torch.float64, device=device)
-    return (float(base) ** (-2.0 * i / dim)).float()
+    i = torch.arange(dim // 2, dtype=torch.float64, device="cpu")    # (the same numbers for every device)
+    return (float(base) ** (-2.0 * i / dim)).float().to(device)
 
 
 class RotaryFunction(torch.autograd.Function):
@@ -144,6 +144,8 @@ class RotaryFunction(torch.autograd.Function):
             raise ValueError("expected Q [T, H_q, d] and K [T, H_kv, d]")
         if (cu_seqlens is None) == (positions is None):
             raise ValueError("positions are those in the documents of cu_seqlens, or given: one of the two")
+        if ctx.needs_input_grad[2]:
+            raise ValueError("freqs get no gradient")
         if positions is not None and positions.shape != (T,):
             raise ValueError(f"expected positions [{T}], got {list(positions.shape)}")
         if K.dtype != Q.dtype or freqs.dtype != torch.float32 or freqs.dim() != 1 or (cu_seqlens if positions is None else positions).dtype != torch.int32:
@@ -197,9 +199,16 @@ class DynamicMaskAttention(torch.nn.Module):
         if rotary_dim % 16 or not 0 <= rotary_dim <= head_dim:
             raise ValueError("rotary_dim must be a multiple of 16 of at most head_dim")
         self.rotary_interleaved = bool(rotary_interleaved)
+        self.rotary_dim, self.rotary_base = rotary_dim, rotary_base
         freqs = rotary_freqs(rotary_dim, rotary_base, device) if rotary_dim else None
         self.register_buffer("rotary_freqs", freqs, persistent=False)
         self.A = torch.nn.Parameter(torch.full((num_heads,), -1.0, dtype=torch.float32, device=device))
+
+    def _apply(self, fn, *args, **kwargs):
+        super()._apply(fn, *args, **kwargs)
+        if self.rotary_freqs is not None:   # (formed anew where the module now is: a change of type does not round them)
+            self.rotary_freqs = rotary_freqs(self.rotary_dim, self.rotary_base, self.rotary_freqs.device)
+        return self
 
     def forward(self, q, k, v, cu_seqlens=None, max_seqlen=0, positions=None):
         if q.dim() == 4:

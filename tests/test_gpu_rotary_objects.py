@@ -252,3 +252,48 @@ def test_captured_step_replays(gpu):
 
     for a, b in zip(run(True), run(False)):
         assert torch.equal(a, b)
+
+
+def test_prefixes_held_by_requests_that_are_not_there(gpu):
+    cache = PagedCache(3, 8, 2, 1, 64, page_size=16, device=gpu)
+    cache.assign([0, 9, 20], 29)
+    shared = cache.prefixes([2, 3, -1, 1, 2 ** 31 - 1], [0, 1, 2])
+    assert shared.len.tolist() == [20, 0, 0, 9, 0] and shared.len.dtype == torch.int32
+    assert cache.prefixes([], [-1] * 3).len.shape == (0,)
+    with pytest.raises(ValueError):
+        cache.prefixes([2], [0, 0])
+    with pytest.raises(ValueError):
+        cache.prefixes([2, 1], [0, 0, 0], [4])
+
+
+def test_frequencies_get_no_gradient(gpu):
+    q, f = torch.zeros(4, 2, 64, device=gpu), rotary_freqs(64, device=gpu).requires_grad_()
+    with pytest.raises(ValueError):
+        rotary(q, q, f, positions=torch.arange(4, device=gpu).int())
+
+
+def test_a_captured_backward(gpu):
+    """Forward and backward in one graph; every replay against the eager result."""
+    freqs, pos = rotary_freqs(64, 100.0, gpu), torch.arange(30, device=gpu).int()
+    x = normal(gpu, 1, 30, 3, 64).requires_grad_()
+    w = normal(gpu, 2, 30, 2, 64)
+    def run():
+        y, _ = rotary(x[:, :2], x[:, 2:], freqs, positions=pos)
+        (g,) = torch.autograd.grad(y, x, w)
+        return y.detach(), g
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, g = run()
+    for seed in (3, 4, 5):
+        with torch.no_grad():
+            x.copy_(normal(gpu, seed, 30, 3, 64))
+        pos.add_(11)
+        graph.replay()
+        torch.cuda.synchronize()
+        ye, ge = run()
+        assert torch.equal(y, ye) and torch.equal(g, ge)

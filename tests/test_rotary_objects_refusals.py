@@ -92,3 +92,14 @@ def test_rotary_arguments():
     assert set(m.state_dict()) == {"W", "A"} == set(DynamicMaskAttention(2, 1, 64, 8).state_dict())
     with pytest.raises(ValueError):
         DynamicMaskAttention(2, 1, 64, 8)(q, k, k, cu_seqlens=ints(2), positions=ints(4))
+
+
+def test_a_module_s_frequencies_are_not_rounded():
+    m = DynamicMaskAttention(H_Q, H_KV, D, 8, rotary_dim=32, rotary_base=5e5)
+    want = m.rotary_freqs.clone()
+    assert want.dtype == torch.float32 and torch.equal(want, (5e5 ** (-torch.arange(0, 32, 2).double() / 32)).float())
+    for there in (lambda: m.bfloat16(), lambda: m.float(), lambda: m.double()):
+        assert torch.equal(there().rotary_freqs, want) and m.rotary_freqs.dtype == torch.float32
+    empty = DynamicMaskAttention(H_Q, H_KV, D, 8, rotary_dim=32, rotary_base=5e5, device="meta")
+    assert empty.rotary_freqs.device.type == "meta" and torch.equal(empty.to_empty(device="cpu").rotary_freqs, want)
+    assert "rotary_freqs" not in m.state_dict()

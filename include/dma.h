@@ -221,7 +221,8 @@ int dma_bwd_scores(const dma_shape* shape, const void* Q, const void* K, const v
  *   Q, K       in   T rows of [H_q, d] and [H_kv, d], q_stride and k_stride elements apart (multiples of 8 of at least the row: both may be
  *                   parts of one projection's output); either may be NULL and is then left out
  *   positions  in   nullable: [T] int32, of any sign; NULL: a token's position is its place in its document (cu_seqlens, else not read)
- *   freqs      in   [rot / 2] float, e.g. base^(-2 i / rot)
+ *   freqs      in   [rot / 2] float, e.g. base^(-2 i / rot); |position * freqs[i]| is below 2^50 (a pair beyond that, or with a frequency
+ *                   that is no number, gets values without meaning, and no other pair does)
  *   rot        a multiple of 16, at most d
  *   inverse    != 0: turned by -a.  That is the transpose, so the gradients of Q and K are those of Qo and Ko turned with inverse = 1
  *   Qo, Ko     out  rows qo_stride and ko_stride elements apart (what lies between rows is left as it is); Qo may be Q, and Ko K, with the
@@ -413,7 +414,7 @@ int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K
  *   row_req     in  nullable (row r is then request r, n_rows <= n_reqs); row_len in, as dma_cache_assign gives them
  *   n_prefixes, prefix_len [n_prefixes], req_prefix [n_reqs]   as for dma_cache_decode_prefix; with n_prefixes == 0 neither is read, nor row_req
  *   Q           in  nullable: n_rows rows of [H_q, d], q_stride elements apart, every row turned, also one without a slot
- *   Qo          out [n_rows, H_q, d]; may be Q if that is packed
+ *   Qo          out [n_rows, H_q, d]; may be Q if that is packed, else it overlaps no input
  *   freqs, rot, interleaved   as for dma_rope
  * The codes are those of the turned value as 64 bits give it: nothing is rounded before them (rows that dma_rope wrote have been, to their
  * type).  V and the scores, which come from V, are dma_cache_append's bit for bit, and so is everything else.
@@ -468,7 +469,9 @@ int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, fl
  *   q, q_stride, pages, block_table, row_req, row_len, softmax_scale, o, lse   as for dma_cache_decode; a row that has no request or no
  *                keys of its own, or a page out of range among its own or its prefix's, sees nothing
  *   ws           dma_cache_decode_prefix_bytes(shape, n_rows, k, n_prefixes, max_prefix) bytes of scratch; calls that overlap need one
- *                each.  It holds the lists of kept keys, 8 bytes for each of (n_rows + n_prefixes) * H_q * min(k, max_pages * page_size)
+ *                each.  Of every row and head it holds the list of its own kept keys, 4 bytes for each of min(k, max_pages * page_size), 8
+ *                where max_len allows rows of more than max(k, 2048) keys; of every prefix and head 8 for each; and the parts of the
+ *                prefixes' attention, (d + 4) * 4 bytes for each row and head, of at least 8192
  * A prefix is selected from, gathered and decoded once for all of its rows.  The limit on rows is dma_cache_decode's, with n_rows + n_prefixes
  * in the place of n_rows.
  */

@@ -152,9 +152,10 @@ __global__ __launch_bounds__(512, 4) void prefix_slice_kernel(CacheRef c, Select
 // one ballot a register needed three scalar instructions, which four SIMDs share (64 rows of 32 heads, 2048 + 400 keys: 83 us instead of 26).
 // A row with more than k keys of its own has a list of the best of them, unless the caller's bound says that there are none; else they are
 // read where they are.
+constexpr int CUT_LIST = 1024, CUT_OWN = 512;  // keys that a wave holds, of the list and of the row's own
 template <int NW>
 __global__ __launch_bounds__(64 * NW) void prefix_cut_kernel(CacheRef c, PrefixArgs p) {
-  constexpr int RC = 16, RO = 8;
+  constexpr int RC = CUT_LIST / 64, RO = CUT_OWN / 64;
   constexpr uint32_t NEAR = 64;  // keys that a wave ranks, a lane each
   __shared__ uint32_t sums[4][NW], n_near[NW];
   __shared__ unsigned long long near[NW][NEAR];  // key and place
@@ -534,18 +535,26 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
   if (any) fetch(cur);
   const Cut cut = n < tile.count ? p.cuts[(size_t)row * c.H_q + h] : Cut{0u, -1, 0, 0};
   // channel 8 s + e of this half of the row: the lane's part of product s
-  Terms<NTQ> qf[KS];
-  {
-    const TQ* src = q + (size_t)row * q_stride + (size_t)h * D + hh * (D / 2);
-#pragma unroll
-    for (int s = 0; s < KS; s++) {
-      if constexpr (F32) {
-#pragma unroll
-        for (int e = 0; e < 8; e += 2) qf[s].split(e, (float)src[8 * s + e], (float)src[8 * s + e + 1]);
-      } else {
-        qf[s].t[0] = *reinterpret_cast<const bf16x8*>(src + 8 * s);
-      }
+  // (fp32 queries are split where they are used: kept, their three terms took 192 registers at 256 channels, and 87 spilled -- 17 rows of 16
+  // heads, window 1024: the call 46.8 -> 37.9; 64 rows 76.0 -> 66.3, of 128 channels 64.5 -> 63.9, of 64 47.0 -> 46.3)
+  const TQ* src = q + (size_t)row * q_stride + (size_t)h * D + hh * (D / 2);
+  auto query = [&](int s) __attribute__((always_inline)) {
+    Terms<NTQ> x;
+    if constexpr (F32) {
+      const float4 a = reinterpret_cast<const float4*>(src + 8 * s)[0], b = reinterpret_cast<const float4*>(src + 8 * s)[1];
+      x.split(0, a.x, a.y);
+      x.split(2, a.z, a.w);
+      x.split(4, b.x, b.y);
+      x.split(6, b.z, b.w);
+    } else {
+      x.t[0] = *reinterpret_cast<const bf16x8*>(src + 8 * s);
     }
+    return x;
+  };
+  Terms<NTQ> qf[F32 ? 1 : KS];
+  if constexpr (!F32) {
+#pragma unroll
+    for (int s = 0; s < KS; s++) qf[s] = query(s);
   }
   FragOffsets<D> fo;
   fo.init(l);
@@ -603,8 +612,9 @@ __global__ __launch_bounds__(64 * NW) void prefix_tile_kernel(CacheRef c, Prefix
         a.y = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 1));
         a.z = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 2));
         a.w = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(code[i], sc, 3));
+        const Terms<NTQ> qn = F32 ? query(4 * b + i) : qf[F32 ? 0 : 4 * b + i];
 #pragma unroll
-        for (int x = NTQ - 1; x >= 0; x--) s = mfma32(__builtin_bit_cast(bf16x8, a), qf[4 * b + i].t[x], s);
+        for (int x = NTQ - 1; x >= 0; x--) s = mfma32(__builtin_bit_cast(bf16x8, a), qn.t[x], s);
       }
     }
     // this lane's keys: 8 (v / 4) + 4 hh + v % 4; the row keeps those before its cut, and where it falls among equal ones in this tile, those
@@ -894,6 +904,7 @@ struct PrefixWork {
   SelectWork pre, own;
   bool listed;
   int max_tiles, nsplit;
+  long own_bound;  // on a row's own keys
 };
 // A row of at most so many keys of its own needs no list of the best of them for its cut (40 requests x 5 rows of 500 keys, window 512, 16
 // heads: the lists' launch 13 -> 21 us with them).
@@ -905,7 +916,8 @@ static PrefixWork prefix_work(const dma_cache_shape& s, int n_rows, int k, int n
   const size_t pairs = (size_t)n_rows * s.H_q, pre_pairs = (size_t)n_prefixes * s.H_q;
   PrefixWork wk = {};
   auto take = [&](size_t bytes) { size_t at = wk.total; wk.total = align_up(at + bytes, 256); return at; };
-  wk.listed = (s.max_len > 0 && s.max_len < cap ? s.max_len : cap) > (k > OWN_DIRECT ? k : OWN_DIRECT);
+  wk.own_bound = s.max_len > 0 && s.max_len < cap ? s.max_len : cap;
+  wk.listed = wk.own_bound > (k > OWN_DIRECT ? k : OWN_DIRECT);
   const long groups = n_prefixes < n_rows ? n_prefixes : n_rows;
   wk.max_tiles = n_prefixes ? (int)((n_rows + (TILE_ROWS - 1) * groups) / TILE_ROWS) : 0;
   // parts of the lists: so many that every compute unit has one, as long as a wave has a step to take
@@ -987,8 +999,13 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
   if (hipGetLastError() != hipSuccess) return DMA_EHIP;
   const int G = s.H_q / s.H_kv;
   const unsigned grid = (unsigned)(((long)n_rows * s.H_kv + 7) / 8 * 8 * G);
-  const bool many = pairs >= 4 * CUS;  // (row, head) pairs: two waves to each, else four
+  // Waves of a (row, head) pair: two where there are many pairs, more where there are few.  Whole calls, us, two / four: 2048 pairs (64 rows,
+  // window 2048 of 16384 + 400 keys) 55.9 / 64.0, 3200 60.2 / 69.7, 272 (window 1024 of 4096 + 123) 46.5 / 46.6, 256 (window 4096, 1000 +
+  // 2000) 57.6 / 39.2, 32 (window 4096, 9000 + 9000) 99.8 / 59.2.  Eight for the attention of few pairs: 256 39.9 -> 37.0, 32 59.3 -> 57.5, the
+  // shortest the same; for the cut only where four do not hold a row's keys: 57.5 -> 48.9, but 43.2 -> 44.6 where they do.
+  const bool many = pairs >= 4 * CUS, few = pairs <= CUS;
   if (many) prefix_cut_kernel<2><<<grid, 128, 0, st>>>(c, p);
+  else if (few && (kcap > CUT_LIST * 4 || wk.own_bound > CUT_OWN * 4)) prefix_cut_kernel<8><<<grid, 512, 0, st>>>(c, p);
   else prefix_cut_kernel<4><<<grid, 256, 0, st>>>(c, p);
   auto go = [&](auto t, auto width) {
     using T = std::remove_pointer_t<decltype(t)>;
@@ -998,6 +1015,7 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
       prefix_tile_kernel<T, D, NW><<<tiles, 64 * NW, 0, st>>>(c, p, (const T*)q, q_stride, scale);
     }
     if (many) prefix_own_kernel<T, D, 2><<<grid, 128, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
+    else if (few) prefix_own_kernel<T, D, 8><<<grid, 512, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
     else prefix_own_kernel<T, D, 4><<<grid, 256, 0, st>>>(c, p, (const T*)q, q_stride, (T*)o, lse, scale);
   };
   auto types = [&](auto width) {

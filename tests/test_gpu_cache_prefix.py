@@ -327,3 +327,23 @@ def test_offsets_beyond_four_gigabytes(gpu):
     q = normal(gpu, 4, 2, 8, 256).to(c.type)
     for k in (300, 1000):
         s.check(q, k, [(1, 300), (1, 41)], s.decode(q, k, ints(gpu, [1, 1]), ints(gpu, [300, 41])))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kind", ["ordinary", "levels", "equal", "masked"])
+@pytest.mark.parametrize("n_rows,H_q,d", [(150, 8, 64), (40, 8, 128), (9, 4, 256)])
+def test_many_and_few_long_rows(gpu, n_rows, H_q, d, kind, dtype):
+    """Rows of every number of waves: more keys of the prefix and of their own than the registers hold, with and without lists of the own."""
+    print(f"[case] prefix long rows {n_rows} {H_q} {d} {kind} {dtype}", flush=True)
+    s = Shared(gpu, (5000, 700), (1300, 2600, 40), (0, 0, 1), 64, H_q, 2, d, dtype, z=kind, seed=12)
+    rng = np.random.default_rng(n_rows)
+    rows = [s.row(i % 3, int(rng.integers(1, s.lens[i % 3] + 1)) if i > 5 else s.lens[i % 3]) for i in range(n_rows)]
+    q = normal(gpu, 5, n_rows, H_q, d).to(s.cache.type)
+    req, length = ints(gpu, [b for b, _ in rows]), ints(gpu, [n for _, n in rows])
+    few = rng.permutation(n_rows)[:8]                             # (what the oracle checks in full)
+    few = np.unique(np.concatenate((few, [0, 1, 2])))
+    for k in (2200, 4700, 9000) if kind == "ordinary" else (2400,):
+        o, lse = s.decode(q, k, req, length)
+        at = torch.from_numpy(few).to(gpu)
+        s.check(q[at], k, [rows[i] for i in few], (o[at], lse[:, at]))
+        assert torch.isfinite(o).all()

@@ -48,8 +48,10 @@ typedef enum {
                             unknown dtype, more than 256 q-heads per kv-head,
                             more than 32 heads for the cross-head scores,
                             bf16 dma_fwd / dma_bwd with T >= 2^24 or Q (or K, V) larger than 4 GiB;
+                            rotary channels that are not a multiple of 16;
                             of the paged cache: page sizes and numbers other than stated there             */
-  DMA_EWORKSPACE = -3,   /* ws_bytes smaller than dma_workspace_bytes() / dma_cache_decode_bytes() */
+  DMA_EWORKSPACE = -3,   /* ws_bytes smaller than dma_workspace_bytes() / dma_cache_decode_bytes() /
+                            dma_cache_decode_prefix_bytes() */
   DMA_EHIP = -4          /* a launch failed (hipGetLastError) */
 } dma_status;
 
@@ -220,7 +222,8 @@ int dma_bwd_scores(const dma_shape* shape, const void* Q, const void* K, const v
  * the pairs being the channels (i, i + rot / 2), or the neighbours (2 i, 2 i + 1) if interleaved != 0; channels from rot on stay.
  *   Q, K       in   T rows of [H_q, d] and [H_kv, d], q_stride and k_stride elements apart (multiples of 8 of at least the row: both may be
  *                   parts of one projection's output); either may be NULL and is then left out
- *   positions  in   nullable: [T] int32, of any sign; NULL: a token's position is its place in its document (cu_seqlens, else not read)
+ *   positions  in   nullable: [T] int32, of any sign; NULL: a token's position is its place in its document (cu_seqlens, else not read;
+ *                   tokens behind the last document count on in it)
  *   freqs      in   [rot / 2] float, e.g. base^(-2 i / rot); |position * freqs[i]| is below 2^50 (a pair beyond that, or with a frequency
  *                   that is no number, gets values without meaning, and no other pair does)
  *   rot        a multiple of 16, at most d

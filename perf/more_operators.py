@@ -385,8 +385,8 @@ def _setup(state):
     if case["kind"] == "rope":
         shape = B.make_shape(case["tokens"], case["docs"], H_q, H_kv, d, 1, dtype=dtype)
     elif case["kind"] == "append":
-        # (a request may get 2^17 tokens: those before the new ones, and the prefix, are in other pages)
-        shape = B.make_cache_shape(case["reqs"], state["pages"].shape[0], (1 << 17) // case["ps"], case["ps"], H_q, H_kv, d, dtype=dtype)
+        n_pages = state["pages"].shape[0]
+        shape = B.make_cache_shape(case["reqs"], n_pages, n_pages, case["ps"], H_q, H_kv, d, dtype=dtype)
     else:
         n_pages, max_pages, longest, longest_prefix = state["sizes"]
         shape = B.make_cache_shape(case["reqs"] + case["prefixes"], n_pages, max_pages, case["ps"], H_q, H_kv, d, dtype=dtype,

@@ -814,7 +814,7 @@ __global__ __launch_bounds__(64 * NW) void prefix_own_kernel(CacheRef c, PrefixA
     x.there = 0;
 #pragma unroll
     for (int u = 0; u < U; u++) {
-      const bool there = i0 + u * NG + grp < count;
+      const bool there = i0 + u * NG + grp < count && id[u] < c.n_slots;
       const uint32_t slot = there ? id[u] : 0u, place = cache_place(c, slot);
       const char* page = c.pages + (unsigned long long)(slot >> c.shift) * page_bytes;
       const uint4* codes = reinterpret_cast<const uint4*>(page + (k_off + place * D));
@@ -959,42 +959,36 @@ int launch_cache_decode_prefix(const dma_cache_shape& s, int n_rows, int k, floa
                         (int32_t*)(base + wk.off_list_pre), (int32_t*)(base + wk.off_list_own), (uint32_t*)(base + wk.off_keys_pre),
                         (uint32_t*)(base + wk.off_keys_own), (Cut*)(base + wk.off_cuts), (float*)(base + wk.off_part), wk.max_tiles, wk.nsplit, wk.listed};
   const int pairs = n_rows * s.H_q;
-  // the lists: prefixes first, rows behind them; more pairs than a launch has room for take several
-  auto set_of = [&](const CacheRows& rows, const SelectWork& w, int32_t* list, uint32_t* keys, bool used) {
-    SelectSet x = {rows, {(uint2*)(base + w.off_counts), (uint2*)(base + w.off_listed), (uint4*)(base + w.off_bounds), w.room, w.parts, 0, w.pairs},
-                   list, keys, 0};
-    if (!used) x.sw.pairs = x.sw.parts = 0;
-    return x;
+  // the lists: prefixes first, rows behind them.  A set without slices has no share of what slices tell each other: all of its pairs
+  // are in the first launch.  One with slices goes through that room in as many launches as it takes.
+  auto set_of = [&](const CacheRows& rows, const SelectWork& w, int32_t* list, uint32_t* keys) {
+    return SelectSet{rows, {(uint2*)(base + w.off_counts), (uint2*)(base + w.off_listed), (uint4*)(base + w.off_bounds), w.room, w.parts, 0, 0},
+                     list, keys, 0};
   };
-  SelectSet a = set_of(p.pre, wk.pre, p.list_pre, p.keys_pre, n_prefixes > 0), b = set_of(p.own, wk.own, p.list_own, p.keys_own, wk.listed);
+  SelectSet a = set_of(p.pre, wk.pre, p.list_pre, p.keys_pre), b = set_of(p.own, wk.own, p.list_own, p.keys_own);
+  const int pre_pairs = n_prefixes * s.H_q, own_pairs = wk.listed ? pairs : 0;
   const bool sliced = wk.pre.parts > 0 || wk.own.parts > 0;
   auto select = [&](auto width) {
     constexpr int S = decltype(width)::value;
-    bool group = true;
-    const int pre_pairs = n_prefixes * s.H_q;
-    auto left = [](SelectSet& x, int all, int per) {  // pairs of this launch
-      x.sw.pairs = all - x.sw.first < per ? all - x.sw.first : per;
+    auto share = [](SelectSet& x, int all, int per) {  // pairs of this launch
+      const int left = all - x.sw.first;
+      x.sw.pairs = x.sw.parts && left > per ? per : left;
       x.wgs = x.sw.pairs * (x.sw.parts ? x.sw.parts : 1);
     };
-    for (;;) {
-      if (n_prefixes) left(a, pre_pairs, wk.pre.pairs);
-      if (wk.listed) left(b, pairs, wk.own.pairs);
+    for (bool group = true;; group = false) {
+      share(a, pre_pairs, wk.pre.pairs);
+      share(b, own_pairs, wk.own.pairs);
       const unsigned wgs = (unsigned)(a.wgs + b.wgs);
-      if (group) {
-        if (sliced) prefix_select_kernel<S, true, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
-        else prefix_select_kernel<S, false, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
-      } else if (wgs) {
-        if (sliced) prefix_select_kernel<S, true, false><<<wgs, 512, 0, st>>>(c, p, a, b);
-        else prefix_select_kernel<S, false, false><<<wgs, 512, 0, st>>>(c, p, a, b);
-      }
+      if (!sliced) prefix_select_kernel<S, false, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
+      else if (group) prefix_select_kernel<S, true, true><<<wgs + 1, 512, 0, st>>>(c, p, a, b);
+      else prefix_select_kernel<S, true, false><<<wgs, 512, 0, st>>>(c, p, a, b);
       SelectSet a2 = a, b2 = b;
       if (!a.sw.parts) a2.wgs = 0;
       if (!b.sw.parts) b2.wgs = 0;
       if (a2.wgs + b2.wgs) prefix_slice_kernel<S><<<(unsigned)(a2.wgs + b2.wgs), 512, 0, st>>>(c, a2, b2);
-      group = false;
       a.sw.first += a.sw.pairs;
       b.sw.first += b.sw.pairs;
-      if (a.sw.first >= (n_prefixes ? pre_pairs : 0) && b.sw.first >= (wk.listed ? pairs : 0)) break;
+      if (a.sw.first >= pre_pairs && b.sw.first >= own_pairs) break;
     }
   };
   if (s.page_size >= 64) select(std::integral_constant<int, 1>{});

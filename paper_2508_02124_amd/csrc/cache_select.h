@@ -575,7 +575,7 @@ __device__ __forceinline__ void list_slices(const CacheRef& c, const CacheRow& r
 template <int S, bool SLICED, bool KEYS, bool EITHER = false>
 __device__ __forceinline__ void select_block(const CacheRef& c, const CacheRows& p, const SliceWork& sw, int32_t* kept, uint32_t* keys, int block,
                                              bool whole = true) {
-  const int part = SLICED ? block / sw.pairs : 0, pair = block - part * sw.pairs, rh = (SLICED ? sw.first : 0) + pair;
+  const int part = SLICED ? block / sw.pairs : 0, pair = block - part * sw.pairs, rh = sw.first + pair;
   const int r = rh / c.H_q, h = rh - r * c.H_q;
   const int tid = threadIdx.x;
   const CacheRow row = cache_row(c, p, r);

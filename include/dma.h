@@ -416,6 +416,8 @@ int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K
  * same call.  The token of row r has the position row_len[r] - 1 (0 if that is below 0) behind the prefix of its request:
  *   row_req     in  nullable (row r is then request r, n_rows <= n_reqs); row_len in, as dma_cache_assign gives them
  *   n_prefixes, prefix_len [n_prefixes], req_prefix [n_reqs]   as for dma_cache_decode_prefix; with n_prefixes == 0 neither is read, nor row_req
+ *               A prefix counts with its prefix_len as given (below 0: 0), also beyond max_pages * page_size and whatever request holds it;
+ *               positions end at 2^31 - 1
  *   Q           in  nullable: n_rows rows of [H_q, d], q_stride elements apart, every row turned, also one without a slot
  *   Qo          out [n_rows, H_q, d]; may be Q if that is packed, else it overlaps no input
  *   freqs, rot, interleaved   as for dma_rope
@@ -466,7 +468,8 @@ int dma_cache_decode(const dma_cache_shape* shape, int32_t n_rows, int32_t k, fl
  *   max_prefix   upper bound on their lengths (0 => max_pages * page_size).  Like shape->max_len, the bound on a row's own keys, it chooses
  *                between equal ways of working; one that is too small costs time but changes no result
  *   prefix_req   in [n_prefixes] int32: the request that holds each; one out of range is a prefix without tokens
- *   prefix_len   in [n_prefixes] int32: its tokens (their number may be less than that request has)
+ *   prefix_len   in [n_prefixes] int32: its tokens (their number may be less than that request has; beyond max_pages * page_size a row sees
+ *                the first max_pages * page_size)
  *   req_prefix   in [n_reqs] int32: the prefix of each request, 0 to n_prefixes - 1; any other value: none.  (A prefix of a prefix is not
  *                looked at.)  The last three are not read if n_prefixes is 0
  *   q, q_stride, pages, block_table, row_req, row_len, softmax_scale, o, lse   as for dma_cache_decode; a row that has no request or no

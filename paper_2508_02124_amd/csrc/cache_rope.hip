@@ -82,8 +82,7 @@ __global__ __launch_bounds__(256) void cache_append_rope_kernel(CacheRef c, Appe
   if (p.n_prefixes) {
     const int req = p.row_req ? p.row_req[r] : r;
     const int prefix = (uint32_t)req < (uint32_t)c.n_reqs ? p.req_prefix[req] : -1;
-    const long cap = (long)c.max_pages << c.shift;
-    if ((uint32_t)prefix < (uint32_t)p.n_prefixes) position = max(position, 0l) + max(0l, min((long)p.prefix_len[prefix], cap));
+    if ((uint32_t)prefix < (uint32_t)p.n_prefixes) position = max(position, 0l) + max(0l, (long)p.prefix_len[prefix]);
   }
   position = max(0l, min(position, 0x7fffffffl));
   auto load = [&](const void* base, long stride, int h) __attribute__((always_inline)) {

@@ -207,14 +207,16 @@ class PagedCache:
 
     def _check_decode(self, q, keep_window, rows, softmax_scale, max_len, prefixes=None, max_prefix=0):
         """The shape, window, row_req and row_len of a decode, or what it would raise, for a caller that has something to do before it.
-        A window or a bound beyond the longest request, of whatever size, is one of just that."""
+        A window beyond all that a row can see (the longest request, with prefixes two of them), or a bound beyond the longest request, of
+        whatever size, is one of just that."""
         s, n = self.shape, q.shape[0]
         longest = s.max_pages * s.page_size
-        window, bound = min(int(keep_window), longest), min(int(max_len), longest)
+        seen = longest if prefixes is None else min(2 * longest, 2 ** 31 - 1)
+        window, bound = min(int(keep_window), seen), min(int(max_len), longest)
         name, n_prefixes = ("dma_cache_decode", 0) if prefixes is None else ("dma_cache_decode_prefix", prefixes.req.numel())
         if window <= 0 or bound < 0 or max_prefix < 0 or not softmax_scale >= 0.0:
             raise B.DmaError(B.DMA_EINVAL, name)
-        if (n + n_prefixes + 8) * s.H_q * -(-window // 256) >= 1 << 22 or n_prefixes > 4096:
+        if (n + n_prefixes + 8) * s.H_q * -(-min(window, longest) // 256) >= 1 << 22 or n_prefixes > 4096:
             raise B.DmaError(B.DMA_EUNSUPPORTED, name)
         if prefixes is not None:
             self._check_prefixes(prefixes)

@@ -416,8 +416,9 @@ int dma_cache_append(const dma_cache_shape* shape, int32_t n_rows, const void* K
  * same call.  The token of row r has the position row_len[r] - 1 (0 if that is below 0) behind the prefix of its request:
  *   row_req     in  nullable (row r is then request r, n_rows <= n_reqs); row_len in, as dma_cache_assign gives them
  *   n_prefixes, prefix_len [n_prefixes], req_prefix [n_reqs]   as for dma_cache_decode_prefix; with n_prefixes == 0 neither is read, nor row_req
- *               A prefix counts with its prefix_len as given (below 0: 0), also beyond max_pages * page_size and whatever request holds it;
- *               positions end at 2^31 - 1
+ *               A prefix counts with its prefix_len as given (below 0: 0), also beyond max_pages * page_size and whatever request holds it
+ *               (prefix_req is not given: for a holder out of range, whose prefix has no tokens there, prefix_len has to be 0); positions
+ *               end at 2^31 - 1
  *   Q           in  nullable: n_rows rows of [H_q, d], q_stride elements apart, every row turned, also one without a slot
  *   Qo          out [n_rows, H_q, d]; may be Q if that is packed, else it overlaps no input
  *   freqs, rot, interleaved   as for dma_rope

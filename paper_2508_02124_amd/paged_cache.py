@@ -123,16 +123,18 @@ class PagedCache:
 
     def prefixes(self, req, of, length=None):
         """Prefixes held by the requests `req` (a sequence or int32 tensor), of[b] being that of request b (an index into them, -1: none;
-        a sequence or int32 tensor [n_reqs]).  length: their tokens; left out: all that those requests have now."""
+        a sequence or int32 tensor [n_reqs]).  length: their tokens; left out: all that those requests have now.  Held by a request
+        that is not there, a prefix has none, whatever its length.  (len of what this returns is a tensor of its own; a prefix that gets
+        longer or shorter has it changed there.)"""
         ints = lambda x: x if isinstance(x, torch.Tensor) else torch.tensor([int(i) for i in x], dtype=torch.int32, device=self.device)
         req, of = ints(req), ints(of)
-        if length is None:   # (a request that is not there holds nothing)
-            length = self.seq_lens[req.long().clamp(0, self.shape.n_reqs - 1)].where((req >= 0) & (req < self.shape.n_reqs), 0).int()
-        else:
-            length = ints(length)
-        shared = CachePrefixes(req, length, of)
-        self._check_prefixes(shared)
-        return shared
+        given = length is not None
+        length = ints(length) if given else req
+        self._check_prefixes(CachePrefixes(req, length, of))
+        there = (req >= 0) & (req < self.shape.n_reqs)
+        if not given:
+            length = self.seq_lens[req.long().clamp(0, self.shape.n_reqs - 1)]
+        return CachePrefixes(req, length.where(there, 0).int(), of)
 
     def append_rotary(self, rows, q, k, v, freqs, W=None, A=None, z=None, prefixes=None, interleaved=False):
         """append of the step's rows with k, and q if there is one, turned to their positions (torch_api.rotary): a token's place in its

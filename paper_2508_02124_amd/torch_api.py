@@ -182,7 +182,8 @@ class DynamicMaskAttention(torch.nn.Module):
 
     forward(q, k, v): [B, L, H, d] batches (each sequence its own document), or packed [T, H, d]
     tensors with cu_seqlens.  rotary_dim > 0: q and k are turned to their positions first (rotary), in that many
-    channels; positions [T] (int32, [B, L] with batches) replace those in the documents.
+    channels; positions [T] (int32, [B, L] with batches) replace those in the documents.  Frequencies other than those of
+    rotary_base go into the buffer rotary_freqs (float32), which moves with the module and keeps its values and type.
     """
 
     def __init__(self, num_heads, num_kv_heads, head_dim, keep_window, softmax_scale=None, device=None,
@@ -205,9 +206,14 @@ class DynamicMaskAttention(torch.nn.Module):
         self.A = torch.nn.Parameter(torch.full((num_heads,), -1.0, dtype=torch.float32, device=device))
 
     def _apply(self, fn, *args, **kwargs):
+        held = self.rotary_freqs
         super()._apply(fn, *args, **kwargs)
-        if self.rotary_freqs is not None:   # (formed anew where the module now is: a change of type does not round them)
-            self.rotary_freqs = rotary_freqs(self.rotary_dim, self.rotary_base, self.rotary_freqs.device)
+        if held is not None:   # (a change of type does not round them, and where the device stays, so does the tensor: a graph may read it)
+            device = self.rotary_freqs.device
+            if held.is_meta and device.type != "meta":
+                self.rotary_freqs = rotary_freqs(self.rotary_dim, self.rotary_base, device)
+            else:
+                self.rotary_freqs = held.to(device)
         return self
 
     def forward(self, q, k, v, cu_seqlens=None, max_seqlen=0, positions=None):

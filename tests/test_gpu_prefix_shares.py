@@ -8,6 +8,8 @@ import torch
 
 from cache_harness import normal
 from paper_2508_02124_amd import binding as B
+from paper_2508_02124_amd.paged_cache import PagedCache
+from paper_2508_02124_amd.torch_api import DynamicMaskAttention
 from test_gpu_cache_prefix import Shared, ints
 
 pytestmark = pytest.mark.gpu
@@ -96,3 +98,28 @@ def test_captured_call_of_several_launches(gpu):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(o, ref[0]) and torch.equal(lse, ref[1])
+
+
+@pytest.mark.parametrize("P,m,window,max_tokens", [(3000, 1500, 512, 8192), (14000, 2600, 700, 16640), (900, 2300, 2100, 2400)])
+def test_a_long_question_behind_a_prefix(gpu, P, m, window, max_tokens):
+    """A prompt's thousands of rows go in and attend in one step behind a shared prefix, turned to their positions: the answers of the same
+    tokens as one request, for every row, with bounds on the lengths and without."""
+    H_q, H_kv, d = 32, 4, 64
+    torch.manual_seed(1)
+    layer = DynamicMaskAttention(H_q, H_kv, d, window, device=gpu, rotary_dim=d)
+    make = lambda longest: PagedCache(3, 2 * (P + m) // 64 + 8, H_q, H_kv, d, page_size=64, max_tokens=longest, device=gpu)
+    split = lambda x: x.split((H_q, H_kv, H_kv), 1)
+    first, rest = normal(gpu, 1, P, H_q + 2 * H_kv, d, dtype=torch.bfloat16), normal(gpu, 2, m, H_q + 2 * H_kv, d, dtype=torch.bfloat16)
+    one = make(P + m + 64)
+    for x, n in ((first, P), (rest, m)):
+        ref_rows = one.assign([0, n, 0])
+        ref = layer.step(*split(x), one, ref_rows).float()
+    for bounds in (dict(), dict(max_len=m, max_prefix=P)):
+        two = make(max_tokens)
+        layer.step(*split(first), two, two.assign([0, 0, P]))
+        shared, rows = two.prefixes([2], [-1, 0, -1]), two.assign([0, m, 0])
+        got = layer.step(*split(rest), two, rows, prefixes=shared, **bounds).float()
+        for a, b in zip(one.read(ref_rows.slots), two.read(rows.slots)):
+            assert torch.equal(a, b)
+        # the same number but for weights off by 2^-16 and one rounding each (2^-8 of it, twice)
+        assert ((got - ref).abs() <= 2.0 ** -7 * ref.abs() + 2.0 ** -13).all()

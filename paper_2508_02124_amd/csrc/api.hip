@@ -484,6 +484,6 @@ const char* dma_strerror(int status) {
   }
 }
 
-int dma_version(void) { return 143; }
+int dma_version(void) { return 144; }
 
 }  // extern "C"

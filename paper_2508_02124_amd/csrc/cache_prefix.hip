@@ -3,7 +3,8 @@
 //
 // The min(k, P) best of a prefix are listed once for each of its heads; what a row keeps are the k best of that list and its own keys
 // together, a cut through both.  So a prefix is selected from once, and its listed K and V are gathered and decoded once for 32 rows: they are
-// the columns of two matrix products whose weights each row masks by its own cut.  Four launches (five behind long prefixes):
+// the columns of two matrix products whose weights each row masks by its own cut.  Four launches (five behind long prefixes; where lists
+// of more than 8192 pairs are made in slices, the first two in turns):
 //   prefix_select_kernel (prefix_slice_kernel)   the lists, and the rows in order of their prefixes
 //   prefix_cut_kernel                            a row's cut, and which of its own keys it keeps
 //   prefix_tile_kernel                           attention to the prefixes, in parts

@@ -59,7 +59,7 @@ __device__ __forceinline__ double from_lane(double x, int lane) {
 // A wave has a row: D / 8 lanes a head, eight channels each, 64 / (D / 8) heads at a time, so that a load of the wave covers whole heads in a
 // row.  The angles are the same in every head: each lane forms one (two at 256 channels) and takes the others of its pairs from the lanes that
 // have them.  Pairs half a rotation apart lie in two lanes, which exchange their values.  Nothing is shared between waves.
-// What bounds it is memory: 65536 rows of 32 and 8 heads of 128 320 us (1.44 GB, 4.5 TB/s), one row 5.0 and 333 5.7 (the launch and a
+// What bounds it is memory: 65536 rows of 32 and 8 heads of 128 318 us (1.44 GB, 4.5 TB/s), one row 4.9 and 333 5.9 (the launch and a
 // chain of three loads).  With 64 / (D / 8) rows to a wave, each lane in its place of every head and forming four angles, 350.
 // A loop over rows in the kernel took 153 registers instead of 108 (35 us more).
 template <typename T, int D, bool NEXT>
